@@ -204,7 +204,7 @@ def _weights(s, expert, renorm, scale):
     w = torch.where(expert < 0, torch.zeros_like(w), w)
     if renorm:
         r = w.sum(1, keepdim=True)
-        w = torch.where(r > 0, w / torch.where(r > 0, r, torch.ones_like(r)), torch.zeros_like(w))
+        w = torch.where(r == 0, torch.zeros_like(w), w / r)
     return w * scale
 
 
