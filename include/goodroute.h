@@ -412,6 +412,150 @@ int gr_profile_read_launches(gr_fleet* f, int32_t max_launches, int32_t* kernel_
 int32_t gr_profile_kernel_count(void);
 const char* gr_profile_kernel_name(int32_t id);
 
+/*
+ * ---- Operators of a length predictor -------------------------------------------------------
+ *
+ * The routing above takes predicted lengths.  The paper's predictor of them (Sec. 3.2) is a
+ * mixture of experts: a small network scores the experts of a request, each expert is a
+ * multilayer network, and their results are added up by the scores.  The calls below are what
+ * such a predictor is made of, forward and backward: the choice of experts, one layer of all
+ * experts, the weighted sum, and the clipping of gradients by their global norm.
+ *
+ * T rows (requests) go to top_k experts each: S = T * top_k slots, slot r * top_k + j being
+ * choice j of row r.  The layers work on positions: the slots in the order of experts, those of
+ * expert e at positions off[e] .. off[e+1]-1, in the order of slots.  Slots without an expert
+ * (expert -1) come behind all others.
+ *
+ * Conventions as above: DEVICE pointers, work queued on the stream and nothing else (the calls
+ * can be recorded into a HIP graph), workspace in the handle, calls on one handle must not
+ * overlap.  Arrays are dense and row-major, aligned to their element (rows that are whole 16 bytes on
+ * 16-byte boundaries are faster).  dtype is GR_F32, GR_BF16 or GR_F16 for every `void` array of a call;
+ * sums, softmax statistics and norms are held in 32 bits or more and results are rounded once, to nearest.
+ * Outputs must not overlap inputs unless it is said.  Indexes on the device are not validated: kernels stay in
+ * bounds whatever off, slot, pos and expert hold, and give results only for arrays as gr_expert_plan leaves them.
+ * Results do not depend on the order in which workgroups run: the same call gives the same bits.
+ */
+typedef struct gr_experts gr_experts;
+
+enum { GR_F32 = 0, GR_BF16 = 1, GR_F16 = 2 };                    /* dtype */
+enum { GR_SCORE_SOFTMAX = 0, GR_SCORE_SIGMOID = 1 };             /* scoring */
+#define GR_MAX_EXPERTS 512
+#define GR_MAX_TOP_K 16
+#define GR_MAX_GROUPS 32
+#define GR_MAX_GRADIENTS 4096
+#define GR_MAX_WIDTH 65536      /* features of a layer */
+
+/*
+ * Create the workspace of calls on up to n_expert experts, max_rows rows and max_top_k experts per row, on the
+ * current HIP device.  max_rows * max_top_k <= 2^30.  Device memory held until gr_experts_destroy: 64 MB for the parts of long
+ * sums, 4 * (n_expert + 1) bytes for each 1 024 slots, and 0.4 MB.
+ */
+int gr_experts_create(gr_experts** out, int32_t n_expert, int64_t max_rows, int32_t max_top_k);
+int gr_experts_destroy(gr_experts* h);       /* waits for the device first; NULL is allowed */
+
+/*
+ * The choice of experts.  With s = softmax or sigmoid of a row's logits (softmax over all experts that are not
+ * masked), bias b and c = s + b:
+ *   a logit of -inf masks its expert: score 0, never chosen; so does a c of -inf;
+ *   the experts are n_group groups of equal size, neighbours together; of these the n_group_kept with
+ *   the largest sum of their two largest c stay (a single c where a group has no second);
+ *   the top_k experts of those groups with the largest c are chosen, largest first;
+ *   weight_j = scale * s_j, divided by the sum of the chosen s if `renormalise` (0 where that sum is 0).
+ * Ties go to the lowest index.  The bias enters the choice only.  Where fewer than top_k experts are left the last
+ * slots have expert -1 and weight 0.  A c that is no number ranks below every number and above masked experts; its weight is what
+ * the arithmetic gives (a row whose softmax is not defined has weights that are no numbers).
+ *
+ *   logits      DEVICE dtype[n_rows * n_expert]   n_expert is the handle's
+ *   bias        DEVICE float[n_expert], may be NULL
+ *   out_weight, out_expert      DEVICE float, int32 [n_rows * top_k]
+ *   out_off, out_slot, out_pos  DEVICE, as gr_expert_plan; all three or none (NULL)
+ * top_k <= n_expert; n_group divides n_expert, 1 <= n_group_kept <= n_group; scale is finite.
+ */
+int gr_expert_route(gr_experts* h, int64_t n_rows, int32_t top_k, const void* logits, int32_t dtype, const float* bias,
+                    int32_t scoring, int32_t n_group, int32_t n_group_kept, int32_t renormalise, float scale,
+                    float* out_weight, int32_t* out_expert, int32_t* out_off, int32_t* out_slot, int32_t* out_pos, void* hip_stream);
+
+/*
+ * Its gradient: of the loss by the logits, from that by the weights.  The choice is constant (`expert`, as it was given out; no
+ * expert twice in a row); experts outside [0, n_expert) get nothing and give nothing, whatever dweight holds there.
+ *   dweight     DEVICE float[n_rows * top_k]
+ *   out_dlogits DEVICE dtype[n_rows * n_expert], written whole
+ */
+int gr_expert_route_backward(gr_experts* h, int64_t n_rows, int32_t top_k, const void* logits, int32_t dtype, int32_t scoring,
+                             int32_t renormalise, float scale, const int32_t* expert, const float* dweight,
+                             void* out_dlogits, void* hip_stream);
+
+/*
+ * The slots in the order of given experts (those of gr_expert_route, or a caller's own: the paper trains each
+ * expert on a part of the data of its own).
+ *   expert   DEVICE int32[n_rows * top_k]; outside [0, n_expert): none
+ *   out_off  DEVICE int32[n_expert + 1]
+ *   out_slot DEVICE int32[n_rows * top_k]   the slot at every position; -1 - slot behind off[n_expert]
+ *   out_pos  DEVICE int32[n_rows * top_k]   the position of every slot, -1 for slots without an expert
+ */
+int gr_expert_plan(gr_experts* h, int64_t n_rows, int32_t top_k, const int32_t* expert, int32_t* out_off, int32_t* out_slot,
+                   int32_t* out_pos, void* hip_stream);
+
+/*
+ * One layer of every expert: y[p] = act(W_e x[row] + b_e) for the positions p of expert e.
+ *   n_pos    number of positions (S), and of rows of out_y; rows behind off[n_expert] are set to 0
+ *   off      DEVICE int32[n_expert + 1]; NULL: one matrix for all (W and b are those of a single expert)
+ *   slot     DEVICE int32[n_pos]: x is [ceil(n_pos / top_k), n_in], row = slot[p] / top_k.
+ *            NULL: x is [n_pos, n_in], row = p
+ *   x, w, bias, out_y   DEVICE dtype; w [n_expert, n_out, n_in], bias [n_expert, n_out] or NULL, out_y [n_pos, n_out]
+ *   relu     0: act is the identity; 1: max(0, .) (a value that is no number stays one)
+ */
+int gr_expert_linear(gr_experts* h, int64_t n_pos, int32_t n_in, int32_t n_out, int32_t dtype, const int32_t* off,
+                     const int32_t* slot, int32_t top_k, const void* x, const void* w, const void* bias, int32_t relu,
+                     void* out_y, void* hip_stream);
+
+/*
+ * Its gradient, from dy:  dz = dy where y > 0, else 0 (dy itself without y);
+ *   dx[p] = dz[p] W_e;  dW_e = sum over its positions of dz[p]^T x[row];  db_e = sum of dz[p].
+ *   y        DEVICE, as gr_expert_linear gave it with relu; NULL: the layer had none
+ *   out_dz   DEVICE [n_pos, n_out]: where dz goes; needed with y, NULL without (dy itself is allowed: it is then overwritten)
+ *   out_dx   DEVICE [n_pos, n_in], by position: a row of x that several slots share has the sum of theirs
+ *            (gr_expert_combine without weights); rows behind off[n_expert] are 0.  May be NULL
+ *   out_dw, out_db   DEVICE [n_expert, n_out, n_in], [n_expert, n_out]; 0 for experts without a position; may be NULL
+ */
+int gr_expert_linear_backward(gr_experts* h, int64_t n_pos, int32_t n_in, int32_t n_out, int32_t dtype, const int32_t* off,
+                              const int32_t* slot, int32_t top_k, const void* x, const void* w, const void* y, const void* dy,
+                              void* out_dz, void* out_dx, void* out_dw, void* out_db, void* hip_stream);
+
+/*
+ * The weighted sum of a row's results: out[r] = sum over j of weight[r, j] * y[pos[r, j]].
+ * Slots without an expert add nothing, whatever their weight holds.
+ *   weight   DEVICE float[n_rows * top_k]; NULL: all 1
+ *   pos      DEVICE int32[n_rows * top_k]
+ *   y, out   DEVICE dtype; [n_rows * top_k, n_out], [n_rows, n_out]
+ */
+int gr_expert_combine(gr_experts* h, int64_t n_rows, int32_t top_k, int32_t n_out, int32_t dtype, const float* weight,
+                      const int32_t* pos, const void* y, void* out, void* hip_stream);
+
+/*
+ * Its gradient, from dout [n_rows, n_out]: dy[p] = weight[slot] * dout[row], dweight[slot] = <dout[row], y[p]>, both 0 for slots
+ * without an expert.
+ *   slot        DEVICE int32[n_rows * top_k]
+ *   out_dy      DEVICE dtype[n_rows * top_k, n_out]; may be NULL
+ *   out_dweight DEVICE float[n_rows * top_k]; may be NULL (y is not read then, and may be NULL)
+ */
+int gr_expert_combine_backward(gr_experts* h, int64_t n_rows, int32_t top_k, int32_t n_out, int32_t dtype, const float* weight,
+                               const int32_t* slot, const void* y, const void* dout, void* out_dy, float* out_dweight,
+                               void* hip_stream);
+
+/*
+ * Clipping by the global norm: norm = the root of the sum of the squares of all elements of all gradients;
+ * out_i = grad_i * min(1, max_norm / norm).  Gradients are given out as they are where the norm is not finite
+ * (out_norm says so).  Squares are summed in double precision.
+ *   grad, out HOST arrays of n_grad DEVICE pointers (read during the call); out[i] may be grad[i], NULL for an empty one
+ *   count     HOST int64[n_grad], >= 0, at most 2^40
+ *   dtype     HOST int32[n_grad], of gradient and output alike
+ *   max_norm  >= 0, may be infinite
+ *   out_norm  DEVICE float[1]; may be NULL
+ */
+int gr_clip_gradients(gr_experts* h, int32_t n_grad, const void* const* grad, void* const* out, const int64_t* count,
+                      const int32_t* dtype, float max_norm, float* out_norm, void* hip_stream);
+
 /* Static, human-readable text for a return code. */
 const char* gr_strerror(int code);
 

@@ -17,7 +17,10 @@ MARSHAL_PATH = os.path.join(_HERE, "csrc", "goodroute_marshal.so")
 EXPORTS = ("gr_create", "gr_destroy", "gr_build_status", "gr_score_route", "gr_score_route_noalloc", "gr_score_route_cached", "gr_route_feedback",
            "gr_risk_scan", "gr_observe", "gr_set_blend", "gr_set_batch_cap", "gr_set_small_batch_pairs", "gr_set_feedback_wait", "gr_set_feedback_units", "gr_set_feedback_team", "gr_feedback_team",
            "gr_device_status", "gr_strerror", "gr_profile_enable", "gr_profile_select", "gr_profile_read",
-           "gr_profile_read_launches", "gr_profile_kernel_count", "gr_profile_kernel_name")
+           "gr_profile_read_launches", "gr_profile_kernel_count", "gr_profile_kernel_name",
+           "gr_experts_create", "gr_experts_destroy", "gr_expert_route", "gr_expert_route_backward", "gr_expert_plan",
+           "gr_expert_linear", "gr_expert_linear_backward", "gr_expert_combine", "gr_expert_combine_backward",
+           "gr_clip_gradients")
 
 _lib = None
 _marshal = None
@@ -83,6 +86,18 @@ def lib() -> C.CDLL:
         l.gr_profile_kernel_count.argtypes = []
         l.gr_profile_kernel_name.restype = C.c_char_p
         l.gr_profile_kernel_name.argtypes = [i32]
+        f32 = C.c_float
+        for name, args in {
+                "gr_experts_create": [C.POINTER(p), i32, i64, i32], "gr_experts_destroy": [p],
+                "gr_expert_route": [p, i64, i32, p, i32, p, i32, i32, i32, i32, f32, p, p, p, p, p, p],
+                "gr_expert_route_backward": [p, i64, i32, p, i32, i32, i32, f32, p, p, p, p],
+                "gr_expert_plan": [p, i64, i32, p, p, p, p, p],
+                "gr_expert_linear": [p, i64, i32, i32, i32, p, p, i32, p, p, p, i32, p, p],
+                "gr_expert_linear_backward": [p, i64, i32, i32, i32, p, p, i32, p, p, p, p, p, p, p, p, p],
+                "gr_expert_combine": [p, i64, i32, i32, i32, p, p, p, p, p],
+                "gr_expert_combine_backward": [p, i64, i32, i32, i32, p, p, p, p, p, p, p],
+                "gr_clip_gradients": [p, i32, p, p, p, p, f32, p, p]}.items():
+            getattr(l, name).restype, getattr(l, name).argtypes = C.c_int, args
         l.gr_strerror.restype = C.c_char_p
         l.gr_strerror.argtypes = [C.c_int]
         _lib = l
@@ -366,3 +381,134 @@ class Fleet:
         bits = C.c_int32(0)
         _check(lib().gr_device_status(self._h, C.byref(bits)), "gr_device_status")
         return int(bits.value)
+
+
+_SCORING = {"softmax": 0, "sigmoid": 1}
+
+
+def _dtype(t, name: str) -> int:
+    import torch
+    code = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}.get(t.dtype)
+    if code is None:
+        raise TypeError(f"{name}: need float32, bfloat16 or float16, got {t.dtype}")
+    return code
+
+
+class Experts:
+    """Owns a gr_experts handle on the current device: the workspace of a length predictor's operators.
+
+    Shapes are taken from the tensors: logits [rows, experts], choices and weights [rows, top_k], x [rows or positions, n_in], w [experts,
+    n_out, n_in], y [positions, n_out]; all contiguous, x, w and y of one type."""
+
+    def __init__(self, n_expert: int, max_rows: int, max_top_k: int):
+        self._h = C.c_void_p()
+        self.n_expert = int(n_expert)
+        _check(lib().gr_experts_create(C.byref(self._h), self.n_expert, int(max_rows), int(max_top_k)), "gr_experts_create")
+
+    def close(self) -> None:
+        if self._h:
+            h, self._h = self._h, C.c_void_p()
+            _check(lib().gr_experts_destroy(h), "gr_experts_destroy")
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+    @staticmethod
+    def _shape(t, name, *shape):
+        """A tensor's shape, as far as it is asked for (None: any)."""
+        if t.dim() != len(shape) or any(w is not None and w != g for w, g in zip(shape, t.shape)):
+            raise ValueError(f"{name}: shape {tuple(t.shape)}, need {tuple('any' if w is None else w for w in shape)}")
+        return t.shape
+
+    def _plan(self, n, off, slot, pos):
+        import torch
+        i32 = torch.int32
+        return _dev(off, i32, "out_off", self.n_expert + 1), _dev(slot, i32, "out_slot", n), _dev(pos, i32, "out_pos", n)
+
+    def gr_expert_route(self, logits, out_weight, out_expert, out_off=None, out_slot=None, out_pos=None, bias=None,
+                        scoring="softmax", n_group=1, n_group_kept=1, renormalise=False, scale=1.0) -> None:
+        import torch
+        T, _ = self._shape(logits, "logits", None, self.n_expert)
+        _, k = self._shape(out_expert, "out_expert", T, None)
+        _check(lib().gr_expert_route(
+            self._h, T, k, _dev(logits, logits.dtype, "logits"), _dtype(logits, "logits"),
+            _dev(bias, torch.float32, "bias", self.n_expert), _SCORING[scoring], int(n_group), int(n_group_kept), int(renormalise),
+            float(scale), _dev(out_weight, torch.float32, "out_weight", T * k), _dev(out_expert, torch.int32, "out_expert"),
+            *self._plan(T * k, out_off, out_slot, out_pos), _stream()), "gr_expert_route")
+
+    def gr_expert_route_backward(self, logits, expert, dweight, out_dlogits, scoring="softmax", renormalise=False, scale=1.0) -> None:
+        import torch
+        T, E = self._shape(logits, "logits", None, self.n_expert)
+        _, k = self._shape(expert, "expert", T, None)
+        _check(lib().gr_expert_route_backward(
+            self._h, T, k, _dev(logits, logits.dtype, "logits"), _dtype(logits, "logits"), _SCORING[scoring], int(renormalise),
+            float(scale), _dev(expert, torch.int32, "expert"), _dev(dweight, torch.float32, "dweight", T * k),
+            _dev(out_dlogits, logits.dtype, "out_dlogits", T * E), _stream()), "gr_expert_route_backward")
+
+    def gr_expert_plan(self, expert, out_off, out_slot, out_pos) -> None:
+        import torch
+        T, k = self._shape(expert, "expert", None, None)
+        _check(lib().gr_expert_plan(self._h, T, k, _dev(expert, torch.int32, "expert"), *self._plan(T * k, out_off, out_slot, out_pos),
+                                    _stream()), "gr_expert_plan")
+
+    def _layer(self, x, w, off, slot, top_k, n):
+        """Arguments that a layer's forward and backward share, from `off` to `w`, behind the sizes."""
+        import torch
+        E = 1 if off is None else self.n_expert
+        _, O, I = self._shape(w, "w", E, None, None) if w.dim() == 3 or off is not None else (1, *self._shape(w, "w", None, None))
+        self._shape(x, "x", (n + top_k - 1) // top_k if slot is not None else n, I)
+        i32 = torch.int32
+        return E, I, O, (n, I, O, _dtype(x, "x"), _dev(off, i32, "off", self.n_expert + 1), _dev(slot, i32, "slot", n), int(top_k),
+                         _dev(x, x.dtype, "x"), _dev(w, x.dtype, "w"))
+
+    def gr_expert_linear(self, x, w, out_y, bias=None, off=None, slot=None, top_k=1, relu=False) -> None:
+        n, O = self._shape(out_y, "out_y", None, w.shape[-2])
+        E, I, O, layer = self._layer(x, w, off, slot, int(top_k), n)
+        _check(lib().gr_expert_linear(self._h, *layer, _dev(bias, x.dtype, "bias", E * O), int(relu), _dev(out_y, x.dtype, "out_y"),
+                                      _stream()), "gr_expert_linear")
+
+    def gr_expert_linear_backward(self, x, w, dy, out_dx=None, out_dw=None, out_db=None, y=None, out_dz=None, off=None,
+                                  slot=None, top_k=1) -> None:
+        n, O = self._shape(dy, "dy", None, w.shape[-2])
+        E, I, O, layer = self._layer(x, w, off, slot, int(top_k), n)
+        t = x.dtype
+        _check(lib().gr_expert_linear_backward(
+            self._h, *layer, _dev(y, t, "y", n * O), _dev(dy, t, "dy"), _dev(out_dz, t, "out_dz", n * O),
+            _dev(out_dx, t, "out_dx", n * I), _dev(out_dw, t, "out_dw", E * O * I), _dev(out_db, t, "out_db", E * O), _stream()),
+            "gr_expert_linear_backward")
+
+    def gr_expert_combine(self, y, pos, out, weight=None) -> None:
+        import torch
+        T, k = self._shape(pos, "pos", None, None)
+        _, O = self._shape(out, "out", T, None)
+        _check(lib().gr_expert_combine(self._h, T, k, O, _dtype(out, "out"), _dev(weight, torch.float32, "weight", T * k),
+                                       _dev(pos, torch.int32, "pos"), _dev(y, out.dtype, "y", T * k * O), _dev(out, out.dtype, "out"),
+                                       _stream()), "gr_expert_combine")
+
+    def gr_expert_combine_backward(self, dout, y, slot, out_dy=None, weight=None, out_dweight=None) -> None:
+        import torch
+        T, O = self._shape(dout, "dout", None, None)
+        if T and slot.numel() % T:
+            raise ValueError(f"slot: {slot.numel()} elements, need a multiple of {T}")
+        S = slot.numel()
+        t, f32 = dout.dtype, torch.float32
+        _check(lib().gr_expert_combine_backward(
+            self._h, T, S // T if T else 1, O, _dtype(dout, "dout"), _dev(weight, f32, "weight", S), _dev(slot, torch.int32, "slot"),
+            _dev(y, t, "y", S * O), _dev(dout, t, "dout"), _dev(out_dy, t, "out_dy", S * O),
+            _dev(out_dweight, f32, "out_dweight", S), _stream()), "gr_expert_combine_backward")
+
+    def gr_clip_gradients(self, grads, max_norm, out_norm=None, out=None) -> None:
+        """grads: a list of tensors, scaled in place unless `out` names as many others."""
+        import torch
+        out = grads if out is None else out
+        n = len(grads)
+        if len(out) != n:
+            raise ValueError(f"out: {len(out)} tensors, need {n}")
+        _check(lib().gr_clip_gradients(
+            self._h, n, (C.c_void_p * n)(*[_dev(g, g.dtype, "grads") for g in grads]),
+            (C.c_void_p * n)(*[_dev(o, g.dtype, "out", g.numel()) for o, g in zip(out, grads)]),
+            (C.c_int64 * n)(*[g.numel() for g in grads]), (C.c_int32 * n)(*[_dtype(g, "grads") for g in grads]),
+            float(max_norm), _dev(out_norm, torch.float32, "out_norm", 1), _stream()), "gr_clip_gradients")

@@ -1,0 +1,159 @@
+// The global norm of many gradients, and clipping by it (gfx950).
+//
+// Bound by memory: two reads and a write of every gradient, the second read from the cache where all fit it (256 MB).
+// Squares are summed in double precision: they cannot overflow there, and the order of a sum shows in no digit that is kept.
+#include "experts.h"
+
+namespace gr {
+namespace {
+
+constexpr int kBlock = 256;
+constexpr int kWave = 64;
+constexpr int kPiece = kBlock * 4 * 16;      // bytes of a gradient that a workgroup takes at a time
+
+struct ClipTable {
+    const void* grad[kClipTensors];
+    void* out[kClipTensors];
+    int64_t count_type[kClipTensors];      // 4 * elements + type
+    int pieces_before[kClipTensors + 1];
+    int n;
+};
+
+struct Piece {
+    const char* grad;
+    char* out;
+    int64_t bytes;
+    int type;
+};
+
+__device__ __forceinline__ Piece piece_of(const ClipTable& t, int at)
+{
+    int lo = 0, hi = t.n - 1;      // the last gradient that starts at or before the piece
+    while (lo < hi) {
+        const int mid = (lo + hi + 1) / 2;
+        if (t.pieces_before[mid] <= at) lo = mid;
+        else hi = mid - 1;
+    }
+    const int type = (int)(t.count_type[lo] & 3);
+    const int64_t bytes = (t.count_type[lo] >> 2) * (type == GR_F32 ? 4 : 2), from = (int64_t)(at - t.pieces_before[lo]) * kPiece;
+    return {static_cast<const char*>(t.grad[lo]) + from, static_cast<char*>(t.out[lo]) + from, bytes - from < kPiece ? bytes - from : kPiece, type};
+}
+
+// `f` of every element of a piece: of chunks of 16 bytes where both sides allow, of single ones else and behind
+template <typename T, typename F, typename G>
+__device__ __forceinline__ void each(const Piece& p, bool aligned, F chunk, G one)
+{
+    const int count = (int)(p.bytes / sizeof(T)), chunks = aligned ? count / Chunk<T>::n : 0;
+    for (int i = threadIdx.x; i < chunks; i += kBlock) chunk(i);
+    for (int i = chunks * Chunk<T>::n + threadIdx.x; i < count; i += kBlock) one(i);
+}
+
+template <typename T>
+__device__ __forceinline__ double squares_of(const Piece& p)
+{
+    typedef typename Chunk<T>::Vec Vec;
+    const T* const g = reinterpret_cast<const T*>(p.grad);
+    double sum = 0;
+    const auto add = [&](T v) { sum = fma((double)(float)v, (double)(float)v, sum); };
+    each<T>(p, reinterpret_cast<uintptr_t>(g) % 16 == 0,
+            [&](int i) {
+                const Vec v = reinterpret_cast<const Vec*>(g)[i];
+#pragma unroll
+                for (int j = 0; j < Chunk<T>::n; ++j) add(v[j]);
+            },
+            [&](int i) { add(g[i]); });
+    return sum;
+}
+
+template <typename T>
+__device__ __forceinline__ void scale(const Piece& p, float by)
+{
+    typedef typename Chunk<T>::Vec Vec;
+    const T* const g = reinterpret_cast<const T*>(p.grad);
+    T* const o = reinterpret_cast<T*>(p.out);
+    each<T>(p, reinterpret_cast<uintptr_t>(g) % 16 == 0 && reinterpret_cast<uintptr_t>(o) % 16 == 0,
+            [&](int i) {
+                Vec v = reinterpret_cast<const Vec*>(g)[i];
+#pragma unroll
+                for (int j = 0; j < Chunk<T>::n; ++j) v[j] = (T)((float)v[j] * by);
+                reinterpret_cast<Vec*>(o)[i] = v;
+            },
+            [&](int i) { o[i] = (T)((float)g[i] * by); });
+}
+
+// The workgroup's sum, in thread 0.
+__device__ __forceinline__ double block_sum(double v)
+{
+    __shared__ double part[kBlock / kWave];
+    for (int m = 1; m < kWave; m *= 2) v += __shfl_xor(v, m);
+    if (threadIdx.x % kWave == 0) part[threadIdx.x / kWave] = v;
+    __syncthreads();
+    for (int w = 1; w < kBlock / kWave; ++w) v += threadIdx.x == 0 ? part[w] : 0.0;
+    return v;
+}
+
+__global__ __launch_bounds__(kBlock) void k_norm(ClipTable t, double* squares)
+{
+    double sum = 0;
+    for (int at = blockIdx.x; at < t.pieces_before[t.n]; at += gridDim.x) {
+        const Piece p = piece_of(t, at);
+        sum += p.type == GR_F32 ? squares_of<float>(p) : p.type == GR_BF16 ? squares_of<bf16>(p) : squares_of<f16>(p);
+    }
+    sum = block_sum(sum);
+    if (threadIdx.x == 0) squares[blockIdx.x] = sum;
+}
+
+__global__ __launch_bounds__(kBlock) void k_clip(ClipTable t, const double* squares, int parts, double max_norm, float* norm)
+{
+    __shared__ float by;
+    double sum = 0;
+    for (int i = threadIdx.x; i < parts; i += kBlock) sum += squares[i];
+    sum = block_sum(sum);
+    if (threadIdx.x == 0) {
+        const double all = sqrt(sum);
+        by = all > max_norm && all < __builtin_inf() ? (float)(max_norm / all) : 1.0f;
+        if (norm && blockIdx.x == 0) *norm = (float)all;
+    }
+    __syncthreads();
+    const float f = by;
+    for (int at = blockIdx.x; at < t.pieces_before[t.n]; at += gridDim.x) {
+        const Piece p = piece_of(t, at);
+        if (f == 1.0f && p.grad == p.out) continue;
+        if (p.type == GR_F32) scale<float>(p, f);
+        else if (p.type == GR_BF16) scale<bf16>(p, f);
+        else scale<f16>(p, f);
+    }
+}
+
+}  // namespace
+
+int launch_clip(gr_experts* h, int n, const void* const* grad, void* const* out, const int64_t* count, const int* dtype,
+                float max_norm, float* norm, hipStream_t s)
+{
+    // a table for each launch, made anew for either pass
+    const auto each_table = [&](auto launch) -> int {
+        int parts = 0, i = 0;
+        do {
+            ClipTable t{};
+            while (i < n && t.n < kClipTensors) {
+                const int64_t pieces = (count[i] * (int64_t)size_of(dtype[i]) + kPiece - 1) / kPiece;
+                if (pieces > INT32_MAX - t.pieces_before[t.n]) { if (t.n == 0) return GR_ERR_TOO_LARGE; break; }
+                t.grad[t.n] = grad[i]; t.out[t.n] = out[i]; t.count_type[t.n] = count[i] * 4 + dtype[i];
+                t.pieces_before[t.n + 1] = t.pieces_before[t.n] + (int)pieces;
+                ++t.n;
+                ++i;
+            }
+            const int blocks = t.pieces_before[t.n] < 1 ? 1 : t.pieces_before[t.n] < kClipBlocks ? t.pieces_before[t.n] : kClipBlocks;
+            if ((size_t)(parts + blocks) > kClipParts) return GR_ERR_TOO_LARGE;
+            launch(t, blocks, parts);
+            parts += blocks;
+        } while (i < n);
+        return parts;
+    };
+    const int parts = each_table([&](const ClipTable& t, int blocks, int at) { k_norm<<<blocks, kBlock, 0, s>>>(t, h->squares + at); });
+    if (parts < 0) return parts;
+    each_table([&](const ClipTable& t, int blocks, int at) { k_clip<<<blocks, kBlock, 0, s>>>(t, h->squares, parts, max_norm, at == 0 ? norm : nullptr); });
+    return launched();
+}
+
+}  // namespace gr

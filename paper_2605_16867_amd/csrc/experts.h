@@ -1,0 +1,78 @@
+// Internal declarations shared by the source files of the operators of a length predictor
+// (experts.hip, linear.hip, clip.hip).  The public interface and the mathematics are in goodroute.h.
+#pragma once
+
+#include <hip/hip_runtime.h>
+
+#include <cstddef>
+#include <cstdint>
+
+#include "goodroute.h"
+
+struct gr_experts {
+    int n_expert = 0, max_top_k = 0;
+    int64_t max_rows = 0, max_slots = 0;
+    int* counts = nullptr;       // [units of slots][n_expert + 1] slots of each expert, then those before the unit (see k_plan_*)
+    int* totals = nullptr;       // [n_expert + 1]
+    double* squares = nullptr;   // [kClipParts] sums of squares (see k_norm)
+    float* parts = nullptr;      // [kPartFloats] parts of long sums (see k_linear_*)
+};
+
+namespace gr {
+
+constexpr int kPlanUnit = 1024;      // slots that one wave puts in order
+constexpr size_t kPartFloats = size_t(16) << 20;
+constexpr int kClipBlocks = 1024;    // workgroups of a launch over gradients
+constexpr int kClipTensors = 96;     // gradients that one launch takes: their table is passed by value, 3 KB of the 4 that arguments may be
+constexpr size_t kClipParts = size_t(kClipBlocks) * ((GR_MAX_GRADIENTS + kClipTensors - 1) / kClipTensors);
+
+typedef __bf16 bf16;
+typedef _Float16 f16;
+
+// Calls `f` with a value of the type that `dtype` names.
+template <typename F>
+int by_type(int dtype, F f)
+{
+    return dtype == GR_F32 ? f(float{}) : dtype == GR_BF16 ? f(bf16{}) : f(f16{});
+}
+
+inline bool type_ok(int dtype) { return dtype == GR_F32 || dtype == GR_BF16 || dtype == GR_F16; }
+inline size_t size_of(int dtype) { return dtype == GR_F32 ? 4 : 2; }
+inline bool aligned16(const void* p) { return reinterpret_cast<uintptr_t>(p) % 16 == 0; }
+inline int launched() { return hipGetLastError() == hipSuccess ? GR_OK : GR_ERR_HIP; }
+
+// The 16 bytes that one access moves, as elements.
+template <typename T>
+struct Chunk {
+    static constexpr int n = 16 / sizeof(T);
+    typedef T Vec __attribute__((ext_vector_type(16 / sizeof(T))));
+};
+
+struct RouteIn {
+    const void* logits;
+    const float* bias;
+    int64_t rows;
+    int n_expert, top_k, scoring, n_group, kept, renorm;
+    float scale;
+};
+
+int launch_route(const RouteIn& in, int dtype, float* weight, int* expert, hipStream_t s);
+int launch_route_backward(const RouteIn& in, int dtype, const int* expert, const float* dweight, void* dlogits, hipStream_t s);
+int launch_plan(gr_experts* h, int64_t slots, const int* expert, int* off, int* slot, int* pos, hipStream_t s);
+int launch_combine(int64_t rows, int top_k, int width, int dtype, const float* weight, const int* pos, const void* y, void* out,
+                   hipStream_t s);
+int launch_combine_backward(int64_t rows, int top_k, int width, int dtype, const float* weight, const int* slot, const void* y,
+                            const void* dout, void* dy, float* dweight, hipStream_t s);
+
+struct LinearIn {
+    const int *off, *slot;     // null: one matrix; rows are positions
+    const void *x, *w, *bias, *y, *dy;
+    int64_t n_pos;
+    int n_expert, n_in, n_out, top_k, relu;
+};
+int launch_linear(gr_experts* h, const LinearIn& in, int dtype, void* out_y, hipStream_t s);
+int launch_linear_backward(gr_experts* h, const LinearIn& in, int dtype, void* dz, void* dx, void* dw, void* db, hipStream_t s);
+int launch_clip(gr_experts* h, int n, const void* const* grad, void* const* out, const int64_t* count, const int* dtype,
+                float max_norm, float* norm, hipStream_t s);
+
+}  // namespace gr
