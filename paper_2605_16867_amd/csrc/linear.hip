@@ -17,10 +17,14 @@ enum Product { kForward = 0, kByInput, kByWeight };
 struct LinearArgs {
     const int *off, *slot;
     const void *x, *w, *bias, *dz;
-    void *out, *db;
+    void* out;
     int64_t n_pos;
     int n_expert, n_in, n_out, top_k, relu;
     int tiles;      // in the direction of columns
+    int64_t down;   // and of rows
+    int block;      // rows of tiles taken together
+    uint32_t k_mul;      // slot / top_k: the upper half of slot * k_mul (the slot itself for 0), by 2^k_shift
+    int k_shift;
 };
 
 // Bounds of a range, whatever the offsets hold.
@@ -79,6 +83,27 @@ __device__ __forceinline__ RowTile row_tile(const LinearArgs& a, int64_t t)
     return {a.n_expert, 0, 0};
 }
 
+// Which tile workgroup j takes.  Workgroups go to the eight dies in turn, each with a cache of its own: a die takes blocks of neighbouring tiles, 32
+// at a time, `block` rows down and the rest across, so that what they share is fetched into a die once.
+constexpr int kDies = 8, kTogether = 32;
+
+struct TileNo {
+    int64_t row;      // -1: none
+    int col;
+};
+
+__device__ __forceinline__ TileNo tile_no(int64_t j, int64_t down, int across, int block)
+{
+    const int64_t all = down * across, each = (all + kDies - 1) / kDies;
+    const int run = each < kTogether ? (int)each : kTogether;      // tiles that a die takes together (fewer where there are not 32 for each)
+    if (run == 0) return {-1, 0};
+    const int64_t at = j / kDies, t = (at / run * kDies + j % kDies) * run + at % run;
+    if (t >= all) return {-1, 0};
+    const int64_t band = t / ((int64_t)block * across), in = t - band * block * across, left = down - band * block;
+    const int rows = left < block ? (int)left : block;
+    return {band * block + in % rows, (int)(in / rows)};
+}
+
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef f16 f16x8 __attribute__((ext_vector_type(8)));
@@ -114,8 +139,9 @@ __global__ __launch_bounds__(kBlock) void k_linear_any(LinearArgs a)
     __shared__ __attribute__((aligned(16))) T lds_p[kAnyTile * kLd], lds_q[kAnyTile * kLd];
 
     const int tid = threadIdx.x, lane = tid % kWave, wave = tid / kWave;
-    const int col_tile = blockIdx.x % a.tiles;
-    const int64_t row_no = blockIdx.x / a.tiles;
+    const TileNo no = tile_no(blockIdx.x, a.down, a.tiles, a.block);
+    const int64_t row_no = no.row;
+    if (row_no < 0) return;
     const T* const x = static_cast<const T*>(a.x);
     const T* const dz = static_cast<const T*>(a.dz);
     const int I = a.n_in, O = a.n_out;
@@ -123,7 +149,7 @@ __global__ __launch_bounds__(kBlock) void k_linear_any(LinearArgs a)
     // the output's rows p0 .. p0 + p_n - 1 (positions, or output features of an expert), columns q0 .. q0 + q_n - 1
     int e;
     int64_t p0, lo = 0, depth;
-    int p_n, q0 = col_tile * kAnyTile, q_n;
+    int p_n, q0 = no.col * kAnyTile, q_n;
     if constexpr (kProduct == kByWeight) {
         const int tiles = (O + kAnyTile - 1) / kAnyTile;
         e = (int)(row_no / tiles);
@@ -181,8 +207,6 @@ __global__ __launch_bounds__(kBlock) void k_linear_any(LinearArgs a)
     };
 
     f32x4 acc[4][4] = {};
-    float db = 0;
-    const bool sums = kProduct == kByWeight && a.db && col_tile == 0;
     const int wp = (wave / 2) * 64, wq = (wave % 2) * 64;      // a wave's 64 by 64
     if (depth > 0) load(0);
     for (int64_t r0 = 0; r0 < depth; r0 += D) {
@@ -208,12 +232,7 @@ __global__ __launch_bounds__(kBlock) void k_linear_any(LinearArgs a)
         for (int i = 0; i < 4; ++i)
 #pragma unroll
             for (int j = 0; j < 4; ++j) acc[i][j] = mfma(q[j], p[i], acc[i][j]);
-        if (sums && tid < p_n)
-            for (int r = 0; r < D; ++r) db += (float)lds_p[tid * kLd + r];
     }
-    if (sums && tid < p_n) static_cast<T*>(a.db)[(int64_t)e * O + p0 + tid] = (T)db;
-
-    if (kProduct == kByWeight && !a.out) return;      // (sums of dz alone)
     const int width = kProduct == kForward ? O : I;
     T* const out = static_cast<T*>(a.out) + ((kProduct == kByWeight ? (int64_t)e * O : 0) + p0) * width + q0;
     const T* const bias = kProduct == kForward && a.bias && e < a.n_expert ? static_cast<const T*>(a.bias) + (int64_t)e * O + q0 : nullptr;
@@ -236,238 +255,555 @@ __global__ __launch_bounds__(kBlock) void k_linear_any(LinearArgs a)
 
 // ---- 16-bit types, rows of whole 16 bytes -------------------------------------------------------
 //
-// Tiles of kRows by kCols, 64 reduction indexes at a time, that go from memory straight into shared memory (two tiles in turn: one
-// is filled while the other is multiplied).  An operand lies there as it does in memory:
+// Tiles of kSize by kSize, 64 reduction indexes (a slice) at a time, four waves of half by half each.  Slices go from memory straight into shared
+// memory.  An operand lies there as it does in memory:
 //   long    its reduction is contiguous: [row][64 indexes]; a lane's eight indexes are one read of 16 bytes
 //   across  its rows are contiguous: [64 indexes][row]; a lane's eight indexes are two reads that transpose 4 by 16
 // What is written is one after the other, 16 bytes a lane, so which 16 bytes of memory a lane fetches decides the layout: their number
-// within a row is exclusive-ored with one made of the row's, so that the lanes of a read meet no bank twice.
+// within a line of the tile is exclusive-ored with one made of the line's, so that the lanes of a read meet no bank twice.
 
-constexpr int kDepth = 64;
+constexpr int kDepth = 64, kSlots = 5, kWaves = 4;
 
 __device__ const uint4 kZeros = {0, 0, 0, 0};      // where lanes read that are past the end of the reduction
 
 typedef __attribute__((address_space(3))) char LdsChar;
-typedef const __attribute__((address_space(1))) char GlobalChar;
 
-__device__ __forceinline__ void fetch16(const void* from, char* to)
+__device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
+__device__ __forceinline__ int64_t uniform(int64_t v)
 {
-    const uint32_t at = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(LdsChar*)to);
-    asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" ::"v"(from), "s"(at) : "memory");
+    return (int64_t)((uint64_t)(uint32_t)uniform((int)(v >> 32)) << 32 | (uint32_t)uniform((int)v));
+}
+
+// 16 bytes a lane into shared memory at `to` and after, from an address of the lane's own, or from an offset to one of the wave's.
+__device__ __forceinline__ void fetch16(const char* from, uint32_t to)
+{
+    asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" ::"v"(from), "s"(to) : "memory");
+}
+__device__ __forceinline__ void fetch16(const char* base, uint32_t offset, uint32_t to)
+{
+    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(offset), "s"(base), "s"(to) : "memory");
 }
 
 __device__ __forceinline__ int across_swizzle(int r) { return (r & 3) << 1 | (r >> 3 & 1) << 3; }
 
-// A lane's part of a fragment of 16 rows (or columns) by 32 indexes.
+// A lane's part of fragment `no` (16 rows or columns, 32 indexes), and where in a slice those of a wave start for it: everything that is not the
+// lane's is a constant beside it.
+template <bool kLong, int kSize>
+__device__ __forceinline__ uint32_t fragments_at(int first, int lane)
+{
+    const int g = lane / 16, i = lane % 16;
+    if constexpr (kLong) return (first + i) * (kDepth * 2) + (g ^ (i & 7)) * 16;
+    const int r = g * 8 + i / 4;
+    return r * (kSize * 2) + ((first / 8 + i % 4 / 2) ^ across_swizzle(r)) * 16 + i % 2 * 8;
+}
+
 template <typename T, bool kLong, int kSize>
-__device__ __forceinline__ typename Chunk<T>::Vec fragment(const char* tile, int first, int half, int lane)
+__device__ __forceinline__ typename Chunk<T>::Vec fragment(const char* lds, uint32_t at, int half, int no)
 {
     typedef typename Chunk<T>::Vec Vec;
-    const int g = lane / 16, i = lane % 16;
     if constexpr (kLong) {
-        const int row = first + i;
-        return *reinterpret_cast<const Vec*>(tile + row * (kDepth * 2) + ((half * 4 + g) ^ (row & 7)) * 16);
+        return *reinterpret_cast<const Vec*>(lds + (at ^ half * 64) + no * (16 * kDepth * 2));
     } else {
         typedef short s16x4 __attribute__((ext_vector_type(4)));
         typedef __attribute__((address_space(3))) s16x4 Lds4;
         union { s16x4 part[2]; Vec all; } v;
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            const int r = half * 32 + g * 8 + h * 4 + i / 4;
-            const int chunk = (first / 8 + i % 4 / 2) ^ across_swizzle(r);
-            v.part[h] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lds4*)(tile + r * (kSize * 2) + chunk * 16 + i % 2 * 8));
-        }
+        for (int h = 0; h < 2; ++h)
+            v.part[h] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lds4*)(lds + (at ^ no * 32) + (half * 32 + h * 4) * (kSize * 2)));
         return v.all;
     }
 }
 
-// Where a lane fetches its share of an operand's tiles from, one tile of the reduction after the other.
-template <typename T, bool kLong, int kSize, int kWaves>
-struct Source {
-    static constexpr int kLoads = kSize * kDepth * 2 / 1024 / kWaves;      // of a wave, 1 KB each
-    static constexpr int kPerRow = kSize / 8;                              // across: pieces of 16 bytes
-    const char* at[kLoads];
-    int64_t step;      // bytes from one tile to the next
-
-    // The number within the tile of what load i of a lane brings: across its index, long its row; and its piece of 16 bytes.
-    static __device__ __forceinline__ int line(int i, int wave, int lane)
-    {
-        const int no = (wave * kLoads + i) * kWave + lane;
-        return kLong ? no / 8 : no / kPerRow;
-    }
+// A lane's share of an operand's slice: load i of a wave, 1 KB each, brings line(i) (the reduction's index across, the row
+// else), its piece(i) of 16 bytes.
+template <bool kLong, int kSize>
+struct Share {
+    static constexpr int kLoads = kSize * kDepth * 2 / 1024 / kWaves;
+    static constexpr int kPerLine = kLong ? 8 : kSize / 8;
+    static constexpr int kLines = kWave / kPerLine;      // of a load
+    static __device__ __forceinline__ int line(int i, int wave, int lane) { return ((wave * kLoads + i) * kWave + lane) / kPerLine; }
     static __device__ __forceinline__ int piece(int i, int wave, int lane)
     {
-        const int no = (wave * kLoads + i) * kWave + lane;
-        return kLong ? no % 8 ^ (no / 8 & 7) : no % kPerRow ^ across_swizzle(no / kPerRow);
+        const int l = line(i, wave, lane);
+        return lane % kPerLine ^ (kLong ? l & 7 : across_swizzle(l));
     }
-
-    // left: indexes of the reduction from this tile on
-    __device__ __forceinline__ void fetch(char* tile, int64_t left, int wave, int lane)
+    // whether it is past the end of a reduction of which `left` indexes are left
+    static __device__ __forceinline__ bool past(int i, int wave, int lane, int64_t left)
     {
-#pragma unroll
-        for (int i = 0; i < kLoads; ++i) {
-            const char* from = at[i];
-            if (left < kDepth && (kLong ? piece(i, wave, lane) * 8 : line(i, wave, lane)) >= left) from = reinterpret_cast<const char*>(&kZeros);
-            fetch16(from, tile + (wave * kLoads + i) * 1024);
-            at[i] += step;
-        }
+        return (kLong ? piece(i, wave, lane) * 8 : line(i, wave, lane)) >= left;
     }
 };
 
-template <typename T, Product kProduct, int kRows, int kCols, int kWavesP, int kWavesQ>
-__global__ __launch_bounds__(kWavesP * kWavesQ * kWave, kWavesP * kWavesQ / 4) void k_linear_tiles(LinearArgs a)
+// acc += a * b with the sums where the compiler leaves them alone: there are as many as there are registers of their kind, and it moves them about.
+__device__ __forceinline__ void mfma_in_place(f32x4& acc, bf16x8 a, bf16x8 b)
 {
-    constexpr int kWaves = kWavesP * kWavesQ, kP = kRows / kWavesP / 16, kQ = kCols / kWavesQ / 16;      // fragments of a wave
-    constexpr bool kPLong = kProduct != kByWeight, kQLong = kProduct == kForward;
-    constexpr int kPBytes = kRows * kDepth * 2, kBytes = (kRows + kCols) * kDepth * 2;
-    typedef typename Chunk<T>::Vec Vec;
-    __shared__ __attribute__((aligned(1024))) char lds[2 * kBytes];
+    asm volatile("v_mfma_f32_16x16x32_bf16 %0, %1, %2, %0" : "+a"(acc) : "v"(a), "v"(b));
+}
+__device__ __forceinline__ void mfma_in_place(f32x4& acc, f16x8 a, f16x8 b)
+{
+    asm volatile("v_mfma_f32_16x16x32_f16 %0, %1, %2, %0" : "+a"(acc) : "v"(a), "v"(b));
+}
 
-    const int tid = threadIdx.x, lane = tid % kWave, wave = __builtin_amdgcn_readfirstlane(tid / kWave);
+// An expert's range and its tiles, by lane, where a wave has a lane for each (kept from tile to tile).
+struct Ranges {
+    int lo, hi, tiles, end;      // `end`: tiles up to and with this expert's
+};
+
+struct Tile {
+    int e, p_n, q0, q_n;
+    int64_t p0, lo, depth;      // rows from p0 on (positions, or by weight output features); the reduction's start, by weight, and length
+};
+
+template <typename T, Product kProduct, int kSize>
+__global__ __launch_bounds__(kWaves * kWave, kSize > 128 ? 1 : 2) void k_linear_tiles(LinearArgs a)
+{
+    constexpr int kFrag = kSize / 2 / 16;      // fragments of a wave, either way
+    constexpr bool kPLong = kProduct != kByWeight, kQLong = kProduct == kForward;
+    constexpr int kSlotBytes = kSize * kDepth * 2;
+    typedef typename Chunk<T>::Vec Vec;
+    typedef Share<kPLong, kSize> ShareP;
+    typedef Share<kQLong, kSize> ShareQ;
+    constexpr int kLoads = ShareP::kLoads;
+    __shared__ __attribute__((aligned(1024))) char lds[kSlots * kSlotBytes];
+
+    const int lane = threadIdx.x % kWave, wave = uniform((int)threadIdx.x / kWave);
     const T* const x = static_cast<const T*>(a.x);
     const T* const dz = static_cast<const T*>(a.dz);
-    const int I = a.n_in, O = a.n_out;
+    const int I = a.n_in, O = a.n_out, width = kProduct == kForward ? O : I;
+    const uint32_t lds_base = uniform((int)(uint32_t)(uintptr_t)(LdsChar*)lds) + wave * kLoads * 1024;
 
-    const int col_tile = blockIdx.x % a.tiles;
-    const int64_t row_no = blockIdx.x / a.tiles;
-    int e;
-    int64_t p0, lo = 0, depth;
-    int p_n, q0 = col_tile * kCols, q_n;
-    if constexpr (kProduct == kByWeight) {
-        const int tiles = (O + kRows - 1) / kRows;
-        e = (int)(row_no / tiles);
-        p0 = (row_no - (int64_t)e * tiles) * kRows;
-        p_n = O - p0 < kRows ? (int)(O - p0) : kRows;
-        q_n = I - q0 < kCols ? I - q0 : kCols;
-        lo = bound(a.off, e, a.n_expert, a.n_pos);
-        depth = bound(a.off, e + 1, a.n_expert, a.n_pos) - lo;
-    } else {
-        const RowTile t = row_tile<kRows>(a, row_no);
-        if (t.hi <= t.lo) return;
-        e = t.expert;
-        p0 = t.lo;
-        p_n = (int)(t.hi - t.lo);
-        const int width = kProduct == kForward ? O : I;
-        q_n = width - q0 < kCols ? width - q0 : kCols;
-        depth = e == a.n_expert ? 0 : kProduct == kForward ? I : O;
-    }
-    const T* const w = static_cast<const T*>(a.w) + (kProduct == kByWeight || e == a.n_expert ? 0 : (int64_t)e * O * I);
-
-    // (rows and columns past the edge are fetched from within it: what becomes of them is not stored)
-    Source<T, kPLong, kRows, kWaves> from_p;
-    Source<T, kQLong, kCols, kWaves> from_q;
-#pragma unroll
-    for (int i = 0; i < from_p.kLoads; ++i) {
-        const int line = from_p.line(i, wave, lane), piece = from_p.piece(i, wave, lane);
-        const T* at;
-        if constexpr (kPLong) {
-            const int64_t p = p0 + (line < p_n ? line : p_n - 1);
-            at = (kProduct == kForward ? x + (e < a.n_expert ? row_of(a, p) : 0) * I : dz + p * O) + piece * 8;
-        } else {
-            at = dz + (lo + line) * O + p0 + (piece * 8 < p_n ? piece * 8 : 0);
-        }
-        from_p.at[i] = reinterpret_cast<const char*>(at);
-    }
-    from_p.step = kPLong ? kDepth * 2 : (int64_t)kDepth * 2 * O;
-    int64_t next[from_q.kLoads];      // by weight: rows of x of the next tile
-#pragma unroll
-    for (int i = 0; i < from_q.kLoads; ++i) {
-        const int line = from_q.line(i, wave, lane), piece = from_q.piece(i, wave, lane);
-        const T* at;
-        if constexpr (kQLong) at = w + (int64_t)(q0 + (line < q_n ? line : q_n - 1)) * I + piece * 8;
-        else at = (kProduct == kByInput ? w + (int64_t)line * I : x) + q0 + (piece * 8 < q_n ? piece * 8 : 0);
-        from_q.at[i] = reinterpret_cast<const char*>(at);
-    }
-    from_q.step = kQLong ? kDepth * 2 : kProduct == kByInput ? (int64_t)kDepth * 2 * I : 0;
-    const auto look_up = [&](int64_t r0) {
-#pragma unroll
-        for (int i = 0; i < from_q.kLoads; ++i) {
-            const int64_t r = r0 + from_q.line(i, wave, lane);
-            next[i] = r < depth ? row_of(a, lo + r) * I * 2 : 0;
-        }
-    };
-    const auto fetch = [&](int64_t r0, char* to) {
-        from_p.fetch(to, depth - r0, wave, lane);
-        if constexpr (kProduct == kByWeight) {
-            Source<T, kQLong, kCols, kWaves> now = from_q;
-#pragma unroll
-            for (int i = 0; i < from_q.kLoads; ++i) now.at[i] += next[i];
-            now.fetch(to + kPBytes, depth - r0, wave, lane);
-            look_up(r0 + kDepth);
-        } else {
-            from_q.fetch(to + kPBytes, depth - r0, wave, lane);
-        }
+    // The lane's number, anew: what is made of it is not kept over the products, whose registers are all there are.
+    const auto lane_now = [&]() __attribute__((always_inline)) {
+        int l = lane;
+        asm volatile("" : "+v"(l));
+        return l;
     };
 
-    f32x4 acc[kP][kQ] = {};
-    const int wp = wave / kWavesQ * (kP * 16), wq = wave % kWavesQ * (kQ * 16);
-    if (depth > 0) {
-        if constexpr (kProduct == kByWeight) look_up(0);
-        fetch(0, lds);
-    }
-    int turn = 0;
-    for (int64_t r0 = 0; r0 < depth; r0 += kDepth, turn ^= 1) {
-        // this tile is there, and the one before has been read
-        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
-        if (r0 + kDepth < depth) fetch(r0 + kDepth, lds + (turn ^ 1) * kBytes);
-        const char* const tile = lds + turn * kBytes;
-#pragma unroll
-        for (int half = 0; half < 2; ++half) {
-            Vec p[kP], q[kQ];
-#pragma unroll
-            for (int j = 0; j < kQ; ++j) q[j] = fragment<T, kQLong, kCols>(tile + kPBytes, wq + j * 16, half, lane);
-#pragma unroll
-            for (int i = 0; i < kP; ++i) p[i] = fragment<T, kPLong, kRows>(tile, wp + i * 16, half, lane);
-#pragma unroll
-            for (int i = 0; i < kP; ++i)
-#pragma unroll
-                for (int j = 0; j < kQ; ++j) acc[i][j] = mfma(q[j], p[i], acc[i][j]);
-        }
-    }
-
-    const int width = kProduct == kForward ? O : I;
-    T* const out = static_cast<T*>(a.out) + ((kProduct == kByWeight ? (int64_t)e * O : 0) + p0) * width + q0;
-    const T* const bias = kProduct == kForward && a.bias && e < a.n_expert ? static_cast<const T*>(a.bias) + (int64_t)e * O + q0 : nullptr;
-    typedef T Four __attribute__((ext_vector_type(4)));
-#pragma unroll
-    for (int j = 0; j < kQ; ++j) {
-        const int col = wq + j * 16 + lane / 16 * 4;
-        if (col >= q_n) continue;
-        float b[4] = {};
-        if (bias)
-#pragma unroll
-            for (int k = 0; k < 4; ++k) b[k] = (float)bias[col + k];
-#pragma unroll
-        for (int i = 0; i < kP; ++i) {
-            const int row = wp + i * 16 + lane % 16;
-            if (row >= p_n) continue;
-            Four o;
-#pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                float v = acc[i][j][k] + b[k];
-                if (kProduct == kForward && a.relu && v < 0) v = 0;
-                o[k] = (T)v;
+    // ---- which tiles
+    Ranges mine{};
+    int64_t down = a.down;
+    const bool by_lane = a.n_expert < kWave;
+    if constexpr (kProduct != kByWeight) {
+        if (by_lane) {
+            if (lane <= a.n_expert) {
+                mine.lo = (int)bound(a.off, lane, a.n_expert, a.n_pos);
+                mine.hi = lane < a.n_expert ? (int)bound(a.off, lane + 1, a.n_expert, a.n_pos) : (int)a.n_pos;
             }
-            *reinterpret_cast<Four*>(out + (int64_t)row * width + col) = o;
+            mine.tiles = mine.hi > mine.lo ? (mine.hi - mine.lo + kSize - 1) / kSize : 0;
+            mine.end = mine.tiles;
+            for (int d = 1; d < kWave; d *= 2) {
+                const int o = __shfl_up(mine.end, d);
+                if (lane >= d) mine.end += o;
+            }
+            down = __builtin_amdgcn_readlane(mine.end, kWave - 1);
         }
+    }
+    const auto find = [&](int64_t j, Tile& t) __attribute__((always_inline)) {
+        const TileNo no = tile_no(j, down, a.tiles, a.block);
+        if (no.row < 0) return false;
+        t.q0 = no.col * kSize;
+        t.q_n = width - t.q0 < kSize ? width - t.q0 : kSize;
+        t.lo = 0;
+        if constexpr (kProduct == kByWeight) {
+            const int tiles = (O + kSize - 1) / kSize;
+            t.e = (int)(no.row / tiles);
+            t.p0 = (no.row - (int64_t)t.e * tiles) * kSize;
+            t.p_n = O - t.p0 < kSize ? (int)(O - t.p0) : kSize;
+            t.lo = uniform(bound(a.off, t.e, a.n_expert, a.n_pos));
+            t.depth = uniform(bound(a.off, t.e + 1, a.n_expert, a.n_pos)) - t.lo;
+        } else {
+            RowTile r{a.n_expert, 0, 0};
+            if (by_lane) {
+                const unsigned long long here = __ballot(no.row >= mine.end - mine.tiles && no.row < mine.end);
+                if (here) {
+                    const int l = __ffsll((long long)here) - 1;
+                    const int64_t first = __builtin_amdgcn_readlane(mine.lo, l) + (no.row - (__builtin_amdgcn_readlane(mine.end, l) - __builtin_amdgcn_readlane(mine.tiles, l))) * kSize;
+                    const int64_t last = __builtin_amdgcn_readlane(mine.hi, l);
+                    r = {l, first, first + kSize < last ? first + kSize : last};
+                }
+            } else {
+                r = row_tile<kSize>(a, no.row);
+            }
+            t.e = uniform(r.expert);
+            t.p0 = uniform(r.lo);
+            t.p_n = uniform((int)(r.hi - r.lo));
+            t.depth = t.e == a.n_expert || t.p_n <= 0 ? 0 : kProduct == kForward ? I : O;
+        }
+        return true;
+    };
+
+    // ---- where their slices come from: an address of the wave's that moves on from slice to slice, and a lane's offset to it; but rows of x are a
+    // lane's own.  (Rows and columns past the edge are fetched from within it: what becomes of them is not stored.)
+    const char *base_p = nullptr, *base_q = nullptr;
+    const int64_t step_p = kPLong ? kDepth * 2 : (int64_t)kDepth * 2 * O, step_q = kQLong ? kDepth * 2 : (int64_t)kDepth * 2 * I;
+    uint32_t off_p[kLoads], off_q[kLoads];
+    const char* x_at[kLoads];      // forward: a lane's rows of x; by weight: those of a slice
+    int x_row[kLoads];             // forward: the rows of the next tile
+    const auto look_up = [&](const Tile& t) __attribute__((always_inline)) {
+        const int lane = lane_now();
+        if constexpr (kProduct == kForward)
+#pragma unroll
+            for (int i = 0; i < kLoads; ++i) {
+                const int line = ShareP::line(i, wave, lane);
+                x_row[i] = t.depth > 0 ? (int)row_of(a, t.p0 + (line < t.p_n ? line : t.p_n - 1)) : 0;
+            }
+    };
+    const auto aim = [&](const Tile& t) __attribute__((always_inline)) {
+        const int lane = lane_now();
+        const T* const w = static_cast<const T*>(a.w) + (t.depth > 0 ? (int64_t)t.e * O * I : 0);
+        if constexpr (kProduct == kForward) base_q = reinterpret_cast<const char*>(w + (int64_t)t.q0 * I);
+        if constexpr (kProduct == kByInput) {
+            base_p = reinterpret_cast<const char*>(dz + t.p0 * O);
+            base_q = reinterpret_cast<const char*>(w + t.q0);
+        }
+        if constexpr (kProduct == kByWeight) {
+            base_p = reinterpret_cast<const char*>(dz + t.lo * O + t.p0);
+            base_q = reinterpret_cast<const char*>(x + t.q0);
+        }
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i) {
+            const int line = ShareP::line(i, wave, lane), piece = ShareP::piece(i, wave, lane), row = line < t.p_n ? line : t.p_n - 1;
+            if constexpr (kProduct == kForward) x_at[i] = reinterpret_cast<const char*>(x + (int64_t)x_row[i] * I + piece * 8);
+            if constexpr (kProduct == kByInput) off_p[i] = (uint32_t)row * O * 2 + piece * 16;
+            if constexpr (kProduct == kByWeight) off_p[i] = (uint32_t)line * O * 2 + (piece * 8 < t.p_n ? piece * 16 : 0);
+        }
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i) {
+            const int line = ShareQ::line(i, wave, lane), piece = ShareQ::piece(i, wave, lane);
+            if constexpr (kProduct == kForward) off_q[i] = (uint32_t)(line < t.q_n ? line : t.q_n - 1) * I * 2 + piece * 16;
+            if constexpr (kProduct == kByInput) off_q[i] = (uint32_t)line * I * 2 + (piece * 8 < t.q_n ? piece * 16 : 0);
+            if constexpr (kProduct == kByWeight) off_q[i] = piece * 8 < t.q_n ? piece * 16 : 0;
+        }
+    };
+    // By weight: the rows of x of 16 slices, a wave's lines of four slices in a register; a slice's are handed to the lanes that fetch them.
+    constexpr int kLinesOfWave = kDepth / kWaves, kRowRegs = 16 * kLinesOfWave / kWave;
+    int rows[kRowRegs], rows_later[kRowRegs];
+    const auto load_rows = [&](int (&to)[kRowRegs], int64_t p) __attribute__((always_inline)) {
+        const int lane = lane_now();
+#pragma unroll
+        for (int r = 0; r < kRowRegs; ++r) {
+            const int line = r * kWave + lane;
+            int64_t at = p + line / kLinesOfWave * kDepth + wave * kLinesOfWave + line % kLinesOfWave;
+            if (at >= a.n_pos) at = a.n_pos - 1;
+            uint32_t s = a.slot ? (uint32_t)a.slot[at] : (uint32_t)at;
+            if (s >= a.n_pos) s = (uint32_t)a.n_pos - 1;
+            if (a.slot) s = (a.k_mul ? __umulhi(s, a.k_mul) : s) >> a.k_shift;
+            to[r] = (int)s;
+        }
+    };
+    const auto aim_rows = [&](int slice) __attribute__((always_inline)) {
+        constexpr int kOfReg = kWave / kLinesOfWave;
+        const int lane = lane_now(), c = slice % 16;
+        int from = rows[0];
+#pragma unroll
+        for (int r = 1; r < kRowRegs; ++r) from = c / kOfReg == r ? rows[r] : from;
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i) {
+            const int row = __builtin_amdgcn_ds_bpermute((c % kOfReg * kLinesOfWave + i * ShareQ::kLines + lane / ShareQ::kPerLine) * 4, from);
+            x_at[i] = base_q + ((uint64_t)(uint32_t)row * ((uint32_t)I * 2) + off_q[i]);
+        }
+    };
+    // what slice `slice` of a tile needs of them (the first 16 are there)
+    const auto turn_rows = [&](const Tile& t, int slice) __attribute__((always_inline)) {
+        if (slice % 16 == 8) load_rows(rows_later, t.lo + (int64_t)(slice / 16 + 1) * (16 * kDepth));
+        if (slice % 16 == 0)
+#pragma unroll
+            for (int r = 0; r < kRowRegs; ++r) rows[r] = rows_later[r];
+        aim_rows(slice);
+    };
+
+    const char* const zeros = reinterpret_cast<const char*>(&kZeros);
+    const auto fetch_p = [&](int i, uint32_t slot, int64_t left, bool whole) __attribute__((always_inline)) {
+        const uint32_t to = lds_base + slot + i * 1024;
+        if constexpr (kProduct == kForward) {
+            fetch16(!whole && ShareP::past(i, wave, lane_now(), left) ? zeros : x_at[i], to);
+            x_at[i] += kDepth * 2;
+        } else if (whole) {
+            fetch16(base_p, off_p[i], to);
+        } else {
+            fetch16(ShareP::past(i, wave, lane_now(), left) ? zeros : base_p + off_p[i], to);
+        }
+        if (i == kLoads - 1) base_p += step_p;
+    };
+    const auto fetch_q = [&](int i, uint32_t slot, int64_t left, bool whole) __attribute__((always_inline)) {
+        const uint32_t to = lds_base + slot + i * 1024;
+        if constexpr (kProduct == kByWeight) {
+            fetch16(!whole && ShareQ::past(i, wave, lane_now(), left) ? zeros : x_at[i], to);
+        } else if (whole) {
+            fetch16(base_q, off_q[i], to);
+        } else {
+            fetch16(ShareQ::past(i, wave, lane_now(), left) ? zeros : base_q + off_q[i], to);
+        }
+        if (kProduct != kByWeight && i == kLoads - 1) base_q += step_q;
+    };
+
+    // ---- multiplication.  A slice is multiplied in two halves of its depth.  While one is multiplied the other is read from shared memory, a fragment
+    // after every few products.  Between them the slice has been read whole, and the next one has to be there.  Of five places in shared memory the
+    // operands of a slice take two; in the first half the left operand two slices on is asked for, in the second the right one, a load
+    // after every eight products: more at a time than memory's queue takes would hold the products up.
+    constexpr int kGroups = 2 * kFrag;
+    f32x4 acc[kFrag][kFrag];
+    const int wp = wave / 2 * (kSize / 2), wq = wave % 2 * (kSize / 2);
+    const uint32_t p_at = fragments_at<kPLong, kSize>(wp, lane), q_at = fragments_at<kQLong, kSize>(wq, lane);
+    Vec p[2][kFrag], q[2][kFrag];
+    const auto read = [&](uint32_t slot_p, uint32_t slot_q, int half, int no) __attribute__((always_inline)) {
+        if (no < kFrag) q[half][no] = fragment<T, kQLong, kSize>(lds, q_at + slot_q, half, no);
+        else p[half][no - kFrag] = fragment<T, kPLong, kSize>(lds, p_at + slot_p, half, no - kFrag);
+    };
+    // `fetch(g)` is called before the products of group g
+    const auto multiply = [&](int half, bool reads, uint32_t slot_p, uint32_t slot_q, auto fetch) __attribute__((always_inline)) {
+#pragma unroll
+        for (int g = 0; g < kGroups; ++g) {
+            __builtin_amdgcn_sched_barrier(0);
+            if (reads) read(slot_p, slot_q, half ^ 1, g);
+            fetch(g);
+            asm volatile("s_nop 1");      // (between what the vector unit has written and a product that might read it)
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int j = 0; j < kFrag / 2; ++j) {
+                const int col = g % 2 * (kFrag / 2) + j;
+                mfma_in_place(acc[g / 2][col], q[half][col], p[half][g / 2]);
+            }
+        }
+        __builtin_amdgcn_sched_barrier(0);
+    };
+    const auto settle = [&]() __attribute__((always_inline)) {      // (products write their sums some cycles after they are issued)
+        asm volatile("s_nop 15\n\ts_nop 15" ::: "memory");
+#pragma unroll
+        for (int i = 0; i < kFrag; ++i)
+#pragma unroll
+            for (int j = 0; j < kFrag; ++j) asm volatile("" : "+a"(acc[i][j]));
+    };
+    // (through a descriptor, whose bounds drop what is past the edge: the same stores whatever the tile's size)
+    const auto store = [&](const Tile& t) __attribute__((always_inline)) {
+        typedef T Four __attribute__((ext_vector_type(4)));
+        typedef uint32_t Two __attribute__((ext_vector_type(2)));
+        constexpr uint32_t kNowhere = ~0u;
+        T* const out = static_cast<T*>(a.out) + ((kProduct == kByWeight ? (int64_t)t.e * O : 0) + t.p0) * width + t.q0;
+        const int lane = lane_now();
+        const __amdgpu_buffer_rsrc_t to = __builtin_amdgcn_make_buffer_rsrc(out, 0, 0x7fffffff, 0x00027000);
+        const bool biased = kProduct == kForward && a.bias && t.e < a.n_expert;
+        const T* const bias = static_cast<const T*>(a.bias) + (int64_t)t.e * O + t.q0;
+#pragma unroll
+        for (int j = 0; j < kFrag; ++j) {
+            const int col = wq + j * 16 + lane / 16 * 4;
+            float b[4] = {};
+            if (biased && col < t.q_n) {
+                const Four v = *reinterpret_cast<const Four*>(bias + col);
+#pragma unroll
+                for (int k = 0; k < 4; ++k) b[k] = (float)v[k];
+            }
+#pragma unroll
+            for (int i = 0; i < kFrag; ++i) {
+                const int row = wp + i * 16 + lane % 16;
+                union { Four value; Two bits; } o;
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    float v = acc[i][j][k] + b[k];
+                    if (kProduct == kForward && a.relu && v < 0) v = 0;
+                    o.value[k] = (T)v;
+                }
+                __builtin_amdgcn_raw_buffer_store_b64(o.bits, to, row < t.p_n && col < t.q_n ? (uint32_t)(row * width + col) * 2 : kNowhere, 0, 0);
+            }
+        }
+    };
+
+    constexpr uint32_t kRing = kSlots * kSlotBytes;
+    const auto further = [](uint32_t slot) { return slot + 2 * kSlotBytes < kRing ? slot + 2 * kSlotBytes : slot + 2 * kSlotBytes - kRing; };
+    const auto after = [](uint32_t slot) { return slot + kSlotBytes < kRing ? slot + kSlotBytes : 0; };
+    const auto nothing = [](int) {};
+
+    // The first two slices of a tile, into the first four places: part g of kGroups.
+    const auto begin = [&](const Tile& t, int g) __attribute__((always_inline)) {
+        constexpr int kEach = 4 * kLoads / kGroups;
+#pragma unroll
+        for (int l = g * kEach; l < (g + 1) * kEach; ++l) {
+            const int slice = l / (2 * kLoads), in = l % (2 * kLoads);
+            const int64_t left = t.depth - slice * kDepth;
+            if (kProduct == kByWeight && in == 0) aim_rows(slice);
+            if (in < kLoads) fetch_p(in, slice * 2 * kSlotBytes, left, false);
+            else fetch_q(in - kLoads, (slice * 2 + 1) * kSlotBytes, left, false);
+        }
+    };
+
+    Tile now, then;
+    int64_t j = blockIdx.x;
+    if (!find(j, now)) return;
+    look_up(now);
+    if constexpr (kProduct == kByWeight) load_rows(rows, now.lo);
+    aim(now);
+#pragma unroll
+    for (int g = 0; g < kGroups; ++g) begin(now, g);
+    bool behind = false;      // whether a tile's stores are behind those loads
+    for (;;) {
+        j += gridDim.x;
+        const bool more = find(j, then);
+        if (!more) then = Tile{0, 1, 0, 8, 0, 0, 0};      // (nothing is fetched of a tile without depth)
+        look_up(then);
+#pragma unroll
+        for (int i = 0; i < kFrag; ++i)
+#pragma unroll
+            for (int k = 0; k < kFrag; ++k) acc[i][k] = f32x4{0, 0, 0, 0};
+        settle();
+        const int slices = (int)((now.depth + kDepth - 1) / kDepth), whole = (int)(now.depth / kDepth);
+        if (slices > 0) {
+            // the first slice: behind it there may be the second, and the stores
+            constexpr int kStores = kFrag * kFrag;
+            if (slices == 1) asm volatile("s_waitcnt vmcnt(0)\n\ts_barrier" ::: "memory");
+            else if (behind) asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" ::"n"(2 * kLoads + kStores < 63 ? 2 * kLoads + kStores : 63) : "memory");
+            else asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" ::"n"(2 * kLoads) : "memory");
+#pragma unroll
+            for (int no = 0; no < 2 * kFrag; ++no) read(0, kSlotBytes, 0, no);
+            uint32_t slot = 0;      // of the left operand of slice s; the right one's is the next
+            int s = 0;
+            for (; s + 2 < whole; ++s) {
+                const uint32_t next = further(slot), far = further(next);
+                multiply(0, true, slot, after(slot), [&](int g) __attribute__((always_inline)) {
+                    if (g % (kGroups / kLoads) == 0) fetch_p(g / (kGroups / kLoads), far, 0, true);
+                });
+                asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(kLoads) : "memory");
+                if constexpr (kProduct == kByWeight) turn_rows(now, s + 2);
+                multiply(1, true, next, after(next), [&](int g) __attribute__((always_inline)) {
+                    if (g % (kGroups / kLoads) == 0) fetch_q(g / (kGroups / kLoads), after(far), 0, true);
+                });
+                slot = next;
+            }
+            for (; s + 1 < slices; ++s) {
+                const uint32_t next = further(slot), far = further(next);
+                const int64_t left = now.depth - (int64_t)(s + 2) * kDepth;
+                if (left > 0)
+#pragma unroll
+                    for (int i = 0; i < kLoads; ++i) fetch_p(i, far, left, false);
+                multiply(0, true, slot, after(slot), nothing);
+                if (left > 0) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(kLoads) : "memory");
+                else asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+                if (left > 0) {
+                    if constexpr (kProduct == kByWeight) turn_rows(now, s + 2);
+#pragma unroll
+                    for (int i = 0; i < kLoads; ++i) fetch_q(i, after(far), left, false);
+                }
+                multiply(1, true, next, after(next), nothing);
+                slot = next;
+            }
+            multiply(0, true, slot, after(slot), nothing);
+            asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+        }
+        // (shared memory has been read to the end by all waves)
+        aim(then);
+        if constexpr (kProduct == kByWeight) load_rows(rows, then.lo);
+        if (slices > 0) {
+            multiply(1, false, 0, 0, [&](int g) __attribute__((always_inline)) { begin(then, g); });
+        } else {
+#pragma unroll
+            for (int g = 0; g < kGroups; ++g) begin(then, g);
+        }
+        settle();
+        store(now);
+        if (!more) break;
+        behind = true;
+        now = then;
+    }
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+}
+
+// dz = dy where y > 0, and its sums over blocks of rows, no block reaching from one expert's range into the next: one pass over dy and y.
+// A thread takes N neighbouring columns of every (kBlock >> lg)-th row of the block.
+template <typename T, int N>
+struct Piece {
+    typedef T Vec __attribute__((ext_vector_type(N)));
+};
+template <typename T>
+struct Piece<T, 1> {
+    struct Vec {
+        T v;
+        __device__ T& operator[](int) { return v; }
+        __device__ T operator[](int) const { return v; }
+    };
+};
+
+struct SumArgs {
+    const int* off;
+    const void *y, *dy;
+    void *dz, *db;
+    float* parts;      // [blocks of rows][columns]; null: no sums
+    int64_t n_pos;
+    int n_expert, width, first, cols;      // columns first .. first + cols - 1
+    int lg, across, rows;                  // lanes across, workgroups across, rows of a block
+};
+
+// Rows of block t (see row_tile; here all blocks of an expert have the same number of rows but the last).
+__device__ __forceinline__ RowTile row_block(const int* off, int n_expert, int64_t n_pos, int rows, int64_t t)
+{
+    int64_t before = 0;
+    for (int e = 0; e <= n_expert; ++e) {
+        const int64_t lo = bound(off, e, n_expert, n_pos), hi = e < n_expert ? bound(off, e + 1, n_expert, n_pos) : n_pos;
+        const int64_t own = hi > lo ? (hi - lo + rows - 1) / rows : 0;
+        if (t < before + own) {
+            const int64_t first = lo + (t - before) * rows;
+            return {e, first, first + rows < hi ? first + rows : hi};
+        }
+        before += own;
+    }
+    return {n_expert, 0, 0};
+}
+
+template <typename T, int N>
+__global__ __launch_bounds__(kBlock) void k_unrelu_sums(SumArgs a)
+{
+    typedef typename Piece<T, N>::Vec Vec;
+    __shared__ float part[kBlock * N];
+    const int64_t t = blockIdx.x / a.across;
+    const RowTile r = row_block(a.off, a.n_expert, a.n_pos, a.rows, t);
+    const int lane = threadIdx.x & ((1 << a.lg) - 1), group = threadIdx.x >> a.lg, groups = kBlock >> a.lg;
+    const int c = ((int)(blockIdx.x % a.across) << a.lg | lane) * N;
+    const bool in = c < a.cols;
+    float sum[N] = {};
+    if (in) {
+        const int64_t at = a.first + c;
+        for (int64_t p = r.lo + group; p < r.hi; p += groups) {
+            Vec d = *reinterpret_cast<const Vec*>(static_cast<const T*>(a.dy) + p * a.width + at);
+            if (a.y) {
+                const Vec v = *reinterpret_cast<const Vec*>(static_cast<const T*>(a.y) + p * a.width + at);
+#pragma unroll
+                for (int n = 0; n < N; ++n) d[n] = (float)v[n] > 0 ? d[n] : (T)0.0f;
+                *reinterpret_cast<Vec*>(static_cast<T*>(a.dz) + p * a.width + at) = d;
+            }
+#pragma unroll
+            for (int n = 0; n < N; ++n) sum[n] += (float)d[n];
+        }
+    }
+    if (!a.parts || r.expert == a.n_expert) return;
+#pragma unroll
+    for (int n = 0; n < N; ++n) part[threadIdx.x * N + n] = sum[n];
+    __syncthreads();
+    if (group > 0 || !in) return;
+#pragma unroll
+    for (int n = 0; n < N; ++n) {
+        for (int g = 1; g < groups; ++g) sum[n] += part[(g << a.lg | lane) * N + n];
+        a.parts[t * a.cols + c + n] = sum[n];
     }
 }
 
-// dz = dy where y > 0; rows without an expert are rows as any other (no product reads them).
+// The sums over an expert's blocks: 32 columns a workgroup, eight threads a column.
 template <typename T>
-__global__ __launch_bounds__(kBlock) void k_unrelu(const T* y, const T* dy, T* dz, int64_t count, int64_t chunks)
+__global__ __launch_bounds__(kBlock) void k_sum_blocks(SumArgs a)
 {
-    typedef typename Chunk<T>::Vec Vec;
-    constexpr int n = Chunk<T>::n;
-    const int64_t stride = (int64_t)gridDim.x * kBlock, from = (int64_t)blockIdx.x * kBlock + threadIdx.x;
-    for (int64_t i = from; i < chunks; i += stride) {
-        const Vec v = reinterpret_cast<const Vec*>(y)[i];
-        Vec d = reinterpret_cast<const Vec*>(dy)[i];
-#pragma unroll
-        for (int j = 0; j < n; ++j) d[j] = (float)v[j] > 0 ? d[j] : (T)0.0f;
-        reinterpret_cast<Vec*>(dz)[i] = d;
+    __shared__ float part[kBlock];
+    const int across = (a.cols + 31) / 32, e = blockIdx.x / across, c = blockIdx.x % across * 32 + threadIdx.x % 32;
+    int64_t before = 0, own = 0;
+    for (int i = 0; i <= e; ++i) {
+        const int64_t lo = bound(a.off, i, a.n_expert, a.n_pos), hi = bound(a.off, i + 1, a.n_expert, a.n_pos);
+        before += own;
+        own = hi > lo ? (hi - lo + a.rows - 1) / a.rows : 0;
     }
-    for (int64_t i = chunks * n + from; i < count; i += stride) dz[i] = (float)y[i] > 0 ? dy[i] : (T)0.0f;
+    float sum = 0;
+    if (c < a.cols)
+        for (int64_t t = threadIdx.x / 32; t < own; t += kBlock / 32) sum += a.parts[(before + t) * a.cols + c];
+    part[threadIdx.x] = sum;
+    __syncthreads();
+    if (threadIdx.x >= 32 || c >= a.cols) return;
+    for (int g = 1; g < kBlock / 32; ++g) sum += part[g * 32 + threadIdx.x];
+    static_cast<T*>(a.db)[(int64_t)e * a.width + a.first + c] = (T)sum;
 }
 
 int64_t row_tiles(const LinearIn& in, int rows)
@@ -478,8 +814,10 @@ int64_t row_tiles(const LinearIn& in, int rows)
 LinearArgs args_of(const LinearIn& in)
 {
     LinearArgs a{};
-    a.off = in.off; a.slot = in.slot; a.x = in.x; a.w = in.w; a.bias = in.bias; a.n_pos = in.n_pos;
+    a.off = in.off; a.slot = in.n_pos > 0 ? in.slot : nullptr; a.x = in.x; a.w = in.w; a.bias = in.bias; a.n_pos = in.n_pos;
     a.n_expert = in.off ? in.n_expert : 1; a.n_in = in.n_in; a.n_out = in.n_out; a.top_k = in.top_k; a.relu = in.relu;
+    while ((2 << a.k_shift) <= in.top_k) ++a.k_shift;
+    if (in.top_k & (in.top_k - 1)) a.k_mul = (uint32_t)(((uint64_t(1) << (32 + a.k_shift)) + in.top_k - 1) / in.top_k);
     return a;
 }
 
@@ -492,25 +830,56 @@ bool in_tiles(const LinearIn& in, const void* a, const void* b, const void* c)
     return sizeof(T) == 2 && in.n_in % 8 == 0 && in.n_out % 8 == 0 && aligned16(a) && aligned16(b) && aligned16(c);
 }
 
+constexpr int kUnits = 256;      // compute units: workgroups of large tiles that run at a time
+
 template <typename T, Product kProduct>
 void product(const LinearIn& in, LinearArgs a, bool tiles, hipStream_t s)
 {
-    constexpr int kRows = 256, kCols = 256;
     const int width = kProduct == kForward ? in.n_out : in.n_in;
-    const auto grid = [&](int rows, int cols) {
-        a.tiles = tiles_of(width, cols);
-        const int64_t down = kProduct == kByWeight ? (int64_t)a.n_expert * tiles_of(in.n_out, rows) : row_tiles(in, rows);
-        return (unsigned)(down * a.tiles);
+    const auto grid = [&](int size) {
+        a.tiles = tiles_of(width, size);
+        a.block = a.tiles < 8 ? 8 : 4;
+        a.down = kProduct == kByWeight ? (int64_t)a.n_expert * tiles_of(in.n_out, size) : row_tiles(in, size);
+        const int64_t all = a.down * a.tiles, round = all < kDies * kTogether ? kDies : kDies * kTogether;
+        return (all + round - 1) / round * round;
     };
     if constexpr (sizeof(T) == 2) {
         if (tiles) {
-            const unsigned n = grid(kRows, kCols);
-            k_linear_tiles<T, kProduct, kRows, kCols, 2, 4><<<n, 512, 0, s>>>(a);
+            const int64_t n = grid(256);
+            k_linear_tiles<T, kProduct, 256><<<(unsigned)(n < kUnits ? n : kUnits), kWaves * kWave, 0, s>>>(a);
             return;
         }
     }
-    const unsigned n = grid(kAnyTile, kAnyTile);
-    k_linear_any<T, kProduct><<<n, kBlock, 0, s>>>(a);
+    k_linear_any<T, kProduct><<<(unsigned)grid(kAnyTile), kBlock, 0, s>>>(a);
+}
+
+// dz and db
+template <typename T>
+void unrelu_sums(gr_experts* h, const LinearIn& in, void* dz, void* db, hipStream_t s)
+{
+    constexpr int64_t kMost = 1024;      // blocks of rows, but for what a range does not fill
+    SumArgs a{};
+    a.off = in.off; a.y = in.y; a.dy = in.dy; a.dz = dz; a.db = db; a.n_pos = in.n_pos;
+    a.n_expert = in.off ? in.n_expert : 1; a.width = in.n_out;
+    const bool chunks = in.n_out % Chunk<T>::n == 0 && (!in.y || (aligned16(in.y) && aligned16(dz))) && aligned16(in.dy);
+    const int n = chunks ? Chunk<T>::n : 1;
+    a.rows = in.n_pos > 128 * kMost ? (int)((in.n_pos + kMost - 1) / kMost) : 128;
+    const int64_t blocks = row_tiles(in, a.rows) + 1;      // (one more: no positions and no experts leave none)
+    const int64_t fit = (int64_t)kPartFloats / blocks / Chunk<T>::n * Chunk<T>::n;
+    const int most = fit < in.n_out ? (int)fit : in.n_out;      // columns whose parts there is room for
+    for (a.first = 0; a.first < in.n_out; a.first += most) {
+        a.cols = in.n_out - a.first < most ? in.n_out - a.first : most;
+        a.parts = db ? h->parts : nullptr;
+        const int pieces = (a.cols + n - 1) / n;
+        a.lg = 0;
+        while ((1 << a.lg) < pieces && a.lg < 5) ++a.lg;
+        a.across = ((pieces - 1) >> a.lg) + 1;
+        if (in.n_pos > 0) {
+            if (chunks) k_unrelu_sums<T, Chunk<T>::n><<<blocks * a.across, kBlock, 0, s>>>(a);
+            else k_unrelu_sums<T, 1><<<blocks * a.across, kBlock, 0, s>>>(a);
+        }
+        if (db) k_sum_blocks<T><<<a.n_expert * ((a.cols + 31) / 32), kBlock, 0, s>>>(a);
+    }
 }
 
 }  // namespace
@@ -526,36 +895,21 @@ int launch_linear(gr_experts*, const LinearIn& in, int dtype, void* out_y, hipSt
     });
 }
 
-int launch_linear_backward(gr_experts*, const LinearIn& in, int dtype, void* dz, void* dx, void* dw, void* db, hipStream_t s)
+int launch_linear_backward(gr_experts* h, const LinearIn& in, int dtype, void* dz, void* dx, void* dw, void* db, hipStream_t s)
 {
     return by_type(dtype, [&](auto t) {
         typedef decltype(t) T;
         LinearArgs a = args_of(in);
         a.dz = in.dy;
-        if (in.y && in.n_pos > 0) {
-            const int64_t count = in.n_pos * in.n_out;
-            const int64_t chunks = aligned16(in.y) && aligned16(in.dy) && aligned16(dz) ? count / Chunk<T>::n : 0;
-            const int64_t blocks = ((chunks ? chunks : count) + kBlock - 1) / kBlock;
-            k_unrelu<T><<<blocks < 4096 ? blocks : 4096, kBlock, 0, s>>>(static_cast<const T*>(in.y), static_cast<const T*>(in.dy),
-                                                                         static_cast<T*>(dz), count, chunks);
-            a.dz = dz;
-        }
+        if (db || (in.y && in.n_pos > 0)) unrelu_sums<T>(h, in, dz, db, s);
+        if (in.y) a.dz = dz;
         if (dx && in.n_pos > 0) {
             a.out = dx;
             product<T, kByInput>(in, a, in_tiles<T>(in, a.dz, in.w, dx), s);
         }
-        if (dw || db) {
+        if (dw) {
             a.out = dw;
-            a.db = db;
-            const bool tiles = dw && in_tiles<T>(in, a.dz, in.x, dw);
-            if (tiles) {
-                product<T, kByWeight>(in, a, true, s);
-                a.out = nullptr;
-            }
-            if (!tiles || db) {
-                a.tiles = a.out ? tiles_of(in.n_in, kAnyTile) : 1;
-                k_linear_any<T, kByWeight><<<(int64_t)a.n_expert * tiles_of(in.n_out, kAnyTile) * a.tiles, kBlock, 0, s>>>(a);
-            }
+            product<T, kByWeight>(in, a, in_tiles<T>(in, a.dz, in.x, dw), s);
         }
         return launched();
     });
