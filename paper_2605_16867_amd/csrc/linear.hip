@@ -4,6 +4,8 @@
 //   forward   y[p, n]  = sum over k of x[row(p), k] * W_e[n, k]        p in the range of e
 //   by input  dx[p, k] = sum over n of dz[p, n] * W_e[n, k]            p in the range of e
 //   by weight dW_e[n, k] = sum over p in the range of e of dz[p, n] * x[row(p), k]
+#include <type_traits>
+
 #include "experts.h"
 
 namespace gr {
@@ -23,6 +25,8 @@ struct LinearArgs {
     int tiles;      // in the direction of columns
     int64_t down;   // and of rows
     int block;      // rows of tiles taken together
+    int parts_n;    // by weight: parts of an expert's positions that are summed apart,
+    float* parts;   // and where: [parts_n][n_expert][n_out][n_in]
     uint32_t k_mul;      // slot / top_k: the upper half of slot * k_mul (the slot itself for 0), by 2^k_shift
     int k_shift;
 };
@@ -122,21 +126,19 @@ __device__ __forceinline__ f32x4 mfma(f16x8 a, f16x8 b, f32x4 acc) { return __bu
 
 // ---- any sizes, any alignment -------------------------------------------------------------------
 //
-// Tiles of 128 rows by 128 columns, 64 bytes of the reduction at a time, loaded element by element into registers while the
+// Tiles of kTile by kTile, 64 bytes of the reduction at a time, loaded element by element into registers while the
 // tile before is multiplied, and laid into shared memory with the reduction contiguous.
-
-constexpr int kAnyTile = 128;
 
 template <typename T>
 constexpr int kAnyDepth = 64 / sizeof(T);
 
-template <typename T, Product kProduct>
+template <typename T, Product kProduct, int kTile>
 __global__ __launch_bounds__(kBlock) void k_linear_any(LinearArgs a)
 {
-    constexpr int D = kAnyDepth<T>, kLd = D + Chunk<T>::n, kPer = kAnyTile * D / kBlock;
+    constexpr int D = kAnyDepth<T>, kLd = D + Chunk<T>::n, kPer = kTile * D / kBlock;
     typedef typename Chunk<T>::Vec Vec;
     constexpr int n = Chunk<T>::n;
-    __shared__ __attribute__((aligned(16))) T lds_p[kAnyTile * kLd], lds_q[kAnyTile * kLd];
+    __shared__ __attribute__((aligned(16))) T lds_p[kTile * kLd], lds_q[kTile * kLd];
 
     const int tid = threadIdx.x, lane = tid % kWave, wave = tid / kWave;
     const TileNo no = tile_no(blockIdx.x, a.down, a.tiles, a.block);
@@ -149,23 +151,23 @@ __global__ __launch_bounds__(kBlock) void k_linear_any(LinearArgs a)
     // the output's rows p0 .. p0 + p_n - 1 (positions, or output features of an expert), columns q0 .. q0 + q_n - 1
     int e;
     int64_t p0, lo = 0, depth;
-    int p_n, q0 = no.col * kAnyTile, q_n;
+    int p_n, q0 = no.col * kTile, q_n;
     if constexpr (kProduct == kByWeight) {
-        const int tiles = (O + kAnyTile - 1) / kAnyTile;
+        const int tiles = (O + kTile - 1) / kTile;
         e = (int)(row_no / tiles);
-        p0 = (row_no - (int64_t)e * tiles) * kAnyTile;
-        p_n = O - p0 < kAnyTile ? (int)(O - p0) : kAnyTile;
-        q_n = I - q0 < kAnyTile ? I - q0 : kAnyTile;
+        p0 = (row_no - (int64_t)e * tiles) * kTile;
+        p_n = O - p0 < kTile ? (int)(O - p0) : kTile;
+        q_n = I - q0 < kTile ? I - q0 : kTile;
         lo = bound(a.off, e, a.n_expert, a.n_pos);
         depth = bound(a.off, e + 1, a.n_expert, a.n_pos) - lo;
     } else {
-        const RowTile t = row_tile<kAnyTile>(a, row_no);
+        const RowTile t = row_tile<kTile>(a, row_no);
         if (t.hi <= t.lo) return;
         e = t.expert;
         p0 = t.lo;
         p_n = (int)(t.hi - t.lo);
         const int width = kProduct == kForward ? O : I;
-        q_n = width - q0 < kAnyTile ? width - q0 : kAnyTile;
+        q_n = width - q0 < kTile ? width - q0 : kTile;
         depth = e == a.n_expert ? 0 : kProduct == kForward ? I : O;
     }
     const T* const w = static_cast<const T*>(a.w) + (kProduct == kByWeight || e == a.n_expert ? 0 : (int64_t)e * O * I);
@@ -175,7 +177,7 @@ __global__ __launch_bounds__(kBlock) void k_linear_any(LinearArgs a)
     const auto place = [&](bool along, int i, int& row, int& r) {
         const int at = i * kBlock + tid;
         if (along) { row = at / D; r = at % D; }
-        else { r = at / kAnyTile; row = at % kAnyTile; }
+        else { r = at / kTile; row = at % kTile; }
     };
     int64_t p_row[kPer];      // where the rows of the left operand start
 #pragma unroll
@@ -206,8 +208,9 @@ __global__ __launch_bounds__(kBlock) void k_linear_any(LinearArgs a)
         }
     };
 
-    f32x4 acc[4][4] = {};
-    const int wp = (wave / 2) * 64, wq = (wave % 2) * 64;      // a wave's 64 by 64
+    constexpr int kFrag = kTile / 32;      // fragments of a wave, either way
+    f32x4 acc[kFrag][kFrag] = {};
+    const int wp = wave / 2 * (kTile / 2), wq = wave % 2 * (kTile / 2);
     if (depth > 0) load(0);
     for (int64_t r0 = 0; r0 < depth; r0 += D) {
         __syncthreads();
@@ -221,27 +224,27 @@ __global__ __launch_bounds__(kBlock) void k_linear_any(LinearArgs a)
         }
         __syncthreads();
         if (r0 + D < depth) load(r0 + D);
-        Vec p[4], q[4];
+        Vec p[kFrag], q[kFrag];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
+        for (int i = 0; i < kFrag; ++i) {
             p[i] = *reinterpret_cast<const Vec*>(&lds_p[(wp + i * 16 + lane % 16) * kLd + lane / 16 * n]);
             q[i] = *reinterpret_cast<const Vec*>(&lds_q[(wq + i * 16 + lane % 16) * kLd + lane / 16 * n]);
         }
         // (columns as the first operand: a lane then holds four neighbours of a row)
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
+        for (int i = 0; i < kFrag; ++i)
 #pragma unroll
-            for (int j = 0; j < 4; ++j) acc[i][j] = mfma(q[j], p[i], acc[i][j]);
+            for (int j = 0; j < kFrag; ++j) acc[i][j] = mfma(q[j], p[i], acc[i][j]);
     }
     const int width = kProduct == kForward ? O : I;
     T* const out = static_cast<T*>(a.out) + ((kProduct == kByWeight ? (int64_t)e * O : 0) + p0) * width + q0;
     const T* const bias = kProduct == kForward && a.bias && e < a.n_expert ? static_cast<const T*>(a.bias) + (int64_t)e * O + q0 : nullptr;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
+    for (int i = 0; i < kFrag; ++i) {
         const int row = wp + i * 16 + lane % 16;
         if (row >= p_n) continue;
 #pragma unroll
-        for (int j = 0; j < 4; ++j)
+        for (int j = 0; j < kFrag; ++j)
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
                 const int col = wq + j * 16 + lane / 16 * 4 + k;
@@ -350,11 +353,11 @@ struct Ranges {
 };
 
 struct Tile {
-    int e, p_n, q0, q_n;
+    int e, part, p_n, q0, q_n;
     int64_t p0, lo, depth;      // rows from p0 on (positions, or by weight output features); the reduction's start, by weight, and length
 };
 
-template <typename T, Product kProduct, int kSize>
+template <typename T, Product kProduct, int kSize, bool kParts>
 __global__ __launch_bounds__(kWaves * kWave, kSize > 128 ? 1 : 2) void k_linear_tiles(LinearArgs a)
 {
     constexpr int kFrag = kSize / 2 / 16;      // fragments of a wave, either way
@@ -405,12 +408,16 @@ __global__ __launch_bounds__(kWaves * kWave, kSize > 128 ? 1 : 2) void k_linear_
         t.q_n = width - t.q0 < kSize ? width - t.q0 : kSize;
         t.lo = 0;
         if constexpr (kProduct == kByWeight) {
-            const int tiles = (O + kSize - 1) / kSize;
-            t.e = (int)(no.row / tiles);
-            t.p0 = (no.row - (int64_t)t.e * tiles) * kSize;
+            const int tiles = (O + kSize - 1) / kSize, part = (int)(no.row / tiles);
+            t.e = part / a.parts_n;
+            t.part = part - t.e * a.parts_n;
+            t.p0 = (no.row - (int64_t)part * tiles) * kSize;
             t.p_n = O - t.p0 < kSize ? (int)(O - t.p0) : kSize;
-            t.lo = uniform(bound(a.off, t.e, a.n_expert, a.n_pos));
-            t.depth = uniform(bound(a.off, t.e + 1, a.n_expert, a.n_pos)) - t.lo;
+            const int64_t from = uniform(bound(a.off, t.e, a.n_expert, a.n_pos)), until = uniform(bound(a.off, t.e + 1, a.n_expert, a.n_pos));
+            const int64_t slices = (until - from + kDepth - 1) / kDepth, each = (slices + a.parts_n - 1) / a.parts_n * kDepth;
+            t.lo = from + t.part * each;
+            t.depth = until - t.lo < each ? until - t.lo : each;
+            if (t.depth < 0) t.depth = 0;
         } else {
             RowTile r{a.n_expert, 0, 0};
             if (by_lane) {
@@ -477,8 +484,10 @@ __global__ __launch_bounds__(kWaves * kWave, kSize > 128 ? 1 : 2) void k_linear_
     };
     // By weight: the rows of x of 16 slices, a wave's lines of four slices in a register; a slice's are handed to the lanes that fetch them.
     constexpr int kLinesOfWave = kDepth / kWaves, kRowRegs = 16 * kLinesOfWave / kWave;
-    int rows[kRowRegs], rows_later[kRowRegs];
-    const auto load_rows = [&](int (&to)[kRowRegs], int64_t p) __attribute__((always_inline)) {
+    typedef int RowRegs __attribute__((ext_vector_type(kRowRegs)));
+    RowRegs rows{}, rows_later{};
+    const auto load_rows = [&](int64_t p) __attribute__((always_inline)) {
+        RowRegs to;
         const int lane = lane_now();
 #pragma unroll
         for (int r = 0; r < kRowRegs; ++r) {
@@ -490,6 +499,7 @@ __global__ __launch_bounds__(kWaves * kWave, kSize > 128 ? 1 : 2) void k_linear_
             if (a.slot) s = (a.k_mul ? __umulhi(s, a.k_mul) : s) >> a.k_shift;
             to[r] = (int)s;
         }
+        return to;
     };
     const auto aim_rows = [&](int slice) __attribute__((always_inline)) {
         constexpr int kOfReg = kWave / kLinesOfWave;
@@ -505,10 +515,8 @@ __global__ __launch_bounds__(kWaves * kWave, kSize > 128 ? 1 : 2) void k_linear_
     };
     // what slice `slice` of a tile needs of them (the first 16 are there)
     const auto turn_rows = [&](const Tile& t, int slice) __attribute__((always_inline)) {
-        if (slice % 16 == 8) load_rows(rows_later, t.lo + (int64_t)(slice / 16 + 1) * (16 * kDepth));
-        if (slice % 16 == 0)
-#pragma unroll
-            for (int r = 0; r < kRowRegs; ++r) rows[r] = rows_later[r];
+        if (slice % 16 == 8) rows_later = load_rows(t.lo + (int64_t)(slice / 16 + 1) * (16 * kDepth));
+        if (slice % 16 == 0) rows = rows_later;
         aim_rows(slice);
     };
 
@@ -579,7 +587,9 @@ __global__ __launch_bounds__(kWaves * kWave, kSize > 128 ? 1 : 2) void k_linear_
         typedef T Four __attribute__((ext_vector_type(4)));
         typedef uint32_t Two __attribute__((ext_vector_type(2)));
         constexpr uint32_t kNowhere = ~0u;
-        T* const out = static_cast<T*>(a.out) + ((kProduct == kByWeight ? (int64_t)t.e * O : 0) + t.p0) * width + t.q0;
+        typedef std::conditional_t<kParts, float, T> Out;
+        const int64_t first = kProduct == kByWeight ? ((int64_t)t.part * a.n_expert + t.e) * O : 0;
+        Out* const out = (kParts ? reinterpret_cast<Out*>(a.parts) : static_cast<Out*>(a.out)) + (first + t.p0) * width + t.q0;
         const int lane = lane_now();
         const __amdgpu_buffer_rsrc_t to = __builtin_amdgcn_make_buffer_rsrc(out, 0, 0x7fffffff, 0x00027000);
         const bool biased = kProduct == kForward && a.bias && t.e < a.n_expert;
@@ -596,14 +606,22 @@ __global__ __launch_bounds__(kWaves * kWave, kSize > 128 ? 1 : 2) void k_linear_
 #pragma unroll
             for (int i = 0; i < kFrag; ++i) {
                 const int row = wp + i * 16 + lane % 16;
-                union { Four value; Two bits; } o;
+                const uint32_t at = row < t.p_n && col < t.q_n ? (uint32_t)(row * width + col) * (uint32_t)sizeof(Out) : kNowhere;
+                if constexpr (kParts) {
+                    typedef uint32_t Bits __attribute__((ext_vector_type(4)));
+                    union { f32x4 value; Bits bits; } o;
+                    o.value = acc[i][j];
+                    __builtin_amdgcn_raw_buffer_store_b128(o.bits, to, at, 0, 0);
+                } else {
+                    union { Four value; Two bits; } o;
 #pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                    float v = acc[i][j][k] + b[k];
-                    if (kProduct == kForward && a.relu && v < 0) v = 0;
-                    o.value[k] = (T)v;
+                    for (int k = 0; k < 4; ++k) {
+                        float v = acc[i][j][k] + b[k];
+                        if (kProduct == kForward && a.relu && v < 0) v = 0;
+                        o.value[k] = (T)v;
+                    }
+                    __builtin_amdgcn_raw_buffer_store_b64(o.bits, to, at, 0, 0);
                 }
-                __builtin_amdgcn_raw_buffer_store_b64(o.bits, to, row < t.p_n && col < t.q_n ? (uint32_t)(row * width + col) * 2 : kNowhere, 0, 0);
             }
         }
     };
@@ -630,7 +648,7 @@ __global__ __launch_bounds__(kWaves * kWave, kSize > 128 ? 1 : 2) void k_linear_
     int64_t j = blockIdx.x;
     if (!find(j, now)) return;
     look_up(now);
-    if constexpr (kProduct == kByWeight) load_rows(rows, now.lo);
+    if constexpr (kProduct == kByWeight) rows = load_rows(now.lo);
     aim(now);
 #pragma unroll
     for (int g = 0; g < kGroups; ++g) begin(now, g);
@@ -638,7 +656,7 @@ __global__ __launch_bounds__(kWaves * kWave, kSize > 128 ? 1 : 2) void k_linear_
     for (;;) {
         j += gridDim.x;
         const bool more = find(j, then);
-        if (!more) then = Tile{0, 1, 0, 8, 0, 0, 0};      // (nothing is fetched of a tile without depth)
+        if (!more) then = Tile{0, 0, 1, 0, 8, 0, 0, 0};      // (nothing is fetched of a tile without depth)
         look_up(then);
 #pragma unroll
         for (int i = 0; i < kFrag; ++i)
@@ -690,7 +708,7 @@ __global__ __launch_bounds__(kWaves * kWave, kSize > 128 ? 1 : 2) void k_linear_
         }
         // (shared memory has been read to the end by all waves)
         aim(then);
-        if constexpr (kProduct == kByWeight) load_rows(rows, then.lo);
+        if constexpr (kProduct == kByWeight) rows = load_rows(then.lo);
         if (slices > 0) {
             multiply(1, false, 0, 0, [&](int g) __attribute__((always_inline)) { begin(then, g); });
         } else {
@@ -704,6 +722,78 @@ __global__ __launch_bounds__(kWaves * kWave, kSize > 128 ? 1 : 2) void k_linear_
         now = then;
     }
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+}
+
+// The parts of sums, added in their order.
+template <typename T>
+__global__ __launch_bounds__(kBlock) void k_join(const float* parts, int n, int64_t count, T* out)
+{
+    const int64_t i = ((int64_t)blockIdx.x * kBlock + threadIdx.x) * 4;      // (both widths are multiples of 8)
+    if (i >= count) return;
+    f32x4 sum = *reinterpret_cast<const f32x4*>(parts + i);
+    for (int k = 1; k < n; ++k) sum += *reinterpret_cast<const f32x4*>(parts + k * count + i);
+    typedef T Four __attribute__((ext_vector_type(4)));
+    Four o;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) o[k] = (T)sum[k];
+    *reinterpret_cast<Four*>(out + i) = o;
+}
+
+// ---- few rows an expert ------------------------------------------------------------------------
+//
+// Bound by reading the weights, each once: a workgroup takes 16 output features of an expert, its waves a part of the reduction each, straight from memory
+// into registers; their sums meet in shared memory.  Rows of x are taken 16 at a time.
+
+constexpr int kFewWaves = 4, kFewDepth = 32, kFewAhead = 8;      // indexes of a product; products asked for together
+
+template <typename T>
+__global__ __launch_bounds__(kFewWaves * kWave) void k_linear_few(LinearArgs a)
+{
+    typedef typename Chunk<T>::Vec Vec;
+    __shared__ f32x4 sums[kFewWaves - 1][kWave];
+    const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave, g = lane / 16, i = lane % 16;
+    const int e = blockIdx.x / a.tiles, n0 = blockIdx.x % a.tiles * 16, I = a.n_in, O = a.n_out;
+    const int64_t lo = bound(a.off, e, a.n_expert, a.n_pos), hi = e < a.n_expert ? bound(a.off, e + 1, a.n_expert, a.n_pos) : a.n_pos;
+    const T* const w = static_cast<const T*>(a.w) + ((int64_t)(e < a.n_expert ? e : 0) * O + (n0 + i < O ? n0 + i : O - 1)) * I + g * 8;
+    const int products = e < a.n_expert ? (I + kFewDepth - 1) / kFewDepth : 0, each = (products + kFewWaves - 1) / kFewWaves;
+    const int from = wave * each, until = from + each < products ? from + each : products;
+    for (int64_t p0 = lo; p0 < hi; p0 += 16) {
+        const int64_t p = p0 + i < hi ? p0 + i : hi - 1;
+        const T* const x = static_cast<const T*>(a.x) + (e < a.n_expert ? row_of(a, p) : 0) * I + g * 8;
+        f32x4 acc = {0, 0, 0, 0};
+        for (int d = from; d < until; d += kFewAhead) {
+            Vec wv[kFewAhead], xv[kFewAhead];
+#pragma unroll
+            for (int k = 0; k < kFewAhead; ++k) {
+                wv[k] = xv[k] = Vec{};
+                if (d + k < until && (d + k) * kFewDepth + g * 8 < I) {
+                    wv[k] = *reinterpret_cast<const Vec*>(w + (int64_t)(d + k) * kFewDepth);
+                    xv[k] = *reinterpret_cast<const Vec*>(x + (int64_t)(d + k) * kFewDepth);
+                }
+            }
+#pragma unroll
+            for (int k = 0; k < kFewAhead; ++k) acc = mfma(wv[k], xv[k], acc);
+        }
+        if (wave > 0) sums[wave - 1][lane] = acc;
+        __syncthreads();
+        if (wave == 0) {
+#pragma unroll
+            for (int k = 0; k < kFewWaves - 1; ++k) acc += sums[k][lane];
+            const int n = n0 + g * 4;
+            if (p0 + i < hi && n < O) {
+                typedef T Four __attribute__((ext_vector_type(4)));
+                Four o;
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    float v = acc[k] + (a.bias && e < a.n_expert ? (float)static_cast<const T*>(a.bias)[(int64_t)e * O + n + k] : 0.0f);
+                    if (a.relu && v < 0) v = 0;
+                    o[k] = (T)v;
+                }
+                *reinterpret_cast<Four*>(static_cast<T*>(a.out) + (p0 + i) * O + n) = o;
+            }
+        }
+        __syncthreads();
+    }
 }
 
 // dz = dy where y > 0, and its sums over blocks of rows, no block reaching from one expert's range into the next: one pass over dy and y.
@@ -830,27 +920,65 @@ bool in_tiles(const LinearIn& in, const void* a, const void* b, const void* c)
     return sizeof(T) == 2 && in.n_in % 8 == 0 && in.n_out % 8 == 0 && aligned16(a) && aligned16(b) && aligned16(c);
 }
 
-constexpr int kUnits = 256;      // compute units: workgroups of large tiles that run at a time
+// Which form a product takes (bfloat16, 9 experts, before / after the change of form):
+constexpr int kUnits = 256;          // compute units: workgroups of large tiles that run at a time
+// Large tiles from four rounds of them on.  Forward, 128 / 256: 8 192 x 4 096 -> 1 024 (165 tiles) 93 / 101 us, 65 536 x 1 024 -> 512 (530) 85 / 104,
+// 65 536 x 4 096 -> 1 024 (1 060) 607 / 535; by input 65 536 x 1 024 -> 512 (1 060) 111 / 112, 65 536 x 1 024 -> 4 096 (4 240) 703 / 614.
+constexpr int kLargeRounds = 4;
+constexpr int kAnyRounds = 4;        // the same of the tiles for any sizes: 4 099 x 2 positions, 1 023 -> 511, single precision, 128 / 64: 180 / 130 us
+// Few rows: up to 16 an expert on average, 256 in all (an expert may have them all, and its weights are read again for every 16).
+// 4 096 -> 1 024, tiles / this: 9 positions 39 / 17 us, 72 39 / 21, 144 39 / 36, 288 38 / 59.
+constexpr int kFewRows = 16, kFewExperts = 16;
+// By weight, where the tiles are fewer than two rounds: as many parts of the positions as fill those, of at least 1 024 positions each.
+// One part / several: 131 072 x 512 -> 128 (36 tiles) 279 / 56 us, 65 536 x 1 024 -> 512 (288) 172 / 137, 16 384 x 1 024 -> 512 50 / 52.
+constexpr int kPartRounds = 2, kPartRows = 1024;
 
 template <typename T, Product kProduct>
-void product(const LinearIn& in, LinearArgs a, bool tiles, hipStream_t s)
+void product(gr_experts* h, const LinearIn& in, LinearArgs a, bool tiles, hipStream_t s)
 {
     const int width = kProduct == kForward ? in.n_out : in.n_in;
+    a.parts_n = 1;
     const auto grid = [&](int size) {
         a.tiles = tiles_of(width, size);
         a.block = a.tiles < 8 ? 8 : 4;
-        a.down = kProduct == kByWeight ? (int64_t)a.n_expert * tiles_of(in.n_out, size) : row_tiles(in, size);
+        a.down = kProduct == kByWeight ? (int64_t)a.n_expert * tiles_of(in.n_out, size) * a.parts_n : row_tiles(in, size);
         const int64_t all = a.down * a.tiles, round = all < kDies * kTogether ? kDies : kDies * kTogether;
         return (all + round - 1) / round * round;
     };
     if constexpr (sizeof(T) == 2) {
         if (tiles) {
-            const int64_t n = grid(256);
-            k_linear_tiles<T, kProduct, 256><<<(unsigned)(n < kUnits ? n : kUnits), kWaves * kWave, 0, s>>>(a);
+            if constexpr (kProduct == kForward) {
+                if (in.n_pos <= kFewRows * (a.n_expert < kFewExperts ? a.n_expert : kFewExperts)) {
+                    a.tiles = tiles_of(width, 16);
+                    k_linear_few<T><<<(a.n_expert + 1) * a.tiles, kFewWaves * kWave, 0, s>>>(a);
+                    return;
+                }
+            }
+            if (grid(256) >= kLargeRounds * kUnits) {
+                k_linear_tiles<T, kProduct, 256, false><<<kUnits, kWaves * kWave, 0, s>>>(a);
+                return;
+            }
+            int64_t n = grid(128);
+            if constexpr (kProduct == kByWeight) {
+                const int64_t one = (int64_t)a.n_expert * in.n_out * in.n_in, fit = (int64_t)kPartFloats / one;
+                int64_t parts = 2 * kUnits * kPartRounds / n;
+                if (parts > fit) parts = fit;
+                if (parts > in.n_pos / a.n_expert / kPartRows) parts = in.n_pos / a.n_expert / kPartRows;
+                if (parts > 1) {
+                    a.parts_n = (int)parts;
+                    a.parts = h->parts;
+                    n = grid(128);
+                    k_linear_tiles<T, kProduct, 128, true><<<(unsigned)(n < 2 * kUnits ? n : 2 * kUnits), kWaves * kWave, 0, s>>>(a);
+                    k_join<T><<<(unsigned)((one / 4 + kBlock - 1) / kBlock), kBlock, 0, s>>>(h->parts, a.parts_n, one, static_cast<T*>(a.out));
+                    return;
+                }
+            }
+            k_linear_tiles<T, kProduct, 128, false><<<(unsigned)(n < 2 * kUnits ? n : 2 * kUnits), kWaves * kWave, 0, s>>>(a);
             return;
         }
     }
-    k_linear_any<T, kProduct><<<(unsigned)grid(kAnyTile), kBlock, 0, s>>>(a);
+    if (grid(128) >= kAnyRounds * kUnits) k_linear_any<T, kProduct, 128><<<(unsigned)grid(128), kBlock, 0, s>>>(a);
+    else k_linear_any<T, kProduct, 64><<<(unsigned)grid(64), kBlock, 0, s>>>(a);
 }
 
 // dz and db
@@ -884,13 +1012,13 @@ void unrelu_sums(gr_experts* h, const LinearIn& in, void* dz, void* db, hipStrea
 
 }  // namespace
 
-int launch_linear(gr_experts*, const LinearIn& in, int dtype, void* out_y, hipStream_t s)
+int launch_linear(gr_experts* h, const LinearIn& in, int dtype, void* out_y, hipStream_t s)
 {
     LinearArgs a = args_of(in);
     a.out = out_y;
     return by_type(dtype, [&](auto t) {
         typedef decltype(t) T;
-        product<T, kForward>(in, a, in_tiles<T>(in, in.x, in.w, out_y), s);
+        product<T, kForward>(h, in, a, in_tiles<T>(in, in.x, in.w, out_y), s);
         return launched();
     });
 }
@@ -905,11 +1033,11 @@ int launch_linear_backward(gr_experts* h, const LinearIn& in, int dtype, void* d
         if (in.y) a.dz = dz;
         if (dx && in.n_pos > 0) {
             a.out = dx;
-            product<T, kByInput>(in, a, in_tiles<T>(in, a.dz, in.w, dx), s);
+            product<T, kByInput>(h, in, a, in_tiles<T>(in, a.dz, in.w, dx), s);
         }
         if (dw) {
             a.out = dw;
-            product<T, kByWeight>(in, a, in_tiles<T>(in, a.dz, in.x, dw), s);
+            product<T, kByWeight>(h, in, a, in_tiles<T>(in, a.dz, in.x, dw), s);
         }
         return launched();
     });
