@@ -12,15 +12,14 @@
 struct gr_experts {
     int n_expert = 0, max_top_k = 0;
     int64_t max_rows = 0, max_slots = 0;
-    int* counts = nullptr;       // [units of slots][n_expert + 1] slots of each expert, then those before the unit (see k_plan_*)
-    int* totals = nullptr;       // [n_expert + 1]
+    int* counts = nullptr;       // [n_expert + 1][units of slots] slots of each expert, then those before the unit; behind them those of all units (see k_plan_*)
     double* squares = nullptr;   // [kClipParts] sums of squares (see k_norm)
     float* parts = nullptr;      // [kPartFloats] parts of long sums (see k_linear_*)
 };
 
 namespace gr {
 
-constexpr int kPlanUnit = 1024;      // slots that one wave puts in order
+constexpr int kPlanUnit = 1024;      // slots of given experts that a workgroup puts in order
 constexpr size_t kPartFloats = size_t(16) << 20;
 constexpr int kClipBlocks = 1024;    // workgroups of a launch over gradients
 constexpr int kClipTensors = 96;     // gradients that one launch takes: their table is passed by value, 3 KB of the 4 that arguments may be
@@ -48,6 +47,23 @@ struct Chunk {
     typedef T Vec __attribute__((ext_vector_type(16 / sizeof(T))));
 };
 
+constexpr int kRouteBlock = 256, kLaneExperts = 16;      // threads of a workgroup of the choice; scores of a row that a lane holds
+
+// log2 of the lanes that share a row's scores
+inline int team_log(int n_expert)
+{
+    int lg = 0;
+    while ((kLaneExperts << lg) < n_expert) ++lg;
+    return lg;
+}
+
+// Most units of slots of a call: the choice's workgroups, or units of given experts.
+inline size_t plan_units(int n_expert, int64_t rows, int64_t slots)
+{
+    const int64_t of_rows = kRouteBlock >> team_log(n_expert), a = (rows + of_rows - 1) / of_rows, b = (slots + kPlanUnit - 1) / kPlanUnit;
+    return (size_t)(a > b ? a : b);
+}
+
 struct RouteIn {
     const void* logits;
     const float* bias;
@@ -56,7 +72,8 @@ struct RouteIn {
     float scale;
 };
 
-int launch_route(const RouteIn& in, int dtype, float* weight, int* expert, hipStream_t s);
+// off, slot, pos: null, or the order of the slots as well
+int launch_route(gr_experts* h, const RouteIn& in, int dtype, float* weight, int* expert, int* off, int* slot, int* pos, hipStream_t s);
 int launch_route_backward(const RouteIn& in, int dtype, const int* expert, const float* dweight, void* dlogits, hipStream_t s);
 int launch_plan(gr_experts* h, int64_t slots, const int* expert, int* off, int* slot, int* pos, hipStream_t s);
 int launch_combine(int64_t rows, int top_k, int width, int dtype, const float* weight, const int* pos, const void* y, void* out,

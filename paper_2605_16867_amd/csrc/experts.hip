@@ -1,49 +1,94 @@
 // The choice of experts, the order of their slots, and the weighted sum of their results (gfx950).
+#include <type_traits>
+
 #include "experts.h"
 
 namespace gr {
 namespace {
 
-constexpr int kBlock = 256;
+constexpr int kBlock = kRouteBlock;
 constexpr int kWave = 64;
-constexpr int kLaneExperts = 16;     // scores of a row that one lane holds
+constexpr int kPlanWaves = kBlock / kWave;
+constexpr int kScanBlock = 1024;
+constexpr int kFewUnits = 32;        // units of slots whose counts every workgroup adds up by itself
+
+// ---- within a team of lanes ----------------------------------------------------------------------
+//
+// 2^lg neighbouring lanes share a row.  Step m exchanges between halves of 2m lanes whose lanes all hold the same already, so which lane of the other half
+// is asked does not matter: within 16 lanes the register file's own permutations do.
+
+template <int kStep>
+__device__ __forceinline__ int other_half(int v)
+{
+    if constexpr (kStep == 1) return __builtin_amdgcn_mov_dpp(v, 0xB1, 0xF, 0xF, true);        // quad_perm 1 0 3 2
+    if constexpr (kStep == 2) return __builtin_amdgcn_mov_dpp(v, 0x4E, 0xF, 0xF, true);        // quad_perm 2 3 0 1
+    if constexpr (kStep == 4) return __builtin_amdgcn_mov_dpp(v, 0x141, 0xF, 0xF, true);       // row_half_mirror
+    if constexpr (kStep == 8) return __builtin_amdgcn_mov_dpp(v, 0x140, 0xF, 0xF, true);       // row_mirror
+    return __shfl_xor(v, kStep);
+}
+template <int kStep>
+__device__ __forceinline__ float other_half(float v) { return __int_as_float(other_half<kStep>(__float_as_int(v))); }
+template <int kStep>
+__device__ __forceinline__ double other_half(double v)
+{
+    return __hiloint2double(other_half<kStep>(__double2hiint(v)), other_half<kStep>(__double2loint(v)));
+}
+
+// `join` (a value, the other half's) at every step
+template <typename V, typename F>
+__device__ __forceinline__ V over_team(V v, int lg, F join)
+{
+    if (lg > 0) v = join(v, other_half<1>(v));
+    if (lg > 1) v = join(v, other_half<2>(v));
+    if (lg > 2) v = join(v, other_half<4>(v));
+    if (lg > 3) v = join(v, other_half<8>(v));
+    if (lg > 4) v = join(v, other_half<16>(v));
+    if (lg > 5) v = join(v, other_half<32>(v));
+    return v;
+}
+
+__device__ __forceinline__ float team_max(float v, int lg)
+{
+    return over_team(v, lg, [](float a, float b) { return __builtin_fmaxf(a, b); });
+}
+__device__ __forceinline__ float team_sum(float v, int lg)
+{
+    return over_team(v, lg, [](float a, float b) { return a + b; });
+}
 
 // ---- choice ------------------------------------------------------------------------------------
 //
 // A score and its expert are one number of 64 bits: a score in single precision leaves 29 bits of a double's mantissa
 // free, and the lowest nine take the expert, so that of two equal scores the lower index is the larger number.
-// The largest top_k of a list are then found with minima and maxima alone.
+// The largest top_k of a list are then found with minima and maxima alone: 2 top_k of them a score.
 constexpr double kNoExpert = -1.0e300;      // below every score
 
-__device__ __forceinline__ double key_of(float c, int e, bool masked)
+__device__ __forceinline__ double key_of(float c, int e)
 {
-    if (masked || c == -__builtin_inff()) return kNoExpert;
-    double d = (double)(c + 0.0f);            // (-0 counts as 0)
-    if (!(c == c)) d = -1.0e200;
-    if (c == __builtin_inff()) d = 1.0e200;
-    const int64_t b = __double_as_longlong(d);
-    return __longlong_as_double((b & ~int64_t(511)) | (b < 0 ? e : 511 - e));
+    const bool none = c == -__builtin_inff();
+    c = c == c ? c + 0.0f : -3.4028235e38f;                                    // (-0 counts as 0; no number is the least score)
+    const double d = (double)__builtin_fminf(c, 3.4028235e38f);
+    const int hi = __double2hiint(d), lo = __double2loint(d) | ((511 - e) ^ (hi >> 31 & 511));
+    return none ? kNoExpert : __hiloint2double(hi, lo);
 }
 
 __device__ __forceinline__ int expert_of(double key)
 {
-    const int64_t b = __double_as_longlong(key);
-    return key < -1.0e299 ? -1 : (int)(b & 511) ^ (b < 0 ? 0 : 511);
+    return key < -1.0e299 ? -1 : 511 - ((__double2loint(key) ^ __double2hiint(key) >> 31) & 511);
 }
 
-__device__ __forceinline__ float larger(float a, float b) { return __builtin_fmaxf(a, b); }
-
-// over the 2^lg lanes of a row's team
-__device__ __forceinline__ float team_max(float v, int lg)
+// (fmax and fmin would first quiet what might be a signalling not-a-number; keys are numbers)
+__device__ __forceinline__ double key_max(double a, double b)
 {
-    for (int m = 1; m < (1 << lg); m *= 2) v = larger(v, __shfl_xor(v, m));
-    return v;
+    double r;
+    asm("v_max_f64 %0, %1, %2" : "=v"(r) : "v"(a), "v"(b));
+    return r;
 }
-
-__device__ __forceinline__ float team_sum(float v, int lg)
+__device__ __forceinline__ double key_min(double a, double b)
 {
-    for (int m = 1; m < (1 << lg); m *= 2) v += __shfl_xor(v, m);
-    return v;
+    double r;
+    asm("v_min_f64 %0, %1, %2" : "=v"(r) : "v"(a), "v"(b));
+    return r;
 }
 
 // What turns a row's logits into its scores: softmax is exp(x - shift) * inv, sigmoid needs neither.
@@ -56,9 +101,9 @@ __device__ __forceinline__ Softmax softmax_of(const float (&x)[V], int lg)
 {
     float m = -__builtin_inff();
 #pragma unroll
-    for (int i = 0; i < V; ++i) m = larger(m, x[i]);
+    for (int i = 0; i < V; ++i) m = __builtin_fmaxf(m, x[i]);
     m = team_max(m, lg);
-    if (m == -__builtin_inff()) return {0.0f, 0.0f};       // (nothing but masked experts)
+    if (m == -__builtin_inff()) m = 0;       // (nothing but masked experts, whose scores are 0 whatever this is)
     float sum = 0;
 #pragma unroll
     for (int i = 0; i < V; ++i) sum += expf(x[i] - m);
@@ -96,12 +141,28 @@ __device__ __forceinline__ void load_row(float (&x)[V], const T* row, int first,
     for (int i = 0; i < V; ++i) x[i] = first + i < n_expert ? (float)row[first + i] : -__builtin_inff();
 }
 
+// The order of slots (see below), as far as a workgroup has a part in it.
+struct PlanArgs {
+    const int* expert;
+    int* counts;      // [n_expert + 1][units]
+    int *off, *slot, *pos;
+    int64_t slots;
+    int n_expert, units, per_unit;      // slots of a unit, of the last one fewer
+    int summed;                         // counts are those of the units before, the last column's successor those of all
+};
+
+__device__ __forceinline__ int bin_of(int e, int n_expert) { return (unsigned)e < (unsigned)n_expert ? e : n_expert; }
+
+template <typename F>
+__device__ void place_unit(const PlanArgs& a, int unit, int (*hist)[GR_MAX_EXPERTS + 1], F expert_at);
+
 struct RouteArgs {
     RouteIn in;
     float* weight;
     int* expert;
     int lg;          // log2 of the lanes per row
     int whole;       // rows are whole chunks of a lane, 16 bytes aligned
+    PlanArgs plan;   // units 0: no order is asked for
 };
 
 template <typename T, int K, bool kSigmoid, bool kGroups>
@@ -111,7 +172,7 @@ __global__ __launch_bounds__(kBlock) void k_route(RouteArgs a)
     const int lg = a.lg, team = 1 << lg, lane = threadIdx.x & (team - 1);
     const int64_t row = ((int64_t)blockIdx.x * kBlock + threadIdx.x) >> lg;
     const bool there = row < a.in.rows;
-    const int E = a.in.n_expert, first = lane * V;
+    const int E = a.in.n_expert, k = a.in.top_k, first = lane * V;
     const T* const at = static_cast<const T*>(a.in.logits) + (there ? row : 0) * E;
 
     float x[V];
@@ -122,8 +183,8 @@ __global__ __launch_bounds__(kBlock) void k_route(RouteArgs a)
     float c[V];
 #pragma unroll
     for (int i = 0; i < V; ++i) {
-        const bool masked = x[i] == -__builtin_inff();
-        c[i] = masked ? x[i] : score_of<kSigmoid>(x[i], sm) + (a.in.bias ? a.in.bias[first + i] : 0.0f);
+        const float s = score_of<kSigmoid>(x[i], sm) + (a.in.bias && first + i < E ? a.in.bias[first + i] : 0.0f);
+        c[i] = x[i] == -__builtin_inff() ? x[i] : s;
     }
 
     uint32_t kept = ~0u;
@@ -140,16 +201,14 @@ __global__ __launch_bounds__(kBlock) void k_route(RouteArgs a)
         for (int g = lane; g < a.in.n_group; g += team) {
             double b0 = kNoExpert, b1 = kNoExpert;
             for (int i = 0; i < n; ++i) {
-                const float v = mine[g * n + i];
-                const double k = key_of(v, 0, false);
-                b1 = fmax(b1, fmin(b0, k));
-                b0 = fmax(b0, k);
+                const double key = key_of(mine[g * n + i], 0);
+                b1 = key_max(b1, key_min(b0, key));
+                b0 = key_max(b0, key);
             }
-            // (the keys hold the scores but for the index bits, which are the same in all)
-            const auto value = [](double k) { return k == kNoExpert ? 0.0f : k < -1.0e199 ? __builtin_nanf("") : (float)k; };
-            float sum = value(b0) + value(b1);
-            if (b0 == kNoExpert) sum = -__builtin_inff();
-            g_mine[g] = key_of(sum, g, false);
+            // (the least score stands for what is no number)
+            const auto value = [](double key) { return key == kNoExpert ? 0.0f : key < -3.4028234e38 ? __builtin_nanf("") : (float)key; };
+            const float sum = value(b0) + value(b1);
+            g_mine[g] = key_of(b0 == kNoExpert ? -__builtin_inff() : sum, g);
         }
         __syncthreads();
         kept = 0;
@@ -158,7 +217,7 @@ __global__ __launch_bounds__(kBlock) void k_route(RouteArgs a)
             for (int i = 0; i < a.in.n_group; ++i) better += g_mine[i] > g_mine[g];
             if (better < a.in.kept) kept |= 1u << g;
         }
-        for (int m = 1; m < team; m *= 2) kept |= __shfl_xor(kept, m);
+        kept = (uint32_t)over_team((int)kept, lg, [](int p, int q) { return p | q; });
     }
 
     double best[K];
@@ -172,41 +231,47 @@ __global__ __launch_bounds__(kBlock) void k_route(RouteArgs a)
     }
 #pragma unroll
     for (int i = 0; i < V; ++i) {
-        double k = key_of(c[i], first + i, false);
+        double key = key_of(c[i], first + i);
         if constexpr (kGroups) {
-            if (!(kept >> (group_no & 31) & 1)) k = kNoExpert;
+            key = kept >> (group_no & 31) & 1 ? key : kNoExpert;
             if (++in_group == group_size) { in_group = 0; ++group_no; }
         }
 #pragma unroll
         for (int j = 0; j < (i + 1 < K ? i + 1 : K); ++j) {
-            const double up = fmax(best[j], k);
-            k = fmin(best[j], k);
+            const double up = key_max(best[j], key);
+            key = key_min(best[j], key);
             best[j] = up;
         }
     }
     // lanes' lists, each in order, become the team's: the larger of one list's j-th and the other's j-th from the end are
     // the K largest of both
-    for (int m = 1; m < team; m *= 2) {
+    const auto join = [&](auto step) __attribute__((always_inline)) {
+        constexpr int kStep = decltype(step)::value;
         double other[K];
 #pragma unroll
-        for (int j = 0; j < K; ++j) other[j] = __shfl_xor(best[K - 1 - j], m);
+        for (int j = 0; j < K; ++j) other[j] = other_half<kStep>(best[K - 1 - j]);
 #pragma unroll
-        for (int j = 0; j < K; ++j) best[j] = fmax(best[j], other[j]);
+        for (int j = 0; j < K; ++j) best[j] = key_max(best[j], other[j]);
 #pragma unroll
         for (int d = K / 2; d > 0; d /= 2)
 #pragma unroll
             for (int j = 0; j < K; ++j)
                 if (!(j & d)) {
-                    const double hi = fmax(best[j], best[j + d]), lo = fmin(best[j], best[j + d]);
+                    const double hi = key_max(best[j], best[j + d]), lo = key_min(best[j], best[j + d]);
                     best[j] = hi;
                     best[j + d] = lo;
                 }
-    }
+    };
+    if (lg > 0) join(std::integral_constant<int, 1>{});
+    if (lg > 1) join(std::integral_constant<int, 2>{});
+    if (lg > 2) join(std::integral_constant<int, 4>{});
+    if (lg > 3) join(std::integral_constant<int, 8>{});
+    if (lg > 4) join(std::integral_constant<int, 16>{});
     float s[K], sum = 0;
 #pragma unroll
     for (int j = 0; j < K; ++j) {
         s[j] = 0;
-        if (j < a.in.top_k && (j & (team - 1)) == lane) {
+        if (j < k && (j & (team - 1)) == lane) {
             const int e = expert_of(best[j]);
             if (e >= 0) s[j] = score_of<kSigmoid>((float)at[e], sm);
             sum += s[j];
@@ -217,13 +282,37 @@ __global__ __launch_bounds__(kBlock) void k_route(RouteArgs a)
         sum = team_sum(sum, lg);
         by = sum == 0 ? 0.0f : a.in.scale / sum;
     }
-    if (!there) return;
+    if (there) {
 #pragma unroll
-    for (int j = 0; j < K; ++j)
-        if (j < a.in.top_k && (j & (team - 1)) == lane) {
-            a.weight[row * a.in.top_k + j] = s[j] * by;
-            a.expert[row * a.in.top_k + j] = expert_of(best[j]);
+        for (int j = 0; j < K; ++j)
+            if (j < k && (j & (team - 1)) == lane) {
+                a.weight[row * k + j] = s[j] * by;
+                a.expert[row * k + j] = expert_of(best[j]);
+            }
+    }
+    if (a.plan.units == 0) return;
+    // how many of its slots each expert has; a workgroup alone puts them in order as well
+    __shared__ int hist[kPlanWaves][GR_MAX_EXPERTS + 1];
+    if (a.plan.units > 1) {
+        for (int e = threadIdx.x; e <= E; e += kBlock) hist[0][e] = 0;
+        __syncthreads();
+        if (there) {
+#pragma unroll
+            for (int j = 0; j < K; ++j)
+                if (j < k && (j & (team - 1)) == lane) atomicAdd(&hist[0][bin_of(expert_of(best[j]), E)], 1);
         }
+        __syncthreads();
+        for (int e = threadIdx.x; e <= E; e += kBlock) a.plan.counts[(int64_t)e * a.plan.units + blockIdx.x] = hist[0][e];
+        return;
+    }
+    __shared__ int ids[kBlock * K];
+    if (there) {
+#pragma unroll
+        for (int j = 0; j < K; ++j)
+            if (j < k && (j & (team - 1)) == lane) ids[row * k + j] = expert_of(best[j]);
+    }
+    __syncthreads();
+    place_unit(a.plan, 0, hist, [&](int i) { return ids[i]; });
 }
 
 struct RouteBackArgs {
@@ -303,14 +392,6 @@ __global__ __launch_bounds__(kBlock) void k_route_back(RouteBackArgs a)
         if (first + i < E) out[first + i] = (T)d[i];
 }
 
-// Lanes per row: each holds kLaneExperts scores.
-int team_log(int n_expert)
-{
-    int lg = 0;
-    while ((kLaneExperts << lg) < n_expert) ++lg;
-    return lg;
-}
-
 template <typename T>
 bool whole_rows(const void* a, const void* b, int n_expert)
 {
@@ -333,30 +414,27 @@ void route_by_form(const RouteArgs& a, hipStream_t s)
 // A counting sort by expert that keeps the order of slots: how many slots of each expert every unit of slots holds, the sums
 // of those over the units before, and every slot to its place.  Slots without an expert are those of expert E.
 
-__device__ __forceinline__ int bin_of(int e, int n_expert) { return (unsigned)e < (unsigned)n_expert ? e : n_expert; }
-
-__global__ __launch_bounds__(kWave) void k_plan_count(const int* expert, int64_t slots, int n_expert, int* counts)
+__global__ __launch_bounds__(kBlock) void k_plan_count(PlanArgs a)
 {
     __shared__ int cnt[GR_MAX_EXPERTS + 1];
-    for (int e = threadIdx.x; e <= n_expert; e += kWave) cnt[e] = 0;
+    for (int e = threadIdx.x; e <= a.n_expert; e += kBlock) cnt[e] = 0;
     __syncthreads();
-    const int64_t from = (int64_t)blockIdx.x * kPlanUnit;
-    for (int i = threadIdx.x; i < kPlanUnit; i += kWave)
-        if (from + i < slots) atomicAdd(&cnt[bin_of(expert[from + i], n_expert)], 1);
+    const int64_t from = (int64_t)blockIdx.x * a.per_unit;
+    for (int i = threadIdx.x; i < a.per_unit; i += kBlock)
+        if (from + i < a.slots) atomicAdd(&cnt[bin_of(a.expert[from + i], a.n_expert)], 1);
     __syncthreads();
-    for (int e = threadIdx.x; e <= n_expert; e += kWave) counts[(int64_t)blockIdx.x * (n_expert + 1) + e] = cnt[e];
+    for (int e = threadIdx.x; e <= a.n_expert; e += kBlock) a.counts[(int64_t)e * a.units + blockIdx.x] = cnt[e];
 }
 
-// One workgroup per expert: its counts become the sums over the units before.
-__global__ __launch_bounds__(kBlock) void k_plan_scan(int* counts, int units, int n_expert, int* totals)
+// One workgroup per expert: its counts become the sums over the units before; the sum of all goes behind them all.
+__global__ __launch_bounds__(kScanBlock) void k_plan_sum(PlanArgs a)
 {
-    __shared__ int wave_sum[kBlock / kWave];
+    __shared__ int wave_sum[kScanBlock / kWave];
     const int e = blockIdx.x, lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
+    int* const at = a.counts + (int64_t)e * a.units;
     int before = 0;
-    for (int u0 = 0; u0 < units; u0 += kBlock) {
-        const int u = u0 + threadIdx.x;
-        int* const at = counts + (int64_t)u * (n_expert + 1) + e;
-        const int own = u < units ? *at : 0;
+    for (int u0 = 0; u0 < a.units; u0 += kScanBlock) {
+        const int u = u0 + threadIdx.x, own = u < a.units ? at[u] : 0;
         int v = own;
         for (int d = 1; d < kWave; d *= 2) {
             const int o = __shfl_up(v, d);
@@ -365,66 +443,120 @@ __global__ __launch_bounds__(kBlock) void k_plan_scan(int* counts, int units, in
         if (lane == kWave - 1) wave_sum[wave] = v;
         __syncthreads();
         int base = before, all = 0;
-        for (int w = 0; w < kBlock / kWave; ++w) {
+        for (int w = 0; w < kScanBlock / kWave; ++w) {
             if (w < wave) base += wave_sum[w];
             all += wave_sum[w];
         }
-        if (u < units) *at = base + v - own;
+        if (u < a.units) at[u] = base + v - own;
         before += all;
         __syncthreads();
     }
-    if (threadIdx.x == 0) totals[e] = before;
+    if (threadIdx.x == 0) a.counts[(int64_t)(a.n_expert + 1) * a.units + e] = before;
 }
 
-__global__ __launch_bounds__(kWave) void k_plan_place(const int* expert, int64_t slots, int n_expert, const int* counts,
-                                                      const int* totals, int* off, int* slot, int* pos)
+// A unit's slots to their places, by four waves: each counts its own part, then puts it in order 64 slots at a time.  `expert_at`(i): of the
+// unit's slot i.
+template <typename F>
+__device__ void place_unit(const PlanArgs& a, int unit, int (*hist)[GR_MAX_EXPERTS + 1], F expert_at)
 {
-    __shared__ int next[GR_MAX_EXPERTS + 1];
-    const int lane = threadIdx.x;
-    int before = 0;
-    for (int e0 = 0; e0 <= n_expert; e0 += kWave) {
-        const int e = e0 + lane, own = e <= n_expert ? totals[e] : 0;
-        int v = own;
+    __shared__ int wave_sum[kPlanWaves], carry;
+    const int E = a.n_expert, lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
+    const int64_t from = (int64_t)unit * a.per_unit;
+    const int n = a.slots - from < a.per_unit ? (int)(a.slots - from) : a.per_unit;
+    const int part = (n + kPlanWaves * kWave - 1) / (kPlanWaves * kWave) * kWave, begin = wave * part, end = begin + part < n ? begin + part : n;
+    for (int i = threadIdx.x; i < kPlanWaves * (E + 1); i += kBlock) hist[i / (E + 1)][i % (E + 1)] = 0;
+    if (threadIdx.x == 0) carry = 0;
+    __syncthreads();
+    for (int i = begin + lane; i < end; i += kWave) atomicAdd(&hist[wave][bin_of(expert_at(i), E)], 1);
+    __syncthreads();
+    // where each expert's slots of this unit go: behind all of the experts before, those of the units before, those of the waves before
+    for (int e0 = 0; e0 <= E; e0 += kBlock) {
+        const int e = e0 + threadIdx.x;
+        int mine = 0, all = 0, own[kPlanWaves] = {};
+        if (e <= E) {
+            for (int w = 0; w < kPlanWaves; ++w) own[w] = hist[w][e];
+            if (a.units == 1) {
+                for (int w = 0; w < kPlanWaves; ++w) all += own[w];
+            } else if (a.summed) {
+                mine = a.counts[(int64_t)e * a.units + unit];
+                all = a.counts[(int64_t)(E + 1) * a.units + e];
+            } else {
+                for (int u = 0; u < a.units; ++u) {
+                    const int c = a.counts[(int64_t)e * a.units + u];
+                    if (u < unit) mine += c;
+                    all += c;
+                }
+            }
+        }
+        int v = all;
         for (int d = 1; d < kWave; d *= 2) {
             const int o = __shfl_up(v, d);
             if (lane >= d) v += o;
         }
-        if (e <= n_expert) {
-            const int at = before + v - own;
-            next[e] = at + counts[(int64_t)blockIdx.x * (n_expert + 1) + e];
-            if (blockIdx.x == 0) off[e] = at;
+        if (lane == kWave - 1) wave_sum[wave] = v;
+        __syncthreads();
+        int at = carry + v - all, sum = 0;
+        for (int w = 0; w < kPlanWaves; ++w) {
+            if (w < wave) at += wave_sum[w];
+            sum += wave_sum[w];
         }
-        before += __shfl(v, kWave - 1);
+        if (e <= E) {
+            if (unit == 0) a.off[e] = at;
+            at += mine;
+            for (int w = 0; w < kPlanWaves; ++w) {
+                hist[w][e] = at;
+                at += own[w];
+            }
+        }
+        __syncthreads();
+        if (threadIdx.x == 0) carry += sum;
+        __syncthreads();
     }
-    __syncthreads();
-    const int64_t from = (int64_t)blockIdx.x * kPlanUnit;
     int bits = 0;
-    while ((n_expert >> bits) > 0) ++bits;
-    for (int i = 0; i < kPlanUnit; i += kWave) {
-        const int64_t s = from + i + lane;
-        const bool there = s < slots;
-        const int e = there ? bin_of(expert[s], n_expert) : 0;
+    while ((E >> bits) > 0) ++bits;
+    for (int i0 = begin; i0 < end; i0 += kWave) {
+        const int i = i0 + lane;
+        const bool there = i < end;
+        const int e = there ? bin_of(expert_at(i), E) : 0;
         unsigned long long alike = __ballot(there);
         for (int b = 0; b < bits; ++b) {
             const unsigned long long with = __ballot(e >> b & 1);
             alike &= e >> b & 1 ? with : ~with;
         }
-        const int rank = __popcll(alike & ((1ull << lane) - 1));
-        int at = 0;
-        if (there) at = next[e];
-        __syncthreads();
         if (there) {
-            if (rank == 0) next[e] = at + __popcll(alike);
-            slot[at + rank] = e < n_expert ? (int)s : -1 - (int)s;
-            pos[s] = e < n_expert ? at + rank : -1;
+            const int rank = __popcll(alike & ((1ull << lane) - 1)), at = hist[wave][e] + rank;
+            const int64_t s = from + i;
+            a.slot[at] = e < E ? (int)s : -1 - (int)s;
+            a.pos[s] = e < E ? at : -1;
         }
-        __syncthreads();
+        // (a wave's reads come before its later writes)
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        if (there && (alike >> lane) == 1) hist[wave][e] += __popcll(alike);
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     }
+}
+
+__global__ __launch_bounds__(kBlock) void k_plan_place(PlanArgs a)
+{
+    __shared__ int hist[kPlanWaves][GR_MAX_EXPERTS + 1];
+    const int64_t from = (int64_t)blockIdx.x * a.per_unit;
+    place_unit(a, blockIdx.x, hist, [&](int i) { return a.expert[from + i]; });
 }
 
 __global__ void k_no_slots(int* off, int n_expert)
 {
     for (int e = threadIdx.x; e <= n_expert; e += blockDim.x) off[e] = 0;
+}
+
+// behind the counts
+int finish_plan(PlanArgs a, hipStream_t s)
+{
+    if (a.units > kFewUnits) {
+        k_plan_sum<<<a.n_expert + 1, kScanBlock, 0, s>>>(a);
+        a.summed = 1;
+    }
+    k_plan_place<<<a.units, kBlock, 0, s>>>(a);
+    return launched();
 }
 
 // ---- weighted sum ------------------------------------------------------------------------------
@@ -522,13 +654,17 @@ bool by_chunk(int width, const void* a, const void* b, const void* c)
 
 }  // namespace
 
-int launch_route(const RouteIn& in, int dtype, float* weight, int* expert, hipStream_t s)
+int launch_route(gr_experts* h, const RouteIn& in, int dtype, float* weight, int* expert, int* off, int* slot, int* pos, hipStream_t s)
 {
     return by_type(dtype, [&](auto t) {
         typedef decltype(t) T;
-        const RouteArgs a{in, weight, expert, team_log(in.n_expert), whole_rows<T>(in.logits, nullptr, in.n_expert)};
+        RouteArgs a{in, weight, expert, team_log(in.n_expert), whole_rows<T>(in.logits, nullptr, in.n_expert), {}};
+        if (off) {
+            const int rows = kBlock >> a.lg;
+            a.plan = {expert, h->counts, off, slot, pos, in.rows * in.top_k, in.n_expert, (int)((in.rows + rows - 1) / rows), rows * in.top_k, 0};
+        }
         in.top_k <= 2 ? route_by_form<T, 2>(a, s) : in.top_k <= 8 ? route_by_form<T, 8>(a, s) : route_by_form<T, 16>(a, s);
-        return launched();
+        return a.plan.units > 1 ? finish_plan(a.plan, s) : launched();
     });
 }
 
@@ -546,15 +682,14 @@ int launch_route_backward(const RouteIn& in, int dtype, const int* expert, const
 
 int launch_plan(gr_experts* h, int64_t slots, const int* expert, int* off, int* slot, int* pos, hipStream_t s)
 {
-    const int E = h->n_expert, units = (int)((slots + kPlanUnit - 1) / kPlanUnit);
-    if (units == 0) {
+    const int E = h->n_expert;
+    if (slots == 0) {
         k_no_slots<<<1, kBlock, 0, s>>>(off, E);
         return launched();
     }
-    k_plan_count<<<units, kWave, 0, s>>>(expert, slots, E, h->counts);
-    k_plan_scan<<<E + 1, kBlock, 0, s>>>(h->counts, units, E, h->totals);
-    k_plan_place<<<units, kWave, 0, s>>>(expert, slots, E, h->counts, h->totals, off, slot, pos);
-    return launched();
+    const PlanArgs a{expert, h->counts, off, slot, pos, slots, E, (int)((slots + kPlanUnit - 1) / kPlanUnit), kPlanUnit, 0};
+    if (a.units > 1) k_plan_count<<<a.units, kBlock, 0, s>>>(a);
+    return finish_plan(a, s);
 }
 
 int launch_combine(int64_t rows, int top_k, int width, int dtype, const float* weight, const int* pos, const void* y, void* out,

@@ -60,8 +60,7 @@ int gr_experts_create(gr_experts** out, int32_t n_expert, int64_t max_rows, int3
     h->max_rows = max_rows;
     h->max_top_k = max_top_k;
     h->max_slots = max_rows * max_top_k;
-    const size_t units = (size_t)(h->max_slots + kPlanUnit - 1) / kPlanUnit;
-    if (!dev_alloc(&h->counts, units * (n_expert + 1)) || !dev_alloc(&h->totals, n_expert + 1) || !dev_alloc(&h->squares, kClipParts) ||
+    if (!dev_alloc(&h->counts, (plan_units(n_expert, max_rows, h->max_slots) + 1) * (n_expert + 1)) || !dev_alloc(&h->squares, kClipParts) ||
         !dev_alloc(&h->parts, kPartFloats)) {
         gr_experts_destroy(h);
         return GR_ERR_NOMEM;
@@ -75,7 +74,7 @@ int gr_experts_destroy(gr_experts* h)
     if (!h) return GR_OK;
     (void)hipDeviceSynchronize();
     int rc = GR_OK;
-    for (void* p : {(void*)h->counts, (void*)h->totals, (void*)h->squares, (void*)h->parts})
+    for (void* p : {(void*)h->counts, (void*)h->squares, (void*)h->parts})
         if (p && hipFree(p) != hipSuccess) rc = GR_ERR_HIP;
     delete h;
     return rc;
@@ -93,12 +92,9 @@ int gr_expert_route(gr_experts* h, int64_t n_rows, int32_t top_k, const void* lo
     if (plan && (!out_off || (n_rows > 0 && (!out_slot || !out_pos)))) return GR_ERR_INVALID_ARG;
     if (n_rows > 0 && (!logits || !out_weight || !out_expert)) return GR_ERR_INVALID_ARG;
     hipStream_t s = static_cast<hipStream_t>(hip_stream);
-    if (n_rows > 0) {
-        const RouteIn in{logits, bias, n_rows, h->n_expert, top_k, scoring, n_group, n_group_kept, renormalise != 0, scale};
-        rc = launch_route(in, dtype, out_weight, out_expert, s);
-    }
-    if (rc == GR_OK && plan) rc = launch_plan(h, n_rows * top_k, out_expert, out_off, out_slot, out_pos, s);
-    return rc;
+    if (n_rows == 0) return plan ? launch_plan(h, 0, out_expert, out_off, out_slot, out_pos, s) : GR_OK;
+    const RouteIn in{logits, bias, n_rows, h->n_expert, top_k, scoring, n_group, n_group_kept, renormalise != 0, scale};
+    return launch_route(h, in, dtype, out_weight, out_expert, out_off, out_slot, out_pos, s);
 }
 
 int gr_expert_route_backward(gr_experts* h, int64_t n_rows, int32_t top_k, const void* logits, int32_t dtype, int32_t scoring,
