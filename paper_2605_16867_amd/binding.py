@@ -131,7 +131,8 @@ def _native(l):
     loader.exec_module(m)
     m.connect(_check_slowly, *[C.cast(getattr(l, n), C.c_void_p).value for n in (
         "gr_build_status", "gr_score_route", "gr_score_route_noalloc", "gr_score_route_cached", "gr_route_feedback",
-        "gr_risk_scan")])
+        "gr_risk_scan", "gr_expert_route", "gr_expert_route_backward", "gr_expert_plan", "gr_expert_linear",
+        "gr_expert_linear_backward", "gr_expert_combine", "gr_expert_combine_backward", "gr_clip_gradients")])
     return m
 
 
@@ -394,6 +395,21 @@ def _dtype(t, name: str) -> int:
     return code
 
 
+def _done(code: int, where: str) -> None:
+    if code:
+        _check(code, where)
+
+
+class _Unclear:
+    """In the place of the native marshalling where that is not built: every call is for the binding to marshal."""
+
+    def __getattr__(self, name):
+        return lambda *args: None
+
+
+_Unclear = _Unclear()
+
+
 class Experts:
     """Owns a gr_experts handle on the current device: the workspace of a length predictor's operators.
 
@@ -401,13 +417,17 @@ class Experts:
     n_out, n_in], y [positions, n_out]; all contiguous, x, w and y of one type."""
 
     def __init__(self, n_expert: int, max_rows: int, max_top_k: int):
-        self._h = C.c_void_p()
+        self._h, self._at = C.c_void_p(), None
+        self._m = marshal()
+        if self._m is _Ctypes:
+            self._m = _Unclear
         self.n_expert = int(n_expert)
         _check(lib().gr_experts_create(C.byref(self._h), self.n_expert, int(max_rows), int(max_top_k)), "gr_experts_create")
+        self._at = self._h.value
 
     def close(self) -> None:
         if self._h:
-            h, self._h = self._h, C.c_void_p()
+            h, self._h, self._at = self._h, C.c_void_p(), None
             _check(lib().gr_experts_destroy(h), "gr_experts_destroy")
 
     def __del__(self):
@@ -430,6 +450,10 @@ class Experts:
 
     def gr_expert_route(self, logits, out_weight, out_expert, out_off=None, out_slot=None, out_pos=None, bias=None,
                         scoring="softmax", n_group=1, n_group_kept=1, renormalise=False, scale=1.0) -> None:
+        rc = self._m.expert_route(self._at, self.n_expert, logits, out_weight, out_expert, out_off, out_slot, out_pos, bias,
+                                  _SCORING[scoring], n_group, n_group_kept, renormalise, scale)
+        if rc is not None:
+            return _done(rc, "gr_expert_route")
         import torch
         T, _ = self._shape(logits, "logits", None, self.n_expert)
         _, k = self._shape(out_expert, "out_expert", T, None)
@@ -440,6 +464,10 @@ class Experts:
             *self._plan(T * k, out_off, out_slot, out_pos), _stream()), "gr_expert_route")
 
     def gr_expert_route_backward(self, logits, expert, dweight, out_dlogits, scoring="softmax", renormalise=False, scale=1.0) -> None:
+        rc = self._m.expert_route_backward(self._at, self.n_expert, logits, expert, dweight, out_dlogits, _SCORING[scoring], renormalise,
+                                           scale)
+        if rc is not None:
+            return _done(rc, "gr_expert_route_backward")
         import torch
         T, E = self._shape(logits, "logits", None, self.n_expert)
         _, k = self._shape(expert, "expert", T, None)
@@ -449,6 +477,9 @@ class Experts:
             _dev(out_dlogits, logits.dtype, "out_dlogits", T * E), _stream()), "gr_expert_route_backward")
 
     def gr_expert_plan(self, expert, out_off, out_slot, out_pos) -> None:
+        rc = self._m.expert_plan(self._at, self.n_expert, expert, out_off, out_slot, out_pos)
+        if rc is not None:
+            return _done(rc, "gr_expert_plan")
         import torch
         T, k = self._shape(expert, "expert", None, None)
         _check(lib().gr_expert_plan(self._h, T, k, _dev(expert, torch.int32, "expert"), *self._plan(T * k, out_off, out_slot, out_pos),
@@ -465,6 +496,9 @@ class Experts:
                          _dev(x, x.dtype, "x"), _dev(w, x.dtype, "w"))
 
     def gr_expert_linear(self, x, w, out_y, bias=None, off=None, slot=None, top_k=1, relu=False) -> None:
+        rc = self._m.expert_linear(self._at, self.n_expert, x, w, out_y, bias, off, slot, top_k, relu)
+        if rc is not None:
+            return _done(rc, "gr_expert_linear")
         n, O = self._shape(out_y, "out_y", None, w.shape[-2])
         E, I, O, layer = self._layer(x, w, off, slot, int(top_k), n)
         _check(lib().gr_expert_linear(self._h, *layer, _dev(bias, x.dtype, "bias", E * O), int(relu), _dev(out_y, x.dtype, "out_y"),
@@ -472,6 +506,9 @@ class Experts:
 
     def gr_expert_linear_backward(self, x, w, dy, out_dx=None, out_dw=None, out_db=None, y=None, out_dz=None, off=None,
                                   slot=None, top_k=1) -> None:
+        rc = self._m.expert_linear_backward(self._at, self.n_expert, x, w, dy, out_dx, out_dw, out_db, y, out_dz, off, slot, top_k)
+        if rc is not None:
+            return _done(rc, "gr_expert_linear_backward")
         n, O = self._shape(dy, "dy", None, w.shape[-2])
         E, I, O, layer = self._layer(x, w, off, slot, int(top_k), n)
         t = x.dtype
@@ -481,6 +518,9 @@ class Experts:
             "gr_expert_linear_backward")
 
     def gr_expert_combine(self, y, pos, out, weight=None) -> None:
+        rc = self._m.expert_combine(self._at, y, pos, out, weight)
+        if rc is not None:
+            return _done(rc, "gr_expert_combine")
         import torch
         T, k = self._shape(pos, "pos", None, None)
         _, O = self._shape(out, "out", T, None)
@@ -489,6 +529,9 @@ class Experts:
                                        _stream()), "gr_expert_combine")
 
     def gr_expert_combine_backward(self, dout, y, slot, out_dy=None, weight=None, out_dweight=None) -> None:
+        rc = self._m.expert_combine_backward(self._at, dout, y, slot, out_dy, weight, out_dweight)
+        if rc is not None:
+            return _done(rc, "gr_expert_combine_backward")
         import torch
         T, O = self._shape(dout, "dout", None, None)
         if T and slot.numel() % T:
@@ -502,6 +545,9 @@ class Experts:
 
     def gr_clip_gradients(self, grads, max_norm, out_norm=None, out=None) -> None:
         """grads: a list of tensors, scaled in place unless `out` names as many others."""
+        rc = self._m.clip_gradients(self._at, grads, max_norm, out_norm, grads if out is None else out)
+        if rc is not None:
+            return _done(rc, "gr_clip_gradients")
         import torch
         out = grads if out is None else out
         n = len(grads)

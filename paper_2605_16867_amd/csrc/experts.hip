@@ -10,6 +10,7 @@ constexpr int kBlock = kRouteBlock;
 constexpr int kWave = 64;
 constexpr int kPlanWaves = kBlock / kWave;
 constexpr int kScanBlock = 1024;
+constexpr int kEnoughUnits = 1024;   // four workgroups a compute unit
 constexpr int kFewUnits = 32;        // units of slots whose counts every workgroup adds up by itself
 
 // ---- within a team of lanes ----------------------------------------------------------------------
@@ -63,18 +64,17 @@ __device__ __forceinline__ float team_sum(float v, int lg)
 // The largest top_k of a list are then found with minima and maxima alone: 2 top_k of them a score.
 constexpr double kNoExpert = -1.0e300;      // below every score
 
-__device__ __forceinline__ double key_of(float c, int e)
+__device__ __forceinline__ double key_of(float c, int e)      // (c is not -0: a score is not)
 {
-    const bool none = c == -__builtin_inff();
-    c = c == c ? c + 0.0f : -3.4028235e38f;                                    // (-0 counts as 0; no number is the least score)
-    const double d = (double)__builtin_fminf(c, 3.4028235e38f);
+    const double d = (double)__builtin_amdgcn_fmed3f(c, -3.4028235e38f, 3.4028235e38f);      // (what is no number is the least score)
     const int hi = __double2hiint(d), lo = __double2loint(d) | ((511 - e) ^ (hi >> 31 & 511));
-    return none ? kNoExpert : __hiloint2double(hi, lo);
+    return c == -__builtin_inff() ? kNoExpert : __hiloint2double(hi, lo);
 }
 
 __device__ __forceinline__ int expert_of(double key)
 {
-    return key < -1.0e299 ? -1 : 511 - ((__double2loint(key) ^ __double2hiint(key) >> 31) & 511);
+    const int hi = __double2hiint(key);
+    return hi == (int)0xFE37E43C ? -1 : 511 - ((__double2loint(key) ^ hi >> 31) & 511);      // (kNoExpert's; every score's is larger)
 }
 
 // (fmax and fmin would first quiet what might be a signalling not-a-number; keys are numbers)
@@ -89,6 +89,44 @@ __device__ __forceinline__ double key_min(double a, double b)
     double r;
     asm("v_min_f64 %0, %1, %2" : "=v"(r) : "v"(a), "v"(b));
     return r;
+}
+
+// The larger first.
+__device__ __forceinline__ void in_order(double& a, double& b)
+{
+    const double up = key_max(a, b);
+    b = key_min(a, b);
+    a = up;
+}
+
+// Lists of N in order, by odd-even merges: 19 exchanges for 8, 63 for 16, where insertion takes 28 and 120.
+template <int N>
+__device__ __forceinline__ void sort_list(double* v)
+{
+#pragma unroll
+    for (int p = 1; p < N; p *= 2)
+#pragma unroll
+        for (int k = p; k >= 1; k /= 2)
+#pragma unroll
+            for (int i = k % p; i + k < N; ++i)
+                if ((i - k % p) / k % 2 == 0 && i / (2 * p) == (i + k) / (2 * p)) in_order(v[i], v[i + k]);
+}
+
+// The N largest of two lists in order, in order: the larger of one's j-th and the other's j-th from the end are those, falling and
+// rising once; `other`(j) gives the other's.
+template <int N, typename F>
+__device__ __forceinline__ void join_lists(double* v, F other)
+{
+    double of[N];
+#pragma unroll
+    for (int j = 0; j < N; ++j) of[j] = other(N - 1 - j);
+#pragma unroll
+    for (int j = 0; j < N; ++j) v[j] = key_max(v[j], of[j]);
+#pragma unroll
+    for (int d = N / 2; d > 0; d /= 2)
+#pragma unroll
+        for (int j = 0; j < N; ++j)
+            if (!(j & d)) in_order(v[j], v[j + d]);
 }
 
 // What turns a row's logits into its scores: softmax is exp(x - shift) * inv, sigmoid needs neither.
@@ -117,28 +155,41 @@ __device__ __forceinline__ float score_of(float x, Softmax sm)
     return expf(x - sm.shift) * sm.inv;
 }
 
-// A lane's share of a row: experts first .. first + V - 1; -inf where there is none.
+// Which expert is number i of a lane's share of a row: neighbouring lanes of a team take neighbouring 16 bytes, or elements where rows are not whole
+// ones of all lanes.
+struct Share {
+    int lg, lane, n_expert;
+    bool whole;
+
+    template <int kChunk>
+    __device__ __forceinline__ int operator()(int i) const
+    {
+        return whole ? ((i / kChunk << lg) + lane) * kChunk + i % kChunk : (i << lg) + lane;
+    }
+};
+
+// A lane's share of a row; -inf where there is no expert.
 template <typename T, int V>
-__device__ __forceinline__ void load_row(float (&x)[V], const T* row, int first, int n_expert, bool whole)
+__device__ __forceinline__ void load_row(float (&x)[V], const T* row, const Share& of)
 {
-    if (whole) {
+    constexpr int n = Chunk<T>::n;
+    if (of.whole) {
         typedef typename Chunk<T>::Vec Vec;
-        constexpr int n = Chunk<T>::n;
-        if (first < n_expert) {
 #pragma unroll
-            for (int i = 0; i < V / n; ++i) {
-                const Vec v = reinterpret_cast<const Vec*>(row + first)[i];
+        for (int i = 0; i < V; i += n) {
+            const int e = of.template operator()<n>(i);
+            const Vec v = *reinterpret_cast<const Vec*>(row + (e < of.n_expert ? e : 0));
 #pragma unroll
-                for (int j = 0; j < n; ++j) x[i * n + j] = (float)v[j];
-            }
-        } else {
-#pragma unroll
-            for (int i = 0; i < V; ++i) x[i] = -__builtin_inff();
+            for (int j = 0; j < n; ++j) x[i + j] = e < of.n_expert ? (float)v[j] : -__builtin_inff();
         }
         return;
     }
 #pragma unroll
-    for (int i = 0; i < V; ++i) x[i] = first + i < n_expert ? (float)row[first + i] : -__builtin_inff();
+    for (int i = 0; i < V; ++i) {
+        const int e = of.template operator()<n>(i);
+        const float v = (float)row[e < of.n_expert ? e : 0];
+        x[i] = e < of.n_expert ? v : -__builtin_inff();
+    }
 }
 
 // The order of slots (see below), as far as a workgroup has a part in it.
@@ -161,157 +212,152 @@ struct RouteArgs {
     float* weight;
     int* expert;
     int lg;          // log2 of the lanes per row
-    int whole;       // rows are whole chunks of a lane, 16 bytes aligned
+    int whole;       // rows are whole 16 bytes of each, on boundaries of 16
+    uint32_t group_mul;      // 2^20 / experts of a group, rounded up
     PlanArgs plan;   // units 0: no order is asked for
 };
 
 template <typename T, int K, bool kSigmoid, bool kGroups>
 __global__ __launch_bounds__(kBlock) void k_route(RouteArgs a)
 {
-    constexpr int V = kLaneExperts;
-    const int lg = a.lg, team = 1 << lg, lane = threadIdx.x & (team - 1);
-    const int64_t row = ((int64_t)blockIdx.x * kBlock + threadIdx.x) >> lg;
-    const bool there = row < a.in.rows;
-    const int E = a.in.n_expert, k = a.in.top_k, first = lane * V;
-    const T* const at = static_cast<const T*>(a.in.logits) + (there ? row : 0) * E;
-
-    float x[V];
-    load_row<T, V>(x, at, first, E, a.whole);
-    Softmax sm{};
-    if (!kSigmoid) sm = softmax_of<V>(x, lg);
-
-    float c[V];
-#pragma unroll
-    for (int i = 0; i < V; ++i) {
-        const float s = score_of<kSigmoid>(x[i], sm) + (a.in.bias && first + i < E ? a.in.bias[first + i] : 0.0f);
-        c[i] = x[i] == -__builtin_inff() ? x[i] : s;
-    }
-
-    uint32_t kept = ~0u;
-    if constexpr (kGroups) {
-        // the groups' two largest, by lanes of the team in turn; each group's rank by counting the better ones
-        __shared__ float all[kBlock * V];
-        __shared__ double group[kBlock * V];       // (of each team the first n_group: a group has at least one expert)
-        float* const mine = all + (threadIdx.x >> lg) * (team * V);
-        double* const g_mine = group + (threadIdx.x >> lg) * (team * V);
-#pragma unroll
-        for (int i = 0; i < V; ++i) mine[first + i] = c[i];
-        __syncthreads();
-        const int n = E / a.in.n_group;
-        for (int g = lane; g < a.in.n_group; g += team) {
-            double b0 = kNoExpert, b1 = kNoExpert;
-            for (int i = 0; i < n; ++i) {
-                const double key = key_of(mine[g * n + i], 0);
-                b1 = key_max(b1, key_min(b0, key));
-                b0 = key_max(b0, key);
-            }
-            // (the least score stands for what is no number)
-            const auto value = [](double key) { return key == kNoExpert ? 0.0f : key < -3.4028234e38 ? __builtin_nanf("") : (float)key; };
-            const float sum = value(b0) + value(b1);
-            g_mine[g] = key_of(b0 == kNoExpert ? -__builtin_inff() : sum, g);
-        }
-        __syncthreads();
-        kept = 0;
-        for (int g = lane; g < a.in.n_group; g += team) {
-            int better = 0;
-            for (int i = 0; i < a.in.n_group; ++i) better += g_mine[i] > g_mine[g];
-            if (better < a.in.kept) kept |= 1u << g;
-        }
-        kept = (uint32_t)over_team((int)kept, lg, [](int p, int q) { return p | q; });
-    }
-
-    double best[K];
-#pragma unroll
-    for (int j = 0; j < K; ++j) best[j] = kNoExpert;
-    int in_group = 0, group_no = 0, group_size = E;
-    if constexpr (kGroups) {
-        group_size = E / a.in.n_group;
-        group_no = first / group_size;
-        in_group = first - group_no * group_size;
-    }
-#pragma unroll
-    for (int i = 0; i < V; ++i) {
-        double key = key_of(c[i], first + i);
-        if constexpr (kGroups) {
-            key = kept >> (group_no & 31) & 1 ? key : kNoExpert;
-            if (++in_group == group_size) { in_group = 0; ++group_no; }
-        }
-#pragma unroll
-        for (int j = 0; j < (i + 1 < K ? i + 1 : K); ++j) {
-            const double up = key_max(best[j], key);
-            key = key_min(best[j], key);
-            best[j] = up;
-        }
-    }
-    // lanes' lists, each in order, become the team's: the larger of one list's j-th and the other's j-th from the end are
-    // the K largest of both
-    const auto join = [&](auto step) __attribute__((always_inline)) {
-        constexpr int kStep = decltype(step)::value;
-        double other[K];
-#pragma unroll
-        for (int j = 0; j < K; ++j) other[j] = other_half<kStep>(best[K - 1 - j]);
-#pragma unroll
-        for (int j = 0; j < K; ++j) best[j] = key_max(best[j], other[j]);
-#pragma unroll
-        for (int d = K / 2; d > 0; d /= 2)
-#pragma unroll
-            for (int j = 0; j < K; ++j)
-                if (!(j & d)) {
-                    const double hi = key_max(best[j], best[j + d]), lo = key_min(best[j], best[j + d]);
-                    best[j] = hi;
-                    best[j + d] = lo;
-                }
-    };
-    if (lg > 0) join(std::integral_constant<int, 1>{});
-    if (lg > 1) join(std::integral_constant<int, 2>{});
-    if (lg > 2) join(std::integral_constant<int, 4>{});
-    if (lg > 3) join(std::integral_constant<int, 8>{});
-    if (lg > 4) join(std::integral_constant<int, 16>{});
-    float s[K], sum = 0;
-#pragma unroll
-    for (int j = 0; j < K; ++j) {
-        s[j] = 0;
-        if (j < k && (j & (team - 1)) == lane) {
-            const int e = expert_of(best[j]);
-            if (e >= 0) s[j] = score_of<kSigmoid>((float)at[e], sm);
-            sum += s[j];
-        }
-    }
-    float by = a.in.scale;
-    if (a.in.renorm) {
-        sum = team_sum(sum, lg);
-        by = sum == 0 ? 0.0f : a.in.scale / sum;
-    }
-    if (there) {
-#pragma unroll
-        for (int j = 0; j < K; ++j)
-            if (j < k && (j & (team - 1)) == lane) {
-                a.weight[row * k + j] = s[j] * by;
-                a.expert[row * k + j] = expert_of(best[j]);
-            }
-    }
-    if (a.plan.units == 0) return;
-    // how many of its slots each expert has; a workgroup alone puts them in order as well
+    constexpr int V = kLaneExperts, n = Chunk<T>::n;
+    const int lg = a.lg, team = 1 << lg, lane = threadIdx.x & (team - 1), rows = kBlock >> lg;
+    const int E = a.in.n_expert, k = a.in.top_k;
+    const Share of{lg, lane, E, a.whole != 0};
     __shared__ int hist[kPlanWaves][GR_MAX_EXPERTS + 1];
+    // scores of the team's row, by expert, and then weights of the wave's rows, by choice; the workgroup's choices
+    __shared__ __attribute__((aligned(16))) float scores[kBlock * V];
+    __shared__ int ids[kBlock * K];
+    float* const mine = scores + (threadIdx.x - lane) * V;
+    const int batches = a.plan.units > 0 ? a.plan.per_unit / (rows * k) : 1;
     if (a.plan.units > 1) {
         for (int e = threadIdx.x; e <= E; e += kBlock) hist[0][e] = 0;
         __syncthreads();
-        if (there) {
+    }
+    for (int batch = 0; batch < batches; ++batch) {
+        const int64_t row = ((int64_t)blockIdx.x * batches + batch) * rows + (threadIdx.x >> lg);
+        const bool there = row < a.in.rows;
+        const T* const at = static_cast<const T*>(a.in.logits) + (there ? row : 0) * E;
+        float x[V], c[V] = {};
+        load_row<T, V>(x, at, of);
+        if (a.in.bias)
 #pragma unroll
-            for (int j = 0; j < K; ++j)
-                if (j < k && (j & (team - 1)) == lane) atomicAdd(&hist[0][bin_of(expert_of(best[j]), E)], 1);
+            for (int i = 0; i < V; ++i) {
+                const int e = of.template operator()<n>(i);
+                c[i] = a.in.bias[e < E ? e : 0];
+            }
+        Softmax sm{};
+        if (!kSigmoid) sm = softmax_of<V>(x, lg);
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+            const float s = score_of<kSigmoid>(x[i], sm);
+            if (a.in.bias) mine[of.template operator()<n>(i)] = s;
+            c[i] = x[i] == -__builtin_inff() ? x[i] : s + c[i];
         }
-        __syncthreads();
+
+        uint32_t kept = ~0u;
+        if constexpr (kGroups) {
+            // the groups' two largest, by lanes of the team in turn; each group's rank by counting the better ones
+            __shared__ float all[kBlock * V];
+            __shared__ double group[kBlock * V];       // (of each team the first n_group: a group has at least one expert)
+            float* const c_mine = all + (threadIdx.x >> lg) * (team * V);
+            double* const g_mine = group + (threadIdx.x >> lg) * (team * V);
+            __syncthreads();
+#pragma unroll
+            for (int i = 0; i < V; ++i) c_mine[of.template operator()<n>(i)] = c[i];
+            __syncthreads();
+            const int size = E / a.in.n_group;
+            for (int g = lane; g < a.in.n_group; g += team) {
+                double b0 = kNoExpert, b1 = kNoExpert;
+                for (int i = 0; i < size; ++i) {
+                    const double key = key_of(c_mine[g * size + i], 0);
+                    b1 = key_max(b1, key_min(b0, key));
+                    b0 = key_max(b0, key);
+                }
+                // (the least score stands for what is no number)
+                const auto value = [](double key) { return key == kNoExpert ? 0.0f : key < -3.4028234e38 ? __builtin_nanf("") : (float)key; };
+                const float sum = value(b0) + value(b1);
+                g_mine[g] = key_of(b0 == kNoExpert ? -__builtin_inff() : sum, g);
+            }
+            __syncthreads();
+            kept = 0;
+            for (int g = lane; g < a.in.n_group; g += team) {
+                int better = 0;
+                for (int i = 0; i < a.in.n_group; ++i) better += g_mine[i] > g_mine[g];
+                if (better < a.in.kept) kept |= 1u << g;
+            }
+            kept = (uint32_t)over_team((int)kept, lg, [](int p, int q) { return p | q; });
+        }
+
+        // the lane's K best of its own, in order, then the team's
+        double keys[V];
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+            const int e = of.template operator()<n>(i);
+            keys[i] = key_of(c[i], e);
+            if constexpr (kGroups) keys[i] = kept >> ((uint32_t)e * a.group_mul >> 20 & 31) & 1 ? keys[i] : kNoExpert;
+        }
+#pragma unroll
+        for (int i = 0; i < V; i += K) sort_list<K>(keys + i);
+#pragma unroll
+        for (int m = K; m < V; m *= 2)
+#pragma unroll
+            for (int i = 0; i < V; i += 2 * m) join_lists<K>(keys + i, [&](int j) { return keys[i + m + j]; });
+        double* const best = keys;
+        if (lg > 0) join_lists<K>(best, [&](int j) { return other_half<1>(best[j]); });
+        if (lg > 1) join_lists<K>(best, [&](int j) { return other_half<2>(best[j]); });
+        if (lg > 2) join_lists<K>(best, [&](int j) { return other_half<4>(best[j]); });
+        if (lg > 3) join_lists<K>(best, [&](int j) { return other_half<8>(best[j]); });
+        if (lg > 4) join_lists<K>(best, [&](int j) { return other_half<16>(best[j]); });
+        // their scores: c itself without a bias
+        float s[K], sum = 0;
+        int id[K];
+#pragma unroll
+        for (int j = 0; j < K; ++j) id[j] = j < k ? expert_of(best[j]) : -1;
+        if (a.in.bias) {
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");      // (a team is of one wave)
+#pragma unroll
+            for (int j = 0; j < K; ++j) s[j] = mine[id[j] < 0 ? 0 : id[j]];
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        } else {
+#pragma unroll
+            for (int j = 0; j < K; ++j)      // (the least score: no number)
+                s[j] = __double2hiint(best[j]) == (int)0xC7EFFFFF ? __builtin_nanf("") : (float)best[j];
+        }
+#pragma unroll
+        for (int j = 0; j < K; ++j) {
+            s[j] = id[j] >= 0 ? s[j] : 0.0f;
+            sum += s[j];
+        }
+        float by = a.in.scale;
+        if (a.in.renorm) by = sum == 0 ? 0.0f : a.in.scale / sum;
+        // out through shared memory, one after the other
+        const int wave = threadIdx.x / kWave, at_wave = (wave * kWave >> lg) * k, own = ((threadIdx.x & (kWave - 1)) >> lg) * k;
+        float* const weights = scores + wave * kWave * V;
+#pragma unroll
+        for (int j = 0; j < K; ++j)
+            if (j < k && (j & (team - 1)) == lane) {
+                weights[own + j] = s[j] * by;
+                ids[at_wave + own + j] = id[j];
+            }
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        const int64_t first = ((int64_t)blockIdx.x * batches + batch) * rows * k + at_wave, left = a.in.rows * k - first;
+        const int count = (kWave >> lg) * k < left ? (kWave >> lg) * k : (int)left;
+        for (int i = threadIdx.x & (kWave - 1); i < count; i += kWave) {
+            const int e = ids[at_wave + i];
+            a.weight[first + i] = weights[i];
+            a.expert[first + i] = e;
+            if (a.plan.units > 1) atomicAdd(&hist[0][bin_of(e, E)], 1);
+        }
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    }
+    // how many of its slots each expert has; a workgroup alone puts them in order as well
+    if (a.plan.units == 0) return;
+    __syncthreads();
+    if (a.plan.units > 1) {
         for (int e = threadIdx.x; e <= E; e += kBlock) a.plan.counts[(int64_t)e * a.plan.units + blockIdx.x] = hist[0][e];
         return;
     }
-    __shared__ int ids[kBlock * K];
-    if (there) {
-#pragma unroll
-        for (int j = 0; j < K; ++j)
-            if (j < k && (j & (team - 1)) == lane) ids[row * k + j] = expert_of(best[j]);
-    }
-    __syncthreads();
     place_unit(a.plan, 0, hist, [&](int i) { return ids[i]; });
 }
 
@@ -326,37 +372,46 @@ struct RouteBackArgs {
 template <typename T, bool kSigmoid>
 __global__ __launch_bounds__(kBlock) void k_route_back(RouteBackArgs a)
 {
-    constexpr int V = kLaneExperts;
-    const int lg = a.lg, team = 1 << lg, lane = threadIdx.x & (team - 1);
+    constexpr int V = kLaneExperts, n = Chunk<T>::n;
+    __shared__ __attribute__((aligned(16))) float given[kBlock * V];      // by expert, where there is one
+    __shared__ uint32_t marks[kBlock];                                    // 16 experts each
+    const int lg = a.lg, team = 1 << lg, lane = threadIdx.x & (team - 1), mine = threadIdx.x - lane;
     const int64_t row = ((int64_t)blockIdx.x * kBlock + threadIdx.x) >> lg;
     const bool there = row < a.in.rows;
-    const int E = a.in.n_expert, first = lane * V, k = a.in.top_k;
+    const int E = a.in.n_expert, k = a.in.top_k;
     const int64_t r = there ? row : 0;
+    const Share of{lg, lane, E, a.whole != 0};
     const T* const at = static_cast<const T*>(a.in.logits) + r * E;
+    marks[threadIdx.x] = 0;
     float x[V];
-    load_row<T, V>(x, at, first, E, a.whole);
+    load_row<T, V>(x, at, of);
+    __syncthreads();
+    for (int j = lane; j < k; j += team) {
+        const int e = a.expert[r * k + j];
+        if ((unsigned)e < (unsigned)E) {
+            given[mine * V + e] = a.dweight[r * k + j] * a.in.scale;
+            atomicOr(&marks[mine + e / 16], 1u << e % 16);
+        }
+    }
     Softmax sm{};
     if (!kSigmoid) sm = softmax_of<V>(x, lg);
-    float s[V], u[V];
-    bool chosen[V];
+    float s[V];
+#pragma unroll
+    for (int i = 0; i < V; ++i) s[i] = x[i] == -__builtin_inff() ? 0.0f : score_of<kSigmoid>(x[i], sm);
+    __syncthreads();
+    // sum of u over the shares, and of the chosen scores
+    float u[V], dot = 0, sum = 0;
+    uint32_t chosen = 0;
 #pragma unroll
     for (int i = 0; i < V; ++i) {
-        s[i] = x[i] == -__builtin_inff() ? 0.0f : score_of<kSigmoid>(x[i], sm);
-        u[i] = 0;
-        chosen[i] = false;
+        const int e = of.template operator()<n>(i);      // (below team * V)
+        const bool is = marks[mine + e / 16] >> e % 16 & 1;
+        const float g = given[mine * V + e];
+        u[i] = is ? g : 0.0f;
+        chosen |= (uint32_t)is << i;
+        dot += is ? g * s[i] : 0.0f;
+        sum += is ? s[i] : 0.0f;
     }
-    for (int j = 0; j < k; ++j) {
-        const int e = a.expert[r * k + j] - first;
-        const float d = a.dweight[r * k + j];
-#pragma unroll
-        for (int i = 0; i < V; ++i)
-            if (e == i && first + i < E) { u[i] = d * a.in.scale; chosen[i] = true; }
-    }
-    // sum of u over the shares, and of the chosen scores
-    float dot = 0, sum = 0;
-#pragma unroll
-    for (int i = 0; i < V; ++i)
-        if (chosen[i]) { dot += u[i] * s[i]; sum += s[i]; }
     dot = team_sum(dot, lg);
     float inv = 1;
     if (a.in.renorm) {
@@ -368,40 +423,41 @@ __global__ __launch_bounds__(kBlock) void k_route_back(RouteBackArgs a)
     float d[V];
 #pragma unroll
     for (int i = 0; i < V; ++i) {
-        if (a.in.renorm) d[i] = chosen[i] ? s[i] * inv * (u[i] - dot) * (kSigmoid ? 1 - s[i] : 1.0f) : 0.0f;
-        else if (kSigmoid) d[i] = chosen[i] ? s[i] * (1 - s[i]) * u[i] : 0.0f;
+        const bool is = chosen >> i & 1;
+        if (a.in.renorm) d[i] = is ? s[i] * inv * (u[i] - dot) * (kSigmoid ? 1 - s[i] : 1.0f) : 0.0f;
+        else if (kSigmoid) d[i] = is ? s[i] * (1 - s[i]) * u[i] : 0.0f;
         else d[i] = s[i] * (u[i] - dot);
     }
     T* const out = static_cast<T*>(a.dlogits) + row * E;
     if (a.whole) {
         typedef typename Chunk<T>::Vec Vec;
-        constexpr int n = Chunk<T>::n;
-        if (first < E) {
 #pragma unroll
-            for (int i = 0; i < V / n; ++i) {
-                Vec v;
+        for (int i = 0; i < V; i += n) {
+            const int e = of.template operator()<n>(i);
+            Vec v;
 #pragma unroll
-                for (int j = 0; j < n; ++j) v[j] = (T)d[i * n + j];
-                reinterpret_cast<Vec*>(out + first)[i] = v;
-            }
+            for (int j = 0; j < n; ++j) v[j] = (T)d[i + j];
+            if (e < E) *reinterpret_cast<Vec*>(out + e) = v;
         }
         return;
     }
 #pragma unroll
-    for (int i = 0; i < V; ++i)
-        if (first + i < E) out[first + i] = (T)d[i];
+    for (int i = 0; i < V; ++i) {
+        const int e = of.template operator()<n>(i);
+        if (e < E) out[e] = (T)d[i];
+    }
 }
 
 template <typename T>
 bool whole_rows(const void* a, const void* b, int n_expert)
 {
-    return n_expert % kLaneExperts == 0 && aligned16(a) && aligned16(b);
+    return n_expert % Chunk<T>::n == 0 && aligned16(a) && aligned16(b);
 }
 
 template <typename T, int K>
 void route_by_form(const RouteArgs& a, hipStream_t s)
 {
-    const int64_t blocks = ((a.in.rows << a.lg) + kBlock - 1) / kBlock;
+    const int64_t blocks = a.plan.units > 0 ? a.plan.units : ((a.in.rows << a.lg) + kBlock - 1) / kBlock;
     const bool groups = a.in.kept < a.in.n_group;
     if (a.in.scoring == GR_SCORE_SIGMOID)
         groups ? k_route<T, K, true, true><<<blocks, kBlock, 0, s>>>(a) : k_route<T, K, true, false><<<blocks, kBlock, 0, s>>>(a);
@@ -467,7 +523,22 @@ __device__ void place_unit(const PlanArgs& a, int unit, int (*hist)[GR_MAX_EXPER
     for (int i = threadIdx.x; i < kPlanWaves * (E + 1); i += kBlock) hist[i / (E + 1)][i % (E + 1)] = 0;
     if (threadIdx.x == 0) carry = 0;
     __syncthreads();
-    for (int i = begin + lane; i < end; i += kWave) atomicAdd(&hist[wave][bin_of(expert_at(i), E)], 1);
+    // (several slots of a lane asked for at a time)
+    constexpr int kHeld = 8;
+    int held[kHeld];
+    const auto hold = [&](int i0) {
+#pragma unroll
+        for (int h = 0; h < kHeld; ++h) {
+            const int i = i0 + h * kWave + lane;
+            held[h] = expert_at(i < end ? i : begin);
+        }
+    };
+    for (int i0 = begin; i0 < end; i0 += kHeld * kWave) {
+        hold(i0);
+#pragma unroll
+        for (int h = 0; h < kHeld; ++h)
+            if (i0 + h * kWave + lane < end) atomicAdd(&hist[wave][bin_of(held[h], E)], 1);
+    }
     __syncthreads();
     // where each expert's slots of this unit go: behind all of the experts before, those of the units before, those of the waves before
     for (int e0 = 0; e0 <= E; e0 += kBlock) {
@@ -514,25 +585,30 @@ __device__ void place_unit(const PlanArgs& a, int unit, int (*hist)[GR_MAX_EXPER
     }
     int bits = 0;
     while ((E >> bits) > 0) ++bits;
-    for (int i0 = begin; i0 < end; i0 += kWave) {
-        const int i = i0 + lane;
-        const bool there = i < end;
-        const int e = there ? bin_of(expert_at(i), E) : 0;
-        unsigned long long alike = __ballot(there);
-        for (int b = 0; b < bits; ++b) {
-            const unsigned long long with = __ballot(e >> b & 1);
-            alike &= e >> b & 1 ? with : ~with;
+    for (int i0 = begin; i0 < end; i0 += kHeld * kWave) {
+        if (end - begin > kHeld * kWave) hold(i0);
+#pragma unroll
+        for (int h = 0; h < kHeld; ++h) {
+            const int i = i0 + h * kWave + lane;
+            if (i0 + h * kWave >= end) break;
+            const bool there = i < end;
+            const int e = there ? bin_of(held[h], E) : 0;
+            unsigned long long alike = __ballot(there);
+            for (int b = 0; b < bits; ++b) {
+                const unsigned long long with = __ballot(e >> b & 1);
+                alike &= e >> b & 1 ? with : ~with;
+            }
+            if (there) {
+                const int rank = __popcll(alike & ((1ull << lane) - 1)), at = hist[wave][e] + rank;
+                const int64_t s = from + i;
+                a.slot[at] = e < E ? (int)s : -1 - (int)s;
+                a.pos[s] = e < E ? at : -1;
+            }
+            // (a wave's reads come before its later writes)
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+            if (there && (alike >> lane) == 1) hist[wave][e] += __popcll(alike);
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
         }
-        if (there) {
-            const int rank = __popcll(alike & ((1ull << lane) - 1)), at = hist[wave][e] + rank;
-            const int64_t s = from + i;
-            a.slot[at] = e < E ? (int)s : -1 - (int)s;
-            a.pos[s] = e < E ? at : -1;
-        }
-        // (a wave's reads come before its later writes)
-        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-        if (there && (alike >> lane) == 1) hist[wave][e] += __popcll(alike);
-        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     }
 }
 
@@ -658,9 +734,14 @@ int launch_route(gr_experts* h, const RouteIn& in, int dtype, float* weight, int
 {
     return by_type(dtype, [&](auto t) {
         typedef decltype(t) T;
-        RouteArgs a{in, weight, expert, team_log(in.n_expert), whole_rows<T>(in.logits, nullptr, in.n_expert), {}};
+        const int size = in.n_expert / in.n_group;
+        RouteArgs a{in, weight, expert, team_log(in.n_expert), whole_rows<T>(in.logits, nullptr, in.n_expert), (uint32_t)(((1 << 20) + size - 1) / size), {}};
         if (off) {
-            const int rows = kBlock >> a.lg;
+            // a unit of slots is what a workgroup chooses: more than one batch of rows where that leaves enough workgroups
+            int rows = kBlock >> a.lg;
+            const int64_t batches = (in.rows + rows - 1) / rows;
+            if (batches >= 4 * kEnoughUnits) rows *= 4;
+            else if (batches >= 2 * kEnoughUnits) rows *= 2;
             a.plan = {expert, h->counts, off, slot, pos, in.rows * in.top_k, in.n_expert, (int)((in.rows + rows - 1) / rows), rows * in.top_k, 0};
         }
         in.top_k <= 2 ? route_by_form<T, 2>(a, s) : in.top_k <= 8 ? route_by_form<T, 8>(a, s) : route_by_form<T, 16>(a, s);

@@ -14,6 +14,7 @@
 
 #include <cstdint>
 #include <exception>
+#include <vector>
 
 namespace {
 
@@ -30,11 +31,24 @@ struct Entries {
     int (*route_feedback)(void*, int64_t, int64_t, const void*, const void*, const void*, const void*, void*, void*, void*, void*);
     int (*risk_scan)(void*, const void*, const void*, const void*, const void*, int64_t, const void*, const void*, const void*,
                      int64_t, const void*, void*, void*, void*, void*, void*, void*);
+    int (*expert_route)(void*, int64_t, int32_t, const void*, int32_t, const void*, int32_t, int32_t, int32_t, int32_t, float, void*, void*,
+                        void*, void*, void*, void*);
+    int (*expert_route_backward)(void*, int64_t, int32_t, const void*, int32_t, int32_t, int32_t, float, const void*, const void*, void*, void*);
+    int (*expert_plan)(void*, int64_t, int32_t, const void*, void*, void*, void*, void*);
+    int (*expert_linear)(void*, int64_t, int32_t, int32_t, int32_t, const void*, const void*, int32_t, const void*, const void*, const void*,
+                         int32_t, void*, void*);
+    int (*expert_linear_backward)(void*, int64_t, int32_t, int32_t, int32_t, const void*, const void*, int32_t, const void*, const void*,
+                                  const void*, const void*, void*, void*, void*, void*, void*);
+    int (*expert_combine)(void*, int64_t, int32_t, int32_t, int32_t, const void*, const void*, const void*, void*, void*);
+    int (*expert_combine_backward)(void*, int64_t, int32_t, int32_t, int32_t, const void*, const void*, const void*, const void*, void*, void*,
+                                   void*);
+    int (*clip_gradients)(void*, int32_t, const void* const*, void* const*, const int64_t*, const int32_t*, float, void*, void*);
 } entries;
 
 PyObject* check_slowly = nullptr;      // (tensor, type code, name, elements or None) -> address or None, or raises
 
 struct Raised {};      // a Python exception is set
+struct Unclear {};     // for the binding itself to judge (calls of a length predictor)
 
 constexpr int64_t kAny = -1;
 
@@ -108,6 +122,8 @@ PyObject* guarded(PyObject*, PyObject* const* a, Py_ssize_t n)
     try {
         return kCall(a);
     } catch (const Raised&) {
+    } catch (const Unclear&) {
+        Py_RETURN_NONE;
     } catch (const std::exception& e) {
         PyErr_SetString(PyExc_RuntimeError, e.what());
     }
@@ -215,6 +231,174 @@ PyObject* risk_scan(PyObject* const* a)
                 target, slack, n_flagged, stream());
 }
 
+// ---- the calls of a length predictor: None is returned, and nothing called, where an argument is not plainly right
+
+const at::TensorBase& plain(PyObject* o, int64_t dims = kAny)
+{
+    if (!THPVariable_CheckExact(o)) throw Unclear{};
+    const at::TensorBase& t = THPVariable_Unpack(o);
+    if (!t.is_cuda() || !t.is_contiguous() || (dims != kAny && t.dim() != dims)) throw Unclear{};
+    return t;
+}
+
+void* plain(PyObject* o, at::ScalarType type, int64_t need)
+{
+    if (o == Py_None) return nullptr;
+    const at::TensorBase& t = plain(o);
+    if (t.scalar_type() != type || t.numel() < need) throw Unclear{};
+    return t.data_ptr();
+}
+
+int32_t type_code(const at::TensorBase& t)
+{
+    switch (t.scalar_type()) {
+        case at::kFloat: return 0;
+        case at::kBFloat16: return 1;
+        case at::kHalf: return 2;
+        default: throw Unclear{};
+    }
+}
+
+void must(bool ok)
+{
+    if (!ok) throw Unclear{};
+}
+
+int32_t small(PyObject* o)
+{
+    const int64_t v = integer(o);
+    must(v >= INT32_MIN && v <= INT32_MAX);
+    return (int32_t)v;
+}
+
+float real(PyObject* o)
+{
+    const double v = PyFloat_AsDouble(o);
+    if (v == -1 && PyErr_Occurred()) throw Raised{};
+    return (float)v;
+}
+
+// n_expert, logits, out_weight, out_expert, out_off, out_slot, out_pos, bias, scoring, n_group, n_group_kept, renormalise, scale
+PyObject* expert_route(PyObject* const* a)
+{
+    const int64_t E = integer(a[1]);
+    const at::TensorBase &x = plain(a[2], 2), &e = plain(a[4], 2);
+    const int64_t T = x.size(0), k = e.size(1), S = T * k;
+    must(x.size(1) == E && e.size(0) == T && k <= INT32_MAX);
+    return call(entries.expert_route, handle(a[0]), T, (int32_t)k, (const void*)x.data_ptr(), type_code(x), (const void*)plain(a[8], at::kFloat, E),
+                small(a[9]), small(a[10]), small(a[11]), small(a[12]), real(a[13]), plain(a[3], at::kFloat, S), plain(a[4], at::kInt, S),
+                plain(a[5], at::kInt, E + 1), plain(a[6], at::kInt, S), plain(a[7], at::kInt, S), stream());
+}
+
+// n_expert, logits, expert, dweight, out_dlogits, scoring, renormalise, scale
+PyObject* expert_route_backward(PyObject* const* a)
+{
+    const at::TensorBase &x = plain(a[2], 2), &e = plain(a[3], 2);
+    const int64_t T = x.size(0), k = e.size(1);
+    must(x.size(1) == integer(a[1]) && e.size(0) == T && k <= INT32_MAX);
+    return call(entries.expert_route_backward, handle(a[0]), T, (int32_t)k, (const void*)x.data_ptr(), type_code(x), small(a[6]), small(a[7]), real(a[8]),
+                (const void*)plain(a[3], at::kInt, T * k), (const void*)plain(a[4], at::kFloat, T * k), plain(a[5], x.scalar_type(), x.numel()), stream());
+}
+
+// n_expert, expert, out_off, out_slot, out_pos
+PyObject* expert_plan(PyObject* const* a)
+{
+    const at::TensorBase& e = plain(a[2], 2);
+    must(e.size(1) <= INT32_MAX);
+    return call(entries.expert_plan, handle(a[0]), (int64_t)e.size(0), (int32_t)e.size(1), (const void*)plain(a[2], at::kInt, 0),
+                plain(a[3], at::kInt, integer(a[1]) + 1), plain(a[4], at::kInt, e.numel()), plain(a[5], at::kInt, e.numel()), stream());
+}
+
+struct Layer {
+    int64_t E, n;
+    int32_t I, O, type, top_k;
+    at::ScalarType scalar;
+    const void *off, *slot, *x, *w;
+
+    // n_expert, x, w; what has a row per position; off, slot, top_k
+    Layer(PyObject* n_expert, PyObject* x_, PyObject* w_, PyObject* by_position, PyObject* off_, PyObject* slot_, PyObject* top_k_)
+    {
+        const at::TensorBase &x_t = plain(x_, 2), &w_t = plain(w_), &p = plain(by_position, 2);
+        const int64_t N = integer(n_expert), d = w_t.dim();
+        E = off_ == Py_None ? 1 : N;
+        must(d == 3 ? w_t.size(0) == E : d == 2 && off_ == Py_None);
+        must(w_t.size(d - 1) <= INT32_MAX && w_t.size(d - 2) <= INT32_MAX);
+        I = (int32_t)w_t.size(d - 1);
+        O = (int32_t)w_t.size(d - 2);
+        n = p.size(0);
+        top_k = small(top_k_);
+        type = type_code(x_t);
+        scalar = x_t.scalar_type();
+        must(p.size(1) == O && x_t.size(1) == I && w_t.scalar_type() == scalar && p.scalar_type() == scalar);
+        must(slot_ == Py_None ? x_t.size(0) == n : top_k >= 1 && x_t.size(0) == (n + top_k - 1) / top_k);
+        off = plain(off_, at::kInt, N + 1);
+        slot = plain(slot_, at::kInt, n);
+        x = x_t.data_ptr();
+        w = w_t.data_ptr();
+    }
+};
+
+// n_expert, x, w, out_y, bias, off, slot, top_k, relu
+PyObject* expert_linear(PyObject* const* a)
+{
+    const Layer l(a[1], a[2], a[3], a[4], a[6], a[7], a[8]);
+    return call(entries.expert_linear, handle(a[0]), l.n, l.I, l.O, l.type, l.off, l.slot, l.top_k, l.x, l.w, (const void*)plain(a[5], l.scalar, l.E * l.O),
+                small(a[9]), plain(a[4], l.scalar, l.n * l.O), stream());
+}
+
+// n_expert, x, w, dy, out_dx, out_dw, out_db, y, out_dz, off, slot, top_k
+PyObject* expert_linear_backward(PyObject* const* a)
+{
+    const Layer l(a[1], a[2], a[3], a[4], a[10], a[11], a[12]);
+    const int64_t of_y = l.n * l.O;
+    return call(entries.expert_linear_backward, handle(a[0]), l.n, l.I, l.O, l.type, l.off, l.slot, l.top_k, l.x, l.w, (const void*)plain(a[8], l.scalar, of_y),
+                (const void*)plain(a[4], l.scalar, of_y), plain(a[9], l.scalar, of_y), plain(a[5], l.scalar, l.n * l.I),
+                plain(a[6], l.scalar, l.E * l.O * l.I), plain(a[7], l.scalar, l.E * l.O), stream());
+}
+
+// y, pos, out, weight
+PyObject* expert_combine(PyObject* const* a)
+{
+    const at::TensorBase &pos = plain(a[2], 2), &out = plain(a[3], 2);
+    const int64_t T = pos.size(0), S = pos.numel(), O = out.size(1);
+    must(out.size(0) == T && O <= INT32_MAX && pos.size(1) <= INT32_MAX);
+    return call(entries.expert_combine, handle(a[0]), T, (int32_t)pos.size(1), (int32_t)O, type_code(out), (const void*)plain(a[4], at::kFloat, S),
+                (const void*)plain(a[2], at::kInt, S), (const void*)plain(a[1], out.scalar_type(), S * O), out.data_ptr(), stream());
+}
+
+// dout, y, slot, out_dy, weight, out_dweight
+PyObject* expert_combine_backward(PyObject* const* a)
+{
+    const at::TensorBase &d = plain(a[1], 2), &slot = plain(a[3]);
+    const int64_t T = d.size(0), O = d.size(1), S = slot.numel();
+    must(T > 0 && S % T == 0 && S / T <= INT32_MAX && O <= INT32_MAX);
+    return call(entries.expert_combine_backward, handle(a[0]), T, (int32_t)(S / T), (int32_t)O, type_code(d), (const void*)plain(a[5], at::kFloat, S),
+                (const void*)plain(a[3], at::kInt, S), (const void*)plain(a[2], d.scalar_type(), S * O), (const void*)d.data_ptr(),
+                plain(a[4], d.scalar_type(), S * O), plain(a[6], at::kFloat, S), stream());
+}
+
+// grads, max_norm, out_norm, out (lists of as many)
+PyObject* clip_gradients(PyObject* const* a)
+{
+    must(PyList_CheckExact(a[1]) && PyList_CheckExact(a[4]));
+    const Py_ssize_t n = PyList_GET_SIZE(a[1]);
+    must(PyList_GET_SIZE(a[4]) == n && n <= INT32_MAX);
+    std::vector<const void*> grad(n);
+    std::vector<void*> out(n);
+    std::vector<int64_t> count(n);
+    std::vector<int32_t> type(n);
+    for (Py_ssize_t i = 0; i < n; ++i) {
+        const at::TensorBase& g = plain(PyList_GET_ITEM(a[1], i));
+        grad[i] = g.data_ptr();
+        count[i] = g.numel();
+        type[i] = type_code(g);
+        must(PyList_GET_ITEM(a[4], i) != Py_None);
+        out[i] = plain(PyList_GET_ITEM(a[4], i), g.scalar_type(), count[i]);
+    }
+    return call(entries.clip_gradients, handle(a[0]), (int32_t)n, (const void* const*)grad.data(), (void* const*)out.data(), (const int64_t*)count.data(),
+                (const int32_t*)type.data(), real(a[2]), plain(a[3], at::kFloat, 1), stream());
+}
+
 // check_slowly, then the addresses of the entry points in the order of Entries
 PyObject* connect(PyObject* const* a)
 {
@@ -228,7 +412,10 @@ PyObject* connect(PyObject* const* a)
 #define GR_METHOD(name, n) {#name, (PyCFunction)(void (*)(void))guarded<n, name>, METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {GR_METHOD(build_status, 13), GR_METHOD(score_route, 10), GR_METHOD(score_route_noalloc, 8),
                          GR_METHOD(score_route_cached, 13), GR_METHOD(route_feedback, 9), GR_METHOD(risk_scan, 15),
-                         GR_METHOD(connect, 7), {nullptr, nullptr, 0, nullptr}};
+                         GR_METHOD(expert_route, 14), GR_METHOD(expert_route_backward, 9), GR_METHOD(expert_plan, 6),
+                         GR_METHOD(expert_linear, 10), GR_METHOD(expert_linear_backward, 13), GR_METHOD(expert_combine, 5),
+                         GR_METHOD(expert_combine_backward, 7), GR_METHOD(clip_gradients, 5),
+                         GR_METHOD(connect, 15), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "marshal", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace
