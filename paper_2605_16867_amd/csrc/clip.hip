@@ -9,6 +9,8 @@ namespace {
 
 constexpr int kBlock = 256;
 constexpr int kWave = 64;
+constexpr int kFewThreads = 1024, kFewTensors = 16;
+constexpr int64_t kFewBytes = 512 << 10, kAloneBytes = 64 << 10;
 constexpr int kPiece = kBlock * 4 * 16;      // bytes of a gradient that a workgroup takes at a time
 
 struct ClipTable {
@@ -44,8 +46,9 @@ template <typename T, typename F, typename G>
 __device__ __forceinline__ void each(const Piece& p, bool aligned, F chunk, G one)
 {
     const int count = (int)(p.bytes / sizeof(T)), chunks = aligned ? count / Chunk<T>::n : 0;
-    for (int i = threadIdx.x; i < chunks; i += kBlock) chunk(i);
-    for (int i = chunks * Chunk<T>::n + threadIdx.x; i < count; i += kBlock) one(i);
+#pragma unroll 4
+    for (int i = threadIdx.x; i < chunks; i += blockDim.x) chunk(i);
+    for (int i = chunks * Chunk<T>::n + threadIdx.x; i < count; i += blockDim.x) one(i);
 }
 
 template <typename T>
@@ -82,14 +85,33 @@ __device__ __forceinline__ void scale(const Piece& p, float by)
 }
 
 // The workgroup's sum, in thread 0.
+template <int kThreads>
 __device__ __forceinline__ double block_sum(double v)
 {
-    __shared__ double part[kBlock / kWave];
+    __shared__ double part[kThreads / kWave];
     for (int m = 1; m < kWave; m *= 2) v += __shfl_xor(v, m);
     if (threadIdx.x % kWave == 0) part[threadIdx.x / kWave] = v;
     __syncthreads();
-    for (int w = 1; w < kBlock / kWave; ++w) v += threadIdx.x == 0 ? part[w] : 0.0;
+    for (int w = 1; w < kThreads / kWave; ++w) v += threadIdx.x == 0 ? part[w] : 0.0;
     return v;
+}
+
+__device__ __forceinline__ double squares_of(const Piece& p, int)
+{
+    return p.type == GR_F32 ? squares_of<float>(p) : p.type == GR_BF16 ? squares_of<bf16>(p) : squares_of<f16>(p);
+}
+
+__device__ __forceinline__ void scale(const Piece& p, float by, int)
+{
+    if (p.type == GR_F32) scale<float>(p, by);
+    else if (p.type == GR_BF16) scale<bf16>(p, by);
+    else scale<f16>(p, by);
+}
+
+// What gradients are multiplied by.
+__device__ __forceinline__ float factor(double norm, double max_norm)
+{
+    return norm > max_norm && norm < __builtin_inf() ? (float)(max_norm / norm) : 1.0f;
 }
 
 __global__ __launch_bounds__(kBlock) void k_norm(ClipTable t, double* squares)
@@ -97,9 +119,9 @@ __global__ __launch_bounds__(kBlock) void k_norm(ClipTable t, double* squares)
     double sum = 0;
     for (int at = blockIdx.x; at < t.pieces_before[t.n]; at += gridDim.x) {
         const Piece p = piece_of(t, at);
-        sum += p.type == GR_F32 ? squares_of<float>(p) : p.type == GR_BF16 ? squares_of<bf16>(p) : squares_of<f16>(p);
+        sum += squares_of(p, 0);
     }
-    sum = block_sum(sum);
+    sum = block_sum<kBlock>(sum);
     if (threadIdx.x == 0) squares[blockIdx.x] = sum;
 }
 
@@ -108,10 +130,10 @@ __global__ __launch_bounds__(kBlock) void k_clip(ClipTable t, const double* squa
     __shared__ float by;
     double sum = 0;
     for (int i = threadIdx.x; i < parts; i += kBlock) sum += squares[i];
-    sum = block_sum(sum);
+    sum = block_sum<kBlock>(sum);
     if (threadIdx.x == 0) {
         const double all = sqrt(sum);
-        by = all > max_norm && all < __builtin_inf() ? (float)(max_norm / all) : 1.0f;
+        by = factor(all, max_norm);
         if (norm && blockIdx.x == 0) *norm = (float)all;
     }
     __syncthreads();
@@ -119,10 +141,28 @@ __global__ __launch_bounds__(kBlock) void k_clip(ClipTable t, const double* squa
     for (int at = blockIdx.x; at < t.pieces_before[t.n]; at += gridDim.x) {
         const Piece p = piece_of(t, at);
         if (f == 1.0f && p.grad == p.out) continue;
-        if (p.type == GR_F32) scale<float>(p, f);
-        else if (p.type == GR_BF16) scale<bf16>(p, f);
-        else scale<f16>(p, f);
+        scale(p, f, 0);
     }
+}
+
+// Little enough that every workgroup reads all of it, and one launch does: the same sum in each, and a share of the pieces.
+__global__ __launch_bounds__(kFewThreads) void k_clip_few(ClipTable t, double max_norm, float* norm)
+{
+    __shared__ float by;
+    double sum = 0;
+    for (int i = 0; i < t.n; ++i) {
+        const int type = (int)(t.count_type[i] & 3);
+        sum += squares_of(Piece{static_cast<const char*>(t.grad[i]), nullptr, (t.count_type[i] >> 2) * (type == GR_F32 ? 4 : 2), type}, 0);
+    }
+    sum = block_sum<kFewThreads>(sum);
+    if (threadIdx.x == 0) {
+        const double all = sqrt(sum);
+        by = factor(all, max_norm);
+        if (norm && blockIdx.x == 0) *norm = (float)all;
+    }
+    __syncthreads();
+    const float f = by;
+    for (int at = blockIdx.x; at < t.pieces_before[t.n]; at += gridDim.x) scale(piece_of(t, at), f, 0);
 }
 
 }  // namespace
@@ -150,6 +190,16 @@ int launch_clip(gr_experts* h, int n, const void* const* grad, void* const* out,
         } while (i < n);
         return parts;
     };
+    int64_t bytes = 0;
+    bool apart = true;      // (a workgroup may be done while another still reads: in place only one may do all)
+    for (int i = 0; i < n && bytes <= kFewBytes; ++i) {
+        bytes += count[i] * (int64_t)size_of(dtype[i]);
+        apart = apart && (out[i] != grad[i] || count[i] == 0);
+    }
+    if (n <= kFewTensors && bytes <= (apart ? kFewBytes : kAloneBytes)) {
+        each_table([&](const ClipTable& t, int blocks, int) { k_clip_few<<<apart ? blocks : 1, kFewThreads, 0, s>>>(t, max_norm, norm); });
+        return launched();
+    }
     const int parts = each_table([&](const ClipTable& t, int blocks, int at) { k_norm<<<blocks, kBlock, 0, s>>>(t, h->squares + at); });
     if (parts < 0) return parts;
     each_table([&](const ClipTable& t, int blocks, int at) { k_clip<<<blocks, kBlock, 0, s>>>(t, h->squares, parts, max_norm, at == 0 ? norm : nullptr); });

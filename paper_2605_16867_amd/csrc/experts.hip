@@ -11,7 +11,7 @@ constexpr int kWave = 64;
 constexpr int kPlanWaves = kBlock / kWave;
 constexpr int kScanBlock = 1024;
 constexpr int kEnoughUnits = 1024;   // four workgroups a compute unit
-constexpr int kFewUnits = 32;        // units of slots whose counts every workgroup adds up by itself
+constexpr int kFewUnits = 128;       // units of slots whose counts every workgroup adds up by itself
 
 // ---- within a team of lanes ----------------------------------------------------------------------
 //
@@ -268,16 +268,17 @@ __global__ __launch_bounds__(kBlock) void k_route(RouteArgs a)
             __syncthreads();
             const int size = E / a.in.n_group;
             for (int g = lane; g < a.in.n_group; g += team) {
-                double b0 = kNoExpert, b1 = kNoExpert;
+                // (what is no number counts as the least score meanwhile)
+                constexpr float kNone = -__builtin_inff(), kLeast = -3.4028235e38f;
+                float b0 = kNone, b1 = kNone;
+#pragma unroll 4
                 for (int i = 0; i < size; ++i) {
-                    const double key = key_of(c_mine[g * size + i], 0);
-                    b1 = key_max(b1, key_min(b0, key));
-                    b0 = key_max(b0, key);
+                    const float v = c_mine[g * size + i], w = v == v ? v : kLeast;
+                    b1 = __builtin_fmaxf(b1, __builtin_fminf(b0, w));
+                    b0 = __builtin_fmaxf(b0, w);
                 }
-                // (the least score stands for what is no number)
-                const auto value = [](double key) { return key == kNoExpert ? 0.0f : key < -3.4028234e38 ? __builtin_nanf("") : (float)key; };
-                const float sum = value(b0) + value(b1);
-                g_mine[g] = key_of(b0 == kNoExpert ? -__builtin_inff() : sum, g);
+                const auto value = [](float v) { return v == kNone ? 0.0f : v == kLeast ? __builtin_nanf("") : v; };
+                g_mine[g] = key_of(b0 == kNone ? kNone : value(b0) + value(b1), g);
             }
             __syncthreads();
             kept = 0;
@@ -552,9 +553,10 @@ __device__ void place_unit(const PlanArgs& a, int unit, int (*hist)[GR_MAX_EXPER
                 mine = a.counts[(int64_t)e * a.units + unit];
                 all = a.counts[(int64_t)(E + 1) * a.units + e];
             } else {
+#pragma unroll 8
                 for (int u = 0; u < a.units; ++u) {
-                    const int c = a.counts[(int64_t)e * a.units + u];
-                    if (u < unit) mine += c;
+                    const int c = a.counts[e * a.units + u];
+                    mine += u < unit ? c : 0;
                     all += c;
                 }
             }

@@ -39,13 +39,27 @@ __device__ __forceinline__ int64_t bound(const int* off, int e, int n_expert, in
     return v < 0 ? 0 : v > n_pos ? n_pos : v;
 }
 
+// The row of a slot: a product in the place of a division (exact below 2^30, see args_of).
+__device__ __forceinline__ uint32_t row_of_slot(const LinearArgs& a, uint32_t s) { return (a.k_mul ? __umulhi(s, a.k_mul) : s) >> a.k_shift; }
+
 __device__ __forceinline__ int64_t row_of(const LinearArgs& a, int64_t p)
 {
     if (!a.slot) return p;
-    int64_t s = a.slot[p];
+    int s = a.slot[p];
     if (s < 0) s = -1 - s;
-    if (s >= a.n_pos) s = a.n_pos - 1;
-    return s / a.top_k;
+    return row_of_slot(a, s < a.n_pos ? s : (uint32_t)a.n_pos - 1);
+}
+
+// A part of an expert's positions (all of them where they are not cut), in whole slices of the reduction.
+constexpr int kDepth = 64;
+
+__device__ __forceinline__ void part_of(const LinearArgs& a, int e, int part, int64_t& lo, int64_t& depth)
+{
+    const int64_t from = bound(a.off, e, a.n_expert, a.n_pos), until = bound(a.off, e + 1, a.n_expert, a.n_pos);
+    const int64_t slices = (until - from + kDepth - 1) / kDepth, each = (slices + a.parts_n - 1) / a.parts_n * kDepth;
+    lo = from + part * each;
+    depth = until - lo < each ? until - lo : each;
+    if (depth < 0) depth = 0;
 }
 
 // A block of rows of the output: an expert (n_expert: rows without one) and positions lo .. hi - 1.
@@ -126,19 +140,23 @@ __device__ __forceinline__ f32x4 mfma(f16x8 a, f16x8 b, f32x4 acc) { return __bu
 
 // ---- any sizes, any alignment -------------------------------------------------------------------
 //
-// Tiles of kTile by kTile, 64 bytes of the reduction at a time, loaded element by element into registers while the
+// Tiles of 64 by 64, 64 bytes of the reduction at a time, loaded into registers (element by element, or 16 bytes at a time in single precision where rows are whole ones) while the
 // tile before is multiplied, and laid into shared memory with the reduction contiguous.
+
+constexpr int kAnyTile = 64;
 
 template <typename T>
 constexpr int kAnyDepth = 64 / sizeof(T);
 
-template <typename T, Product kProduct, int kTile>
+template <typename T, Product kProduct, int kVec>
 __global__ __launch_bounds__(kBlock) void k_linear_any(LinearArgs a)
 {
-    constexpr int D = kAnyDepth<T>, kLd = D + Chunk<T>::n, kPer = kTile * D / kBlock;
+    constexpr int kRows = kAnyTile, kCols = kAnyTile;
+    constexpr int D = kAnyDepth<T>, kLd = D + Chunk<T>::n, kPerP = kRows * D / kBlock / kVec, kPerQ = kCols * D / kBlock / kVec;
     typedef typename Chunk<T>::Vec Vec;
     constexpr int n = Chunk<T>::n;
-    __shared__ __attribute__((aligned(16))) T lds_p[kTile * kLd], lds_q[kTile * kLd];
+    typedef T Get __attribute__((ext_vector_type(kVec)));
+    __shared__ __attribute__((aligned(16))) T lds_p[kRows * kLd], lds_q[kCols * kLd];
 
     const int tid = threadIdx.x, lane = tid % kWave, wave = tid / kWave;
     const TileNo no = tile_no(blockIdx.x, a.down, a.tiles, a.block);
@@ -149,109 +167,137 @@ __global__ __launch_bounds__(kBlock) void k_linear_any(LinearArgs a)
     const int I = a.n_in, O = a.n_out;
 
     // the output's rows p0 .. p0 + p_n - 1 (positions, or output features of an expert), columns q0 .. q0 + q_n - 1
-    int e;
+    int e, part = 0;
     int64_t p0, lo = 0, depth;
-    int p_n, q0 = no.col * kTile, q_n;
+    int p_n, q0 = no.col * kCols, q_n;
     if constexpr (kProduct == kByWeight) {
-        const int tiles = (O + kTile - 1) / kTile;
-        e = (int)(row_no / tiles);
-        p0 = (row_no - (int64_t)e * tiles) * kTile;
-        p_n = O - p0 < kTile ? (int)(O - p0) : kTile;
-        q_n = I - q0 < kTile ? I - q0 : kTile;
-        lo = bound(a.off, e, a.n_expert, a.n_pos);
-        depth = bound(a.off, e + 1, a.n_expert, a.n_pos) - lo;
+        const int tiles = (O + kRows - 1) / kRows, of = (int)(row_no / tiles);
+        e = of / a.parts_n;
+        part = of - e * a.parts_n;
+        p0 = (row_no - (int64_t)of * tiles) * kRows;
+        p_n = O - p0 < kRows ? (int)(O - p0) : kRows;
+        q_n = I - q0 < kCols ? I - q0 : kCols;
+        part_of(a, e, part, lo, depth);
     } else {
-        const RowTile t = row_tile<kTile>(a, row_no);
+        const RowTile t = row_tile<kRows>(a, row_no);
         if (t.hi <= t.lo) return;
         e = t.expert;
         p0 = t.lo;
         p_n = (int)(t.hi - t.lo);
         const int width = kProduct == kForward ? O : I;
-        q_n = width - q0 < kTile ? width - q0 : kTile;
+        q_n = width - q0 < kCols ? width - q0 : kCols;
         depth = e == a.n_expert ? 0 : kProduct == kForward ? I : O;
     }
     const T* const w = static_cast<const T*>(a.w) + (kProduct == kByWeight || e == a.n_expert ? 0 : (int64_t)e * O * I);
 
-    // which of the tile's elements a thread loads: kPer of each operand, along the direction that is contiguous in memory
+    // which of the tile's elements a thread loads, kVec at a time: along the direction that is contiguous in memory
     constexpr bool kPLong = kProduct != kByWeight, kQLong = kProduct == kForward;      // that is the reduction's
-    const auto place = [&](bool along, int i, int& row, int& r) {
-        const int at = i * kBlock + tid;
+    const auto place = [&](bool along, int size, int i, int& row, int& r) {
+        const int at = (i * kBlock + tid) * kVec;
         if (along) { row = at / D; r = at % D; }
-        else { r = at / kTile; row = at % kTile; }
+        else { r = at / size; row = at % size; }
     };
-    int64_t p_row[kPer];      // where the rows of the left operand start
+    // (rows past the edge are loaded from within it: what becomes of them is not stored; past the end of the reduction there are zeros)
+    const T *from_p[kPerP], *from_q[kPerQ];
 #pragma unroll
-    for (int i = 0; i < kPer; ++i) {
+    for (int i = 0; i < kPerP; ++i) {
         int row, r;
-        place(kPLong, i, row, r);
-        p_row[i] = 0;
-        if (kProduct == kForward && row < p_n && e < a.n_expert) p_row[i] = row_of(a, p0 + row) * I;
-        if (kProduct == kByInput) p_row[i] = (p0 + row) * O;
+        place(kPLong, kRows, i, row, r);
+        row = row < p_n ? row : p_n - 1;
+        if constexpr (kProduct == kForward) from_p[i] = x + (e < a.n_expert ? row_of(a, p0 + row) : 0) * I + r;
+        if constexpr (kProduct == kByInput) from_p[i] = dz + (p0 + row) * O + r;
+        if constexpr (kProduct == kByWeight) from_p[i] = dz + (lo + r) * O + p0 + row;
     }
-    T get_p[kPer], get_q[kPer];
-    const auto load = [&](int64_t r0) {
 #pragma unroll
-        for (int i = 0; i < kPer; ++i) {
+    for (int i = 0; i < kPerQ; ++i) {
+        int row, r;
+        place(kQLong, kCols, i, row, r);
+        row = row < q_n ? row : q_n - 1;
+        if constexpr (kProduct == kForward) from_q[i] = w + (int64_t)(q0 + row) * I + r;
+        if constexpr (kProduct == kByInput) from_q[i] = w + (int64_t)r * I + q0 + row;
+        if constexpr (kProduct == kByWeight) from_q[i] = x + q0 + row;
+    }
+    const int64_t step_p = kPLong ? D : (int64_t)D * O, step_q = kQLong ? D : (int64_t)D * I;
+    Get get_p[kPerP], get_q[kPerQ];
+    const auto load = [&](int64_t r0, bool whole) __attribute__((always_inline)) {
+#pragma unroll
+        for (int i = 0; i < kPerP; ++i) {
             int row, r;
-            place(kPLong, i, row, r);
-            const bool in = row < p_n && r0 + r < depth;
-            get_p[i] = (T)0.0f;
-            if (in) get_p[i] = kProduct == kForward ? x[p_row[i] + r0 + r] : kProduct == kByInput ? dz[p_row[i] + r0 + r] : dz[(lo + r0 + r) * O + p0 + row];
+            place(kPLong, kRows, i, row, r);
+            get_p[i] = Get{};
+            if (whole || r0 + r < depth) get_p[i] = *reinterpret_cast<const Get*>(from_p[i]);
+            from_p[i] += step_p;
         }
 #pragma unroll
-        for (int i = 0; i < kPer; ++i) {
+        for (int i = 0; i < kPerQ; ++i) {
             int row, r;
-            place(kQLong, i, row, r);
-            const bool in = row < q_n && r0 + r < depth;
-            get_q[i] = (T)0.0f;
-            if (in) get_q[i] = kProduct == kForward ? w[(int64_t)(q0 + row) * I + r0 + r] : kProduct == kByInput ? w[(r0 + r) * I + q0 + row] : x[row_of(a, lo + r0 + r) * I + q0 + row];
+            place(kQLong, kCols, i, row, r);
+            get_q[i] = Get{};
+            if (whole || r0 + r < depth) get_q[i] = *reinterpret_cast<const Get*>(from_q[i] + (kProduct == kByWeight ? row_of(a, lo + r0 + r) * I : 0));
+            if (kProduct != kByWeight) from_q[i] += step_q;
         }
     };
 
-    constexpr int kFrag = kTile / 32;      // fragments of a wave, either way
-    f32x4 acc[kFrag][kFrag] = {};
-    const int wp = wave / 2 * (kTile / 2), wq = wave % 2 * (kTile / 2);
-    if (depth > 0) load(0);
+    const auto put = [&](T* lds, bool along, int row, int r, const Get& v) __attribute__((always_inline)) {
+        if (along) *reinterpret_cast<Get*>(&lds[row * kLd + r]) = v;
+        else
+#pragma unroll
+            for (int k = 0; k < kVec; ++k) lds[(row + k) * kLd + r] = v[k];
+    };
+    constexpr int kP = kRows / 32, kQ = kCols / 32;      // fragments of a wave
+    f32x4 acc[kP][kQ] = {};
+    const int wp = wave / 2 * (kRows / 2), wq = wave % 2 * (kCols / 2);
+    if (depth > 0) load(0, depth >= D);
     for (int64_t r0 = 0; r0 < depth; r0 += D) {
         __syncthreads();
 #pragma unroll
-        for (int i = 0; i < kPer; ++i) {
+        for (int i = 0; i < kPerP; ++i) {
             int row, r;
-            place(kPLong, i, row, r);
-            lds_p[row * kLd + r] = get_p[i];
-            place(kQLong, i, row, r);
-            lds_q[row * kLd + r] = get_q[i];
+            place(kPLong, kRows, i, row, r);
+            put(lds_p, kPLong, row, r, get_p[i]);
+        }
+#pragma unroll
+        for (int i = 0; i < kPerQ; ++i) {
+            int row, r;
+            place(kQLong, kCols, i, row, r);
+            put(lds_q, kQLong, row, r, get_q[i]);
         }
         __syncthreads();
-        if (r0 + D < depth) load(r0 + D);
-        Vec p[kFrag], q[kFrag];
+        if (r0 + 2 * D <= depth) load(r0 + D, true);
+        else if (r0 + D < depth) load(r0 + D, false);
 #pragma unroll
-        for (int i = 0; i < kFrag; ++i) {
-            p[i] = *reinterpret_cast<const Vec*>(&lds_p[(wp + i * 16 + lane % 16) * kLd + lane / 16 * n]);
-            q[i] = *reinterpret_cast<const Vec*>(&lds_q[(wq + i * 16 + lane % 16) * kLd + lane / 16 * n]);
+        for (int d = 0; d < D; d += 4 * n) {
+            Vec p[kP], q[kQ];
+#pragma unroll
+            for (int i = 0; i < kP; ++i) p[i] = *reinterpret_cast<const Vec*>(&lds_p[(wp + i * 16 + lane % 16) * kLd + d + lane / 16 * n]);
+#pragma unroll
+            for (int i = 0; i < kQ; ++i) q[i] = *reinterpret_cast<const Vec*>(&lds_q[(wq + i * 16 + lane % 16) * kLd + d + lane / 16 * n]);
+            // (columns as the first operand: a lane then holds four neighbours of a row)
+#pragma unroll
+            for (int i = 0; i < kP; ++i)
+#pragma unroll
+                for (int j = 0; j < kQ; ++j) acc[i][j] = mfma(q[j], p[i], acc[i][j]);
         }
-        // (columns as the first operand: a lane then holds four neighbours of a row)
-#pragma unroll
-        for (int i = 0; i < kFrag; ++i)
-#pragma unroll
-            for (int j = 0; j < kFrag; ++j) acc[i][j] = mfma(q[j], p[i], acc[i][j]);
     }
+
     const int width = kProduct == kForward ? O : I;
-    T* const out = static_cast<T*>(a.out) + ((kProduct == kByWeight ? (int64_t)e * O : 0) + p0) * width + q0;
+    const int64_t at = ((kProduct == kByWeight ? ((int64_t)part * a.n_expert + e) * O : 0) + p0) * width + q0;
+    T* const out = static_cast<T*>(a.out) + at;
     const T* const bias = kProduct == kForward && a.bias && e < a.n_expert ? static_cast<const T*>(a.bias) + (int64_t)e * O + q0 : nullptr;
 #pragma unroll
-    for (int i = 0; i < kFrag; ++i) {
+    for (int i = 0; i < kP; ++i) {
         const int row = wp + i * 16 + lane % 16;
         if (row >= p_n) continue;
 #pragma unroll
-        for (int j = 0; j < kFrag; ++j)
+        for (int j = 0; j < kQ; ++j)
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
                 const int col = wq + j * 16 + lane / 16 * 4 + k;
                 if (col >= q_n) continue;
                 float v = acc[i][j][k] + (bias ? (float)bias[col] : 0.0f);
                 if (kProduct == kForward && a.relu && v < 0) v = 0;
-                out[(int64_t)row * width + col] = (T)v;
+                if (kProduct == kByWeight && a.parts) a.parts[at + (int64_t)row * width + col] = v;
+                else out[(int64_t)row * width + col] = (T)v;
             }
     }
 }
@@ -265,7 +311,7 @@ __global__ __launch_bounds__(kBlock) void k_linear_any(LinearArgs a)
 // What is written is one after the other, 16 bytes a lane, so which 16 bytes of memory a lane fetches decides the layout: their number
 // within a line of the tile is exclusive-ored with one made of the line's, so that the lanes of a read meet no bank twice.
 
-constexpr int kDepth = 64, kSlots = 5, kWaves = 4;
+constexpr int kSlots = 5, kWaves = 4;
 
 __device__ const uint4 kZeros = {0, 0, 0, 0};      // where lanes read that are past the end of the reduction
 
@@ -413,11 +459,9 @@ __global__ __launch_bounds__(kWaves * kWave, kSize > 128 ? 1 : 2) void k_linear_
             t.part = part - t.e * a.parts_n;
             t.p0 = (no.row - (int64_t)part * tiles) * kSize;
             t.p_n = O - t.p0 < kSize ? (int)(O - t.p0) : kSize;
-            const int64_t from = uniform(bound(a.off, t.e, a.n_expert, a.n_pos)), until = uniform(bound(a.off, t.e + 1, a.n_expert, a.n_pos));
-            const int64_t slices = (until - from + kDepth - 1) / kDepth, each = (slices + a.parts_n - 1) / a.parts_n * kDepth;
-            t.lo = from + t.part * each;
-            t.depth = until - t.lo < each ? until - t.lo : each;
-            if (t.depth < 0) t.depth = 0;
+            part_of(a, t.e, t.part, t.lo, t.depth);
+            t.lo = uniform(t.lo);
+            t.depth = uniform(t.depth);
         } else {
             RowTile r{a.n_expert, 0, 0};
             if (by_lane) {
@@ -496,7 +540,7 @@ __global__ __launch_bounds__(kWaves * kWave, kSize > 128 ? 1 : 2) void k_linear_
             if (at >= a.n_pos) at = a.n_pos - 1;
             uint32_t s = a.slot ? (uint32_t)a.slot[at] : (uint32_t)at;
             if (s >= a.n_pos) s = (uint32_t)a.n_pos - 1;
-            if (a.slot) s = (a.k_mul ? __umulhi(s, a.k_mul) : s) >> a.k_shift;
+            if (a.slot) s = row_of_slot(a, s);
             to[r] = (int)s;
         }
         return to;
@@ -724,19 +768,20 @@ __global__ __launch_bounds__(kWaves * kWave, kSize > 128 ? 1 : 2) void k_linear_
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
 }
 
-// The parts of sums, added in their order.
-template <typename T>
+// The parts of sums, added in their order; N at a time.
+template <typename T, int N>
 __global__ __launch_bounds__(kBlock) void k_join(const float* parts, int n, int64_t count, T* out)
 {
-    const int64_t i = ((int64_t)blockIdx.x * kBlock + threadIdx.x) * 4;      // (both widths are multiples of 8)
+    typedef float Sums __attribute__((ext_vector_type(N)));
+    typedef T Out __attribute__((ext_vector_type(N)));
+    const int64_t i = ((int64_t)blockIdx.x * kBlock + threadIdx.x) * N;
     if (i >= count) return;
-    f32x4 sum = *reinterpret_cast<const f32x4*>(parts + i);
-    for (int k = 1; k < n; ++k) sum += *reinterpret_cast<const f32x4*>(parts + k * count + i);
-    typedef T Four __attribute__((ext_vector_type(4)));
-    Four o;
+    Sums sum = *reinterpret_cast<const Sums*>(parts + i);
+    for (int k = 1; k < n; ++k) sum += *reinterpret_cast<const Sums*>(parts + k * count + i);
+    Out o;
 #pragma unroll
-    for (int k = 0; k < 4; ++k) o[k] = (T)sum[k];
-    *reinterpret_cast<Four*>(out + i) = o;
+    for (int k = 0; k < N; ++k) o[k] = (T)sum[k];
+    *reinterpret_cast<Out*>(out + i) = o;
 }
 
 // ---- few rows an expert ------------------------------------------------------------------------
@@ -917,7 +962,7 @@ int tiles_of(int width, int tile) { return (width + tile - 1) / tile; }
 template <typename T>
 bool in_tiles(const LinearIn& in, const void* a, const void* b, const void* c)
 {
-    return sizeof(T) == 2 && in.n_in % 8 == 0 && in.n_out % 8 == 0 && aligned16(a) && aligned16(b) && aligned16(c);
+    return in.n_in % Chunk<T>::n == 0 && in.n_out % Chunk<T>::n == 0 && aligned16(a) && aligned16(b) && aligned16(c);
 }
 
 // Which form a product takes (bfloat16, 9 experts, before / after the change of form):
@@ -925,25 +970,44 @@ constexpr int kUnits = 256;          // compute units: workgroups of large tiles
 // Large tiles from four rounds of them on.  Forward, 128 / 256: 8 192 x 4 096 -> 1 024 (165 tiles) 93 / 101 us, 65 536 x 1 024 -> 512 (530) 85 / 104,
 // 65 536 x 4 096 -> 1 024 (1 060) 607 / 535; by input 65 536 x 1 024 -> 512 (1 060) 111 / 112, 65 536 x 1 024 -> 4 096 (4 240) 703 / 614.
 constexpr int kLargeRounds = 4;
-constexpr int kAnyRounds = 4;        // the same of the tiles for any sizes: 4 099 x 2 positions, 1 023 -> 511, single precision, 128 / 64: 180 / 130 us
 // Few rows: up to 16 an expert on average, 256 in all (an expert may have them all, and its weights are read again for every 16).
 // 4 096 -> 1 024, tiles / this: 9 positions 39 / 17 us, 72 39 / 21, 144 39 / 36, 288 38 / 59.
 constexpr int kFewRows = 16, kFewExperts = 16;
 // By weight, where the tiles are fewer than two rounds: as many parts of the positions as fill those, of at least 1 024 positions each.
 // One part / several: 131 072 x 512 -> 128 (36 tiles) 279 / 56 us, 65 536 x 1 024 -> 512 (288) 172 / 137, 16 384 x 1 024 -> 512 50 / 52.
 constexpr int kPartRounds = 2, kPartRows = 1024;
+// The tiles for any sizes are of 64 by 64 (8 198 x 1 023 -> 511 forward, single precision: 149 us, of 128 by 128 189; 65 536 x 257 -> 129 99, 152), eight
+// to a compute unit: by weight in parts up to there (65 536 x 257 -> 129: 590 us in one, 156).
+constexpr int kAnyEnough = 8 * kUnits;
 
 template <typename T, Product kProduct>
 void product(gr_experts* h, const LinearIn& in, LinearArgs a, bool tiles, hipStream_t s)
 {
     const int width = kProduct == kForward ? in.n_out : in.n_in;
-    a.parts_n = 1;
     const auto grid = [&](int size) {
         a.tiles = tiles_of(width, size);
         a.block = a.tiles < 8 ? 8 : 4;
         a.down = kProduct == kByWeight ? (int64_t)a.n_expert * tiles_of(in.n_out, size) * a.parts_n : row_tiles(in, size);
         const int64_t all = a.down * a.tiles, round = all < kDies * kTogether ? kDies : kDies * kTogether;
         return (all + round - 1) / round * round;
+    };
+    a.parts_n = 1;
+    // by weight: where the tiles are few, parts of the positions apart, as many as make up for it
+    const int64_t one = (int64_t)a.n_expert * in.n_out * in.n_in;
+    const auto cut = [&](int size, int64_t enough) {
+        int64_t parts = enough / grid(size);
+        if (parts > (int64_t)kPartFloats / one) parts = (int64_t)kPartFloats / one;
+        if (parts > in.n_pos / a.n_expert / kPartRows) parts = in.n_pos / a.n_expert / kPartRows;
+        if (kProduct != kByWeight || parts < 2) return false;
+        a.parts_n = (int)parts;
+        a.parts = h->parts;
+        return true;
+    };
+    const auto join = [&]() {
+        if (one % 4 == 0 && reinterpret_cast<uintptr_t>(a.out) % (4 * sizeof(T)) == 0)
+            k_join<T, 4><<<(unsigned)((one / 4 + kBlock - 1) / kBlock), kBlock, 0, s>>>(h->parts, a.parts_n, one, static_cast<T*>(a.out));
+        else
+            k_join<T, 1><<<(unsigned)((one + kBlock - 1) / kBlock), kBlock, 0, s>>>(h->parts, a.parts_n, one, static_cast<T*>(a.out));
     };
     if constexpr (sizeof(T) == 2) {
         if (tiles) {
@@ -958,27 +1022,25 @@ void product(gr_experts* h, const LinearIn& in, LinearArgs a, bool tiles, hipStr
                 k_linear_tiles<T, kProduct, 256, false><<<kUnits, kWaves * kWave, 0, s>>>(a);
                 return;
             }
-            int64_t n = grid(128);
             if constexpr (kProduct == kByWeight) {
-                const int64_t one = (int64_t)a.n_expert * in.n_out * in.n_in, fit = (int64_t)kPartFloats / one;
-                int64_t parts = 2 * kUnits * kPartRounds / n;
-                if (parts > fit) parts = fit;
-                if (parts > in.n_pos / a.n_expert / kPartRows) parts = in.n_pos / a.n_expert / kPartRows;
-                if (parts > 1) {
-                    a.parts_n = (int)parts;
-                    a.parts = h->parts;
-                    n = grid(128);
+                if (cut(128, 2 * kUnits * kPartRounds)) {
+                    const int64_t n = grid(128);
                     k_linear_tiles<T, kProduct, 128, true><<<(unsigned)(n < 2 * kUnits ? n : 2 * kUnits), kWaves * kWave, 0, s>>>(a);
-                    k_join<T><<<(unsigned)((one / 4 + kBlock - 1) / kBlock), kBlock, 0, s>>>(h->parts, a.parts_n, one, static_cast<T*>(a.out));
-                    return;
+                    return join();
                 }
             }
+            const int64_t n = grid(128);
             k_linear_tiles<T, kProduct, 128, false><<<(unsigned)(n < 2 * kUnits ? n : 2 * kUnits), kWaves * kWave, 0, s>>>(a);
             return;
         }
     }
-    if (grid(128) >= kAnyRounds * kUnits) k_linear_any<T, kProduct, 128><<<(unsigned)grid(128), kBlock, 0, s>>>(a);
-    else k_linear_any<T, kProduct, 64><<<(unsigned)grid(64), kBlock, 0, s>>>(a);
+    const bool parts = cut(kAnyTile, kAnyEnough);
+    const unsigned n = (unsigned)grid(kAnyTile);
+    if constexpr (sizeof(T) == 4) {
+        if (tiles) k_linear_any<T, kProduct, 4><<<n, kBlock, 0, s>>>(a);
+    }
+    if (sizeof(T) == 2 || !tiles) k_linear_any<T, kProduct, 1><<<n, kBlock, 0, s>>>(a);
+    if (parts) join();
 }
 
 // dz and db
