@@ -64,6 +64,19 @@ inline size_t plan_units(int n_expert, int64_t rows, int64_t slots)
     return (size_t)(a > b ? a : b);
 }
 
+// N neighbouring elements at any address of an element: one access where the hardware has one of that size, aligned or not.
+template <typename T, int N>
+struct Elements {
+    T v[N];
+    __device__ __forceinline__ static Elements load(const T* at)
+    {
+        Elements e;
+        __builtin_memcpy(&e, at, sizeof e);
+        return e;
+    }
+    __device__ __forceinline__ void store(T* at) const { __builtin_memcpy(at, this, sizeof *this); }
+};
+
 struct RouteIn {
     const void* logits;
     const float* bias;

@@ -639,21 +639,8 @@ int finish_plan(PlanArgs a, hipStream_t s)
 
 // ---- weighted sum ------------------------------------------------------------------------------
 //
-// Bound by memory: every result is read once, every sum written once.  A thread takes 16 bytes of a row's width (one element where
-// rows are not whole 16 bytes).
-
-template <typename T, int N>
-struct Piece {
-    typedef T Vec __attribute__((ext_vector_type(N)));
-};
-template <typename T>
-struct Piece<T, 1> {
-    struct Vec {
-        T v;
-        __device__ T& operator[](int) { return v; }
-        __device__ T operator[](int) const { return v; }
-    };
-};
+// Bound by memory: every result is read once, every sum written once.  A thread takes 16 bytes of a row's width, at any
+// address; where a row is no whole number of those the last ones reach back into the ones before, and both come to the same values.
 
 struct CombineArgs {
     const float* weight;
@@ -668,30 +655,31 @@ struct CombineArgs {
 template <typename T, int N>
 __global__ __launch_bounds__(kBlock) void k_combine(CombineArgs a)
 {
-    typedef typename Piece<T, N>::Vec Vec;
+    typedef Elements<T, N> Of;
     const int64_t i = (int64_t)blockIdx.x * kBlock + threadIdx.x, row = i / a.pieces;
     if (row >= a.rows) return;
-    const int c = (int)(i - row * a.pieces) * N;
+    int c = (int)(i - row * a.pieces) * N;
+    if (c + N > a.width) c = a.width - N;
     float sum[N] = {};
     for (int j = 0; j < a.top_k; ++j) {
         const int p = a.pos[row * a.top_k + j];
         if (p < 0 || p >= a.slots) continue;
         const float w = a.weight ? a.weight[row * a.top_k + j] : 1.0f;
-        const Vec v = *reinterpret_cast<const Vec*>(static_cast<const T*>(a.y) + (int64_t)p * a.width + c);
+        const Of v = Of::load(static_cast<const T*>(a.y) + (int64_t)p * a.width + c);
 #pragma unroll
-        for (int n = 0; n < N; ++n) sum[n] = fmaf(w, (float)v[n], sum[n]);
+        for (int n = 0; n < N; ++n) sum[n] = fmaf(w, (float)v.v[n], sum[n]);
     }
-    Vec o;
+    Of o;
 #pragma unroll
-    for (int n = 0; n < N; ++n) o[n] = (T)sum[n];
-    *reinterpret_cast<Vec*>(static_cast<T*>(a.out) + row * a.width + c) = o;
+    for (int n = 0; n < N; ++n) o.v[n] = (T)sum[n];
+    o.store(static_cast<T*>(a.out) + row * a.width + c);
 }
 
 // A team of 2^lg lanes takes a position.
 template <typename T, int N>
 __global__ __launch_bounds__(kBlock) void k_combine_back(CombineArgs a)
 {
-    typedef typename Piece<T, N>::Vec Vec;
+    typedef Elements<T, N> Of;
     const int lane = threadIdx.x & ((1 << a.lg) - 1);
     const int64_t p = ((int64_t)blockIdx.x * kBlock + threadIdx.x) >> a.lg;
     if (p >= a.slots) return;             // (whole teams)
@@ -702,32 +690,27 @@ __global__ __launch_bounds__(kBlock) void k_combine_back(CombineArgs a)
     const int64_t row = s / a.top_k;
     const float w = a.weight ? a.weight[s] : 1.0f;
     float dot = 0;
-    for (int c = lane * N; c < a.width; c += N << a.lg) {
-        Vec o;
+    for (int at = lane * N; at < a.width; at += N << a.lg) {
+        const int c = at + N > a.width ? a.width - N : at, again = at - c;      // columns that the lane before has as well: not added twice
+        Of o;
         if (kept) {
-            const Vec d = *reinterpret_cast<const Vec*>(static_cast<const T*>(a.dout) + row * a.width + c);
+            const Of d = Of::load(static_cast<const T*>(a.dout) + row * a.width + c);
             if (a.dweight) {
-                const Vec y = *reinterpret_cast<const Vec*>(static_cast<const T*>(a.y) + p * a.width + c);
+                const Of y = Of::load(static_cast<const T*>(a.y) + p * a.width + c);
 #pragma unroll
-                for (int n = 0; n < N; ++n) dot = fmaf((float)d[n], (float)y[n], dot);
+                for (int n = 0; n < N; ++n) dot = n >= again ? fmaf((float)d.v[n], (float)y.v[n], dot) : dot;
             }
 #pragma unroll
-            for (int n = 0; n < N; ++n) o[n] = (T)(w * (float)d[n]);
+            for (int n = 0; n < N; ++n) o.v[n] = (T)(w * (float)d.v[n]);
         } else {
 #pragma unroll
-            for (int n = 0; n < N; ++n) o[n] = (T)0.0f;
+            for (int n = 0; n < N; ++n) o.v[n] = (T)0.0f;
         }
-        if (a.dy) *reinterpret_cast<Vec*>(static_cast<T*>(a.dy) + p * a.width + c) = o;
+        if (a.dy) o.store(static_cast<T*>(a.dy) + p * a.width + c);
     }
     if (!a.dweight) return;
     dot = team_sum(dot, a.lg);
     if (lane == 0) a.dweight[s] = dot;
-}
-
-template <typename T>
-bool by_chunk(int width, const void* a, const void* b, const void* c)
-{
-    return width % Chunk<T>::n == 0 && aligned16(a) && aligned16(b) && aligned16(c);
 }
 
 }  // namespace
@@ -783,8 +766,8 @@ int launch_combine(int64_t rows, int top_k, int width, int dtype, const float* w
         CombineArgs a{};
         a.weight = weight; a.pos = pos; a.y = y; a.out = out;
         a.rows = rows; a.slots = rows * top_k; a.top_k = top_k; a.width = width;
-        const bool chunks = by_chunk<T>(width, y, out, nullptr);
-        a.pieces = chunks ? width / Chunk<T>::n : width;
+        const bool chunks = width >= Chunk<T>::n;
+        a.pieces = chunks ? (width + Chunk<T>::n - 1) / Chunk<T>::n : width;
         const int64_t blocks = (rows * a.pieces + kBlock - 1) / kBlock;
         if (chunks) k_combine<T, Chunk<T>::n><<<blocks, kBlock, 0, s>>>(a);
         else k_combine<T, 1><<<blocks, kBlock, 0, s>>>(a);
@@ -800,8 +783,8 @@ int launch_combine_backward(int64_t rows, int top_k, int width, int dtype, const
         CombineArgs a{};
         a.weight = weight; a.pos = slot; a.y = y; a.dout = dout; a.dy = dy; a.dweight = dweight;
         a.rows = rows; a.slots = rows * top_k; a.top_k = top_k; a.width = width;
-        const bool chunks = by_chunk<T>(width, y, dout, dy);
-        const int pieces = chunks ? width / Chunk<T>::n : width;
+        const bool chunks = width >= Chunk<T>::n;
+        const int pieces = chunks ? (width + Chunk<T>::n - 1) / Chunk<T>::n : width;
         while ((1 << a.lg) < pieces && a.lg < 6) ++a.lg;
         const int64_t blocks = ((a.slots << a.lg) + kBlock - 1) / kBlock;
         if (chunks) k_combine_back<T, Chunk<T>::n><<<blocks, kBlock, 0, s>>>(a);
