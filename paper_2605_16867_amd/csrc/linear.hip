@@ -155,7 +155,7 @@ __global__ __launch_bounds__(kBlock) void k_linear_any(LinearArgs a)
     constexpr int D = kAnyDepth<T>, kLd = D + Chunk<T>::n, kPerP = kRows * D / kBlock / kVec, kPerQ = kCols * D / kBlock / kVec;
     typedef typename Chunk<T>::Vec Vec;
     constexpr int n = Chunk<T>::n;
-    typedef T Get __attribute__((ext_vector_type(kVec)));
+    typedef Elements<T, kVec> Get;
     __shared__ __attribute__((aligned(16))) T lds_p[kRows * kLd], lds_q[kCols * kLd];
 
     const int tid = threadIdx.x, lane = tid % kWave, wave = tid / kWave;
@@ -190,20 +190,22 @@ __global__ __launch_bounds__(kBlock) void k_linear_any(LinearArgs a)
     }
     const T* const w = static_cast<const T*>(a.w) + (kProduct == kByWeight || e == a.n_expert ? 0 : (int64_t)e * O * I);
 
-    // which of the tile's elements a thread loads, kVec at a time: along the direction that is contiguous in memory
-    constexpr bool kPLong = kProduct != kByWeight, kQLong = kProduct == kForward;      // that is the reduction's
-    const auto place = [&](bool along, int size, int i, int& row, int& r) {
+    // which of the tile's elements a thread loads, kVec neighbours in memory at a time
+    constexpr bool kPLong = kProduct != kByWeight, kQLong = kProduct == kForward;      // those along the reduction
+    // Rows past the edge are loaded from within it: what becomes of them is not stored.  Where neighbours are rows, the ones at the edge reach
+    // back from it, before the tile if it has fewer rows than they are.
+    const auto place = [&](bool along, int size, int rows, int i, int& row, int& r) __attribute__((always_inline)) {
         const int at = (i * kBlock + tid) * kVec;
         if (along) { row = at / D; r = at % D; }
         else { r = at / size; row = at % size; }
+        const int last = rows - (along ? 1 : kVec);
+        if (row > last) row = last;
     };
-    // (rows past the edge are loaded from within it: what becomes of them is not stored; past the end of the reduction there are zeros)
     const T *from_p[kPerP], *from_q[kPerQ];
 #pragma unroll
     for (int i = 0; i < kPerP; ++i) {
         int row, r;
-        place(kPLong, kRows, i, row, r);
-        row = row < p_n ? row : p_n - 1;
+        place(kPLong, kRows, p_n, i, row, r);
         if constexpr (kProduct == kForward) from_p[i] = x + (e < a.n_expert ? row_of(a, p0 + row) : 0) * I + r;
         if constexpr (kProduct == kByInput) from_p[i] = dz + (p0 + row) * O + r;
         if constexpr (kProduct == kByWeight) from_p[i] = dz + (lo + r) * O + p0 + row;
@@ -211,38 +213,47 @@ __global__ __launch_bounds__(kBlock) void k_linear_any(LinearArgs a)
 #pragma unroll
     for (int i = 0; i < kPerQ; ++i) {
         int row, r;
-        place(kQLong, kCols, i, row, r);
-        row = row < q_n ? row : q_n - 1;
+        place(kQLong, kCols, q_n, i, row, r);
         if constexpr (kProduct == kForward) from_q[i] = w + (int64_t)(q0 + row) * I + r;
         if constexpr (kProduct == kByInput) from_q[i] = w + (int64_t)r * I + q0 + row;
         if constexpr (kProduct == kByWeight) from_q[i] = x + q0 + row;
     }
     const int64_t step_p = kPLong ? D : (int64_t)D * O, step_q = kQLong ? D : (int64_t)D * I;
     Get get_p[kPerP], get_q[kPerQ];
+    // past the end of the reduction there are zeros
+    const auto get = [&](const T* from, bool along, int64_t r, bool whole) __attribute__((always_inline)) {
+        Get v{};
+        if (whole || r + (along ? kVec : 1) <= depth) v = Get::load(from);
+        else if (along)
+#pragma unroll
+            for (int k = 0; k < kVec - 1; ++k)
+                if (r + k < depth) v.v[k] = from[k];
+        return v;
+    };
     const auto load = [&](int64_t r0, bool whole) __attribute__((always_inline)) {
 #pragma unroll
         for (int i = 0; i < kPerP; ++i) {
             int row, r;
-            place(kPLong, kRows, i, row, r);
-            get_p[i] = Get{};
-            if (whole || r0 + r < depth) get_p[i] = *reinterpret_cast<const Get*>(from_p[i]);
+            place(kPLong, kRows, p_n, i, row, r);
+            get_p[i] = get(from_p[i], kPLong, r0 + r, whole);
             from_p[i] += step_p;
         }
 #pragma unroll
         for (int i = 0; i < kPerQ; ++i) {
             int row, r;
-            place(kQLong, kCols, i, row, r);
-            get_q[i] = Get{};
-            if (whole || r0 + r < depth) get_q[i] = *reinterpret_cast<const Get*>(from_q[i] + (kProduct == kByWeight ? row_of(a, lo + r0 + r) * I : 0));
+            place(kQLong, kCols, q_n, i, row, r);
+            const bool in = whole || r0 + r < depth;
+            get_q[i] = get(from_q[i] + (kProduct == kByWeight && in ? row_of(a, lo + r0 + r) * I : 0), kQLong, r0 + r, whole);
             if (kProduct != kByWeight) from_q[i] += step_q;
         }
     };
 
     const auto put = [&](T* lds, bool along, int row, int r, const Get& v) __attribute__((always_inline)) {
-        if (along) *reinterpret_cast<Get*>(&lds[row * kLd + r]) = v;
+        if (along) __builtin_memcpy(__builtin_assume_aligned(&lds[row * kLd + r], kVec * sizeof(T)), &v, sizeof v);
         else
 #pragma unroll
-            for (int k = 0; k < kVec; ++k) lds[(row + k) * kLd + r] = v[k];
+            for (int k = 0; k < kVec; ++k)
+                if (row + k >= 0) lds[(row + k) * kLd + r] = v.v[k];
     };
     constexpr int kP = kRows / 32, kQ = kCols / 32;      // fragments of a wave
     f32x4 acc[kP][kQ] = {};
@@ -253,13 +264,13 @@ __global__ __launch_bounds__(kBlock) void k_linear_any(LinearArgs a)
 #pragma unroll
         for (int i = 0; i < kPerP; ++i) {
             int row, r;
-            place(kPLong, kRows, i, row, r);
+            place(kPLong, kRows, p_n, i, row, r);
             put(lds_p, kPLong, row, r, get_p[i]);
         }
 #pragma unroll
         for (int i = 0; i < kPerQ; ++i) {
             int row, r;
-            place(kQLong, kCols, i, row, r);
+            place(kQLong, kCols, q_n, i, row, r);
             put(lds_q, kQLong, row, r, get_q[i]);
         }
         __syncthreads();
@@ -289,16 +300,28 @@ __global__ __launch_bounds__(kBlock) void k_linear_any(LinearArgs a)
         const int row = wp + i * 16 + lane % 16;
         if (row >= p_n) continue;
 #pragma unroll
-        for (int j = 0; j < kQ; ++j)
+        for (int j = 0; j < kQ; ++j) {
+            const int col = wq + j * 16 + lane / 16 * 4;
+            Elements<T, 4> o;
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
-                const int col = wq + j * 16 + lane / 16 * 4 + k;
-                if (col >= q_n) continue;
-                float v = acc[i][j][k] + (bias ? (float)bias[col] : 0.0f);
+                float v = acc[i][j][k] + (bias && col + k < q_n ? (float)bias[col + k] : 0.0f);
                 if (kProduct == kForward && a.relu && v < 0) v = 0;
-                if (kProduct == kByWeight && a.parts) a.parts[at + (int64_t)row * width + col] = v;
-                else out[(int64_t)row * width + col] = (T)v;
+                o.v[k] = (T)v;
             }
+            const int64_t to = (int64_t)row * width + col;
+            if (kProduct == kByWeight && a.parts) {
+#pragma unroll
+                for (int k = 0; k < 4; ++k)
+                    if (col + k < q_n) a.parts[at + to + k] = acc[i][j][k];
+            } else if (col + 4 <= q_n) {
+                o.store(out + to);
+            } else {
+#pragma unroll
+                for (int k = 0; k < 4; ++k)
+                    if (col + k < q_n) out[to + k] = o.v[k];
+            }
+        }
     }
 }
 
@@ -784,88 +807,6 @@ __global__ __launch_bounds__(kBlock) void k_join(const float* parts, int n, int6
     *reinterpret_cast<Out*>(out + i) = o;
 }
 
-// ---- few rows an expert ------------------------------------------------------------------------
-//
-// Bound by reading the weights, each once: a workgroup takes 16 output features of an expert, its waves a part of the reduction each, straight from memory
-// into registers; their sums meet in shared memory.  Rows of x are taken 16 at a time.
-
-constexpr int kFewWaves = 4, kFewDepth = 32, kFewAhead = 8;      // indexes of a product; products asked for together
-
-template <typename T>
-__global__ __launch_bounds__(kFewWaves * kWave) void k_linear_few(LinearArgs a)
-{
-    typedef typename Chunk<T>::Vec Vec;
-    __shared__ f32x4 sums[kFewWaves - 1][kWave];
-    const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave, g = lane / 16, i = lane % 16;
-    const int e = blockIdx.x / a.tiles, n0 = blockIdx.x % a.tiles * 16, I = a.n_in, O = a.n_out;
-    const int64_t lo = bound(a.off, e, a.n_expert, a.n_pos), hi = e < a.n_expert ? bound(a.off, e + 1, a.n_expert, a.n_pos) : a.n_pos;
-    const T* const w = static_cast<const T*>(a.w) + ((int64_t)(e < a.n_expert ? e : 0) * O + (n0 + i < O ? n0 + i : O - 1)) * I + g * 8;
-    const int products = e < a.n_expert ? (I + kFewDepth - 1) / kFewDepth : 0, each = (products + kFewWaves - 1) / kFewWaves;
-    const int from = wave * each, until = from + each < products ? from + each : products;
-    for (int64_t p0 = lo; p0 < hi; p0 += 16) {
-        const int64_t p = p0 + i < hi ? p0 + i : hi - 1;
-        const T* const x = static_cast<const T*>(a.x) + (e < a.n_expert ? row_of(a, p) : 0) * I + g * 8;
-        f32x4 acc = {0, 0, 0, 0};
-        for (int d = from; d < until; d += kFewAhead) {
-            Vec wv[kFewAhead], xv[kFewAhead];
-#pragma unroll
-            for (int k = 0; k < kFewAhead; ++k) {
-                wv[k] = xv[k] = Vec{};
-                if (d + k < until && (d + k) * kFewDepth + g * 8 < I) {
-                    wv[k] = *reinterpret_cast<const Vec*>(w + (int64_t)(d + k) * kFewDepth);
-                    xv[k] = *reinterpret_cast<const Vec*>(x + (int64_t)(d + k) * kFewDepth);
-                }
-            }
-#pragma unroll
-            for (int k = 0; k < kFewAhead; ++k) acc = mfma(wv[k], xv[k], acc);
-        }
-        if (wave > 0) sums[wave - 1][lane] = acc;
-        __syncthreads();
-        if (wave == 0) {
-#pragma unroll
-            for (int k = 0; k < kFewWaves - 1; ++k) acc += sums[k][lane];
-            const int n = n0 + g * 4;
-            if (p0 + i < hi && n < O) {
-                typedef T Four __attribute__((ext_vector_type(4)));
-                Four o;
-#pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                    float v = acc[k] + (a.bias && e < a.n_expert ? (float)static_cast<const T*>(a.bias)[(int64_t)e * O + n + k] : 0.0f);
-                    if (a.relu && v < 0) v = 0;
-                    o[k] = (T)v;
-                }
-                *reinterpret_cast<Four*>(static_cast<T*>(a.out) + (p0 + i) * O + n) = o;
-            }
-        }
-        __syncthreads();
-    }
-}
-
-// dz = dy where y > 0, and its sums over blocks of rows, no block reaching from one expert's range into the next: one pass over dy and y.
-// A thread takes N neighbouring columns of every (kBlock >> lg)-th row of the block.
-template <typename T, int N>
-struct Piece {
-    typedef T Vec __attribute__((ext_vector_type(N)));
-};
-template <typename T>
-struct Piece<T, 1> {
-    struct Vec {
-        T v;
-        __device__ T& operator[](int) { return v; }
-        __device__ T operator[](int) const { return v; }
-    };
-};
-
-struct SumArgs {
-    const int* off;
-    const void *y, *dy;
-    void *dz, *db;
-    float* parts;      // [blocks of rows][columns]; null: no sums
-    int64_t n_pos;
-    int n_expert, width, first, cols;      // columns first .. first + cols - 1
-    int lg, across, rows;                  // lanes across, workgroups across, rows of a block
-};
-
 // Rows of block t (see row_tile; here all blocks of an expert have the same number of rows but the last).
 __device__ __forceinline__ RowTile row_block(const int* off, int n_expert, int64_t n_pos, int rows, int64_t t)
 {
@@ -882,41 +823,297 @@ __device__ __forceinline__ RowTile row_block(const int* off, int n_expert, int64
     return {n_expert, 0, 0};
 }
 
+// Adds up what the groups of a workgroup have, halving them, into the first one's; all threads call it.
+template <int N>
+__device__ __forceinline__ void sum_groups(float* part, float (&sum)[N], int group, int groups)
+{
+    const int across = kBlock / groups;
+    __syncthreads();
+    for (int half = groups / 2; half > 0; half /= 2) {
+        if (group >= half && group < 2 * half)
+#pragma unroll
+            for (int n = 0; n < N; ++n) part[(threadIdx.x - half * across) * N + n] = sum[n];
+        __syncthreads();
+        if (group < half)
+#pragma unroll
+            for (int n = 0; n < N; ++n) sum[n] += part[threadIdx.x * N + n];
+        __syncthreads();
+    }
+}
+
+// ---- few output features -----------------------------------------------------------------------
+//
+// Up to 16 (a predictor's last layer has one): bound by reading x, or writing dx, once.  Rows of any length and alignment.
+
+constexpr int kNarrow = 16;
+
+// Elements k and after of a row of `size`, zeros past its end.
+template <typename T>
+__device__ __forceinline__ typename Chunk<T>::Vec chunk_of(const T* row, int k, int size)
+{
+    constexpr int n = Chunk<T>::n;
+    typename Chunk<T>::Vec v{};
+    if (k + n <= size) {
+        const Elements<T, n> e = Elements<T, n>::load(row + k);
+#pragma unroll
+        for (int j = 0; j < n; ++j) v[j] = e.v[j];
+    } else {
+#pragma unroll
+        for (int j = 0; j < n - 1; ++j)
+            if (k + j < size) v[j] = row[k + j];
+    }
+    return v;
+}
+
+// Forward: a wave takes 16 positions and all features, straight from memory into registers.
+template <typename T>
+__global__ __launch_bounds__(kBlock) void k_linear_narrow(LinearArgs a)
+{
+    typedef typename Chunk<T>::Vec Vec;
+    constexpr int n = Chunk<T>::n, kStep = 4 * n, kAsked = 4;      // indexes of a product (or four); products asked for together
+    const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave, g = lane / 16, i = lane % 16, I = a.n_in, O = a.n_out;
+    const RowTile t = row_tile<16 * (kBlock / kWave)>(a, blockIdx.x);
+    const int64_t p0 = t.lo + wave * 16;
+    if (p0 >= t.hi) return;
+    const bool any = t.expert < a.n_expert;
+    const int64_t p = p0 + i < t.hi ? p0 + i : t.hi - 1;
+    const T* const x = static_cast<const T*>(a.x) + (any ? row_of(a, p) : 0) * I;
+    const T* const w = static_cast<const T*>(a.w) + ((int64_t)(any ? t.expert : 0) * O + (i < O ? i : O - 1)) * I;
+    f32x4 acc = {0, 0, 0, 0};
+    const int depth = any ? I : 0;
+    int k0 = 0;
+    for (; k0 + kAsked * kStep <= depth; k0 += kAsked * kStep) {      // (no lane asks whether it is within the row)
+        Elements<T, n> xv[kAsked], wv[kAsked];
+#pragma unroll
+        for (int s = 0; s < kAsked; ++s) {
+            xv[s] = Elements<T, n>::load(x + k0 + s * kStep + g * n);
+            wv[s] = Elements<T, n>::load(w + k0 + s * kStep + g * n);
+        }
+#pragma unroll
+        for (int s = 0; s < kAsked; ++s) acc = mfma(__builtin_bit_cast(Vec, wv[s]), __builtin_bit_cast(Vec, xv[s]), acc);
+    }
+    for (; k0 < depth; k0 += kStep) acc = mfma(chunk_of(w, k0 + g * n, depth), chunk_of(x, k0 + g * n, depth), acc);
+    if (p0 + i >= t.hi) return;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        const int o = g * 4 + k;
+        if (o >= O) continue;
+        float v = acc[k] + (a.bias && any ? (float)static_cast<const T*>(a.bias)[(int64_t)t.expert * O + o] : 0.0f);
+        if (a.relu && v < 0) v = 0;
+        static_cast<T*>(a.out)[(p0 + i) * O + o] = (T)v;
+    }
+}
+
+// Threads across a row of n_in, each with neighbouring columns, and down a block of rows.  Where a row is no whole number of those, its last
+// thread's columns reach back into the one's before: both come to the same values.
+struct NarrowShape {
+    int lg, across;      // threads across as a power of two; workgroups across
+};
+
+template <typename T>
+__host__ __device__ constexpr int narrow_columns(int n_in) { return n_in < Chunk<T>::n ? 1 : Chunk<T>::n; }
+
+constexpr int kNarrowRows = 64;
+
+// By input: dx[p] = the sum over the features of dz[p, o] * W[o].
+template <typename T, int N, int kOut>
+__global__ __launch_bounds__(kBlock) void k_narrow_by_input(LinearArgs a, NarrowShape s)
+{
+    __shared__ float dzs[kNarrowRows][kOut];
+    const int I = a.n_in, O = a.n_out, lane = threadIdx.x & ((1 << s.lg) - 1), group = threadIdx.x >> s.lg, groups = kBlock >> s.lg;
+    const RowTile t = row_tile<kNarrowRows>(a, blockIdx.x / s.across);
+    if (t.hi <= t.lo) return;
+    const int rows = (int)(t.hi - t.lo);
+    const bool any = t.expert < a.n_expert;
+    for (int i = threadIdx.x; i < kNarrowRows * kOut; i += kBlock) {
+        const int r = i / kOut, o = i % kOut;
+        dzs[r][o] = any && r < rows && o < O ? (float)static_cast<const T*>(a.dz)[(t.lo + r) * O + o] : 0.0f;
+    }
+    __syncthreads();
+    int c = ((int)(blockIdx.x % s.across) << s.lg | lane) * N;
+    if (c >= I) return;
+    if (c + N > I) c = I - N;
+    const T* const w = static_cast<const T*>(a.w) + (int64_t)(any ? t.expert : 0) * O * I + c;
+    float wv[kOut][N];
+#pragma unroll
+    for (int o = 0; o < kOut; ++o) {
+        const Elements<T, N> e = Elements<T, N>::load(w + (int64_t)(o < O ? o : 0) * I);
+#pragma unroll
+        for (int j = 0; j < N; ++j) wv[o][j] = any && o < O ? (float)e.v[j] : 0.0f;
+    }
+#pragma unroll 2
+    for (int r = group; r < rows; r += groups) {
+        float sum[N] = {};
+#pragma unroll
+        for (int o = 0; o < kOut; ++o)
+#pragma unroll
+            for (int j = 0; j < N; ++j) sum[j] = fmaf(dzs[r][o], wv[o][j], sum[j]);
+        Elements<T, N> e;
+#pragma unroll
+        for (int j = 0; j < N; ++j) e.v[j] = (T)sum[j];
+        e.store(static_cast<T*>(a.out) + (t.lo + r) * I + c);
+    }
+}
+
+// By weight: the sums of a block of rows, [block][n_out][n_in] (see k_sum_blocks for the rest).
+template <typename T, int N, int kOut>
+__global__ __launch_bounds__(kBlock) void k_narrow_by_weight(LinearArgs a, NarrowShape s, int rows)
+{
+    __shared__ float part[kBlock * N], dzs[kNarrowRows][kOut];
+    __shared__ uint32_t xs[kNarrowRows];
+    const int I = a.n_in, O = a.n_out, lane = threadIdx.x & ((1 << s.lg) - 1), group = threadIdx.x >> s.lg, groups = kBlock >> s.lg;
+    const int64_t block = blockIdx.x / s.across;
+    const RowTile t = row_block(a.off, a.n_expert, a.n_pos, rows, block);
+    if (t.expert == a.n_expert) return;
+    int c = ((int)(blockIdx.x % s.across) << s.lg | lane) * N;
+    const bool in = c < I;
+    if (c + N > I) c = I - N;
+    float sum[kOut][N] = {};
+    for (int64_t p0 = t.lo; p0 < t.hi; p0 += kNarrowRows) {
+        const int own = t.hi - p0 < kNarrowRows ? (int)(t.hi - p0) : kNarrowRows;
+        __syncthreads();
+        for (int i = threadIdx.x; i < kNarrowRows * kOut; i += kBlock) {
+            const int r = i / kOut, o = i % kOut;
+            dzs[r][o] = r < own && o < O ? (float)static_cast<const T*>(a.dz)[(p0 + r) * O + o] : 0.0f;
+        }
+        if (threadIdx.x < own) xs[threadIdx.x] = (uint32_t)row_of(a, p0 + threadIdx.x);
+        __syncthreads();
+        if (!in) continue;
+#pragma unroll 4
+        for (int r = group; r < own; r += groups) {
+            const Elements<T, N> e = Elements<T, N>::load(static_cast<const T*>(a.x) + (int64_t)xs[r] * I + c);
+#pragma unroll
+            for (int o = 0; o < kOut; ++o)
+#pragma unroll
+                for (int j = 0; j < N; ++j) sum[o][j] = fmaf(dzs[r][o], (float)e.v[j], sum[o][j]);
+        }
+    }
+#pragma unroll
+    for (int o = 0; o < kOut; ++o) {
+        if (o >= O) continue;
+        sum_groups<N>(part, sum[o], group, groups);
+        if (group > 0 || !in) continue;
+#pragma unroll
+        for (int j = 0; j < N; ++j) a.parts[(block * O + o) * I + c + j] = sum[o][j];
+    }
+}
+
+// ---- few rows an expert ------------------------------------------------------------------------
+//
+// Bound by reading the weights, each once: a workgroup takes 16 output features of an expert, its waves a part of the reduction each, straight from memory
+// into registers; their sums meet in shared memory.  Rows of x are taken 16 at a time.
+
+constexpr int kFewWaves = 4, kFewAhead = 8;      // loads of an operand asked for together
+
+template <typename T>
+__global__ __launch_bounds__(kFewWaves * kWave) void k_linear_few(LinearArgs a)
+{
+    typedef typename Chunk<T>::Vec Vec;
+    constexpr int n = Chunk<T>::n, kStep = 4 * n;
+    __shared__ f32x4 sums[kFewWaves - 1][kWave];
+    const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave, g = lane / 16, i = lane % 16;
+    const int e = blockIdx.x / a.tiles, n0 = blockIdx.x % a.tiles * 16, I = a.n_in, O = a.n_out;
+    const int64_t lo = bound(a.off, e, a.n_expert, a.n_pos), hi = e < a.n_expert ? bound(a.off, e + 1, a.n_expert, a.n_pos) : a.n_pos;
+    const T* const w = static_cast<const T*>(a.w) + ((int64_t)(e < a.n_expert ? e : 0) * O + (n0 + i < O ? n0 + i : O - 1)) * I;
+    const int depth = e < a.n_expert ? I : 0, each = (depth + kFewWaves * kStep - 1) / (kFewWaves * kStep) * kStep;
+    const int from = wave * each, until = from + each < depth ? from + each : depth;
+    for (int64_t p0 = lo; p0 < hi; p0 += 16) {
+        const int64_t p = p0 + i < hi ? p0 + i : hi - 1;
+        const T* const x = static_cast<const T*>(a.x) + (e < a.n_expert ? row_of(a, p) : 0) * I;
+        f32x4 acc = {0, 0, 0, 0};
+        int d = from;
+        for (; d + kFewAhead * kStep <= until; d += kFewAhead * kStep) {
+            Elements<T, n> wv[kFewAhead], xv[kFewAhead];
+#pragma unroll
+            for (int k = 0; k < kFewAhead; ++k) {
+                wv[k] = Elements<T, n>::load(w + d + k * kStep + g * n);
+                xv[k] = Elements<T, n>::load(x + d + k * kStep + g * n);
+            }
+#pragma unroll
+            for (int k = 0; k < kFewAhead; ++k) acc = mfma(__builtin_bit_cast(Vec, wv[k]), __builtin_bit_cast(Vec, xv[k]), acc);
+        }
+        if (d < until) {
+            Vec wv[kFewAhead], xv[kFewAhead];
+#pragma unroll
+            for (int k = 0; k < kFewAhead; ++k) {
+                wv[k] = chunk_of(w, d + k * kStep + g * n, until);
+                xv[k] = chunk_of(x, d + k * kStep + g * n, until);
+            }
+#pragma unroll
+            for (int k = 0; k < kFewAhead; ++k) acc = mfma(wv[k], xv[k], acc);
+        }
+        if (wave > 0) sums[wave - 1][lane] = acc;
+        __syncthreads();
+        if (wave == 0) {
+#pragma unroll
+            for (int k = 0; k < kFewWaves - 1; ++k) acc += sums[k][lane];
+            const int at = n0 + g * 4;
+            if (p0 + i < hi && at < O) {
+                Elements<T, 4> o;
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    float v = acc[k] + (a.bias && e < a.n_expert && at + k < O ? (float)static_cast<const T*>(a.bias)[(int64_t)e * O + at + k] : 0.0f);
+                    if (a.relu && v < 0) v = 0;
+                    o.v[k] = (T)v;
+                }
+                T* const out = static_cast<T*>(a.out) + (p0 + i) * O + at;
+                if (at + 4 <= O) o.store(out);
+                else
+#pragma unroll
+                    for (int k = 0; k < 3; ++k)
+                        if (at + k < O) out[k] = o.v[k];
+            }
+        }
+        __syncthreads();
+    }
+}
+
+// dz = dy where y > 0, and its sums over blocks of rows, no block reaching from one expert's range into the next: one pass over dy and y.
+// A thread takes N neighbouring columns of every (kBlock >> lg)-th row of the block.
+struct SumArgs {
+    const int* off;
+    const void *y, *dy;
+    void *dz, *db;
+    float* parts;      // [blocks of rows][columns]; null: no sums
+    int64_t n_pos;
+    int n_expert, width, first, cols;      // columns first .. first + cols - 1
+    int lg, across, rows;                  // lanes across, workgroups across, rows of a block
+    int64_t blocks;                        // that there are
+};
+
 template <typename T, int N>
 __global__ __launch_bounds__(kBlock) void k_unrelu_sums(SumArgs a)
 {
-    typedef typename Piece<T, N>::Vec Vec;
+    typedef Elements<T, N> Of;
     __shared__ float part[kBlock * N];
     const int64_t t = blockIdx.x / a.across;
     const RowTile r = row_block(a.off, a.n_expert, a.n_pos, a.rows, t);
     const int lane = threadIdx.x & ((1 << a.lg) - 1), group = threadIdx.x >> a.lg, groups = kBlock >> a.lg;
-    const int c = ((int)(blockIdx.x % a.across) << a.lg | lane) * N;
+    // (the last columns reach back into the ones before where they are no whole number: both come to the same values)
+    int c = ((int)(blockIdx.x % a.across) << a.lg | lane) * N;
     const bool in = c < a.cols;
+    if (c + N > a.cols) c = a.cols - N;
     float sum[N] = {};
     if (in) {
         const int64_t at = a.first + c;
+#pragma unroll 2
         for (int64_t p = r.lo + group; p < r.hi; p += groups) {
-            Vec d = *reinterpret_cast<const Vec*>(static_cast<const T*>(a.dy) + p * a.width + at);
+            Of d = Of::load(static_cast<const T*>(a.dy) + p * a.width + at);
             if (a.y) {
-                const Vec v = *reinterpret_cast<const Vec*>(static_cast<const T*>(a.y) + p * a.width + at);
+                const Of v = Of::load(static_cast<const T*>(a.y) + p * a.width + at);
 #pragma unroll
-                for (int n = 0; n < N; ++n) d[n] = (float)v[n] > 0 ? d[n] : (T)0.0f;
-                *reinterpret_cast<Vec*>(static_cast<T*>(a.dz) + p * a.width + at) = d;
+                for (int n = 0; n < N; ++n) d.v[n] = (float)v.v[n] > 0 ? d.v[n] : (T)0.0f;
+                d.store(static_cast<T*>(a.dz) + p * a.width + at);
             }
 #pragma unroll
-            for (int n = 0; n < N; ++n) sum[n] += (float)d[n];
+            for (int n = 0; n < N; ++n) sum[n] += (float)d.v[n];
         }
     }
     if (!a.parts || r.expert == a.n_expert) return;
-#pragma unroll
-    for (int n = 0; n < N; ++n) part[threadIdx.x * N + n] = sum[n];
-    __syncthreads();
+    sum_groups<N>(part, sum, group, groups);
     if (group > 0 || !in) return;
 #pragma unroll
-    for (int n = 0; n < N; ++n) {
-        for (int g = 1; g < groups; ++g) sum[n] += part[(g << a.lg | lane) * N + n];
-        a.parts[t * a.cols + c + n] = sum[n];
-    }
+    for (int n = 0; n < N; ++n) a.parts[t * a.cols + c + n] = sum[n];
 }
 
 // The sums over an expert's blocks: 32 columns a workgroup, eight threads a column.
@@ -931,6 +1128,7 @@ __global__ __launch_bounds__(kBlock) void k_sum_blocks(SumArgs a)
         before += own;
         own = hi > lo ? (hi - lo + a.rows - 1) / a.rows : 0;
     }
+    if (own > a.blocks - before) own = a.blocks - before;      // (offsets that are none)
     float sum = 0;
     if (c < a.cols)
         for (int64_t t = threadIdx.x / 32; t < own; t += kBlock / 32) sum += a.parts[(before + t) * a.cols + c];
@@ -980,6 +1178,53 @@ constexpr int kPartRounds = 2, kPartRows = 1024;
 // to a compute unit: by weight in parts up to there (65 536 x 257 -> 129: 590 us in one, 156).
 constexpr int kAnyEnough = 8 * kUnits;
 
+constexpr int kNarrowParts = 1 << 15;      // most weights of an expert
+
+// The products of a layer of few output features; false where they are not for these sizes.
+template <typename T, Product kProduct>
+bool narrow(gr_experts* h, const LinearIn& in, LinearArgs a, hipStream_t s)
+{
+    if constexpr (kProduct == kForward) {
+        k_linear_narrow<T><<<(unsigned)row_tiles(in, 16 * (kBlock / kWave)), kBlock, 0, s>>>(a);
+        return true;
+    } else {
+        constexpr int n = Chunk<T>::n;
+        if (in.n_in < n || (int64_t)in.n_out * in.n_in > kNarrowParts || in.n_pos == 0) return false;
+        const int pieces = (in.n_in + n - 1) / n;
+        NarrowShape shape{0, 0};
+        while ((1 << shape.lg) < pieces && shape.lg < 8) ++shape.lg;
+        shape.across = ((pieces - 1) >> shape.lg) + 1;
+        int rows = 0;
+        int64_t blocks = row_tiles(in, kNarrowRows);
+        if constexpr (kProduct == kByWeight) {
+            // as many blocks of rows as give each compute unit some, and as there is room for their sums
+            int64_t most = (int64_t)kPartFloats / ((int64_t)in.n_out * in.n_in) - a.n_expert;
+            if (most > 4 * kUnits) most = 4 * kUnits;
+            if (most < kUnits) return false;
+            rows = (int)((in.n_pos + most - 1) / most);
+            if (rows < kNarrowRows) rows = kNarrowRows;
+            blocks = row_tiles(in, rows);
+            a.parts = h->parts;
+        }
+        const auto launch = [&](auto out) {
+            constexpr int kOut = decltype(out)::value;
+            if constexpr (kProduct == kByInput) k_narrow_by_input<T, n, kOut><<<(unsigned)(blocks * shape.across), kBlock, 0, s>>>(a, shape);
+            else k_narrow_by_weight<T, n, kOut><<<(unsigned)(blocks * shape.across), kBlock, 0, s>>>(a, shape, rows);
+        };
+        if (in.n_out == 1) launch(std::integral_constant<int, 1>{});
+        else if (in.n_out <= 4) launch(std::integral_constant<int, 4>{});
+        else if (in.n_out <= 8) launch(std::integral_constant<int, 8>{});
+        else launch(std::integral_constant<int, 16>{});
+        if constexpr (kProduct == kByWeight) {
+            SumArgs sums{};
+            sums.off = in.off; sums.db = a.out; sums.parts = h->parts; sums.n_pos = in.n_pos; sums.n_expert = a.n_expert;
+            sums.width = sums.cols = in.n_out * in.n_in; sums.rows = rows; sums.blocks = blocks;
+            k_sum_blocks<T><<<a.n_expert * ((sums.cols + 31) / 32), kBlock, 0, s>>>(sums);
+        }
+        return true;
+    }
+}
+
 template <typename T, Product kProduct>
 void product(gr_experts* h, const LinearIn& in, LinearArgs a, bool tiles, hipStream_t s)
 {
@@ -1009,15 +1254,16 @@ void product(gr_experts* h, const LinearIn& in, LinearArgs a, bool tiles, hipStr
         else
             k_join<T, 1><<<(unsigned)((one + kBlock - 1) / kBlock), kBlock, 0, s>>>(h->parts, a.parts_n, one, static_cast<T*>(a.out));
     };
+    if constexpr (kProduct == kForward) {
+        if (in.n_pos <= kFewRows * (a.n_expert < kFewExperts ? a.n_expert : kFewExperts)) {
+            a.tiles = tiles_of(width, 16);
+            k_linear_few<T><<<(a.n_expert + 1) * a.tiles, kFewWaves * kWave, 0, s>>>(a);
+            return;
+        }
+    }
+    if (in.n_out <= kNarrow && narrow<T, kProduct>(h, in, a, s)) return;
     if constexpr (sizeof(T) == 2) {
         if (tiles) {
-            if constexpr (kProduct == kForward) {
-                if (in.n_pos <= kFewRows * (a.n_expert < kFewExperts ? a.n_expert : kFewExperts)) {
-                    a.tiles = tiles_of(width, 16);
-                    k_linear_few<T><<<(a.n_expert + 1) * a.tiles, kFewWaves * kWave, 0, s>>>(a);
-                    return;
-                }
-            }
             if (grid(256) >= kLargeRounds * kUnits) {
                 k_linear_tiles<T, kProduct, 256, false><<<kUnits, kWaves * kWave, 0, s>>>(a);
                 return;
@@ -1036,10 +1282,8 @@ void product(gr_experts* h, const LinearIn& in, LinearArgs a, bool tiles, hipStr
     }
     const bool parts = cut(kAnyTile, kAnyEnough);
     const unsigned n = (unsigned)grid(kAnyTile);
-    if constexpr (sizeof(T) == 4) {
-        if (tiles) k_linear_any<T, kProduct, 4><<<n, kBlock, 0, s>>>(a);
-    }
-    if (sizeof(T) == 2 || !tiles) k_linear_any<T, kProduct, 1><<<n, kBlock, 0, s>>>(a);
+    if (in.n_in >= 4 && in.n_out >= 4) k_linear_any<T, kProduct, 4><<<n, kBlock, 0, s>>>(a);
+    else k_linear_any<T, kProduct, 1><<<n, kBlock, 0, s>>>(a);
     if (parts) join();
 }
 
@@ -1051,16 +1295,15 @@ void unrelu_sums(gr_experts* h, const LinearIn& in, void* dz, void* db, hipStrea
     SumArgs a{};
     a.off = in.off; a.y = in.y; a.dy = in.dy; a.dz = dz; a.db = db; a.n_pos = in.n_pos;
     a.n_expert = in.off ? in.n_expert : 1; a.width = in.n_out;
-    const bool chunks = in.n_out % Chunk<T>::n == 0 && (!in.y || (aligned16(in.y) && aligned16(dz))) && aligned16(in.dy);
-    const int n = chunks ? Chunk<T>::n : 1;
     a.rows = in.n_pos > 128 * kMost ? (int)((in.n_pos + kMost - 1) / kMost) : 128;
-    const int64_t blocks = row_tiles(in, a.rows) + 1;      // (one more: no positions and no experts leave none)
+    const int64_t blocks = a.blocks = row_tiles(in, a.rows) + 1;      // (one more: no positions and no experts leave none)
     const int64_t fit = (int64_t)kPartFloats / blocks / Chunk<T>::n * Chunk<T>::n;
     const int most = fit < in.n_out ? (int)fit : in.n_out;      // columns whose parts there is room for
     for (a.first = 0; a.first < in.n_out; a.first += most) {
         a.cols = in.n_out - a.first < most ? in.n_out - a.first : most;
         a.parts = db ? h->parts : nullptr;
-        const int pieces = (a.cols + n - 1) / n;
+        const bool chunks = a.cols >= Chunk<T>::n;
+        const int n = chunks ? Chunk<T>::n : 1, pieces = (a.cols + n - 1) / n;
         a.lg = 0;
         while ((1 << a.lg) < pieces && a.lg < 5) ++a.lg;
         a.across = ((pieces - 1) >> a.lg) + 1;

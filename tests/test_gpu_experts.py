@@ -280,6 +280,15 @@ def test_gradients_of_a_layer(n, E, I, O, k, dtype):
                 assert torch.equal(only, full) and torch.equal(d, dz)
 
 
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("n,E,I,O,k", [  # few features out; rows that are no whole 16 bytes, or shorter than that
+    (1, 3, 5, 16, 1), (200, 3, 9, 4, 2), (4099, 9, 100, 1, 9), (333, 5, 2703, 8, 2), (70, 1, 4101, 16, 0), (2500, 64, 31, 2, 4), (129, 7, 33, 12, 1),
+    (1000, 2, 8192, 8, 1)])
+def test_layers_of_few_features(n, E, I, O, k, dtype):
+    test_layer(n, E, I, O, k, dtype)
+    test_gradients_of_a_layer(n, E, I, O, k, dtype)
+
+
 def test_one_matrix_for_all_rows():
     rng = np.random.default_rng(3)
     n, I, O = 333, 80, 72
@@ -412,6 +421,12 @@ def test_weighted_sum_and_its_gradient(T, k, O, dtype):
     only = empty(S, O, dtype=dtype)
     h.gr_expert_combine_backward(td, None, ints(slot), only)
     assert torch.equal(only, dy)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("T,k,O", [(1, 2, 3), (61, 3, 9), (200, 2, 17), (33, 9, 511), (40, 1, 1021), (7, 4, 2050)])
+def test_weighted_sums_of_odd_widths(T, k, O, dtype):
+    test_weighted_sum_and_its_gradient(T, k, O, dtype)
 
 
 # ---- clipping ---------------------------------------------------------------------------------
