@@ -1168,15 +1168,18 @@ constexpr int kUnits = 256;          // compute units: workgroups of large tiles
 // Large tiles from four rounds of them on.  Forward, 128 / 256: 8 192 x 4 096 -> 1 024 (165 tiles) 93 / 101 us, 65 536 x 1 024 -> 512 (530) 85 / 104,
 // 65 536 x 4 096 -> 1 024 (1 060) 607 / 535; by input 65 536 x 1 024 -> 512 (1 060) 111 / 112, 65 536 x 1 024 -> 4 096 (4 240) 703 / 614.
 constexpr int kLargeRounds = 4;
-// Few rows: up to 16 an expert on average, 256 in all (an expert may have them all, and its weights are read again for every 16).
-// 4 096 -> 1 024, tiles / this: 9 positions 39 / 17 us, 72 39 / 21, 144 39 / 36, 288 38 / 59.
-constexpr int kFewRows = 16, kFewExperts = 16;
+// Few rows: up to 16 an expert on average (32 in single precision), 16 times that in all (an expert may have them all, and its weights are read
+// again for every 16).  Nine experts of 4 096 -> 1 024, tiles / this: bfloat16 9 positions 39 / 18 us, 72 39 / 20, 144 39 / 24 (36 where one expert
+// has most), 288 38 / 59; single precision 9 125 / 30, 144 123 / 45, 288 125 / 89, 432 128 / 133; bfloat16 from 4 095: 153 77 / 118.
+template <typename T>
+constexpr int kFewRows = sizeof(T) == 2 ? 16 : 32;
+constexpr int kFewExperts = 16;
 // By weight, where the tiles are fewer than two rounds: as many parts of the positions as fill those, of at least 1 024 positions each.
 // One part / several: 131 072 x 512 -> 128 (36 tiles) 279 / 56 us, 65 536 x 1 024 -> 512 (288) 172 / 137, 16 384 x 1 024 -> 512 50 / 52.
 constexpr int kPartRounds = 2, kPartRows = 1024;
 // The tiles for any sizes are of 64 by 64 (8 198 x 1 023 -> 511 forward, single precision: 149 us, of 128 by 128 189; 65 536 x 257 -> 129 99, 152), eight
 // to a compute unit: by weight in parts up to there (65 536 x 257 -> 129: 590 us in one, 156).
-constexpr int kAnyEnough = 8 * kUnits;
+constexpr int kAnyEnough = 8 * kUnits, kAnyPartRows = 256;
 
 constexpr int kNarrowParts = 1 << 15;      // most weights of an expert
 
@@ -1239,10 +1242,10 @@ void product(gr_experts* h, const LinearIn& in, LinearArgs a, bool tiles, hipStr
     a.parts_n = 1;
     // by weight: where the tiles are few, parts of the positions apart, as many as make up for it
     const int64_t one = (int64_t)a.n_expert * in.n_out * in.n_in;
-    const auto cut = [&](int size, int64_t enough) {
+    const auto cut = [&](int size, int64_t enough, int rows) {
         int64_t parts = enough / grid(size);
         if (parts > (int64_t)kPartFloats / one) parts = (int64_t)kPartFloats / one;
-        if (parts > in.n_pos / a.n_expert / kPartRows) parts = in.n_pos / a.n_expert / kPartRows;
+        if (parts > in.n_pos / a.n_expert / rows) parts = in.n_pos / a.n_expert / rows;
         if (kProduct != kByWeight || parts < 2) return false;
         a.parts_n = (int)parts;
         a.parts = h->parts;
@@ -1255,7 +1258,7 @@ void product(gr_experts* h, const LinearIn& in, LinearArgs a, bool tiles, hipStr
             k_join<T, 1><<<(unsigned)((one + kBlock - 1) / kBlock), kBlock, 0, s>>>(h->parts, a.parts_n, one, static_cast<T*>(a.out));
     };
     if constexpr (kProduct == kForward) {
-        if (in.n_pos <= kFewRows * (a.n_expert < kFewExperts ? a.n_expert : kFewExperts)) {
+        if (in.n_pos <= kFewRows<T> * (a.n_expert < kFewExperts ? a.n_expert : kFewExperts)) {
             a.tiles = tiles_of(width, 16);
             k_linear_few<T><<<(a.n_expert + 1) * a.tiles, kFewWaves * kWave, 0, s>>>(a);
             return;
@@ -1269,7 +1272,7 @@ void product(gr_experts* h, const LinearIn& in, LinearArgs a, bool tiles, hipStr
                 return;
             }
             if constexpr (kProduct == kByWeight) {
-                if (cut(128, 2 * kUnits * kPartRounds)) {
+                if (cut(128, 2 * kUnits * kPartRounds, kPartRows)) {
                     const int64_t n = grid(128);
                     k_linear_tiles<T, kProduct, 128, true><<<(unsigned)(n < 2 * kUnits ? n : 2 * kUnits), kWaves * kWave, 0, s>>>(a);
                     return join();
@@ -1280,7 +1283,7 @@ void product(gr_experts* h, const LinearIn& in, LinearArgs a, bool tiles, hipStr
             return;
         }
     }
-    const bool parts = cut(kAnyTile, kAnyEnough);
+    const bool parts = cut(kAnyTile, kAnyEnough, kAnyPartRows);
     const unsigned n = (unsigned)grid(kAnyTile);
     if (in.n_in >= 4 && in.n_out >= 4) k_linear_any<T, kProduct, 4><<<n, kBlock, 0, s>>>(a);
     else k_linear_any<T, kProduct, 1><<<n, kBlock, 0, s>>>(a);
