@@ -9,7 +9,7 @@ namespace {
 
 constexpr int kBlock = 256;
 constexpr int kWave = 64;
-constexpr int kFewThreads = 1024, kFewTensors = 16;
+constexpr int kFewThreads = 1024, kFewTensors = 12;
 constexpr int64_t kFewBytes = 512 << 10, kAloneBytes = 64 << 10;
 constexpr int kPiece = kBlock * 4 * 16;      // bytes of a gradient that a workgroup takes at a time
 

@@ -38,6 +38,7 @@ int by_type(int dtype, F f)
 inline bool type_ok(int dtype) { return dtype == GR_F32 || dtype == GR_BF16 || dtype == GR_F16; }
 inline size_t size_of(int dtype) { return dtype == GR_F32 ? 4 : 2; }
 inline bool aligned16(const void* p) { return reinterpret_cast<uintptr_t>(p) % 16 == 0; }
+constexpr int64_t kMostBlocks = UINT32_MAX / 256;      // workgroups of 256 that a launch may have
 inline int launched() { return hipGetLastError() == hipSuccess ? GR_OK : GR_ERR_HIP; }
 
 // The 16 bytes that one access moves, as elements.

@@ -717,6 +717,7 @@ __global__ __launch_bounds__(kBlock) void k_combine_back(CombineArgs a)
 
 int launch_route(gr_experts* h, const RouteIn& in, int dtype, float* weight, int* expert, int* off, int* slot, int* pos, hipStream_t s)
 {
+    if (in.rows > ((kMostBlocks - 1) * kBlock >> team_log(in.n_expert))) return GR_ERR_TOO_LARGE;
     return by_type(dtype, [&](auto t) {
         typedef decltype(t) T;
         const int size = in.n_expert / in.n_group;
@@ -740,6 +741,7 @@ int launch_route_backward(const RouteIn& in, int dtype, const int* expert, const
         typedef decltype(t) T;
         const RouteBackArgs a{in, expert, dweight, dlogits, team_log(in.n_expert), whole_rows<T>(in.logits, dlogits, in.n_expert)};
         const int64_t blocks = ((in.rows << a.lg) + kBlock - 1) / kBlock;
+        if (blocks > kMostBlocks) return (int)GR_ERR_TOO_LARGE;
         if (in.scoring == GR_SCORE_SIGMOID) k_route_back<T, true><<<blocks, kBlock, 0, s>>>(a);
         else k_route_back<T, false><<<blocks, kBlock, 0, s>>>(a);
         return launched();
@@ -769,6 +771,7 @@ int launch_combine(int64_t rows, int top_k, int width, int dtype, const float* w
         const bool chunks = width >= Chunk<T>::n;
         a.pieces = chunks ? (width + Chunk<T>::n - 1) / Chunk<T>::n : width;
         const int64_t blocks = (rows * a.pieces + kBlock - 1) / kBlock;
+        if (blocks > kMostBlocks) return (int)GR_ERR_TOO_LARGE;
         if (chunks) k_combine<T, Chunk<T>::n><<<blocks, kBlock, 0, s>>>(a);
         else k_combine<T, 1><<<blocks, kBlock, 0, s>>>(a);
         return launched();
@@ -787,6 +790,7 @@ int launch_combine_backward(int64_t rows, int top_k, int width, int dtype, const
         const int pieces = chunks ? (width + Chunk<T>::n - 1) / Chunk<T>::n : width;
         while ((1 << a.lg) < pieces && a.lg < 6) ++a.lg;
         const int64_t blocks = ((a.slots << a.lg) + kBlock - 1) / kBlock;
+        if (blocks > kMostBlocks) return (int)GR_ERR_TOO_LARGE;
         if (chunks) k_combine_back<T, Chunk<T>::n><<<blocks, kBlock, 0, s>>>(a);
         else k_combine_back<T, 1><<<blocks, kBlock, 0, s>>>(a);
         return launched();

@@ -68,21 +68,20 @@ struct RowTile {
     int64_t lo, hi;
 };
 
-// The t-th tile of kRows rows, no tile reaching from one expert's range into the next; lo = hi where there are fewer.
+// The t-th tile of `rows` rows, no tile reaching from one expert's range into the next; lo = hi where there are fewer.
 // Every lane of a wave calls it.
-template <int kRows>
-__device__ __forceinline__ RowTile row_tile(const LinearArgs& a, int64_t t)
+__device__ __forceinline__ RowTile row_tile(const int* off, int n_expert, int64_t n_pos, int rows, int64_t t)
 {
     const int lane = threadIdx.x % kWave;
     int64_t before = 0;
-    for (int e0 = 0; e0 <= a.n_expert; e0 += kWave) {
+    for (int e0 = 0; e0 <= n_expert; e0 += kWave) {
         const int e = e0 + lane;
         int64_t lo = 0, hi = 0;
-        if (e <= a.n_expert) {
-            lo = bound(a.off, e, a.n_expert, a.n_pos);
-            hi = e < a.n_expert ? bound(a.off, e + 1, a.n_expert, a.n_pos) : a.n_pos;
+        if (e <= n_expert) {
+            lo = bound(off, e, n_expert, n_pos);
+            hi = e < n_expert ? bound(off, e + 1, n_expert, n_pos) : n_pos;
         }
-        const int own = hi > lo ? (int)((hi - lo + kRows - 1) / kRows) : 0;
+        const int own = hi > lo ? (int)((uint32_t)(hi - lo + rows - 1) / (uint32_t)rows) : 0;
         int v = own;
         for (int d = 1; d < kWave; d *= 2) {
             const int o = __shfl_up(v, d);
@@ -92,13 +91,29 @@ __device__ __forceinline__ RowTile row_tile(const LinearArgs& a, int64_t t)
         const unsigned long long mine = __ballot(t >= end - own && t < end);
         if (mine) {
             const int l = __ffsll((long long)mine) - 1;
-            const int64_t first = __shfl(lo, l) + (t - (__shfl(end, l) - __shfl(own, l))) * kRows;
+            const int64_t first = __shfl(lo, l) + (t - (__shfl(end, l) - __shfl(own, l))) * rows;
             const int64_t last = __shfl(hi, l);
-            return {e0 + l, first, first + kRows < last ? first + kRows : last};
+            return {e0 + l, first, first + rows < last ? first + rows : last};
         }
         before = __shfl(end, kWave - 1);
     }
-    return {a.n_expert, 0, 0};
+    return {n_expert, 0, 0};
+}
+
+// Tiles of all experts before one, and its own; every lane of a wave calls it.
+__device__ __forceinline__ void tiles_before(const int* off, int n_expert, int64_t n_pos, int rows, int expert, int64_t& before, int64_t& own)
+{
+    int64_t sum = 0;
+    own = 0;
+    for (int e = threadIdx.x % kWave; e <= expert; e += kWave) {
+        const int64_t lo = bound(off, e, n_expert, n_pos), hi = bound(off, e + 1, n_expert, n_pos);
+        const int64_t tiles = hi > lo ? (uint32_t)(hi - lo + rows - 1) / (uint32_t)rows : 0;
+        if (e < expert) sum += tiles;
+        else own = tiles;
+    }
+    own = __shfl(own, expert % kWave);
+    for (int d = 1; d < kWave; d *= 2) sum += __shfl_xor(sum, d);
+    before = sum;
 }
 
 // Which tile workgroup j takes.  Workgroups go to the eight dies in turn, each with a cache of its own: a die takes blocks of neighbouring tiles, 32
@@ -179,7 +194,7 @@ __global__ __launch_bounds__(kBlock) void k_linear_any(LinearArgs a)
         q_n = I - q0 < kCols ? I - q0 : kCols;
         part_of(a, e, part, lo, depth);
     } else {
-        const RowTile t = row_tile<kRows>(a, row_no);
+        const RowTile t = row_tile(a.off, a.n_expert, a.n_pos, kRows, row_no);
         if (t.hi <= t.lo) return;
         e = t.expert;
         p0 = t.lo;
@@ -496,7 +511,7 @@ __global__ __launch_bounds__(kWaves * kWave, kSize > 128 ? 1 : 2) void k_linear_
                     r = {l, first, first + kSize < last ? first + kSize : last};
                 }
             } else {
-                r = row_tile<kSize>(a, no.row);
+                r = row_tile(a.off, a.n_expert, a.n_pos, kSize, no.row);
             }
             t.e = uniform(r.expert);
             t.p0 = uniform(r.lo);
@@ -807,22 +822,6 @@ __global__ __launch_bounds__(kBlock) void k_join(const float* parts, int n, int6
     *reinterpret_cast<Out*>(out + i) = o;
 }
 
-// Rows of block t (see row_tile; here all blocks of an expert have the same number of rows but the last).
-__device__ __forceinline__ RowTile row_block(const int* off, int n_expert, int64_t n_pos, int rows, int64_t t)
-{
-    int64_t before = 0;
-    for (int e = 0; e <= n_expert; ++e) {
-        const int64_t lo = bound(off, e, n_expert, n_pos), hi = e < n_expert ? bound(off, e + 1, n_expert, n_pos) : n_pos;
-        const int64_t own = hi > lo ? (hi - lo + rows - 1) / rows : 0;
-        if (t < before + own) {
-            const int64_t first = lo + (t - before) * rows;
-            return {e, first, first + rows < hi ? first + rows : hi};
-        }
-        before += own;
-    }
-    return {n_expert, 0, 0};
-}
-
 // Adds up what the groups of a workgroup have, halving them, into the first one's; all threads call it.
 template <int N>
 __device__ __forceinline__ void sum_groups(float* part, float (&sum)[N], int group, int groups)
@@ -872,7 +871,7 @@ __global__ __launch_bounds__(kBlock) void k_linear_narrow(LinearArgs a)
     typedef typename Chunk<T>::Vec Vec;
     constexpr int n = Chunk<T>::n, kStep = 4 * n, kAsked = 4;      // indexes of a product (or four); products asked for together
     const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave, g = lane / 16, i = lane % 16, I = a.n_in, O = a.n_out;
-    const RowTile t = row_tile<16 * (kBlock / kWave)>(a, blockIdx.x);
+    const RowTile t = row_tile(a.off, a.n_expert, a.n_pos, 16 * (kBlock / kWave), blockIdx.x);
     const int64_t p0 = t.lo + wave * 16;
     if (p0 >= t.hi) return;
     const bool any = t.expert < a.n_expert;
@@ -913,15 +912,15 @@ struct NarrowShape {
 template <typename T>
 __host__ __device__ constexpr int narrow_columns(int n_in) { return n_in < Chunk<T>::n ? 1 : Chunk<T>::n; }
 
-constexpr int kNarrowRows = 64;
+constexpr int kNarrowRows = 64, kNarrowLeast = 8;
 
 // By input: dx[p] = the sum over the features of dz[p, o] * W[o].
 template <typename T, int N, int kOut>
-__global__ __launch_bounds__(kBlock) void k_narrow_by_input(LinearArgs a, NarrowShape s)
+__global__ __launch_bounds__(kBlock) void k_narrow_by_input(LinearArgs a, NarrowShape s, int most)
 {
     __shared__ float dzs[kNarrowRows][kOut];
     const int I = a.n_in, O = a.n_out, lane = threadIdx.x & ((1 << s.lg) - 1), group = threadIdx.x >> s.lg, groups = kBlock >> s.lg;
-    const RowTile t = row_tile<kNarrowRows>(a, blockIdx.x / s.across);
+    const RowTile t = row_tile(a.off, a.n_expert, a.n_pos, most, blockIdx.x / s.across);
     if (t.hi <= t.lo) return;
     const int rows = (int)(t.hi - t.lo);
     const bool any = t.expert < a.n_expert;
@@ -963,7 +962,7 @@ __global__ __launch_bounds__(kBlock) void k_narrow_by_weight(LinearArgs a, Narro
     __shared__ uint32_t xs[kNarrowRows];
     const int I = a.n_in, O = a.n_out, lane = threadIdx.x & ((1 << s.lg) - 1), group = threadIdx.x >> s.lg, groups = kBlock >> s.lg;
     const int64_t block = blockIdx.x / s.across;
-    const RowTile t = row_block(a.off, a.n_expert, a.n_pos, rows, block);
+    const RowTile t = row_tile(a.off, a.n_expert, a.n_pos, rows, block);
     if (t.expert == a.n_expert) return;
     int c = ((int)(blockIdx.x % s.across) << s.lg | lane) * N;
     const bool in = c < I;
@@ -1087,7 +1086,7 @@ __global__ __launch_bounds__(kBlock) void k_unrelu_sums(SumArgs a)
     typedef Elements<T, N> Of;
     __shared__ float part[kBlock * N];
     const int64_t t = blockIdx.x / a.across;
-    const RowTile r = row_block(a.off, a.n_expert, a.n_pos, a.rows, t);
+    const RowTile r = row_tile(a.off, a.n_expert, a.n_pos, a.rows, t);
     const int lane = threadIdx.x & ((1 << a.lg) - 1), group = threadIdx.x >> a.lg, groups = kBlock >> a.lg;
     // (the last columns reach back into the ones before where they are no whole number: both come to the same values)
     int c = ((int)(blockIdx.x % a.across) << a.lg | lane) * N;
@@ -1122,12 +1121,8 @@ __global__ __launch_bounds__(kBlock) void k_sum_blocks(SumArgs a)
 {
     __shared__ float part[kBlock];
     const int across = (a.cols + 31) / 32, e = blockIdx.x / across, c = blockIdx.x % across * 32 + threadIdx.x % 32;
-    int64_t before = 0, own = 0;
-    for (int i = 0; i <= e; ++i) {
-        const int64_t lo = bound(a.off, i, a.n_expert, a.n_pos), hi = bound(a.off, i + 1, a.n_expert, a.n_pos);
-        before += own;
-        own = hi > lo ? (hi - lo + a.rows - 1) / a.rows : 0;
-    }
+    int64_t before, own;
+    tiles_before(a.off, a.n_expert, a.n_pos, a.rows, e, before, own);
     if (own > a.blocks - before) own = a.blocks - before;      // (offsets that are none)
     float sum = 0;
     if (c < a.cols)
@@ -1181,8 +1176,6 @@ constexpr int kPartRounds = 2, kPartRows = 1024;
 // to a compute unit: by weight in parts up to there (65 536 x 257 -> 129: 590 us in one, 156).
 constexpr int kAnyEnough = 8 * kUnits, kAnyPartRows = 256;
 
-constexpr int kNarrowParts = 1 << 15;      // most weights of an expert
-
 // The products of a layer of few output features; false where they are not for these sizes.
 template <typename T, Product kProduct>
 bool narrow(gr_experts* h, const LinearIn& in, LinearArgs a, hipStream_t s)
@@ -1192,27 +1185,26 @@ bool narrow(gr_experts* h, const LinearIn& in, LinearArgs a, hipStream_t s)
         return true;
     } else {
         constexpr int n = Chunk<T>::n;
-        if (in.n_in < n || (int64_t)in.n_out * in.n_in > kNarrowParts || in.n_pos == 0) return false;
+        if (in.n_in < n || in.n_pos == 0) return false;
         const int pieces = (in.n_in + n - 1) / n;
         NarrowShape shape{0, 0};
         while ((1 << shape.lg) < pieces && shape.lg < 8) ++shape.lg;
         shape.across = ((pieces - 1) >> shape.lg) + 1;
-        int rows = 0;
-        int64_t blocks = row_tiles(in, kNarrowRows);
-        if constexpr (kProduct == kByWeight) {
-            // as many blocks of rows as give each compute unit some, and as there is room for their sums
+        // rows of a block: as many as leave four workgroups to each compute unit
+        const int64_t enough = in.n_pos * shape.across / (4 * kUnits);
+        int64_t rows = enough < kNarrowLeast ? kNarrowLeast : enough > kNarrowRows ? kNarrowRows : enough;
+        if constexpr (kProduct == kByWeight) {      // and as there is room for the sums of all blocks
             int64_t most = (int64_t)kPartFloats / ((int64_t)in.n_out * in.n_in) - a.n_expert;
-            if (most > 4 * kUnits) most = 4 * kUnits;
             if (most < kUnits) return false;
-            rows = (int)((in.n_pos + most - 1) / most);
-            if (rows < kNarrowRows) rows = kNarrowRows;
-            blocks = row_tiles(in, rows);
+            if (most > 4 * kUnits) most = 4 * kUnits;
+            if (rows < (in.n_pos + most - 1) / most) rows = (in.n_pos + most - 1) / most;
             a.parts = h->parts;
         }
+        const int64_t blocks = row_tiles(in, (int)rows);
         const auto launch = [&](auto out) {
             constexpr int kOut = decltype(out)::value;
-            if constexpr (kProduct == kByInput) k_narrow_by_input<T, n, kOut><<<(unsigned)(blocks * shape.across), kBlock, 0, s>>>(a, shape);
-            else k_narrow_by_weight<T, n, kOut><<<(unsigned)(blocks * shape.across), kBlock, 0, s>>>(a, shape, rows);
+            if constexpr (kProduct == kByInput) k_narrow_by_input<T, n, kOut><<<(unsigned)(blocks * shape.across), kBlock, 0, s>>>(a, shape, (int)rows);
+            else k_narrow_by_weight<T, n, kOut><<<(unsigned)(blocks * shape.across), kBlock, 0, s>>>(a, shape, (int)rows);
         };
         if (in.n_out == 1) launch(std::integral_constant<int, 1>{});
         else if (in.n_out <= 4) launch(std::integral_constant<int, 4>{});
@@ -1221,7 +1213,7 @@ bool narrow(gr_experts* h, const LinearIn& in, LinearArgs a, hipStream_t s)
         if constexpr (kProduct == kByWeight) {
             SumArgs sums{};
             sums.off = in.off; sums.db = a.out; sums.parts = h->parts; sums.n_pos = in.n_pos; sums.n_expert = a.n_expert;
-            sums.width = sums.cols = in.n_out * in.n_in; sums.rows = rows; sums.blocks = blocks;
+            sums.width = sums.cols = in.n_out * in.n_in; sums.rows = (int)rows; sums.blocks = blocks;
             k_sum_blocks<T><<<a.n_expert * ((sums.cols + 31) / 32), kBlock, 0, s>>>(sums);
         }
         return true;
@@ -1264,7 +1256,8 @@ void product(gr_experts* h, const LinearIn& in, LinearArgs a, bool tiles, hipStr
             return;
         }
     }
-    if (in.n_out <= kNarrow && narrow<T, kProduct>(h, in, a, s)) return;
+    const bool whole = kProduct == kForward && sizeof(T) == 2 && tiles && row_tiles(in, 128) >= kUnits;
+    if (in.n_out <= kNarrow && !whole && narrow<T, kProduct>(h, in, a, s)) return;
     if constexpr (sizeof(T) == 2) {
         if (tiles) {
             if (grid(256) >= kLargeRounds * kUnits) {
@@ -1288,6 +1281,15 @@ void product(gr_experts* h, const LinearIn& in, LinearArgs a, bool tiles, hipStr
     if (in.n_in >= 4 && in.n_out >= 4) k_linear_any<T, kProduct, 4><<<n, kBlock, 0, s>>>(a);
     else k_linear_any<T, kProduct, 1><<<n, kBlock, 0, s>>>(a);
     if (parts) join();
+}
+
+// Whether the smallest tiles are more than a launch may have.
+bool too_many_tiles(const LinearIn& in, bool backward)
+{
+    const int64_t across = tiles_of(in.n_in > in.n_out ? in.n_in : in.n_out, kAnyTile), experts = in.off ? in.n_expert : 1;
+    const int64_t most = kMostBlocks - kDies * kTogether;
+    return row_tiles(in, kAnyTile) > most / across ||
+           (backward && experts * tiles_of(in.n_in, kAnyTile) * tiles_of(in.n_out, kAnyTile) > most);
 }
 
 // dz and db
@@ -1322,6 +1324,7 @@ void unrelu_sums(gr_experts* h, const LinearIn& in, void* dz, void* db, hipStrea
 
 int launch_linear(gr_experts* h, const LinearIn& in, int dtype, void* out_y, hipStream_t s)
 {
+    if (too_many_tiles(in, false)) return GR_ERR_TOO_LARGE;
     LinearArgs a = args_of(in);
     a.out = out_y;
     return by_type(dtype, [&](auto t) {
@@ -1333,6 +1336,7 @@ int launch_linear(gr_experts* h, const LinearIn& in, int dtype, void* out_y, hip
 
 int launch_linear_backward(gr_experts* h, const LinearIn& in, int dtype, void* dz, void* dx, void* dw, void* db, hipStream_t s)
 {
+    if (too_many_tiles(in, true)) return GR_ERR_TOO_LARGE;
     return by_type(dtype, [&](auto t) {
         typedef decltype(t) T;
         LinearArgs a = args_of(in);
