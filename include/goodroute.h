@@ -434,6 +434,7 @@ const char* gr_profile_kernel_name(int32_t id);
  * Outputs must not overlap inputs unless it is said.  Indexes on the device are not validated: kernels stay in
  * bounds whatever off, slot, pos and expert hold, and give results only for arrays as gr_expert_plan leaves them.
  * Results do not depend on the order in which workgroups run: the same call gives the same bits.
+ * A call whose kernels would have 2^32 threads or more (the results of some tens of gigabytes at the least) is GR_ERR_TOO_LARGE.
  */
 typedef struct gr_experts gr_experts;
 
@@ -448,7 +449,8 @@ enum { GR_SCORE_SOFTMAX = 0, GR_SCORE_SIGMOID = 1 };             /* scoring */
 /*
  * Create the workspace of calls on up to n_expert experts, max_rows rows and max_top_k experts per row, on the
  * current HIP device.  max_rows * max_top_k <= 2^30.  Device memory held until gr_experts_destroy: 64 MB for the parts of long
- * sums, 4 * (n_expert + 1) bytes for each 1 024 slots, and 0.4 MB.
+ * sums, 4 * (n_expert + 1) bytes for each 1 024 slots or each 256 / l rows, whichever are more (l = 1, 2, 4, ... 32 lanes a row,
+ * the least with 16 l >= n_expert), and 0.4 MB.
  */
 int gr_experts_create(gr_experts** out, int32_t n_expert, int64_t max_rows, int32_t max_top_k);
 int gr_experts_destroy(gr_experts* h);       /* waits for the device first; NULL is allowed */

@@ -1,6 +1,7 @@
 """Binding of libgoodroute: same names as the C interface, argument
-marshalling only (natively, by csrc/marshal.cpp, for the calls of a serving loop; by ctypes for the
-others, and for all of them where that module is not built or is of another torch: 7 to 9 us a call).
+marshalling only (natively, by csrc/marshal.cpp, for the calls of a serving loop and those of a length
+predictor; by ctypes for the others, and for all of them where that module is not built or is of another
+torch: 7 to 9 us a call).  `Fleet` has the calls on a fleet, `Experts` those of a length predictor.
 Tensors are torch tensors on the GPU (device memory and the current stream come from torch; every step
 of the path runs in the library's kernels).  There is no fallback for those: without the built library every call raises.
 """

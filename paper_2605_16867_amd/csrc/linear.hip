@@ -4,6 +4,12 @@
 //   forward   y[p, n]  = sum over k of x[row(p), k] * W_e[n, k]        p in the range of e
 //   by input  dx[p, k] = sum over n of dz[p, n] * W_e[n, k]            p in the range of e
 //   by weight dW_e[n, k] = sum over p in the range of e of dz[p, n] * x[row(p), k]
+//
+// Products and sums are in single precision; a result is rounded to the type once, at the end.  dx is one row a slot, rounded as such: the sum over a
+// row's slots is another call (gr_expert_combine), so nothing here is added up by atomics and every result is the same from run to run.
+//
+// Bound by matrix instructions where an expert has hundreds of rows, by reading the weights where it has few, by reading x or writing dx where it has
+// few output features.  Each of these has a form of its own; which one a call takes is decided in `product` at the end, with both sides' times.
 #include <type_traits>
 
 #include "experts.h"
@@ -155,8 +161,13 @@ __device__ __forceinline__ f32x4 mfma(f16x8 a, f16x8 b, f32x4 acc) { return __bu
 
 // ---- any sizes, any alignment -------------------------------------------------------------------
 //
-// Tiles of 64 by 64, 64 bytes of the reduction at a time, loaded into registers (element by element, or 16 bytes at a time in single precision where rows are whole ones) while the
-// tile before is multiplied, and laid into shared memory with the reduction contiguous.
+// Tiles of 64 by 64, four waves of 32 by 32, 64 bytes of the reduction at a time: loaded into registers, four neighbours in memory at a time
+// whatever their alignment, while the tile before is multiplied, and laid into shared memory with the reduction contiguous.  Small tiles, eight
+// workgroups to a compute unit: their waits for memory and at barriers fall into each other's products.  Single precision, 8 198 positions of nine
+// experts x 1 023 -> 511: 100 us alone, 112 one after the other: 77 to 86 TFLOP/s of the 153 that a large product reaches: 1 037 tiles are four or
+// five to a unit, so a fifth of it is the last ones' (65 536 x 1 024 -> 512: 100 TFLOP/s; 20 000 x 4 096 -> 1 024: 109).  Loaded element by
+// element the first took 149; twice the reduction at a time gains nothing there (118) and loses a third at short ones (131 072 x 100 -> 64 in
+// bfloat16 30 / 41).
 
 constexpr int kAnyTile = 64;
 
@@ -348,6 +359,13 @@ __global__ __launch_bounds__(kBlock) void k_linear_any(LinearArgs a)
 //   across  its rows are contiguous: [64 indexes][row]; a lane's eight indexes are two reads that transpose 4 by 16
 // What is written is one after the other, 16 bytes a lane, so which 16 bytes of memory a lane fetches decides the layout: their number
 // within a line of the tile is exclusive-ored with one made of the line's, so that the lanes of a read meet no bank twice.
+//
+// Bound by the matrix units and, with them, by power: 131 072 positions of nine experts x 4 096 -> 1 024 in bfloat16 (1.1 TFLOP) forward 910 to
+// 930 us (1 195 TFLOP/s; the library's plain product of one such matrix 874), where the units are busy 62 % of the time at 1.87 GHz.  Tiles of 256
+// by 256 because a fragment read from shared memory then serves eight products of a wave (at 128 by 128 four) and each operand is fetched half as
+// often; the sums of a wave's 128 by 128 take half of all registers.  Five slots of an operand's slice, 32 KB each, are all the shared memory
+// there is.  By input 65 536 x 4 096 <- 1 024 590 us (930 TFLOP/s: a tile is 16 slices, and writing it a quarter of its time); by weight 670 us
+// (820), of 128 by 128 (2 304 tiles on 512 places: 4.5 rounds; of 256, 576 on 256, 2.25, it takes 780).
 
 constexpr int kSlots = 5, kWaves = 4;
 
@@ -806,7 +824,8 @@ __global__ __launch_bounds__(kWaves * kWave, kSize > 128 ? 1 : 2) void k_linear_
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
 }
 
-// The parts of sums, added in their order; N at a time.
+// The parts of sums, added in their order whatever order they came in; N at a time.  Bound by reading them (9 x 33 x 1 024 in 14 parts, 17 MB: 5.8
+// us).
 template <typename T, int N>
 __global__ __launch_bounds__(kBlock) void k_join(const float* parts, int n, int64_t count, T* out)
 {
@@ -842,7 +861,10 @@ __device__ __forceinline__ void sum_groups(float* part, float (&sum)[N], int gro
 
 // ---- few output features -----------------------------------------------------------------------
 //
-// Up to 16 (a predictor's last layer has one): bound by reading x, or writing dx, once.  Rows of any length and alignment.
+// Up to 16 (a predictor's last layer has one): a tile of 64 would be mostly empty.  Bound by reading x, or writing dx, once; rows of any length and
+// alignment.  147 456 positions x 512 -> 1 in bfloat16: forward 25 us (151 MB, from the cache: 6 TB/s), backward 67; in tiles 51 and 404.
+// 32 768 x 2 703 -> 8, bfloat16: forward 132 (rows on odd addresses of two bytes, which 16-byte loads take at half the rate; single precision 99
+// for twice the bytes), backward 161; in tiles, element by element, 600.
 
 constexpr int kNarrow = 16;
 
@@ -864,7 +886,7 @@ __device__ __forceinline__ typename Chunk<T>::Vec chunk_of(const T* row, int k, 
     return v;
 }
 
-// Forward: a wave takes 16 positions and all features, straight from memory into registers.
+// Forward: a wave takes 16 positions and all features, straight from memory into registers, as the operands of one 16 by 16 product after another.
 template <typename T>
 __global__ __launch_bounds__(kBlock) void k_linear_narrow(LinearArgs a)
 {
@@ -903,6 +925,7 @@ __global__ __launch_bounds__(kBlock) void k_linear_narrow(LinearArgs a)
     }
 }
 
+// Backward, no matrix instructions: up to 16 multiplications for every element that moves.
 // Threads across a row of n_in, each with neighbouring columns, and down a block of rows.  Where a row is no whole number of those, its last
 // thread's columns reach back into the one's before: both come to the same values.
 struct NarrowShape {
@@ -912,9 +935,9 @@ struct NarrowShape {
 template <typename T>
 __host__ __device__ constexpr int narrow_columns(int n_in) { return n_in < Chunk<T>::n ? 1 : Chunk<T>::n; }
 
-constexpr int kNarrowRows = 64, kNarrowLeast = 8;
+constexpr int kNarrowRows = 64, kNarrowLeast = 8;      // rows of a block, most (they are held in shared memory) and least
 
-// By input: dx[p] = the sum over the features of dz[p, o] * W[o].
+// By input: dx[p] = the sum over the features of dz[p, o] * W[o]; a thread keeps its columns of W.
 template <typename T, int N, int kOut>
 __global__ __launch_bounds__(kBlock) void k_narrow_by_input(LinearArgs a, NarrowShape s, int most)
 {
@@ -954,7 +977,8 @@ __global__ __launch_bounds__(kBlock) void k_narrow_by_input(LinearArgs a, Narrow
     }
 }
 
-// By weight: the sums of a block of rows, [block][n_out][n_in] (see k_sum_blocks for the rest).
+// By weight: the sums of a block of rows, [block][n_out][n_in], which k_sum_blocks adds up; a thread keeps its columns' sums, and what it reads of x
+// is used for all features at once.
 template <typename T, int N, int kOut>
 __global__ __launch_bounds__(kBlock) void k_narrow_by_weight(LinearArgs a, NarrowShape s, int rows)
 {
@@ -999,8 +1023,10 @@ __global__ __launch_bounds__(kBlock) void k_narrow_by_weight(LinearArgs a, Narro
 
 // ---- few rows an expert ------------------------------------------------------------------------
 //
-// Bound by reading the weights, each once: a workgroup takes 16 output features of an expert, its waves a part of the reduction each, straight from memory
-// into registers; their sums meet in shared memory.  Rows of x are taken 16 at a time.
+// Bound by reading the weights, each once: a workgroup takes 16 output features of an expert, its waves a part of the reduction each, straight
+// from memory into registers; their sums meet in shared memory.  Rows of x are taken 16 at a time.  Nothing is shared between waves but a row of
+// x, which the cache holds, so shared memory would only add a wait.  9 positions of nine experts x 4 096 -> 1 024 in bfloat16 (75 MB): 17.7 us,
+// 4.3 TB/s (a copy reaches 5.0); single precision 30.5, 5.0 TB/s.  (Four loads at a time or sixteen: the same.)
 
 constexpr int kFewWaves = 4, kFewAhead = 8;      // loads of an operand asked for together
 
@@ -1067,7 +1093,9 @@ __global__ __launch_bounds__(kFewWaves * kWave) void k_linear_few(LinearArgs a)
     }
 }
 
-// dz = dy where y > 0, and its sums over blocks of rows, no block reaching from one expert's range into the next: one pass over dy and y.
+// dz = dy where y > 0, and db = its sums over each expert's rows: one pass over dy and y, sums over blocks of rows (no block reaching from one
+// expert's range into the next) and then over blocks, in a fixed order.  Bound by memory: 65 536 x 1 024 in bfloat16, 403 MB read and written, 80 us
+// (5.0 TB/s), and 7 for the second.
 // A thread takes N neighbouring columns of every (kBlock >> lg)-th row of the block.
 struct SumArgs {
     const int* off;
@@ -1158,10 +1186,11 @@ bool in_tiles(const LinearIn& in, const void* a, const void* b, const void* c)
     return in.n_in % Chunk<T>::n == 0 && in.n_out % Chunk<T>::n == 0 && aligned16(a) && aligned16(b) && aligned16(c);
 }
 
-// Which form a product takes (bfloat16, 9 experts, before / after the change of form):
+// Which form a product takes.  Times are of nine experts, in bfloat16 where nothing else is said, without the form / with it.
 constexpr int kUnits = 256;          // compute units: workgroups of large tiles that run at a time
-// Large tiles from four rounds of them on.  Forward, 128 / 256: 8 192 x 4 096 -> 1 024 (165 tiles) 93 / 101 us, 65 536 x 1 024 -> 512 (530) 85 / 104,
-// 65 536 x 4 096 -> 1 024 (1 060) 607 / 535; by input 65 536 x 1 024 -> 512 (1 060) 111 / 112, 65 536 x 1 024 -> 4 096 (4 240) 703 / 614.
+// Tiles of 256 by 256 from four rounds of them on, of 128 by 128 before.  Forward, 128 / 256: 8 192 x 4 096 -> 1 024 (165 tiles) 93 / 101 us, 65
+// 536 x 1 024 -> 512 (530) 85 / 104, 65 536 x 4 096 -> 1 024 (1 060) 607 / 535; by input 65 536 x 1 024 -> 512 (1 060) 111 / 112, 65 536 x 1 024
+// -> 4 096 (4 240) 703 / 614.
 constexpr int kLargeRounds = 4;
 // Few rows: up to 16 an expert on average (32 in single precision), 16 times that in all (an expert may have them all, and its weights are read
 // again for every 16).  Nine experts of 4 096 -> 1 024, tiles / this: bfloat16 9 positions 39 / 18 us, 72 39 / 20, 144 39 / 24 (36 where one expert
@@ -1172,11 +1201,15 @@ constexpr int kFewExperts = 16;
 // By weight, where the tiles are fewer than two rounds: as many parts of the positions as fill those, of at least 1 024 positions each.
 // One part / several: 131 072 x 512 -> 128 (36 tiles) 279 / 56 us, 65 536 x 1 024 -> 512 (288) 172 / 137, 16 384 x 1 024 -> 512 50 / 52.
 constexpr int kPartRounds = 2, kPartRows = 1024;
-// The tiles for any sizes are of 64 by 64 (8 198 x 1 023 -> 511 forward, single precision: 149 us, of 128 by 128 189; 65 536 x 257 -> 129 99, 152), eight
-// to a compute unit: by weight in parts up to there (65 536 x 257 -> 129: 590 us in one, 156).
+// The tiles for any sizes: by weight in parts, of at least 256 positions each, up to eight workgroups to a compute unit.  65 536 x 257 -> 129 590
+// / 156 us (both before the loads by four); least 1 024 positions / 256: 2 000 x 768 -> 768, one matrix, single precision 216 / 114, 131 072 x 100
+// -> 64 167 / 102; 128 and 512 are slower than 256 there.
 constexpr int kAnyEnough = 8 * kUnits, kAnyPartRows = 256;
 
-// The products of a layer of few output features; false where they are not for these sizes.
+// Few output features, unless the tiles for 16 bits have one for every compute unit forward.  Tiles / this form, forward 2 000 x 1 024 -> 8 14 / 9
+// us, 32 000 x 512 -> 8 11.8 / 10.7, 131 072 x 1 024 -> 8 52 / 56, -> 16 53 / 66; single precision, -> 16, 178 / 132; backward, -> 8 216 / 172, ->
+// 16 219 / 257, 32 768 x 4 096 -> 16 241 / 202, 600 x 2 048 -> 8 26 / 30; single precision 481 / 259 and 477 / 296. The products of a layer of few
+// output features; false where they are not for these sizes.
 template <typename T, Product kProduct>
 bool narrow(gr_experts* h, const LinearIn& in, LinearArgs a, hipStream_t s)
 {
