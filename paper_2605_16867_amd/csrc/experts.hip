@@ -235,44 +235,52 @@ __global__ __launch_bounds__(kBlock) void k_route(RouteArgs a)
     constexpr int V = kLaneExperts, n = Chunk<T>::n;
     const int lg = a.lg, team = 1 << lg, lane = threadIdx.x & (team - 1), rows = kBlock >> lg;
     const int E = a.in.n_expert, k = a.in.top_k;
-    const Share of{lg, lane, E, a.whole != 0};
     __shared__ int hist[kPlanWaves][GR_MAX_EXPERTS + 1];
     // scores of the team's row, by expert, and then weights of the wave's rows, by choice; the workgroup's choices
     __shared__ __attribute__((aligned(16))) float scores[kBlock * V];
-    __shared__ int ids[kBlock * K];
+    __shared__ int ids[kBlock * (kGroups ? V : K)];      // (or, before they are known, what the groups are scored by)
     float* const mine = scores + (threadIdx.x - lane) * V;
     const int batches = a.plan.units > 0 ? a.plan.per_unit / (rows * k) : 1;
     if (a.plan.units > 1) {
         for (int e = threadIdx.x; e <= E; e += kBlock) hist[0][e] = 0;
         __syncthreads();
     }
+    float b[V] = {};
+    if (a.in.bias) {
+        const Share of{lg, lane, E, a.whole != 0};
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+            const int e = of.template operator()<n>(i);
+            b[i] = a.in.bias[e < E ? e : 0];
+        }
+    }
     for (int batch = 0; batch < batches; ++batch) {
+        // The lane's number, anew: what is made of it is not kept from batch to batch, which took registers for a third of the waves.
+        int now = lane;
+        asm volatile("" : "+v"(now));
+        const Share of{lg, now, E, a.whole != 0};
         const int64_t row = ((int64_t)blockIdx.x * batches + batch) * rows + (threadIdx.x >> lg);
         const bool there = row < a.in.rows;
         const T* const at = static_cast<const T*>(a.in.logits) + (there ? row : 0) * E;
-        float x[V], c[V] = {};
+        float x[V], c[V];
         load_row<T, V>(x, at, of);
-        if (a.in.bias)
-#pragma unroll
-            for (int i = 0; i < V; ++i) {
-                const int e = of.template operator()<n>(i);
-                c[i] = a.in.bias[e < E ? e : 0];
-            }
         Softmax sm{};
         if (!kSigmoid) sm = softmax_of<V>(x, lg);
 #pragma unroll
         for (int i = 0; i < V; ++i) {
             const float s = score_of<kSigmoid>(x[i], sm);
-            if (a.in.bias) mine[of.template operator()<n>(i)] = s;
-            c[i] = x[i] == -__builtin_inff() ? x[i] : s + c[i];
+            c[i] = x[i] == -__builtin_inff() ? x[i] : s + b[i];
+            x[i] = s;
         }
+        if (a.in.bias)
+#pragma unroll
+            for (int i = 0; i < V; ++i) mine[of.template operator()<n>(i)] = x[i];
 
         uint32_t kept = ~0u;
         if constexpr (kGroups) {
             // the groups' two largest, by lanes of the team in turn; each group's rank by counting the better ones
-            __shared__ float all[kBlock * V];
             __shared__ double group[kBlock * V];       // (of each team the first n_group: a group has at least one expert)
-            float* const c_mine = all + (threadIdx.x >> lg) * (team * V);
+            float* const c_mine = reinterpret_cast<float*>(ids) + (threadIdx.x >> lg) * (team * V);
             double* const g_mine = group + (threadIdx.x >> lg) * (team * V);
             __syncthreads();
 #pragma unroll
