@@ -74,19 +74,19 @@ __device__ __forceinline__ float team_sum(float v, int lg)
 // expert.  Lanes share a row by 16 scores each: 16 are four loads of 16 bytes in single precision, and a list that stays in registers.
 //
 // Scores are computed and leave in single precision whatever the type of the logits.
-constexpr double kNoExpert = -1.0e300;      // below every score
+constexpr int kNoExpert = (int)0xFE37E43C;      // upper half of a number below every score's (-1e300)
 
 __device__ __forceinline__ double key_of(float c, int e)      // (c is not -0: a score is not)
 {
     const double d = (double)__builtin_amdgcn_fmed3f(c, -3.4028235e38f, 3.4028235e38f);      // (what is no number is the least score)
     const int hi = __double2hiint(d), lo = __double2loint(d) | ((511 - e) ^ (hi >> 31 & 511));
-    return c == -__builtin_inff() ? kNoExpert : __hiloint2double(hi, lo);
+    return __hiloint2double(c == -__builtin_inff() ? kNoExpert : hi, lo);
 }
 
 __device__ __forceinline__ int expert_of(double key)
 {
     const int hi = __double2hiint(key);
-    return hi == (int)0xFE37E43C ? -1 : 511 - ((__double2loint(key) ^ hi >> 31) & 511);      // (kNoExpert's; every score's is larger)
+    return hi == kNoExpert ? -1 : 511 - ((__double2loint(key) ^ hi >> 31) & 511);      // (every score's is larger)
 }
 
 // (fmax and fmin would first quiet what might be a signalling not-a-number; keys are numbers)
@@ -167,16 +167,14 @@ __device__ __forceinline__ float score_of(float x, Softmax sm)
     return expf(x - sm.shift) * sm.inv;
 }
 
-// Which expert is number i of a lane's share of a row: neighbouring lanes of a team take neighbouring 16 bytes, or elements where rows are not whole
-// ones of all lanes.
+// Which expert is number i of a lane's share of a row: neighbouring lanes of a team take neighbouring 16 bytes.
 struct Share {
     int lg, lane, n_expert;
-    bool whole;
 
     template <int kChunk>
     __device__ __forceinline__ int operator()(int i) const
     {
-        return whole ? ((i / kChunk << lg) + lane) * kChunk + i % kChunk : (i << lg) + lane;
+        return ((i / kChunk << lg) + lane) * kChunk + i % kChunk;
     }
 };
 
@@ -185,23 +183,24 @@ template <typename T, int V>
 __device__ __forceinline__ void load_row(float (&x)[V], const T* row, const Share& of)
 {
     constexpr int n = Chunk<T>::n;
-    if (of.whole) {
-        typedef typename Chunk<T>::Vec Vec;
+    Elements<T, n> v[V / n];
+    if (of.n_expert == V << of.lg) {      // (all lanes have 16: nothing to ask for between the loads)
 #pragma unroll
-        for (int i = 0; i < V; i += n) {
-            const int e = of.template operator()<n>(i);
-            const Vec v = *reinterpret_cast<const Vec*>(row + (e < of.n_expert ? e : 0));
+        for (int i = 0; i < V / n; ++i) v[i] = Elements<T, n>::load(row + of.template operator()<n>(i * n));
 #pragma unroll
-            for (int j = 0; j < n; ++j) x[i + j] = e < of.n_expert ? (float)v[j] : -__builtin_inff();
-        }
+        for (int i = 0; i < V; ++i) x[i] = (float)v[i / n].v[i % n];
         return;
     }
 #pragma unroll
-    for (int i = 0; i < V; ++i) {
-        const int e = of.template operator()<n>(i);
-        const float v = (float)row[e < of.n_expert ? e : 0];
-        x[i] = e < of.n_expert ? v : -__builtin_inff();
+    for (int i = 0; i < V / n; ++i) {
+        const int e = of.template operator()<n>(i * n);
+        if (e + n <= of.n_expert) v[i] = Elements<T, n>::load(row + e);
+        else
+#pragma unroll
+            for (int j = 0; j < n; ++j) v[i].v[j] = row[e + j < of.n_expert ? e + j : 0];
     }
+#pragma unroll
+    for (int i = 0; i < V; ++i) x[i] = of.template operator()<n>(i) < of.n_expert ? (float)v[i / n].v[i % n] : -__builtin_inff();
 }
 
 // The order of slots (see below), as far as a workgroup has a part in it.
@@ -224,7 +223,6 @@ struct RouteArgs {
     float* weight;
     int* expert;
     int lg;          // log2 of the lanes per row
-    int whole;       // rows are whole 16 bytes of each, on boundaries of 16
     uint32_t group_mul;      // 2^20 / experts of a group, rounded up
     PlanArgs plan;   // units 0: no order is asked for
 };
@@ -247,7 +245,7 @@ __global__ __launch_bounds__(kBlock) void k_route(RouteArgs a)
     }
     float b[V] = {};
     if (a.in.bias) {
-        const Share of{lg, lane, E, a.whole != 0};
+        const Share of{lg, lane, E};
 #pragma unroll
         for (int i = 0; i < V; ++i) {
             const int e = of.template operator()<n>(i);
@@ -258,7 +256,7 @@ __global__ __launch_bounds__(kBlock) void k_route(RouteArgs a)
         // The lane's number, anew: what is made of it is not kept from batch to batch, which took registers for a third of the waves.
         int now = lane;
         asm volatile("" : "+v"(now));
-        const Share of{lg, now, E, a.whole != 0};
+        const Share of{lg, now, E};
         const int64_t row = ((int64_t)blockIdx.x * batches + batch) * rows + (threadIdx.x >> lg);
         const bool there = row < a.in.rows;
         const T* const at = static_cast<const T*>(a.in.logits) + (there ? row : 0) * E;
@@ -316,7 +314,7 @@ __global__ __launch_bounds__(kBlock) void k_route(RouteArgs a)
         for (int i = 0; i < V; ++i) {
             const int e = of.template operator()<n>(i);
             keys[i] = key_of(c[i], e);
-            if constexpr (kGroups) keys[i] = kept >> ((uint32_t)e * a.group_mul >> 20 & 31) & 1 ? keys[i] : kNoExpert;
+            if constexpr (kGroups) keys[i] = kept >> ((uint32_t)e * a.group_mul >> 20 & 31) & 1 ? keys[i] : __hiloint2double(kNoExpert, 0);
         }
 #pragma unroll
         for (int i = 0; i < V; i += K) sort_list<K>(keys + i);
@@ -387,7 +385,7 @@ struct RouteBackArgs {
     const int* expert;
     const float* dweight;
     void* dlogits;
-    int lg, whole;
+    int lg;
 };
 
 // With s the scores, c the chosen, g = scale * dweight there and 0 elsewhere, the gradient by a logit is
@@ -408,7 +406,7 @@ __global__ __launch_bounds__(kBlock) void k_route_back(RouteBackArgs a)
     const bool there = row < a.in.rows;
     const int E = a.in.n_expert, k = a.in.top_k;
     const int64_t r = there ? row : 0;
-    const Share of{lg, lane, E, a.whole != 0};
+    const Share of{lg, lane, E};
     const T* const at = static_cast<const T*>(a.in.logits) + r * E;
     marks[threadIdx.x] = 0;
     float x[V];
@@ -457,29 +455,18 @@ __global__ __launch_bounds__(kBlock) void k_route_back(RouteBackArgs a)
         else d[i] = s[i] * (u[i] - dot);
     }
     T* const out = static_cast<T*>(a.dlogits) + row * E;
-    if (a.whole) {
-        typedef typename Chunk<T>::Vec Vec;
 #pragma unroll
-        for (int i = 0; i < V; i += n) {
-            const int e = of.template operator()<n>(i);
-            Vec v;
-#pragma unroll
-            for (int j = 0; j < n; ++j) v[j] = (T)d[i + j];
-            if (e < E) *reinterpret_cast<Vec*>(out + e) = v;
-        }
-        return;
-    }
-#pragma unroll
-    for (int i = 0; i < V; ++i) {
+    for (int i = 0; i < V; i += n) {
         const int e = of.template operator()<n>(i);
-        if (e < E) out[e] = (T)d[i];
+        Elements<T, n> v;
+#pragma unroll
+        for (int j = 0; j < n; ++j) v.v[j] = (T)d[i + j];
+        if (e + n <= E) v.store(out + e);
+        else
+#pragma unroll
+            for (int j = 0; j < n - 1; ++j)
+                if (e + j < E) out[e + j] = v.v[j];
     }
-}
-
-template <typename T>
-bool whole_rows(const void* a, const void* b, int n_expert)
-{
-    return n_expert % Chunk<T>::n == 0 && aligned16(a) && aligned16(b);
 }
 
 template <typename T, int K>
@@ -756,7 +743,7 @@ int launch_route(gr_experts* h, const RouteIn& in, int dtype, float* weight, int
     return by_type(dtype, [&](auto t) {
         typedef decltype(t) T;
         const int size = in.n_expert / in.n_group;
-        RouteArgs a{in, weight, expert, team_log(in.n_expert), whole_rows<T>(in.logits, nullptr, in.n_expert), (uint32_t)(((1 << 20) + size - 1) / size), {}};
+        RouteArgs a{in, weight, expert, team_log(in.n_expert), (uint32_t)(((1 << 20) + size - 1) / size), {}};
         if (off) {
             // a unit of slots is what a workgroup chooses: more than one batch of rows where that leaves enough workgroups
             int rows = kBlock >> a.lg;
@@ -774,7 +761,7 @@ int launch_route_backward(const RouteIn& in, int dtype, const int* expert, const
 {
     return by_type(dtype, [&](auto t) {
         typedef decltype(t) T;
-        const RouteBackArgs a{in, expert, dweight, dlogits, team_log(in.n_expert), whole_rows<T>(in.logits, dlogits, in.n_expert)};
+        const RouteBackArgs a{in, expert, dweight, dlogits, team_log(in.n_expert)};
         const int64_t blocks = ((in.rows << a.lg) + kBlock - 1) / kBlock;
         if (blocks > kMostBlocks) return (int)GR_ERR_TOO_LARGE;
         if (in.scoring == GR_SCORE_SIGMOID) k_route_back<T, true><<<blocks, kBlock, 0, s>>>(a);
