@@ -131,16 +131,21 @@ struct TileNo {
     int col;
 };
 
+// Tile t in the order of blocks.
+__device__ __forceinline__ TileNo tile_at(int64_t t, int64_t down, int across, int block)
+{
+    const int64_t band = t / ((int64_t)block * across), in = t - band * block * across, left = down - band * block;
+    const int rows = left < block ? (int)left : block;
+    return {band * block + in % rows, (int)(in / rows)};
+}
+
 __device__ __forceinline__ TileNo tile_no(int64_t j, int64_t down, int across, int block)
 {
     const int64_t all = down * across, each = (all + kDies - 1) / kDies;
     const int run = each < kTogether ? (int)each : kTogether;      // tiles that a die takes together (fewer where there are not 32 for each)
     if (run == 0) return {-1, 0};
     const int64_t at = j / kDies, t = (at / run * kDies + j % kDies) * run + at % run;
-    if (t >= all) return {-1, 0};
-    const int64_t band = t / ((int64_t)block * across), in = t - band * block * across, left = down - band * block;
-    const int rows = left < block ? (int)left : block;
-    return {band * block + in % rows, (int)(in / rows)};
+    return t < all ? tile_at(t, down, across, block) : TileNo{-1, 0};
 }
 
 typedef float f32x4 __attribute__((ext_vector_type(4)));
@@ -459,9 +464,15 @@ struct Tile {
     int64_t p0, lo, depth;      // rows from p0 on (positions, or by weight output features); the reduction's start, by weight, and length
 };
 
-template <typename T, Product kProduct, int kSize, bool kParts>
+// A last round of large tiles that at most half of the units would have work in is left to tiles of 128 by 128, four in the place of each (kRest).
+constexpr int kUnits = 256;          // compute units: workgroups of large tiles that run at a time
+
+__device__ __forceinline__ int64_t whole_rounds(int64_t all) { return all % kUnits <= kUnits / 2 ? all / kUnits * kUnits : all; }
+
+template <typename T, Product kProduct, int kSize, bool kParts, bool kRest>
 __global__ __launch_bounds__(kWaves * kWave, kSize > 128 ? 1 : 2) void k_linear_tiles(LinearArgs a)
 {
+    constexpr int kUnit = kRest ? 2 * kSize : kSize;      // rows and columns of what is numbered
     constexpr int kFrag = kSize / 2 / 16;      // fragments of a wave, either way
     constexpr bool kPLong = kProduct != kByWeight, kQLong = kProduct == kForward;
     constexpr int kSlotBytes = kSize * kDepth * 2;
@@ -494,7 +505,7 @@ __global__ __launch_bounds__(kWaves * kWave, kSize > 128 ? 1 : 2) void k_linear_
                 mine.lo = (int)bound(a.off, lane, a.n_expert, a.n_pos);
                 mine.hi = lane < a.n_expert ? (int)bound(a.off, lane + 1, a.n_expert, a.n_pos) : (int)a.n_pos;
             }
-            mine.tiles = mine.hi > mine.lo ? (mine.hi - mine.lo + kSize - 1) / kSize : 0;
+            mine.tiles = mine.hi > mine.lo ? (mine.hi - mine.lo + kUnit - 1) / kUnit : 0;
             mine.end = mine.tiles;
             for (int d = 1; d < kWave; d *= 2) {
                 const int o = __shfl_up(mine.end, d);
@@ -503,18 +514,38 @@ __global__ __launch_bounds__(kWaves * kWave, kSize > 128 ? 1 : 2) void k_linear_
             down = __builtin_amdgcn_readlane(mine.end, kWave - 1);
         }
     }
+    const auto quarter_of = [](Tile& t, int quarter) __attribute__((always_inline)) {      // false where it is past the edge
+        const int down = quarter / 2 * kSize, right = quarter % 2 * kSize;
+        t.p0 += down;
+        t.p_n = t.p_n - down < kSize ? t.p_n - down : kSize;
+        t.q0 += right;
+        t.q_n = t.q_n - right < kSize ? t.q_n - right : kSize;
+        return t.p_n > 0 && t.q_n > 0;
+    };
     const auto find = [&](int64_t j, Tile& t) __attribute__((always_inline)) {
-        const TileNo no = tile_no(j, down, a.tiles, a.block);
-        if (no.row < 0) return false;
-        t.q0 = no.col * kSize;
-        t.q_n = width - t.q0 < kSize ? width - t.q0 : kSize;
+        TileNo no;
+        int quarter = 0;
+        const int64_t all = down * a.tiles, whole = whole_rounds(all);
+        if constexpr (kRest) {      // the quarters of a tile go to one die
+            const int64_t in = j / kDies, at = whole + in / 4 * kDies + j % kDies;
+            if (at >= all) return false;
+            no = tile_at(at, down, a.tiles, a.block);
+            quarter = (int)(in % 4);
+        } else {
+            if (kSize > 128 && whole < all && j >= whole) return false;      // (a round of numbers is the same tiles in `tile_no`'s order)
+            no = tile_no(j, down, a.tiles, a.block);
+            if (no.row < 0) return false;
+        }
+        t.q0 = no.col * kUnit;
+        t.q_n = width - t.q0 < kUnit ? width - t.q0 : kUnit;
         t.lo = 0;
         if constexpr (kProduct == kByWeight) {
-            const int tiles = (O + kSize - 1) / kSize, part = (int)(no.row / tiles);
+            const int tiles = (O + kUnit - 1) / kUnit, part = (int)(no.row / tiles);
             t.e = part / a.parts_n;
             t.part = part - t.e * a.parts_n;
-            t.p0 = (no.row - (int64_t)part * tiles) * kSize;
-            t.p_n = O - t.p0 < kSize ? (int)(O - t.p0) : kSize;
+            t.p0 = (no.row - (int64_t)part * tiles) * kUnit;
+            t.p_n = O - t.p0 < kUnit ? (int)(O - t.p0) : kUnit;
+            if (kRest && !quarter_of(t, quarter)) return false;
             part_of(a, t.e, t.part, t.lo, t.depth);
             t.lo = uniform(t.lo);
             t.depth = uniform(t.depth);
@@ -524,16 +555,17 @@ __global__ __launch_bounds__(kWaves * kWave, kSize > 128 ? 1 : 2) void k_linear_
                 const unsigned long long here = __ballot(no.row >= mine.end - mine.tiles && no.row < mine.end);
                 if (here) {
                     const int l = __ffsll((long long)here) - 1;
-                    const int64_t first = __builtin_amdgcn_readlane(mine.lo, l) + (no.row - (__builtin_amdgcn_readlane(mine.end, l) - __builtin_amdgcn_readlane(mine.tiles, l))) * kSize;
+                    const int64_t first = __builtin_amdgcn_readlane(mine.lo, l) + (no.row - (__builtin_amdgcn_readlane(mine.end, l) - __builtin_amdgcn_readlane(mine.tiles, l))) * kUnit;
                     const int64_t last = __builtin_amdgcn_readlane(mine.hi, l);
-                    r = {l, first, first + kSize < last ? first + kSize : last};
+                    r = {l, first, first + kUnit < last ? first + kUnit : last};
                 }
             } else {
-                r = row_tile(a.off, a.n_expert, a.n_pos, kSize, no.row);
+                r = row_tile(a.off, a.n_expert, a.n_pos, kUnit, no.row);
             }
             t.e = uniform(r.expert);
             t.p0 = uniform(r.lo);
             t.p_n = uniform((int)(r.hi - r.lo));
+            if (kRest && !quarter_of(t, quarter)) return false;
             t.depth = t.e == a.n_expert || t.p_n <= 0 ? 0 : kProduct == kForward ? I : O;
         }
         return true;
@@ -1187,7 +1219,6 @@ bool in_tiles(const LinearIn& in, const void* a, const void* b, const void* c)
 }
 
 // Which form a product takes.  Times are of nine experts, in bfloat16 where nothing else is said, without the form / with it.
-constexpr int kUnits = 256;          // compute units: workgroups of large tiles that run at a time
 // Tiles of 256 by 256 from four rounds of them on, of 128 by 128 before.  Forward, 128 / 256: 8 192 x 4 096 -> 1 024 (165 tiles) 93 / 101 us, 65
 // 536 x 1 024 -> 512 (530) 85 / 104, 65 536 x 4 096 -> 1 024 (1 060) 607 / 535; by input 65 536 x 1 024 -> 512 (1 060) 111 / 112, 65 536 x 1 024
 // -> 4 096 (4 240) 703 / 614.
@@ -1293,19 +1324,22 @@ void product(gr_experts* h, const LinearIn& in, LinearArgs a, bool tiles, hipStr
     if (in.n_out <= kNarrow && !whole && narrow<T, kProduct>(h, in, a, s)) return;
     if constexpr (sizeof(T) == 2) {
         if (tiles) {
-            if (grid(256) >= kLargeRounds * kUnits) {
-                k_linear_tiles<T, kProduct, 256, false><<<kUnits, kWaves * kWave, 0, s>>>(a);
+            const int64_t large = grid(256), rest = a.down * a.tiles % kUnits;      // (by weight; else the most there may be)
+            if (large >= kLargeRounds * kUnits || (kProduct == kByWeight && large >= 2 * kUnits && rest <= kUnits / 2)) {
+                k_linear_tiles<T, kProduct, 256, false, false><<<kUnits, kWaves * kWave, 0, s>>>(a);
+                if (kProduct != kByWeight || (rest > 0 && rest <= kUnits / 2))
+                    k_linear_tiles<T, kProduct, 128, false, true><<<2 * kUnits, kWaves * kWave, 0, s>>>(a);
                 return;
             }
             if constexpr (kProduct == kByWeight) {
                 if (cut(128, 2 * kUnits * kPartRounds, kPartRows)) {
                     const int64_t n = grid(128);
-                    k_linear_tiles<T, kProduct, 128, true><<<(unsigned)(n < 2 * kUnits ? n : 2 * kUnits), kWaves * kWave, 0, s>>>(a);
+                    k_linear_tiles<T, kProduct, 128, true, false><<<(unsigned)(n < 2 * kUnits ? n : 2 * kUnits), kWaves * kWave, 0, s>>>(a);
                     return join();
                 }
             }
             const int64_t n = grid(128);
-            k_linear_tiles<T, kProduct, 128, false><<<(unsigned)(n < 2 * kUnits ? n : 2 * kUnits), kWaves * kWave, 0, s>>>(a);
+            k_linear_tiles<T, kProduct, 128, false, false><<<(unsigned)(n < 2 * kUnits ? n : 2 * kUnits), kWaves * kWave, 0, s>>>(a);
             return;
         }
     }

@@ -289,6 +289,14 @@ def test_layers_of_few_features(n, E, I, O, k, dtype):
     test_gradients_of_a_layer(n, E, I, O, k, dtype)
 
 
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+def test_layers_of_many_tiles(dtype):
+    """More large tiles than rounds of them are whole: forward and by input 1 295 to 1 310, by weight 530 (a round is 256)."""
+    test_layer(66100, 3, 72, 1032, 2, dtype)
+    test_gradients_of_a_layer(66100, 3, 1032, 72, 2, dtype)
+    test_gradients_of_a_layer(300, 2, 13320, 1032, 1, dtype)
+
+
 def test_one_matrix_for_all_rows():
     rng = np.random.default_rng(3)
     n, I, O = 333, 80, 72
