@@ -465,6 +465,8 @@ struct Tile {
 };
 
 // A last round of large tiles that at most half of the units would have work in is left to tiles of 128 by 128, four in the place of each (kRest).
+// Without / with: 65 536 x 4 096 -> 1 024 of nine experts 490 / 466 us, 65 536 x 1 024 -> 1 024 178 / 166, 131 072 x 4 096 -> 1 024 915 / 905;
+// where nothing is left, 270 000 x 512 -> 1 024, 410 / 411.
 constexpr int kUnits = 256;          // compute units: workgroups of large tiles that run at a time
 
 __device__ __forceinline__ int64_t whole_rounds(int64_t all) { return all % kUnits <= kUnits / 2 ? all / kUnits * kUnits : all; }
@@ -1218,10 +1220,10 @@ bool in_tiles(const LinearIn& in, const void* a, const void* b, const void* c)
     return in.n_in % Chunk<T>::n == 0 && in.n_out % Chunk<T>::n == 0 && aligned16(a) && aligned16(b) && aligned16(c);
 }
 
-// Which form a product takes.  Times are of nine experts, in bfloat16 where nothing else is said, without the form / with it.
-// Tiles of 256 by 256 from four rounds of them on, of 128 by 128 before.  Forward, 128 / 256: 8 192 x 4 096 -> 1 024 (165 tiles) 93 / 101 us, 65
-// 536 x 1 024 -> 512 (530) 85 / 104, 65 536 x 4 096 -> 1 024 (1 060) 607 / 535; by input 65 536 x 1 024 -> 512 (1 060) 111 / 112, 65 536 x 1 024
-// -> 4 096 (4 240) 703 / 614.
+// Which form a product takes.  Times are of nine experts, in bfloat16 where nothing else is said, without the form / with it. Tiles of 256 by 256
+// from four rounds of them on, of 128 by 128 before.  Forward, 128 / 256: 8 192 x 4 096 -> 1 024 (165 tiles) 93 / 101 us, 65 536 x 1 024 -> 512
+// (530) 85 / 104, 65 536 x 4 096 -> 1 024 (1 060) 607 / 535; by input 65 536 x 1 024 -> 512 (1 060) 111 / 112, 65 536 x 1 024 -> 4 096 (4 240) 703
+// / 614.
 constexpr int kLargeRounds = 4;
 // Few rows: up to 16 an expert on average (32 in single precision), 16 times that in all (an expert may have them all, and its weights are read
 // again for every 16).  Nine experts of 4 096 -> 1 024, tiles / this: bfloat16 9 positions 39 / 18 us, 72 39 / 20, 144 39 / 24 (36 where one expert
@@ -1324,11 +1326,9 @@ void product(gr_experts* h, const LinearIn& in, LinearArgs a, bool tiles, hipStr
     if (in.n_out <= kNarrow && !whole && narrow<T, kProduct>(h, in, a, s)) return;
     if constexpr (sizeof(T) == 2) {
         if (tiles) {
-            const int64_t large = grid(256), rest = a.down * a.tiles % kUnits;      // (by weight; else the most there may be)
-            if (large >= kLargeRounds * kUnits || (kProduct == kByWeight && large >= 2 * kUnits && rest <= kUnits / 2)) {
+            if (grid(256) >= kLargeRounds * kUnits) {
                 k_linear_tiles<T, kProduct, 256, false, false><<<kUnits, kWaves * kWave, 0, s>>>(a);
-                if (kProduct != kByWeight || (rest > 0 && rest <= kUnits / 2))
-                    k_linear_tiles<T, kProduct, 128, false, true><<<2 * kUnits, kWaves * kWave, 0, s>>>(a);
+                k_linear_tiles<T, kProduct, 128, false, true><<<2 * kUnits, kWaves * kWave, 0, s>>>(a);
                 return;
             }
             if constexpr (kProduct == kByWeight) {

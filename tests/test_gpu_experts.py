@@ -297,6 +297,16 @@ def test_layers_of_many_tiles(dtype):
     test_gradients_of_a_layer(300, 2, 13320, 1032, 1, dtype)
 
 
+def test_gradients_of_many_weights():
+    """1 060 large tiles by weight."""
+    test_gradients_of_a_layer(40, 4, 13320, 1032, 1, torch.bfloat16)
+
+
+def test_gradients_of_many_weights():
+    """1 060 large tiles by weight."""
+    test_gradients_of_a_layer(40, 4, 13320, 1032, 1, torch.bfloat16)
+
+
 def test_one_matrix_for_all_rows():
     rng = np.random.default_rng(3)
     n, I, O = 333, 80, 72
