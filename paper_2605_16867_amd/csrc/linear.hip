@@ -728,34 +728,61 @@ __global__ __launch_bounds__(kWaves * kWave, kSize > 128 ? 1 : 2) void k_linear_
         const __amdgpu_buffer_rsrc_t to = __builtin_amdgcn_make_buffer_rsrc(out, 0, 0x7fffffff, 0x00027000);
         const bool biased = kProduct == kForward && a.bias && t.e < a.n_expert;
         const T* const bias = static_cast<const T*>(a.bias) + (int64_t)t.e * O + t.q0;
+        if constexpr (kParts) {
 #pragma unroll
-        for (int j = 0; j < kFrag; ++j) {
-            const int col = wq + j * 16 + lane / 16 * 4;
-            float b[4] = {};
-            if (biased && col < t.q_n) {
-                const Four v = *reinterpret_cast<const Four*>(bias + col);
+            for (int j = 0; j < kFrag; ++j) {
+                const int col = wq + j * 16 + lane / 16 * 4;
 #pragma unroll
-                for (int k = 0; k < 4; ++k) b[k] = (float)v[k];
+                for (int i = 0; i < kFrag; ++i) {
+                    const int row = wp + i * 16 + lane % 16;
+                    typedef uint32_t Bits __attribute__((ext_vector_type(4)));
+                    union { f32x4 value; Bits bits; } o;
+                    o.value = acc[i][j];
+                    __builtin_amdgcn_raw_buffer_store_b128(
+                        o.bits, to, row < t.p_n && col < t.q_n ? (uint32_t)(row * width + col) * (uint32_t)sizeof(Out) : kNowhere, 0, 0);
+                }
             }
+            return;
+        }
+        // Two fragments' columns at a time: a lane has four of each; exchanged between the wave's rows of 16 lanes they are eight in a row, so that
+        // a store writes 64 bytes of a line instead of 32.
+#pragma unroll
+        for (int j = 0; j < kFrag; j += 2) {
+            float b[2][4] = {};
+#pragma unroll
+            for (int f = 0; f < 2; ++f) {
+                const int of = wq + (j + f) * 16 + lane / 16 * 4;
+                if (biased && of < t.q_n) {
+                    const Four v = *reinterpret_cast<const Four*>(bias + of);
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) b[f][k] = (float)v[k];
+                }
+            }
+            const int col = wq + j * 16 + lane / 16 * 8;
 #pragma unroll
             for (int i = 0; i < kFrag; ++i) {
                 const int row = wp + i * 16 + lane % 16;
                 const uint32_t at = row < t.p_n && col < t.q_n ? (uint32_t)(row * width + col) * (uint32_t)sizeof(Out) : kNowhere;
-                if constexpr (kParts) {
-                    typedef uint32_t Bits __attribute__((ext_vector_type(4)));
-                    union { f32x4 value; Bits bits; } o;
-                    o.value = acc[i][j];
-                    __builtin_amdgcn_raw_buffer_store_b128(o.bits, to, at, 0, 0);
-                } else {
-                    union { Four value; Two bits; } o;
+                union { Four value; Two bits; } o[2];
+#pragma unroll
+                for (int f = 0; f < 2; ++f)
 #pragma unroll
                     for (int k = 0; k < 4; ++k) {
-                        float v = acc[i][j][k] + b[k];
+                        float v = acc[i][j + f][k] + b[f][k];
                         if (kProduct == kForward && a.relu && v < 0) v = 0;
-                        o.value[k] = (T)v;
+                        o[f].value[k] = (T)v;
                     }
-                    __builtin_amdgcn_raw_buffer_store_b64(o.bits, to, at, 0, 0);
+                typedef uint32_t Bits __attribute__((ext_vector_type(4)));
+                Bits all;
+#pragma unroll
+                for (int d = 0; d < 2; ++d) {
+                    const auto half = __builtin_amdgcn_permlane32_swap(o[0].bits[d], o[1].bits[d], false, false);
+                    const auto both = __builtin_amdgcn_permlane16_swap(half[0], half[1], false, false);
+                    all[d] = both[0];
+                    all[2 + d] = both[1];
                 }
+                __builtin_amdgcn_raw_buffer_store_b128(all, to, at, 0, 0);
+                __builtin_amdgcn_sched_barrier(0);      // (sums of one fragment's are in the other registers at a time)
             }
         }
     };
@@ -800,7 +827,7 @@ __global__ __launch_bounds__(kWaves * kWave, kSize > 128 ? 1 : 2) void k_linear_
         const int slices = (int)((now.depth + kDepth - 1) / kDepth), whole = (int)(now.depth / kDepth);
         if (slices > 0) {
             // the first slice: behind it there may be the second, and the stores
-            constexpr int kStores = kFrag * kFrag;
+            constexpr int kStores = kParts ? kFrag * kFrag : kFrag * kFrag / 2;
             if (slices == 1) asm volatile("s_waitcnt vmcnt(0)\n\ts_barrier" ::: "memory");
             else if (behind) asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" ::"n"(2 * kLoads + kStores < 63 ? 2 * kLoads + kStores : 63) : "memory");
             else asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" ::"n"(2 * kLoads) : "memory");
