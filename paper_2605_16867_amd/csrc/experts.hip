@@ -69,9 +69,11 @@ __device__ __forceinline__ float team_sum(float v, int lg)
 // The largest top_k of a list are then found with minima and maxima alone: a lane sorts eight of its scores by a network and merges them, half
 // against half, with what it has; then lanes merge theirs.
 //
-// Bound by those: 262 144 rows of 64 experts in bfloat16, eight of them, take 41 us, where reading the 33.5 MB is 7.  16 rows are about 1 150 vector
-// instructions of a wave, most of them minima and maxima of doubles.  Keys of 32 bits would be cheaper, but cannot hold a score whole and its
-// expert.  Lanes share a row by 16 scores each: 16 are four loads of 16 bytes in single precision, and a list that stays in registers.
+// Bound by vector instructions: 262 144 rows of 64 experts in bfloat16, eight of them, take 31 us, where reading the 33.5 MB is 7.  A batch of 16
+// rows is about 900 of a wave (a third of them exponentials, half scores, keys and the choice), and they keep the units two thirds busy at four
+// waves a unit.  Keys of 32 bits would be cheaper, but cannot hold a score whole and its expert.  Lanes share a row by 16 scores each: 16 are four
+// loads of 16 bytes in single precision, and a list that stays in registers.  Asking for a batch's rows during the one before took longer (48.7 /
+// 45.7 with the places).
 //
 // Scores are computed and leave in single precision whatever the type of the logits.
 constexpr int kNoExpert = (int)0xFE37E43C;      // upper half of a number below every score's (-1e300)
@@ -393,7 +395,7 @@ struct RouteBackArgs {
 //   softmax, renormalised  for chosen i: s_i / S (g_i - sum g s / S), S = the sum of s over c; 0 elsewhere (the other shares cancel)
 //   sigmoid                the same two with another factor 1 - s_i, without the sum where nothing is renormalised
 // Scores are computed again from the logits: reading them back would be as many bytes more.  Bound by memory and a launch: 65 536 rows of 64 in
-// single precision, 38 MB with the choices, 10.9 us (3.5 TB/s).  What is chosen goes by expert through shared memory, as a mark and a gradient
+// single precision, 38 MB with the choices, 10.2 us (3.7 TB/s).  What is chosen goes by expert through shared memory, as a mark and a gradient
 // each.
 template <typename T, bool kSigmoid>
 __global__ __launch_bounds__(kBlock) void k_route_back(RouteBackArgs a)
