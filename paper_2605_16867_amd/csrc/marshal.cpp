@@ -48,7 +48,7 @@ struct Entries {
 PyObject* check_slowly = nullptr;      // (tensor, type code, name, elements or None) -> address or None, or raises
 
 struct Raised {};      // a Python exception is set
-struct Unclear {};     // for the binding itself to judge (calls of a length predictor)
+struct Unclear {};     // for the binding itself to decide (calls of a length predictor)
 
 constexpr int64_t kAny = -1;
 
