@@ -462,7 +462,7 @@ int gr_experts_destroy(gr_experts* h);       /* waits for the device first; NULL
  *   the experts are n_group groups of equal size, neighbours together; of these the n_group_kept with
  *   the largest sum of their two largest c stay (a single c where a group has no second);
  *   the top_k experts of those groups with the largest c are chosen, largest first;
- *   weight_j = scale * s_j, divided by the sum of the chosen s if `renormalise` (0 where that sum is 0).
+ *   weight_j = scale * s_j, divided by the sum of the chosen s if `renormalise` (0 where that sum is 0 in single precision).
  * Ties go to the lowest index.  The bias enters the choice only.  Where fewer than top_k experts are left the last
  * slots have expert -1 and weight 0.  A c that is no number ranks below every number and above masked experts; its weight is what
  * the arithmetic gives (a row whose softmax is not defined has weights that are no numbers).

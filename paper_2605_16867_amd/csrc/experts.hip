@@ -169,6 +169,11 @@ __device__ __forceinline__ float score_of(float x, Softmax sm)
     return expf(x - sm.shift) * sm.inv;
 }
 
+// Chosen scores that add up to less than this (a bias chose them, or all of a row's sigmoids are small) are divided by their sum another way: in
+// single precision they may have lost their digits, and the reciprocal of their sum may be past its range.  So far down a sigmoid is an exponential to within 2^-30, and so is
+// a softmax but for a factor: shares are those of exp(x - the largest chosen x).  (A sum of 0 gives no shares.)
+constexpr float kFaint = 0x1p-30f;
+
 // Which expert is number i of a lane's share of a row: neighbouring lanes of a team take neighbouring 16 bytes.
 struct Share {
     int lg, lane, n_expert;
@@ -350,15 +355,32 @@ __global__ __launch_bounds__(kBlock) void k_route(RouteArgs a)
             s[j] = id[j] >= 0 ? s[j] : 0.0f;
             sum += s[j];
         }
-        float by = a.in.scale;
-        if (a.in.renorm) by = sum == 0 ? 0.0f : a.in.scale / sum;
+        if (a.in.renorm) {
+            if (sum > 0 && sum < kFaint) {
+                float most = -__builtin_inff();
+#pragma unroll
+                for (int j = 0; j < K; ++j) {
+                    s[j] = id[j] >= 0 ? (float)at[id[j]] : -__builtin_inff();
+                    most = __builtin_fmaxf(most, s[j]);
+                }
+                sum = 0;
+#pragma unroll
+                for (int j = 0; j < K; ++j) {
+                    s[j] = expf(s[j] - most);
+                    sum += s[j];
+                }
+            }
+            const float inv = sum == 0 ? 0.0f : 1.0f / sum;
+#pragma unroll
+            for (int j = 0; j < K; ++j) s[j] *= inv;
+        }
         // out through shared memory, one after the other
         const int wave = threadIdx.x / kWave, at_wave = (wave * kWave >> lg) * k, own = ((threadIdx.x & (kWave - 1)) >> lg) * k;
         float* const weights = scores + wave * kWave * V;
 #pragma unroll
         for (int j = 0; j < K; ++j)
             if (j < k && (j & (team - 1)) == lane) {
-                weights[own + j] = s[j] * by;
+                weights[own + j] = s[j] * a.in.scale;
                 ids[at_wave + own + j] = id[j];
             }
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
@@ -426,6 +448,9 @@ __global__ __launch_bounds__(kBlock) void k_route_back(RouteBackArgs a)
     float s[V];
 #pragma unroll
     for (int i = 0; i < V; ++i) s[i] = x[i] == -__builtin_inff() ? 0.0f : score_of<kSigmoid>(x[i], sm);
+    float rest[V];      // (a sigmoid's derivative by its logit is s times this)
+#pragma unroll
+    for (int i = 0; i < V; ++i) rest[i] = kSigmoid ? 1 - s[i] : 1.0f;
     __syncthreads();
     // sum of u over the shares, and of the chosen scores
     float u[V], dot = 0, sum = 0;
@@ -444,6 +469,21 @@ __global__ __launch_bounds__(kBlock) void k_route_back(RouteBackArgs a)
     float inv = 1;
     if (a.in.renorm) {
         sum = team_sum(sum, lg);
+        if (sum > 0 && sum < kFaint) {      // (of the whole team)
+            float most = -__builtin_inff();
+#pragma unroll
+            for (int i = 0; i < V; ++i) most = chosen >> i & 1 ? __builtin_fmaxf(most, x[i]) : most;
+            most = team_max(most, lg);
+            dot = sum = 0;
+#pragma unroll
+            for (int i = 0; i < V; ++i) {
+                s[i] = chosen >> i & 1 ? expf(x[i] - most) : 0.0f;
+                dot += u[i] * s[i];
+                sum += s[i];
+            }
+            dot = team_sum(dot, lg);
+            sum = team_sum(sum, lg);
+        }
         inv = sum == 0 ? 0.0f : 1.0f / sum;
         dot *= inv;
     }
@@ -452,8 +492,8 @@ __global__ __launch_bounds__(kBlock) void k_route_back(RouteBackArgs a)
 #pragma unroll
     for (int i = 0; i < V; ++i) {
         const bool is = chosen >> i & 1;
-        if (a.in.renorm) d[i] = is ? s[i] * inv * (u[i] - dot) * (kSigmoid ? 1 - s[i] : 1.0f) : 0.0f;
-        else if (kSigmoid) d[i] = is ? s[i] * (1 - s[i]) * u[i] : 0.0f;
+        if (a.in.renorm) d[i] = is ? s[i] * inv * (u[i] - dot) * rest[i] : 0.0f;
+        else if (kSigmoid) d[i] = is ? s[i] * rest[i] * u[i] : 0.0f;
         else d[i] = s[i] * (u[i] - dot);
     }
     T* const out = static_cast<T*>(a.dlogits) + row * E;
