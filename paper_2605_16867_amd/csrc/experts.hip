@@ -448,9 +448,12 @@ __global__ __launch_bounds__(kBlock) void k_route_back(RouteBackArgs a)
     float s[V];
 #pragma unroll
     for (int i = 0; i < V; ++i) s[i] = x[i] == -__builtin_inff() ? 0.0f : score_of<kSigmoid>(x[i], sm);
-    float rest[V];      // (a sigmoid's derivative by its logit is s times this)
+    float rest[V];      // 1 - s, which a sigmoid's derivative by its logit is s times; near 1 the difference would have no digits
 #pragma unroll
-    for (int i = 0; i < V; ++i) rest[i] = kSigmoid ? 1 - s[i] : 1.0f;
+    for (int i = 0; i < V; ++i) {
+        const float e = kSigmoid ? expf(-x[i]) : 0.0f;
+        rest[i] = !kSigmoid ? 1.0f : e > 1 ? 1 - s[i] : e * s[i];
+    }
     __syncthreads();
     // sum of u over the shares, and of the chosen scores
     float u[V], dot = 0, sum = 0;

@@ -55,3 +55,30 @@ def test_a_large_scale_of_shares(scoring):
     rw, rids = ref.route(x, 2, None, scoring, 1, 1, True, 3e38)
     assert np.array_equal(ids, rids)
     ref.close(w, rw, torch.float32, magnitude=rw, n=512)
+
+
+@pytest.mark.parametrize("renorm", [False, True])
+def test_gradient_of_sigmoids_near_one(renorm):
+    """1 - s of a large logit is not what single precision leaves of the difference."""
+    rng = np.random.default_rng(2)
+    T, E, k = 50, 24, 5
+    x = f64_of(rng.choice([-20, -16, -12, -3, 0, 3, 12, 16, 20, 30, 60], (T, E)) + rng.normal(size=(T, E)), torch.float32)
+    ids = np.stack([rng.permutation(E)[:k] for _ in range(T)])
+    u = f64_of(rng.normal(size=(T, k)), torch.float32)
+    out, h = empty(T, E), binding.Experts(E, T, k)
+    h.gr_expert_route_backward(put(x, torch.float32), ints(ids), put(u, torch.float32), out, scoring="sigmoid", renormalise=renorm)
+    s = 1 / (1 + np.exp(-x))
+    q = 1 / (1 + np.exp(x))
+    rows = np.arange(T)[:, None]
+    p, c = s[rows, ids], q[rows, ids]
+    if renorm:
+        p = p / p.sum(1, keepdims=True)
+        d = p * c * (u - (u * p).sum(1, keepdims=True))
+        size = p * c * (np.abs(u) + (np.abs(u) * p).sum(1, keepdims=True))
+    else:
+        d = p * c * u
+        size = np.abs(d)
+    r, m = np.zeros((T, E)), np.zeros((T, E))
+    r[rows, ids], m[rows, ids] = d, size
+    # (an exponent of up to 60 magnifies the rounding of x log2(e): 60 units more)
+    ref.close(out, r, torch.float32, magnitude=m, n=k + 64)
