@@ -1236,7 +1236,7 @@ LinearArgs args_of(const LinearIn& in)
     LinearArgs a{};
     a.off = in.off; a.slot = in.n_pos > 0 ? in.slot : nullptr; a.x = in.x; a.w = in.w; a.bias = in.bias; a.n_pos = in.n_pos;
     a.n_expert = in.off ? in.n_expert : 1; a.n_in = in.n_in; a.n_out = in.n_out; a.top_k = in.top_k; a.relu = in.relu;
-    while ((2 << a.k_shift) <= in.top_k) ++a.k_shift;
+    while ((int64_t(2) << a.k_shift) <= in.top_k) ++a.k_shift;
     if (in.top_k & (in.top_k - 1)) a.k_mul = (uint32_t)(((uint64_t(1) << (32 + a.k_shift)) + in.top_k - 1) / in.top_k);
     return a;
 }
