@@ -434,7 +434,8 @@ const char* gr_profile_kernel_name(int32_t id);
  * Outputs must not overlap inputs unless it is said.  Indexes on the device are not validated: kernels stay in
  * bounds whatever off, slot, pos and expert hold, and give results only for arrays as gr_expert_plan leaves them.
  * Results do not depend on the order in which workgroups run: the same call gives the same bits.
- * A call whose kernels would have 2^32 threads or more (the results of some tens of gigabytes at the least) is GR_ERR_TOO_LARGE.
+ * A call whose kernels would have 2^32 threads or more (of a layer: 2^24 tiles of 64 by 64 of its results or of its weights' gradient; else
+ * some tens of gigabytes of results at the least) is GR_ERR_TOO_LARGE.
  */
 typedef struct gr_experts gr_experts;
 

@@ -1380,13 +1380,14 @@ void product(gr_experts* h, const LinearIn& in, LinearArgs a, bool tiles, hipStr
     if (parts) join();
 }
 
-// Whether the smallest tiles are more than a launch may have.
-bool too_many_tiles(const LinearIn& in, bool backward)
+// Whether the smallest tiles of results [positions, width], or of weights, are more than a launch may have.
+constexpr int64_t kMostTiles = kMostBlocks - kDies * kTogether;
+
+bool too_many_tiles(const LinearIn& in, int width) { return row_tiles(in, kAnyTile) > kMostTiles / tiles_of(width, kAnyTile); }
+
+bool too_many_weights(const LinearIn& in)
 {
-    const int64_t across = tiles_of(in.n_in > in.n_out ? in.n_in : in.n_out, kAnyTile), experts = in.off ? in.n_expert : 1;
-    const int64_t most = kMostBlocks - kDies * kTogether;
-    return row_tiles(in, kAnyTile) > most / across ||
-           (backward && experts * tiles_of(in.n_in, kAnyTile) * tiles_of(in.n_out, kAnyTile) > most);
+    return (int64_t)(in.off ? in.n_expert : 1) * tiles_of(in.n_in, kAnyTile) * tiles_of(in.n_out, kAnyTile) > kMostTiles;
 }
 
 // dz and db
@@ -1421,7 +1422,7 @@ void unrelu_sums(gr_experts* h, const LinearIn& in, void* dz, void* db, hipStrea
 
 int launch_linear(gr_experts* h, const LinearIn& in, int dtype, void* out_y, hipStream_t s)
 {
-    if (too_many_tiles(in, false)) return GR_ERR_TOO_LARGE;
+    if (too_many_tiles(in, in.n_out)) return GR_ERR_TOO_LARGE;
     LinearArgs a = args_of(in);
     a.out = out_y;
     return by_type(dtype, [&](auto t) {
@@ -1433,7 +1434,7 @@ int launch_linear(gr_experts* h, const LinearIn& in, int dtype, void* out_y, hip
 
 int launch_linear_backward(gr_experts* h, const LinearIn& in, int dtype, void* dz, void* dx, void* dw, void* db, hipStream_t s)
 {
-    if (too_many_tiles(in, true)) return GR_ERR_TOO_LARGE;
+    if ((dx && too_many_tiles(in, in.n_in)) || (dw && too_many_weights(in))) return GR_ERR_TOO_LARGE;
     return by_type(dtype, [&](auto t) {
         typedef decltype(t) T;
         LinearArgs a = args_of(in);

@@ -27,3 +27,37 @@ def test_one_row_for_all_slots(top_k):
     h.gr_expert_linear_backward(put(x, torch.float32), put(w, torch.float32), y, out_dw=dw, **plan)
     _, (rw, mw), _ = ref.linear_backward(x, w, ref.f64(y), off, slot, top_k)
     ref.close(dw, rw, torch.float32, mw, n)
+
+
+def test_many_rows_of_few_features():
+    """What a launch may have is asked of the results' tiles, not of the features that go in."""
+    n, I = (1 << 20) + 1, 65536
+    g = torch.Generator(device=DEV).manual_seed(0)
+    x, w = torch.randn(2, I, generator=g, device=DEV).bfloat16(), torch.randn(1, I, generator=g, device=DEV).bfloat16()
+    h = binding.Experts(1, n, 1)
+    slot = torch.arange(n, dtype=torch.int32, device=DEV)
+    y = empty(n, 1, dtype=torch.bfloat16)
+    h.gr_expert_linear(x, w, y, slot=slot, top_k=1 << 20)
+    want = ref.f64(x) @ ref.f64(w).T
+    size = np.abs(ref.f64(x)) @ np.abs(ref.f64(w)).T
+    ref.close(y[:1], want[:1], torch.bfloat16, size[:1], I)
+    ref.close(y[-1:], want[1:], torch.bfloat16, size[1:], I)
+    assert bool((y[:-1] == y[0]).all())
+    # by weight the features that go in count, in tiles of them alone
+    dw = empty(1, I, dtype=torch.bfloat16)
+    h.gr_expert_linear_backward(x, w, y, out_dw=dw, slot=slot, top_k=1 << 20)
+    first = float(ref.f64(y[:-1]).sum())
+    r = first * ref.f64(x)[0] + float(y[-1]) * ref.f64(x)[1]
+    ref.close(dw[0], r, torch.bfloat16, np.abs(first * ref.f64(x)[0]) + np.abs(float(y[-1]) * ref.f64(x)[1]), n)
+
+
+def test_more_tiles_than_a_launch_may_have():
+    """Results of which there would be more are refused, before anything is read."""
+    n, I = (1 << 24) - 64, 65536
+    h = binding.Experts(1, n, 1)
+    few = empty(8)
+    at, none = few.data_ptr(), None
+    lib, stream = binding.lib(), torch.cuda.current_stream().cuda_stream
+    layer = lambda i, o: lib.gr_expert_linear(h._h, n, i, o, 0, none, at, 1 << 30, at, at, none, 0, at, stream)
+    assert layer(I, I) == -2 and layer(1, I) == -2
+    assert lib.gr_expert_linear_backward(h._h, n, I, 1, 0, none, at, 1 << 30, at, at, none, at, none, at, none, none, stream) == -2
