@@ -388,11 +388,11 @@ __device__ __forceinline__ int64_t uniform(int64_t v)
 // 16 bytes a lane into shared memory at `to` and after, from an address of the lane's own, or from an offset to one of the wave's.
 __device__ __forceinline__ void fetch16(const char* from, uint32_t to)
 {
-    asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" ::"v"(from), "s"(to) : "memory");
+    asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" ::"v"(from), "s"(to) : "memory", "m0");
 }
 __device__ __forceinline__ void fetch16(const char* base, uint32_t offset, uint32_t to)
 {
-    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(offset), "s"(base), "s"(to) : "memory");
+    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(offset), "s"(base), "s"(to) : "memory", "m0");
 }
 
 __device__ __forceinline__ int across_swizzle(int r) { return (r & 3) << 1 | (r >> 3 & 1) << 3; }

@@ -1,0 +1,24 @@
+"""What the kernels' sources have to say to the compiler, and what it has to say of them (CPU only)."""
+import glob
+import os
+import re
+
+from paper_2605_16867_amd import build
+
+
+def _asm_statements():
+    for path in sorted(glob.glob(os.path.join(build.CSRC, "*.hip")) + glob.glob(os.path.join(build.CSRC, "*.h"))):
+        for m in re.finditer(r"\basm\b[^;\"]*\((.*?)\);", open(path).read(), flags=re.S):
+            yield os.path.basename(path), m.group(1)
+
+
+def test_assembly_names_the_registers_it_writes():
+    """A register that a statement writes by name is one that the compiler must not keep anything in."""
+    seen = 0
+    for path, text in _asm_statements():
+        code = "".join(re.findall(r'"((?:[^"\\]|\\.)*)"', text.split("::")[0].split(" : ")[0]))
+        for name in ("m0", "vcc", "exec", "scc"):
+            if re.search(rf"\b[sv]_\w+ {name}\b", code):
+                seen += 1
+                assert f'"{name}"' in text.rsplit(":", 1)[1], (path, text)
+    assert seen >= 2
