@@ -22,3 +22,22 @@ def test_assembly_names_the_registers_it_writes():
                 seen += 1
                 assert f'"{name}"' in text.rsplit(":", 1)[1], (path, text)
     assert seen >= 2
+
+
+def test_assembly_waits_for_scalars_of_the_vector_unit():
+    """A scalar register that the vector unit has written may be read by memory's five wait states later; nothing but the statement itself sees to
+    that where it has both."""
+    seen = 0
+    for path, text in _asm_statements():
+        code = "".join(re.findall(r'"((?:[^"\\]|\\.)*)"', text.split("::")[0]))
+        constraints = re.findall(r'"([^"]*)"\s*\(', text)
+        states = 0
+        for line in code.replace("\\t", "").split("\\n"):
+            if re.match(r"(global|buffer|flat|scratch)_", line):
+                operands = [int(i) for i in re.findall(r"%(\d)", line)]
+                if any(constraints[i] == "s" for i in operands):
+                    seen += 1
+                    assert states >= 5, (path, text)
+            nop = re.match(r"s_nop (\d+)", line)
+            states += int(nop.group(1)) + 1 if nop else 1
+    assert seen >= 1
