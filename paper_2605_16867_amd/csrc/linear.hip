@@ -385,16 +385,16 @@ __device__ __forceinline__ int64_t uniform(int64_t v)
     return (int64_t)((uint64_t)(uint32_t)uniform((int)(v >> 32)) << 32 | (uint32_t)uniform((int)v));
 }
 
-// 16 bytes a lane into shared memory at `to` and after, from an address of the lane's own, or from an offset to one of the wave's.  (That one
-// may come from the vector unit, a spilled register at the least: five wait states before memory's reads it, which the compiler does not add for a
-// statement of this kind.  They cost large layers 0.4 to 0.8 %.)
+// 16 bytes a lane into shared memory at `to` and after (the compiler hands that over in m0), from an address of the lane's own, or from an offset
+// to one of the wave's.  That one may come from the vector unit, a spilled register at the least: five wait states before memory's reads it, which
+// the compiler does not add for a statement of this kind.  Backward, 65 536 x 4 096 -> 1 024, they are 6 us of 1 275.
 __device__ __forceinline__ void fetch16(const char* from, uint32_t to)
 {
-    asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" ::"v"(from), "s"(to) : "memory", "m0");
+    asm volatile("s_nop 0\n\tglobal_load_lds_dwordx4 %0, off" ::"v"(from), "{m0}"(to) : "memory");
 }
 __device__ __forceinline__ void fetch16(const char* base, uint32_t offset, uint32_t to)
 {
-    asm volatile("s_mov_b32 m0, %2\n\ts_nop 3\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(offset), "s"(base), "s"(to) : "memory", "m0");
+    asm volatile("s_nop 4\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(offset), "s"(base), "{m0}"(to) : "memory");
 }
 
 __device__ __forceinline__ int across_swizzle(int r) { return (r & 3) << 1 | (r >> 3 & 1) << 3; }

@@ -12,15 +12,18 @@ def _asm_statements():
             yield os.path.basename(path), m.group(1)
 
 
-def test_assembly_names_the_registers_it_writes():
-    """A register that a statement writes by name is one that the compiler must not keep anything in."""
+def test_assembly_names_its_special_registers():
+    """A register that a statement writes by name is one that the compiler must not keep anything in; a load into shared memory has its place in m0
+    from the compiler or sets it, and says so."""
     seen = 0
     for path, text in _asm_statements():
         code = "".join(re.findall(r'"((?:[^"\\]|\\.)*)"', text.split("::")[0].split(" : ")[0]))
         for name in ("m0", "vcc", "exec", "scc"):
             if re.search(rf"\b[sv]_\w+ {name}\b", code):
-                seen += 1
                 assert f'"{name}"' in text.rsplit(":", 1)[1], (path, text)
+        if "_lds_" in code:
+            seen += 1
+            assert '"{m0}"' in text or '"m0"' in text, (path, text)
     assert seen >= 2
 
 
