@@ -758,9 +758,9 @@ __global__ __launch_bounds__(kWaves * kWave, kSize > 128 ? 1 : 2) void k_linear_
             for (int f = 0; f < 2; ++f) {
                 const int of = wq + (j + f) * 16 + lane / 16 * 4;
                 if (biased && of < t.q_n) {
-                    const Four v = *reinterpret_cast<const Four*>(bias + of);
+                    const Elements<T, 4> v = Elements<T, 4>::load(bias + of);
 #pragma unroll
-                    for (int k = 0; k < 4; ++k) b[f][k] = (float)v[k];
+                    for (int k = 0; k < 4; ++k) b[f][k] = (float)v.v[k];
                 }
             }
             const int col = wq + j * 16 + lane / 16 * 8;

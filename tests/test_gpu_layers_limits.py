@@ -5,7 +5,7 @@ import torch
 
 from paper_2605_16867_amd import binding
 from tests import experts_reference as ref
-from tests.test_gpu_experts import DEV, empty, f64_of, ints, put
+from tests.test_gpu_experts import DEV, TYPES, empty, f64_of, ints, layer, put, shifted
 
 pytestmark = pytest.mark.gpu
 
@@ -61,3 +61,21 @@ def test_more_tiles_than_a_launch_may_have():
     layer = lambda i, o: lib.gr_expert_linear(h._h, n, i, o, 0, none, at, 1 << 30, at, at, none, 0, at, stream)
     assert layer(I, I) == -2 and layer(1, I) == -2
     assert lib.gr_expert_linear_backward(h._h, n, I, 1, 0, none, at, 1 << 30, at, at, none, at, none, at, none, none, stream) == -2
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("n,E,I,O", [(9, 3, 64, 40), (700, 3, 264, 304), (300, 2, 96, 8), (33_000, 2, 40, 2056), (400, 3, 33, 65)])
+@pytest.mark.parametrize("by", [1, 2, 3])
+def test_a_bias_at_any_address(n, E, I, O, by, dtype):
+    """Only the bias off its boundary of 16 bytes: few rows, tiles of 128 and of 256, few features, odd widths."""
+    rng = np.random.default_rng(n + O)
+    off, slot, x, w, b = layer(rng, n, E, I, O, 1, dtype)
+    h = binding.Experts(E, n, 1)
+    y = empty(n, O, dtype=dtype)
+    h.gr_expert_linear(put(x, dtype), put(w, dtype), y, bias=shifted(put(b, dtype), by), off=ints(off), slot=ints(slot), top_k=1)
+    if n * O <= 1 << 20:
+        r, size = ref.linear(x, w, b, off, slot, 1, False, n)
+        ref.close(y, r, dtype, size, I)
+    plain = empty(n, O, dtype=dtype)
+    h.gr_expert_linear(put(x, dtype), put(w, dtype), plain, bias=put(b, dtype), off=ints(off), slot=ints(slot), top_k=1)
+    assert torch.equal(y, plain)
