@@ -998,9 +998,6 @@ struct NarrowShape {
     int lg, across;      // threads across as a power of two; workgroups across
 };
 
-template <typename T>
-__host__ __device__ constexpr int narrow_columns(int n_in) { return n_in < Chunk<T>::n ? 1 : Chunk<T>::n; }
-
 constexpr int kNarrowRows = 64, kNarrowLeast = 8;      // rows of a block, most (they are held in shared memory) and least
 
 // By input: dx[p] = the sum over the features of dz[p, o] * W[o]; a thread keeps its columns of W.
