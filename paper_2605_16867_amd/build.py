@@ -2,7 +2,9 @@
 from __future__ import annotations
 
 import os
+import re
 import subprocess
+import sys
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(_HERE)
@@ -16,15 +18,46 @@ def hipcc_command() -> list:
             "-ffp-contract=off",
             # packed-FP32 instructions stay off: ordinary float code must not be fused into them
             "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
+            "-Rpass-analysis=kernel-resource-usage",      # (what check_spills reads)
             "-I", os.path.join(ROOT, "include"),
             "-o", LIB] + [os.path.join(CSRC, s) for s in SOURCES]
+
+
+# Kernels whose sums are bound to registers behind the compiler's back: with a vector register spilled they are wrong.
+NOTHING_SPILLED = ("k_linear_tiles",)
+
+
+def check_spills(remarks: str) -> None:
+    """Raises where the compiler's remarks say that one of those kernels spills vector registers or uses scratch memory, or say nothing of it."""
+    seen = set()
+    for part in remarks.split("remark: Function Name: ")[1:]:
+        name = part.split()[0]
+        for kernel in NOTHING_SPILLED:
+            if kernel not in name:
+                continue
+            seen.add(kernel)
+            for what in (r"VGPRs Spill", r"ScratchSize \[bytes/lane\]"):
+                m = re.search(what + r": (\d+)", part)
+                if m is None or int(m.group(1)):
+                    raise RuntimeError(f"{name}: {m.group(0) if m else 'no word of ' + what}, and its sums are wrong if any vector register is spilled")
+    if seen != set(NOTHING_SPILLED):
+        raise RuntimeError(f"the compiler said nothing of {sorted(set(NOTHING_SPILLED) - seen)}")
 
 
 def build_library(verbose: bool = False) -> str:
     cmd = hipcc_command()
     if verbose:
         print(" ".join(cmd), flush=True)
-    subprocess.run(cmd, check=True)
+    made = subprocess.run(cmd, stderr=subprocess.PIPE, text=True)
+    # (a remark is a line, the line of source it names, and a mark under that)
+    said = re.sub(r"^.*: remark: .*\[-Rpass-analysis=kernel-resource-usage\]\n(?:^ *\d* \|.*\n)*", "", made.stderr, flags=re.M)
+    sys.stderr.write(said)
+    made.check_returncode()
+    try:
+        check_spills(made.stderr)
+    except RuntimeError:
+        os.remove(LIB)
+        raise
     return LIB
 
 

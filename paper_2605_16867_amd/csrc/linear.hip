@@ -448,8 +448,8 @@ struct Share {
 };
 
 // acc += a * b with the sums where the compiler leaves them alone: there are as many as there are registers of their kind, and it moves them
-// about. For the same reason nothing of a kernel with these may be spilled (-Rpass-analysis=kernel-resource-usage tells): a variant that was gave
-// wrong sums.
+// about. For the same reason no vector register of a kernel with these may be spilled: a variant that had some gave wrong sums, and the build fails
+// where one does. (Scalar registers are, 24 to 96 a kernel, to lanes of vector registers.)
 __device__ __forceinline__ void mfma_in_place(f32x4& acc, bf16x8 a, bf16x8 b)
 {
     asm volatile("v_mfma_f32_16x16x32_bf16 %0, %1, %2, %0" : "+a"(acc) : "v"(a), "v"(b));

@@ -3,6 +3,8 @@ import glob
 import os
 import re
 
+import pytest
+
 from paper_2605_16867_amd import build
 
 
@@ -44,3 +46,22 @@ def test_assembly_waits_for_scalars_of_the_vector_unit():
             nop = re.match(r"s_nop (\d+)", line)
             states += int(nop.group(1)) + 1 if nop else 1
     assert seen >= 1
+
+
+def _remarks(*kernels):
+    text = "linear.hip:20:1: warning: of something else\n"
+    for name, spilled, scratch in kernels:
+        for line in (f"Function Name: {name}", "    VGPRs: 202", f"    ScratchSize [bytes/lane]: {scratch}", "    SGPRs Spill: 96",
+                     f"    VGPRs Spill: {spilled}", "    LDS Size [bytes/block]: 163840"):
+            text += f"linear.hip:479:1: remark: {line} [-Rpass-analysis=kernel-resource-usage]\n  479 | {{\n      | ^\n"
+    return text
+
+
+def test_a_build_with_spilled_sums_fails():
+    tiles, other = "_ZN2gr14k_linear_tilesIDF16bLi256EEEvNS0_10LinearArgsE", "_ZN2gr7k_routeIfEEvNS_9RouteArgsE"
+    build.check_spills(_remarks((other, 4, 16), (tiles, 0, 0), (tiles, 0, 0)))
+    for bad in (((tiles, 0, 0), (tiles, 1, 0)), ((tiles, 0, 8), (other, 0, 0)), ((other, 0, 0),), ()):
+        with pytest.raises(RuntimeError, match="k_linear_tiles"):
+            build.check_spills(_remarks(*bad))
+    with pytest.raises(RuntimeError, match="no word of"):
+        build.check_spills(_remarks((tiles, 0, 0)).replace("VGPRs Spill", "spilled"))
