@@ -92,10 +92,14 @@ class LengthPredictor:
 
     # ---- training -----------------------------------------------------------------------------
 
-    def _loss(self, out, target, like):
-        """Mean squared error of the logarithms, and its gradient in `like`."""
+    def _loss(self, out, target, like, counts=None):
+        """Mean squared error of the logarithms, and its gradient in `like`; of those rows that `counts` says (None: all)."""
         error = out.float().view(-1) - target
-        return (error * error).mean(), (error * (2.0 / error.numel())).to(self.dtype).view_as(like)
+        if counts is None:
+            return (error * error).mean(), (error * (2.0 / error.numel())).to(self.dtype).view_as(like)
+        error = torch.where(counts, error, torch.zeros_like(error))
+        n = counts.sum().clamp(min=1)
+        return (error * error).mean() * (error.numel() / n), (error * (2.0 / n)).to(self.dtype).view_as(like)
 
     def _update(self, parameters: List[torch.Tensor], gradients: List[torch.Tensor], rate: float) -> None:
         self.h.gr_clip_gradients(gradients, self.max_norm, self.norm)
@@ -103,13 +107,13 @@ class LengthPredictor:
             p.add_(g, alpha=-rate)
 
     def train_experts(self, x: torch.Tensor, target: torch.Tensor, expert: torch.Tensor, rate: float) -> torch.Tensor:
-        """A step of the first phase: requests x with logarithms of lengths `target` [rows], each given to expert [rows] (int32).
-        Returns the loss."""
+        """A step of the first phase: requests x with logarithms of lengths `target` [rows], each given to expert [rows] (int32; a request
+        whose expert there is not is left out).  Returns the loss."""
         T = x.shape[0]
         off, slot, h = self.off, self.slot[:T], self.h
         h.gr_expert_plan(expert.view(T, 1), off, slot, self.pos.view(-1)[:T].view(T, 1))
         y = self._experts(x, T, 1)
-        loss, d = self._loss(y, target[slot.long()], self.dy[-1][:T])
+        loss, d = self._loss(y, target[torch.where(slot < 0, -1 - slot, slot).long()], self.dy[-1][:T], counts=slot >= 0)
         for i in range(len(self.w) - 1, -1, -1):
             relu = i < len(self.w) - 1
             source = x if i == 0 else self.y[i - 1][:T]
