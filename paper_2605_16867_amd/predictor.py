@@ -87,8 +87,9 @@ class LengthPredictor:
         return self.out[:T]
 
     def predict(self, x: torch.Tensor, max_len: int) -> torch.Tensor:
-        """Predicted decode lengths, int32 [rows], in [1, max_len]."""
-        return self.forward(x).float().exp_().round_().clamp_(1, max_len).to(torch.int32).view(-1)
+        """Predicted decode lengths, int32 [rows], in [1, max_len]; max_len where a result is no number."""
+        n = self.forward(x).float().exp_().round_().double()      # (single precision has no room for every max_len)
+        return n.nan_to_num_(nan=max_len).clamp_(1, max_len).to(torch.int32).view(-1)
 
     # ---- training -----------------------------------------------------------------------------
 

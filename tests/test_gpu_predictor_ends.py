@@ -29,3 +29,14 @@ def test_requests_of_no_expert_are_left_out(dtype):
     loss, norm, moved = trained(x, target, torch.full_like(kind, -1))
     start = predictor.LengthPredictor(24, n_expert=4, hidden=(16, 16, 8), router_hidden=8, max_rows=200, dtype=dtype)
     assert loss == 0 and norm == 0 and all(torch.equal(a, b) for a, b in zip(moved, start.w + start.b))
+
+
+@pytest.mark.parametrize("max_len", [1, 4096, (1 << 24) + 1, (1 << 31) - 1])
+@pytest.mark.parametrize("bias,least", [(float("nan"), False), (float("inf"), False), (80.0, False), (float("-inf"), True)])
+def test_lengths_are_in_their_range(bias, least, max_len):
+    """Whatever the experts come to; what is no number is taken for the longest."""
+    p = predictor.LengthPredictor(24, n_expert=4, hidden=(16, 16, 8), router_hidden=8, max_rows=50)
+    p.b[-1].fill_(bias)
+    x, _, _ = predictor.synthetic_requests(50, 24, 4, seed=5)
+    n = p.predict(x, max_len)
+    assert n.dtype == torch.int32 and n.tolist() == [1 if least else max_len] * 50
