@@ -548,8 +548,8 @@ int gr_expert_combine_backward(gr_experts* h, int64_t n_rows, int32_t top_k, int
 
 /*
  * Clipping by the global norm: norm = the root of the sum of the squares of all elements of all gradients;
- * out_i = grad_i * min(1, max_norm / norm).  Gradients are given out as they are where the norm is not finite
- * (out_norm says so).  Squares are summed in double precision.
+ * out_i = grad_i * min(1, max_norm / norm).  Gradients are given out as they are where the norm is not finite.  Squares are
+ * summed and the norm is held in double precision: one past single precision clips as any other, and out_norm is infinite.
  *   grad, out HOST arrays of n_grad DEVICE pointers (read during the call); out[i] may be grad[i], NULL for an empty one
  *   count     HOST int64[n_grad], >= 0, at most 2^40
  *   dtype     HOST int32[n_grad], of gradient and output alike

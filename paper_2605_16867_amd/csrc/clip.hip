@@ -77,8 +77,9 @@ __device__ __forceinline__ double squares_of(const Piece& p)
     return sum;
 }
 
-template <typename T>
-__device__ __forceinline__ void scale(const Piece& p, float by)
+// `by`(an element) of each.
+template <typename T, typename F>
+__device__ __forceinline__ void scale(const Piece& p, F by)
 {
     typedef typename Chunk<T>::Vec Vec;
     const T* const g = reinterpret_cast<const T*>(p.grad);
@@ -87,10 +88,10 @@ __device__ __forceinline__ void scale(const Piece& p, float by)
             [&](int i) {
                 Vec v = reinterpret_cast<const Vec*>(g)[i];
 #pragma unroll
-                for (int j = 0; j < Chunk<T>::n; ++j) v[j] = (T)((float)v[j] * by);
+                for (int j = 0; j < Chunk<T>::n; ++j) v[j] = (T)by((float)v[j]);
                 reinterpret_cast<Vec*>(o)[i] = v;
             },
-            [&](int i) { o[i] = (T)((float)g[i] * by); });
+            [&](int i) { o[i] = (T)by((float)g[i]); });
 }
 
 // The workgroup's sum, in thread 0.
@@ -110,7 +111,8 @@ __device__ __forceinline__ double squares_of(const Piece& p, int)
     return p.type == GR_F32 ? squares_of<float>(p) : p.type == GR_BF16 ? squares_of<bf16>(p) : squares_of<f16>(p);
 }
 
-__device__ __forceinline__ void scale(const Piece& p, float by, int)
+template <typename F>
+__device__ __forceinline__ void scale(const Piece& p, F by, int)
 {
     if (p.type == GR_F32) scale<float>(p, by);
     else if (p.type == GR_BF16) scale<bf16>(p, by);
@@ -118,9 +120,20 @@ __device__ __forceinline__ void scale(const Piece& p, float by, int)
 }
 
 // What gradients are multiplied by.
-__device__ __forceinline__ float factor(double norm, double max_norm)
+__device__ __forceinline__ double factor(double norm, double max_norm)
 {
-    return norm > max_norm && norm < __builtin_inf() ? (float)(max_norm / norm) : 1.0f;
+    return norm > max_norm && norm < __builtin_inf() ? max_norm / norm : 1.0;
+}
+
+// A factor that single precision holds whole is one of single precision; with a smaller one (gradients near the end of their range, clipped to
+// little) products are in double precision, as the results may well be whole.
+constexpr float kLeastFactor = 0x1p-126f;
+
+__device__ __forceinline__ void scale(const Piece& p, double by)
+{
+    const float f = (float)by;
+    if (f >= kLeastFactor || by == 0) scale(p, [f](float v) { return v * f; }, 0);
+    else scale(p, [by](float v) { return (float)((double)v * by); }, 0);
 }
 
 __global__ __launch_bounds__(kBlock) void k_norm(ClipTable t, double* squares)
@@ -136,7 +149,7 @@ __global__ __launch_bounds__(kBlock) void k_norm(ClipTable t, double* squares)
 
 __global__ __launch_bounds__(kBlock) void k_clip(ClipTable t, const double* squares, int parts, double max_norm, float* norm)
 {
-    __shared__ float by;
+    __shared__ double by;
     double sum = 0;
     for (int i = threadIdx.x; i < parts; i += kBlock) sum += squares[i];
     sum = block_sum<kBlock>(sum);
@@ -146,18 +159,18 @@ __global__ __launch_bounds__(kBlock) void k_clip(ClipTable t, const double* squa
         if (norm && blockIdx.x == 0) *norm = (float)all;
     }
     __syncthreads();
-    const float f = by;
+    const double f = by;
     for (int at = blockIdx.x; at < t.pieces_before[t.n]; at += gridDim.x) {
         const Piece p = piece_of(t, at);
-        if (f == 1.0f && p.grad == p.out) continue;
-        scale(p, f, 0);
+        if ((float)f == 1.0f && p.grad == p.out) continue;
+        scale(p, f);
     }
 }
 
 // Little enough that every workgroup reads all of it, and one launch does: the same sum in each, and a share of the pieces.
 __global__ __launch_bounds__(kFewThreads) void k_clip_few(ClipTable t, double max_norm, float* norm)
 {
-    __shared__ float by;
+    __shared__ double by;
     double sum = 0;
     for (int i = 0; i < t.n; ++i) {
         const int type = (int)(t.count_type[i] & 3);
@@ -170,8 +183,8 @@ __global__ __launch_bounds__(kFewThreads) void k_clip_few(ClipTable t, double ma
         if (norm && blockIdx.x == 0) *norm = (float)all;
     }
     __syncthreads();
-    const float f = by;
-    for (int at = blockIdx.x; at < t.pieces_before[t.n]; at += gridDim.x) scale(piece_of(t, at), f, 0);
+    const double f = by;
+    for (int at = blockIdx.x; at < t.pieces_before[t.n]; at += gridDim.x) scale(piece_of(t, at), f);
 }
 
 }  // namespace
