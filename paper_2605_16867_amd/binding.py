@@ -415,7 +415,8 @@ class Experts:
     """Owns a gr_experts handle on the current device: the workspace of a length predictor's operators.
 
     Shapes are taken from the tensors: logits [rows, experts], choices and weights [rows, top_k], x [rows or positions, n_in], w [experts,
-    n_out, n_in], y [positions, n_out]; all contiguous, x, w and y of one type."""
+    n_out, n_in], y [positions, n_out]; all contiguous and on the handle's device, which has to be the current one; x, w and y of one type.
+    Outputs are tensors of the caller's, and nothing is recorded for torch's automatic differentiation: a gradient is a call of its own."""
 
     def __init__(self, n_expert: int, max_rows: int, max_top_k: int):
         self._h, self._at = C.c_void_p(), None
@@ -424,7 +425,9 @@ class Experts:
             self._m = _Unclear
         self.n_expert = int(n_expert)
         _check(lib().gr_experts_create(C.byref(self._h), self.n_expert, int(max_rows), int(max_top_k)), "gr_experts_create")
-        self._at = self._h.value
+        import torch
+        self._device = torch.cuda.current_device()
+        self._at = (self._h.value, self._device)
 
     def close(self) -> None:
         if self._h:
@@ -437,6 +440,17 @@ class Experts:
         except Exception:
             pass
 
+    def _dev(self, t, dtype, name: str, n: Optional[int] = None):
+        if t is not None and t.is_cuda and t.device.index != self._device:
+            raise ValueError(f"{name}: on {t.device}, need the handle's device, cuda:{self._device}")
+        return _dev(t, dtype, name, n)
+
+    def _stream(self):
+        import torch
+        if torch.cuda.current_device() != self._device:
+            raise ValueError(f"the current device is cuda:{torch.cuda.current_device()}, need the handle's, cuda:{self._device}")
+        return _stream()
+
     @staticmethod
     def _shape(t, name, *shape):
         """A tensor's shape, as far as it is asked for (None: any)."""
@@ -447,7 +461,7 @@ class Experts:
     def _plan(self, n, off, slot, pos):
         import torch
         i32 = torch.int32
-        return _dev(off, i32, "out_off", self.n_expert + 1), _dev(slot, i32, "out_slot", n), _dev(pos, i32, "out_pos", n)
+        return self._dev(off, i32, "out_off", self.n_expert + 1), self._dev(slot, i32, "out_slot", n), self._dev(pos, i32, "out_pos", n)
 
     def gr_expert_route(self, logits, out_weight, out_expert, out_off=None, out_slot=None, out_pos=None, bias=None,
                         scoring="softmax", n_group=1, n_group_kept=1, renormalise=False, scale=1.0) -> None:
@@ -459,10 +473,10 @@ class Experts:
         T, _ = self._shape(logits, "logits", None, self.n_expert)
         _, k = self._shape(out_expert, "out_expert", T, None)
         _check(lib().gr_expert_route(
-            self._h, T, k, _dev(logits, logits.dtype, "logits"), _dtype(logits, "logits"),
-            _dev(bias, torch.float32, "bias", self.n_expert), _SCORING[scoring], int(n_group), int(n_group_kept), int(renormalise),
-            float(scale), _dev(out_weight, torch.float32, "out_weight", T * k), _dev(out_expert, torch.int32, "out_expert"),
-            *self._plan(T * k, out_off, out_slot, out_pos), _stream()), "gr_expert_route")
+            self._h, T, k, self._dev(logits, logits.dtype, "logits"), _dtype(logits, "logits"),
+            self._dev(bias, torch.float32, "bias", self.n_expert), _SCORING[scoring], int(n_group), int(n_group_kept), int(renormalise),
+            float(scale), self._dev(out_weight, torch.float32, "out_weight", T * k), self._dev(out_expert, torch.int32, "out_expert"),
+            *self._plan(T * k, out_off, out_slot, out_pos), self._stream()), "gr_expert_route")
 
     def gr_expert_route_backward(self, logits, expert, dweight, out_dlogits, scoring="softmax", renormalise=False, scale=1.0) -> None:
         rc = self._m.expert_route_backward(self._at, self.n_expert, logits, expert, dweight, out_dlogits, _SCORING[scoring], renormalise,
@@ -473,9 +487,9 @@ class Experts:
         T, E = self._shape(logits, "logits", None, self.n_expert)
         _, k = self._shape(expert, "expert", T, None)
         _check(lib().gr_expert_route_backward(
-            self._h, T, k, _dev(logits, logits.dtype, "logits"), _dtype(logits, "logits"), _SCORING[scoring], int(renormalise),
-            float(scale), _dev(expert, torch.int32, "expert"), _dev(dweight, torch.float32, "dweight", T * k),
-            _dev(out_dlogits, logits.dtype, "out_dlogits", T * E), _stream()), "gr_expert_route_backward")
+            self._h, T, k, self._dev(logits, logits.dtype, "logits"), _dtype(logits, "logits"), _SCORING[scoring], int(renormalise),
+            float(scale), self._dev(expert, torch.int32, "expert"), self._dev(dweight, torch.float32, "dweight", T * k),
+            self._dev(out_dlogits, logits.dtype, "out_dlogits", T * E), self._stream()), "gr_expert_route_backward")
 
     def gr_expert_plan(self, expert, out_off, out_slot, out_pos) -> None:
         rc = self._m.expert_plan(self._at, self.n_expert, expert, out_off, out_slot, out_pos)
@@ -483,8 +497,8 @@ class Experts:
             return _done(rc, "gr_expert_plan")
         import torch
         T, k = self._shape(expert, "expert", None, None)
-        _check(lib().gr_expert_plan(self._h, T, k, _dev(expert, torch.int32, "expert"), *self._plan(T * k, out_off, out_slot, out_pos),
-                                    _stream()), "gr_expert_plan")
+        _check(lib().gr_expert_plan(self._h, T, k, self._dev(expert, torch.int32, "expert"), *self._plan(T * k, out_off, out_slot, out_pos),
+                                    self._stream()), "gr_expert_plan")
 
     def _layer(self, x, w, off, slot, top_k, n):
         """Arguments that a layer's forward and backward share, from `off` to `w`, behind the sizes."""
@@ -493,8 +507,8 @@ class Experts:
         _, O, I = self._shape(w, "w", E, None, None) if w.dim() == 3 or off is not None else (1, *self._shape(w, "w", None, None))
         self._shape(x, "x", (n + top_k - 1) // top_k if slot is not None else n, I)
         i32 = torch.int32
-        return E, I, O, (n, I, O, _dtype(x, "x"), _dev(off, i32, "off", self.n_expert + 1), _dev(slot, i32, "slot", n), int(top_k),
-                         _dev(x, x.dtype, "x"), _dev(w, x.dtype, "w"))
+        return E, I, O, (n, I, O, _dtype(x, "x"), self._dev(off, i32, "off", self.n_expert + 1), self._dev(slot, i32, "slot", n), int(top_k),
+                         self._dev(x, x.dtype, "x"), self._dev(w, x.dtype, "w"))
 
     def gr_expert_linear(self, x, w, out_y, bias=None, off=None, slot=None, top_k=1, relu=False) -> None:
         rc = self._m.expert_linear(self._at, self.n_expert, x, w, out_y, bias, off, slot, top_k, relu)
@@ -502,8 +516,8 @@ class Experts:
             return _done(rc, "gr_expert_linear")
         n, O = self._shape(out_y, "out_y", None, w.shape[-2])
         E, I, O, layer = self._layer(x, w, off, slot, int(top_k), n)
-        _check(lib().gr_expert_linear(self._h, *layer, _dev(bias, x.dtype, "bias", E * O), int(relu), _dev(out_y, x.dtype, "out_y"),
-                                      _stream()), "gr_expert_linear")
+        _check(lib().gr_expert_linear(self._h, *layer, self._dev(bias, x.dtype, "bias", E * O), int(relu), self._dev(out_y, x.dtype, "out_y"),
+                                      self._stream()), "gr_expert_linear")
 
     def gr_expert_linear_backward(self, x, w, dy, out_dx=None, out_dw=None, out_db=None, y=None, out_dz=None, off=None,
                                   slot=None, top_k=1) -> None:
@@ -514,8 +528,8 @@ class Experts:
         E, I, O, layer = self._layer(x, w, off, slot, int(top_k), n)
         t = x.dtype
         _check(lib().gr_expert_linear_backward(
-            self._h, *layer, _dev(y, t, "y", n * O), _dev(dy, t, "dy"), _dev(out_dz, t, "out_dz", n * O),
-            _dev(out_dx, t, "out_dx", n * I), _dev(out_dw, t, "out_dw", E * O * I), _dev(out_db, t, "out_db", E * O), _stream()),
+            self._h, *layer, self._dev(y, t, "y", n * O), self._dev(dy, t, "dy"), self._dev(out_dz, t, "out_dz", n * O),
+            self._dev(out_dx, t, "out_dx", n * I), self._dev(out_dw, t, "out_dw", E * O * I), self._dev(out_db, t, "out_db", E * O), self._stream()),
             "gr_expert_linear_backward")
 
     def gr_expert_combine(self, y, pos, out, weight=None) -> None:
@@ -525,9 +539,9 @@ class Experts:
         import torch
         T, k = self._shape(pos, "pos", None, None)
         _, O = self._shape(out, "out", T, None)
-        _check(lib().gr_expert_combine(self._h, T, k, O, _dtype(out, "out"), _dev(weight, torch.float32, "weight", T * k),
-                                       _dev(pos, torch.int32, "pos"), _dev(y, out.dtype, "y", T * k * O), _dev(out, out.dtype, "out"),
-                                       _stream()), "gr_expert_combine")
+        _check(lib().gr_expert_combine(self._h, T, k, O, _dtype(out, "out"), self._dev(weight, torch.float32, "weight", T * k),
+                                       self._dev(pos, torch.int32, "pos"), self._dev(y, out.dtype, "y", T * k * O), self._dev(out, out.dtype, "out"),
+                                       self._stream()), "gr_expert_combine")
 
     def gr_expert_combine_backward(self, dout, y, slot, out_dy=None, weight=None, out_dweight=None) -> None:
         rc = self._m.expert_combine_backward(self._at, dout, y, slot, out_dy, weight, out_dweight)
@@ -540,9 +554,9 @@ class Experts:
         S = slot.numel()
         t, f32 = dout.dtype, torch.float32
         _check(lib().gr_expert_combine_backward(
-            self._h, T, S // T if T else 1, O, _dtype(dout, "dout"), _dev(weight, f32, "weight", S), _dev(slot, torch.int32, "slot"),
-            _dev(y, t, "y", S * O), _dev(dout, t, "dout"), _dev(out_dy, t, "out_dy", S * O),
-            _dev(out_dweight, f32, "out_dweight", S), _stream()), "gr_expert_combine_backward")
+            self._h, T, S // T if T else 1, O, _dtype(dout, "dout"), self._dev(weight, f32, "weight", S), self._dev(slot, torch.int32, "slot"),
+            self._dev(y, t, "y", S * O), self._dev(dout, t, "dout"), self._dev(out_dy, t, "out_dy", S * O),
+            self._dev(out_dweight, f32, "out_dweight", S), self._stream()), "gr_expert_combine_backward")
 
     def gr_clip_gradients(self, grads, max_norm, out_norm=None, out=None) -> None:
         """grads: a list of tensors, scaled in place unless `out` names as many others."""
@@ -555,7 +569,7 @@ class Experts:
         if len(out) != n:
             raise ValueError(f"out: {len(out)} tensors, need {n}")
         _check(lib().gr_clip_gradients(
-            self._h, n, (C.c_void_p * n)(*[_dev(g, g.dtype, "grads") for g in grads]),
-            (C.c_void_p * n)(*[_dev(o, g.dtype, "out", g.numel()) for o, g in zip(out, grads)]),
+            self._h, n, (C.c_void_p * n)(*[self._dev(g, g.dtype, "grads") for g in grads]),
+            (C.c_void_p * n)(*[self._dev(o, g.dtype, "out", g.numel()) for o, g in zip(out, grads)]),
             (C.c_int64 * n)(*[g.numel() for g in grads]), (C.c_int32 * n)(*[_dtype(g, "grads") for g in grads]),
-            float(max_norm), _dev(out_norm, torch.float32, "out_norm", 1), _stream()), "gr_clip_gradients")
+            float(max_norm), self._dev(out_norm, torch.float32, "out_norm", 1), self._stream()), "gr_clip_gradients")

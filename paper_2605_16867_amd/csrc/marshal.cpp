@@ -9,6 +9,7 @@
 #include <Python.h>
 
 #include <ATen/core/TensorBase.h>
+#include <c10/hip/HIPFunctions.h>
 #include <c10/hip/HIPStream.h>
 #include <torch/csrc/autograd/python_variable.h>
 
@@ -231,13 +232,23 @@ PyObject* risk_scan(PyObject* const* a)
                 target, slack, n_flagged, stream());
 }
 
-// ---- the calls of a length predictor: None is returned, and nothing called, where an argument is not plainly right
+// ---- the calls of a length predictor: None is returned, and nothing called, where an argument is not plainly right,
+//      a tensor on another device than the current one and the handle's among them
+
+int64_t here = 0;      // torch's current device, during a call (under the interpreter's lock until the library is called)
+
+template <Py_ssize_t kArgs, PyObject* (*kCall)(PyObject* const*)>
+PyObject* on_one_device(PyObject* self, PyObject* const* a, Py_ssize_t n)
+{
+    here = c10::hip::current_device();
+    return guarded<kArgs, kCall>(self, a, n);
+}
 
 const at::TensorBase& plain(PyObject* o, int64_t dims = kAny)
 {
     if (!THPVariable_CheckExact(o)) throw Unclear{};
     const at::TensorBase& t = THPVariable_Unpack(o);
-    if (!t.is_cuda() || !t.is_contiguous() || (dims != kAny && t.dim() != dims)) throw Unclear{};
+    if (!t.is_cuda() || t.get_device() != here || !t.is_contiguous() || (dims != kAny && t.dim() != dims)) throw Unclear{};
     return t;
 }
 
@@ -278,6 +289,14 @@ float real(PyObject* o)
     return (float)v;
 }
 
+// A handle's address and device, in a pair; None: null.
+void* workspace(PyObject* o)
+{
+    if (o == Py_None) return nullptr;
+    must(PyTuple_CheckExact(o) && PyTuple_GET_SIZE(o) == 2 && integer(PyTuple_GET_ITEM(o, 1)) == here);
+    return handle(PyTuple_GET_ITEM(o, 0));
+}
+
 // n_expert, logits, out_weight, out_expert, out_off, out_slot, out_pos, bias, scoring, n_group, n_group_kept, renormalise, scale
 PyObject* expert_route(PyObject* const* a)
 {
@@ -285,7 +304,7 @@ PyObject* expert_route(PyObject* const* a)
     const at::TensorBase &x = plain(a[2], 2), &e = plain(a[4], 2);
     const int64_t T = x.size(0), k = e.size(1), S = T * k;
     must(x.size(1) == E && e.size(0) == T && k <= INT32_MAX);
-    return call(entries.expert_route, handle(a[0]), T, (int32_t)k, (const void*)x.data_ptr(), type_code(x), (const void*)plain(a[8], at::kFloat, E),
+    return call(entries.expert_route, workspace(a[0]), T, (int32_t)k, (const void*)x.data_ptr(), type_code(x), (const void*)plain(a[8], at::kFloat, E),
                 small(a[9]), small(a[10]), small(a[11]), small(a[12]), real(a[13]), plain(a[3], at::kFloat, S), plain(a[4], at::kInt, S),
                 plain(a[5], at::kInt, E + 1), plain(a[6], at::kInt, S), plain(a[7], at::kInt, S), stream());
 }
@@ -296,7 +315,7 @@ PyObject* expert_route_backward(PyObject* const* a)
     const at::TensorBase &x = plain(a[2], 2), &e = plain(a[3], 2);
     const int64_t T = x.size(0), k = e.size(1);
     must(x.size(1) == integer(a[1]) && e.size(0) == T && k <= INT32_MAX);
-    return call(entries.expert_route_backward, handle(a[0]), T, (int32_t)k, (const void*)x.data_ptr(), type_code(x), small(a[6]), small(a[7]), real(a[8]),
+    return call(entries.expert_route_backward, workspace(a[0]), T, (int32_t)k, (const void*)x.data_ptr(), type_code(x), small(a[6]), small(a[7]), real(a[8]),
                 (const void*)plain(a[3], at::kInt, T * k), (const void*)plain(a[4], at::kFloat, T * k), plain(a[5], x.scalar_type(), x.numel()), stream());
 }
 
@@ -305,7 +324,7 @@ PyObject* expert_plan(PyObject* const* a)
 {
     const at::TensorBase& e = plain(a[2], 2);
     must(e.size(1) <= INT32_MAX);
-    return call(entries.expert_plan, handle(a[0]), (int64_t)e.size(0), (int32_t)e.size(1), (const void*)plain(a[2], at::kInt, 0),
+    return call(entries.expert_plan, workspace(a[0]), (int64_t)e.size(0), (int32_t)e.size(1), (const void*)plain(a[2], at::kInt, 0),
                 plain(a[3], at::kInt, integer(a[1]) + 1), plain(a[4], at::kInt, e.numel()), plain(a[5], at::kInt, e.numel()), stream());
 }
 
@@ -342,7 +361,7 @@ struct Layer {
 PyObject* expert_linear(PyObject* const* a)
 {
     const Layer l(a[1], a[2], a[3], a[4], a[6], a[7], a[8]);
-    return call(entries.expert_linear, handle(a[0]), l.n, l.I, l.O, l.type, l.off, l.slot, l.top_k, l.x, l.w, (const void*)plain(a[5], l.scalar, l.E * l.O),
+    return call(entries.expert_linear, workspace(a[0]), l.n, l.I, l.O, l.type, l.off, l.slot, l.top_k, l.x, l.w, (const void*)plain(a[5], l.scalar, l.E * l.O),
                 small(a[9]), plain(a[4], l.scalar, l.n * l.O), stream());
 }
 
@@ -351,7 +370,7 @@ PyObject* expert_linear_backward(PyObject* const* a)
 {
     const Layer l(a[1], a[2], a[3], a[4], a[10], a[11], a[12]);
     const int64_t of_y = l.n * l.O;
-    return call(entries.expert_linear_backward, handle(a[0]), l.n, l.I, l.O, l.type, l.off, l.slot, l.top_k, l.x, l.w, (const void*)plain(a[8], l.scalar, of_y),
+    return call(entries.expert_linear_backward, workspace(a[0]), l.n, l.I, l.O, l.type, l.off, l.slot, l.top_k, l.x, l.w, (const void*)plain(a[8], l.scalar, of_y),
                 (const void*)plain(a[4], l.scalar, of_y), plain(a[9], l.scalar, of_y), plain(a[5], l.scalar, l.n * l.I),
                 plain(a[6], l.scalar, l.E * l.O * l.I), plain(a[7], l.scalar, l.E * l.O), stream());
 }
@@ -362,7 +381,7 @@ PyObject* expert_combine(PyObject* const* a)
     const at::TensorBase &pos = plain(a[2], 2), &out = plain(a[3], 2);
     const int64_t T = pos.size(0), S = pos.numel(), O = out.size(1);
     must(out.size(0) == T && O <= INT32_MAX && pos.size(1) <= INT32_MAX);
-    return call(entries.expert_combine, handle(a[0]), T, (int32_t)pos.size(1), (int32_t)O, type_code(out), (const void*)plain(a[4], at::kFloat, S),
+    return call(entries.expert_combine, workspace(a[0]), T, (int32_t)pos.size(1), (int32_t)O, type_code(out), (const void*)plain(a[4], at::kFloat, S),
                 (const void*)plain(a[2], at::kInt, S), (const void*)plain(a[1], out.scalar_type(), S * O), out.data_ptr(), stream());
 }
 
@@ -372,7 +391,7 @@ PyObject* expert_combine_backward(PyObject* const* a)
     const at::TensorBase &d = plain(a[1], 2), &slot = plain(a[3]);
     const int64_t T = d.size(0), O = d.size(1), S = slot.numel();
     must(T > 0 && S % T == 0 && S / T <= INT32_MAX && O <= INT32_MAX);
-    return call(entries.expert_combine_backward, handle(a[0]), T, (int32_t)(S / T), (int32_t)O, type_code(d), (const void*)plain(a[5], at::kFloat, S),
+    return call(entries.expert_combine_backward, workspace(a[0]), T, (int32_t)(S / T), (int32_t)O, type_code(d), (const void*)plain(a[5], at::kFloat, S),
                 (const void*)plain(a[3], at::kInt, S), (const void*)plain(a[2], d.scalar_type(), S * O), (const void*)d.data_ptr(),
                 plain(a[4], d.scalar_type(), S * O), plain(a[6], at::kFloat, S), stream());
 }
@@ -395,7 +414,7 @@ PyObject* clip_gradients(PyObject* const* a)
         must(PyList_GET_ITEM(a[4], i) != Py_None);
         out[i] = plain(PyList_GET_ITEM(a[4], i), g.scalar_type(), count[i]);
     }
-    return call(entries.clip_gradients, handle(a[0]), (int32_t)n, (const void* const*)grad.data(), (void* const*)out.data(), (const int64_t*)count.data(),
+    return call(entries.clip_gradients, workspace(a[0]), (int32_t)n, (const void* const*)grad.data(), (void* const*)out.data(), (const int64_t*)count.data(),
                 (const int32_t*)type.data(), real(a[2]), plain(a[3], at::kFloat, 1), stream());
 }
 
@@ -410,11 +429,12 @@ PyObject* connect(PyObject* const* a)
 }
 
 #define GR_METHOD(name, n) {#name, (PyCFunction)(void (*)(void))guarded<n, name>, METH_FASTCALL, nullptr}
+#define GR_METHOD_HERE(name, n) {#name, (PyCFunction)(void (*)(void))on_one_device<n, name>, METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {GR_METHOD(build_status, 13), GR_METHOD(score_route, 10), GR_METHOD(score_route_noalloc, 8),
                          GR_METHOD(score_route_cached, 13), GR_METHOD(route_feedback, 9), GR_METHOD(risk_scan, 15),
-                         GR_METHOD(expert_route, 14), GR_METHOD(expert_route_backward, 9), GR_METHOD(expert_plan, 6),
-                         GR_METHOD(expert_linear, 10), GR_METHOD(expert_linear_backward, 13), GR_METHOD(expert_combine, 5),
-                         GR_METHOD(expert_combine_backward, 7), GR_METHOD(clip_gradients, 5),
+                         GR_METHOD_HERE(expert_route, 14), GR_METHOD_HERE(expert_route_backward, 9), GR_METHOD_HERE(expert_plan, 6),
+                         GR_METHOD_HERE(expert_linear, 10), GR_METHOD_HERE(expert_linear_backward, 13), GR_METHOD_HERE(expert_combine, 5),
+                         GR_METHOD_HERE(expert_combine_backward, 7), GR_METHOD_HERE(clip_gradients, 5),
                          GR_METHOD(connect, 15), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "marshal", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
