@@ -505,7 +505,7 @@ class Experts:
         import torch
         E = 1 if off is None else self.n_expert
         _, O, I = self._shape(w, "w", E, None, None) if w.dim() == 3 or off is not None else (1, *self._shape(w, "w", None, None))
-        self._shape(x, "x", (n + top_k - 1) // top_k if slot is not None else n, I)
+        self._shape(x, "x", n if slot is None else (n + top_k - 1) // top_k if top_k > 0 else None, I)
         i32 = torch.int32
         return E, I, O, (n, I, O, _dtype(x, "x"), self._dev(off, i32, "off", self.n_expert + 1), self._dev(slot, i32, "slot", n), int(top_k),
                          self._dev(x, x.dtype, "x"), self._dev(w, x.dtype, "w"))

@@ -59,3 +59,18 @@ def test_a_handle_of_another_device_is_refused(native, monkeypatch):
     for call in calls:
         with pytest.raises(binding.GoodRouteError):
             call()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("native", [True, False])
+def test_slots_without_a_row_are_the_librarys_to_refuse(native, monkeypatch):
+    if not native:
+        monkeypatch.setattr(binding, "_marshal", binding._Ctypes)
+    h = binding.Experts(2, 8, 1)
+    x, w, y, slot = (torch.zeros(*s, device="cuda:0") for s in ((8, 4), (4, 4), (8, 4), (8,)))
+    for top_k in (0, -1):
+        for call in (lambda: h.gr_expert_linear(x, w, y, slot=slot.int(), top_k=top_k),
+                     lambda: h.gr_expert_linear_backward(x, w, y, out_dx=torch.zeros_like(x), slot=slot.int(), top_k=top_k)):
+            with pytest.raises(binding.GoodRouteError) as e:
+                call()
+            assert e.value.code == -1
