@@ -417,7 +417,7 @@ struct RouteBackArgs {
 //   softmax, renormalised  for chosen i: s_i / S (g_i - sum g s / S), S = the sum of s over c; 0 elsewhere (the other shares cancel)
 //   sigmoid                the same two with another factor 1 - s_i, without the sum where nothing is renormalised
 // Scores are computed again from the logits: reading them back would be as many bytes more.  Bound by memory and a launch: 65 536 rows of 64 in
-// single precision, 38 MB with the choices, 10.2 us (3.7 TB/s).  What is chosen goes by expert through shared memory, as a mark and a gradient
+// single precision, 38 MB with the choices, 10.9 us (3.5 TB/s).  What is chosen goes by expert through shared memory, as a mark and a gradient
 // each.
 template <typename T, bool kSigmoid>
 __global__ __launch_bounds__(kBlock) void k_route_back(RouteBackArgs a)

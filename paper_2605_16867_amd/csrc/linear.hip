@@ -366,12 +366,12 @@ __global__ __launch_bounds__(kBlock) void k_linear_any(LinearArgs a)
 // within a line of the tile is exclusive-ored with one made of the line's, so that the lanes of a read meet no bank twice.
 //
 // Bound by the matrix units and, with them, by power: 131 072 positions of nine experts x 4 096 -> 1 024 in bfloat16 (1.1 TFLOP) forward 880 to
-// 930 us (up to 1 250 TFLOP/s; the library's plain product of one such matrix 874), where the units are busy 62 % of the time at 1.87 GHz. Tiles
+// 930 us (up to 1 250 TFLOP/s; the library's plain product of one such matrix 874), where the units are busy 59 % of the time at 1.89 GHz. Tiles
 // of 256 by 256 because a fragment read from shared memory then serves eight products of a wave (at 128 by 128 four) and each operand is fetched
 // half as often; the sums of a wave's 128 by 128 take half of all registers. Five slots of an operand's slice, 32 KB each, are all the shared
-// memory there is. By input 65 536 x 4 096 <- 1 024 540 us (1 018 TFLOP/s, units busy 45 %: a tile is 16 slices, and writing it, 128 KB from each
+// memory there is. By input 65 536 x 4 096 <- 1 024 540 us (1 018 TFLOP/s, units busy 44 %: a tile is 16 slices, and writing it, 128 KB from each
 // unit at the same time, holds up the loads behind it); by weight 670 us (820), of 128 by 128 (2 304 tiles on 512 places: 4.5 rounds, units busy
-// 36 %: loads into shared memory, 32 KB a slice, take as long as its products; of 256, 576 on 256, 2.25 rounds, it takes 780).
+// 35 %: loads into shared memory, 32 KB a slice, take as long as its products; of 256, 576 on 256, 2.25 rounds, it takes 780).
 
 constexpr int kSlots = 5, kWaves = 4;
 
