@@ -82,3 +82,37 @@ def test_gradient_of_sigmoids_near_one(renorm):
     r[rows, ids], m[rows, ids] = d, size
     # (an exponent of up to 60 magnifies the rounding of x log2(e): 60 units more)
     ref.close(out, r, torch.float32, magnitude=m, n=k + 64)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("scoring", ["softmax", "sigmoid"])
+@pytest.mark.parametrize("with_bias", [False, True])
+def test_masks_of_the_types_lowest_value(with_bias, scoring, dtype):
+    """They are logits like others: chosen where nothing else is left, with a score of 0 beside any other, and equal among themselves."""
+    rng = np.random.default_rng(11)
+    T, E, k = 60, 24, 6
+    x = (np.stack([rng.permutation(E) for _ in range(T)]) - E / 2) * 0.125
+    low = float(torch.finfo(dtype).min)
+    x[rng.random((T, E)) < 0.5] = low
+    x[3], x[4, 1:], x[5], x[6, :4] = low, low, low, -np.inf
+    x[5, 7] = -np.inf
+    x = f64_of(x, dtype)
+    bias = 2.0 * rng.permutation(E) if with_bias else None
+    for renorm in (False, True):
+        w, ids, _ = run_route(x, k, dtype, bias=bias, scoring=scoring, renorm=renorm)
+        rw, rids = ref.route(x, k, bias, scoring, 1, 1, renorm, 1.0)
+        assert np.array_equal(ids, rids)
+        ref.close(w, rw, torch.float32, magnitude=rw, n=E + 8)
+        u = f64_of(rng.normal(size=(T, k)), torch.float32)
+        out, h = empty(T, E, dtype=torch.float32), binding.Experts(E, T, k)
+        h.gr_expert_route_backward(put(x, dtype).float(), ints(ids), put(u, torch.float32), out, scoring=scoring, renormalise=renorm)
+        with np.errstate(over="ignore"):
+            r = ref.route_backward(x, ids, u, scoring, renorm, 1.0)
+            s = ref.scores(x, scoring)
+        big = np.abs(u).sum(1, keepdims=True)
+        if scoring == "softmax" and renorm:      # (chosen of nothing but the lowest value beside others: a sum of 0 in single precision has no shares)
+            total = np.array([s[t, ids[t][ids[t] >= 0]].sum() for t in range(T)])
+            r[total == 0], s = 0, np.ones_like(s)
+        elif renorm:
+            s = np.ones_like(s)
+        ref.close(out, r, torch.float32, magnitude=np.abs(s) * 2 * big, n=E + 16)
