@@ -559,6 +559,86 @@ int gr_expert_combine_backward(gr_experts* h, int64_t n_rows, int32_t top_k, int
 int gr_clip_gradients(gr_experts* h, int32_t n_grad, const void* const* grad, void* const* out, const int64_t* count,
                       const int32_t* dtype, float max_norm, float* out_norm, void* hip_stream);
 
+/*
+ * ---- Operators that read a request's tokens -------------------------------------------------
+ *
+ * A length predictor takes features of requests.  The calls below make them from the tokens: rows of a
+ * table by token, a gated recurrence over the tokens of every request, whose last state stands for the
+ * request, and dropout while it is trained; forward, backward, and token by token while a request runs.
+ *
+ * Conventions as for the operators above, with these besides: `stride` is the number of elements from one row
+ * to the next, at least the width (the halves of one product's result are such arrays); arrays without one are
+ * dense.  Indexes on the device are not validated: kernels stay in bounds whatever token and off hold.
+ */
+typedef struct gr_tokens gr_tokens;
+
+#define GR_MAX_VOCAB (1 << 24)
+
+/*
+ * Create the workspace of calls on up to max_tokens tokens (<= 2^30) of up to max_vocab different ones and rows of up to max_width
+ * elements, on the current HIP device.
+ */
+int gr_tokens_create(gr_tokens** out, int64_t max_tokens, int32_t max_vocab, int32_t max_width);
+int gr_tokens_destroy(gr_tokens* h);         /* waits for the device first; NULL is allowed */
+
+/*
+ * Rows by token: out[t] = scale * table[token[t]]; 0 where token[t] is outside [0, n_vocab) (padding).
+ *   token       DEVICE int32[n_tokens]
+ *   table, out  DEVICE dtype; [n_vocab, width], [n_tokens, width]
+ *   scale       finite
+ */
+int gr_token_embed(gr_tokens* h, int64_t n_tokens, int32_t n_vocab, int32_t width, int32_t dtype, const int32_t* token,
+                   const void* table, float scale, void* out, void* hip_stream);
+
+/*
+ * Its gradient: dtable[v] = scale * the sum of dout[t] over the t with token[t] = v, written whole (0 for a token that is not there).
+ *   dout        DEVICE dtype[n_tokens, width]; rows of tokens outside [0, n_vocab) are not read
+ *   out_dtable  DEVICE dtype[n_vocab, width]
+ */
+int gr_token_embed_backward(gr_tokens* h, int64_t n_tokens, int32_t n_vocab, int32_t width, int32_t dtype, const int32_t* token,
+                            const void* dout, float scale, void* out_dtable, void* hip_stream);
+
+/*
+ * A gated recurrence along every sequence of tokens, channel by channel:
+ *   f_t = sigmoid(gate_t),  h_t = f_t h_{t-1} + (1 - f_t) x_t,  y_t = h_t.
+ * Sequence s has the tokens off[s] .. off[s+1]-1; off does not decrease.  States are held in single precision.  A state that is not
+ * finite leaves the sequence's later ones not finite (an infinity may become no number); other sequences are not affected.
+ *   off         DEVICE int32[n_seq + 1]; NULL: n_seq is n_tokens and every token is a sequence of its own (a step of running requests)
+ *   gate, x     DEVICE dtype[n_tokens, width], rows gate_stride and x_stride apart
+ *   h0          DEVICE float[n_seq, width], the states that sequences start from; NULL: 0
+ *   out_y       DEVICE dtype[n_tokens, width]; rows of no sequence are left as they are.  May be NULL
+ *   out_h       DEVICE float[n_seq, width], the states after the last tokens, h0 for a sequence of none.  May be NULL, may be h0 itself
+ */
+int gr_gated_scan(gr_tokens* h, int64_t n_tokens, int64_t n_seq, int32_t width, int32_t dtype, const int32_t* off,
+                  const void* gate, int64_t gate_stride, const void* x, int64_t x_stride, const float* h0, void* out_y, float* out_h,
+                  void* hip_stream);
+
+/*
+ * Its gradient, from dy (of y) and dh (of the last states), either of which may be NULL (0):
+ *   D_t = dy_t + f_{t+1} D_{t+1}  (dh in the place of the last product after a sequence's last token)
+ *   dx_t = (1 - f_t) D_t,  dgate_t = f_t (1 - f_t) D_t (h_{t-1} - x_t),  dh0 = f D of the first token, dh for a sequence of none.
+ *   y           DEVICE dtype[n_tokens, width], as gr_gated_scan gave it; h_{t-1} is taken from it as it was rounded
+ *   dy          DEVICE dtype[n_tokens, width];  dh DEVICE float[n_seq, width]
+ *   out_dgate, out_dx   DEVICE dtype[n_tokens, width], rows dgate_stride and dx_stride apart; rows of no sequence are left as they are
+ *   out_dh0     DEVICE float[n_seq, width]; may be NULL, may be dh itself
+ */
+int gr_gated_scan_backward(gr_tokens* h, int64_t n_tokens, int64_t n_seq, int32_t width, int32_t dtype, const int32_t* off,
+                           const void* gate, int64_t gate_stride, const void* x, int64_t x_stride, const void* y, const float* h0,
+                           const void* dy, const float* dh, void* out_dgate, int64_t dgate_stride, void* out_dx, int64_t dx_stride,
+                           float* out_dh0, void* hip_stream);
+
+/*
+ * Dropout: out_i = residual_i + (u_i < m ? 0 : x_i * 65536 / (65536 - m)), m = rate * 65536 rounded to the nearest, ties to even.
+ * u_i are 16 random bits of no memory: of a block of eight elements, the four words (lower halves first) that Philox 4x32 of ten
+ * rounds (Salmon et al. 2011) makes of the counter (i / 8, offset) and the key seed, 64 bits each.  The gradient is the same call on
+ * that of out, without a residual.
+ *   x, residual, out  DEVICE dtype[n]; residual may be NULL; out may be x or residual itself.  n <= 2^40
+ *   rate         >= 0, and m < 65536
+ *   offset_add   DEVICE uint64[1], added to offset (modulo 2^64) when the kernel runs, so that the replays of a recorded call draw anew; may be NULL
+ */
+int gr_dropout(gr_tokens* h, int64_t n, int32_t dtype, const void* x, const void* residual, double rate, uint64_t seed,
+               uint64_t offset, const uint64_t* offset_add, void* out, void* hip_stream);
+
 /* Static, human-readable text for a return code. */
 const char* gr_strerror(int code);
 

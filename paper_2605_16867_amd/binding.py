@@ -1,13 +1,15 @@
 """Binding of libgoodroute: same names as the C interface, argument
 marshalling only (natively, by csrc/marshal.cpp, for the calls of a serving loop and those of a length
 predictor; by ctypes for the others, and for all of them where that module is not built or is of another
-torch: 7 to 9 us a call).  `Fleet` has the calls on a fleet, `Experts` those of a length predictor.
+torch: 7 to 9 us a call).  `Fleet` has the calls on a fleet, `Experts` those of a length predictor, `Tokens`
+those that read a request's tokens.
 Tensors are torch tensors on the GPU (device memory and the current stream come from torch; every step
 of the path runs in the library's kernels).  There is no fallback for those: without the built library every call raises.
 """
 from __future__ import annotations
 
 import ctypes as C
+import operator
 import os
 from typing import Optional
 
@@ -21,7 +23,9 @@ EXPORTS = ("gr_create", "gr_destroy", "gr_build_status", "gr_score_route", "gr_s
            "gr_profile_read_launches", "gr_profile_kernel_count", "gr_profile_kernel_name",
            "gr_experts_create", "gr_experts_destroy", "gr_expert_route", "gr_expert_route_backward", "gr_expert_plan",
            "gr_expert_linear", "gr_expert_linear_backward", "gr_expert_combine", "gr_expert_combine_backward",
-           "gr_clip_gradients")
+           "gr_clip_gradients",
+           "gr_tokens_create", "gr_tokens_destroy", "gr_token_embed", "gr_token_embed_backward", "gr_gated_scan", "gr_gated_scan_backward",
+           "gr_dropout")
 
 _lib = None
 _marshal = None
@@ -97,7 +101,13 @@ def lib() -> C.CDLL:
                 "gr_expert_linear_backward": [p, i64, i32, i32, i32, p, p, i32, p, p, p, p, p, p, p, p, p],
                 "gr_expert_combine": [p, i64, i32, i32, i32, p, p, p, p, p],
                 "gr_expert_combine_backward": [p, i64, i32, i32, i32, p, p, p, p, p, p, p],
-                "gr_clip_gradients": [p, i32, p, p, p, p, f32, p, p]}.items():
+                "gr_clip_gradients": [p, i32, p, p, p, p, f32, p, p],
+                "gr_tokens_create": [C.POINTER(p), i64, i32, i32], "gr_tokens_destroy": [p],
+                "gr_token_embed": [p, i64, i32, i32, i32, p, p, f32, p, p],
+                "gr_token_embed_backward": [p, i64, i32, i32, i32, p, p, f32, p, p],
+                "gr_gated_scan": [p, i64, i64, i32, i32, p, p, i64, p, i64, p, p, p, p],
+                "gr_gated_scan_backward": [p, i64, i64, i32, i32, p, p, i64, p, i64, p, p, p, p, p, i64, p, i64, p, p],
+                "gr_dropout": [p, i64, i32, p, p, C.c_double, C.c_uint64, C.c_uint64, p, p, p]}.items():
             getattr(l, name).restype, getattr(l, name).argtypes = C.c_int, args
         l.gr_strerror.restype = C.c_char_p
         l.gr_strerror.argtypes = [C.c_int]
@@ -133,7 +143,8 @@ def _native(l):
     m.connect(_check_slowly, *[C.cast(getattr(l, n), C.c_void_p).value for n in (
         "gr_build_status", "gr_score_route", "gr_score_route_noalloc", "gr_score_route_cached", "gr_route_feedback",
         "gr_risk_scan", "gr_expert_route", "gr_expert_route_backward", "gr_expert_plan", "gr_expert_linear",
-        "gr_expert_linear_backward", "gr_expert_combine", "gr_expert_combine_backward", "gr_clip_gradients")])
+        "gr_expert_linear_backward", "gr_expert_combine", "gr_expert_combine_backward", "gr_clip_gradients",
+        "gr_token_embed", "gr_token_embed_backward", "gr_gated_scan", "gr_gated_scan_backward", "gr_dropout")])
     return m
 
 
@@ -411,20 +422,17 @@ class _Unclear:
 _Unclear = _Unclear()
 
 
-class Experts:
-    """Owns a gr_experts handle on the current device: the workspace of a length predictor's operators.
+class _Workspace:
+    """A handle of the library's on the current device, with its checks of tensors."""
 
-    Shapes are taken from the tensors: logits [rows, experts], choices and weights [rows, top_k], x [rows or positions, n_in], w [experts,
-    n_out, n_in], y [positions, n_out]; all contiguous and on the handle's device, which has to be the current one; x, w and y of one type.
-    Outputs are tensors of the caller's, and nothing is recorded for torch's automatic differentiation: a gradient is a call of its own."""
+    _destroy = None      # name of the entry point
 
-    def __init__(self, n_expert: int, max_rows: int, max_top_k: int):
+    def _create(self, entry, *sizes):
         self._h, self._at = C.c_void_p(), None
         self._m = marshal()
         if self._m is _Ctypes:
             self._m = _Unclear
-        self.n_expert = int(n_expert)
-        _check(lib().gr_experts_create(C.byref(self._h), self.n_expert, int(max_rows), int(max_top_k)), "gr_experts_create")
+        _check(getattr(lib(), entry)(C.byref(self._h), *sizes), entry)
         import torch
         self._device = torch.cuda.current_device()
         self._at = (self._h.value, self._device)
@@ -432,7 +440,7 @@ class Experts:
     def close(self) -> None:
         if self._h:
             h, self._h, self._at = self._h, C.c_void_p(), None
-            _check(lib().gr_experts_destroy(h), "gr_experts_destroy")
+            _check(getattr(lib(), self._destroy)(h), self._destroy)
 
     def __del__(self):
         try:
@@ -457,6 +465,20 @@ class Experts:
         if t.dim() != len(shape) or any(w is not None and w != g for w, g in zip(shape, t.shape)):
             raise ValueError(f"{name}: shape {tuple(t.shape)}, need {tuple('any' if w is None else w for w in shape)}")
         return t.shape
+
+
+class Experts(_Workspace):
+    """Owns a gr_experts handle on the current device: the workspace of a length predictor's operators.
+
+    Shapes are taken from the tensors: logits [rows, experts], choices and weights [rows, top_k], x [rows or positions, n_in], w [experts,
+    n_out, n_in], y [positions, n_out]; all contiguous and on the handle's device, which has to be the current one; x, w and y of one type.
+    Outputs are tensors of the caller's, and nothing is recorded for torch's automatic differentiation: a gradient is a call of its own."""
+
+    _destroy = "gr_experts_destroy"
+
+    def __init__(self, n_expert: int, max_rows: int, max_top_k: int):
+        self.n_expert = int(n_expert)
+        self._create("gr_experts_create", self.n_expert, int(max_rows), int(max_top_k))
 
     def _plan(self, n, off, slot, pos):
         import torch
@@ -573,3 +595,111 @@ class Experts:
             (C.c_void_p * n)(*[self._dev(o, g.dtype, "out", g.numel()) for o, g in zip(out, grads)]),
             (C.c_int64 * n)(*[g.numel() for g in grads]), (C.c_int32 * n)(*[_dtype(g, "grads") for g in grads]),
             float(max_norm), self._dev(out_norm, torch.float32, "out_norm", 1), self._stream()), "gr_clip_gradients")
+
+
+class Tokens(_Workspace):
+    """Owns a gr_tokens handle on the current device: the workspace of the operators that read a request's tokens.
+
+    Shapes are taken from the tensors: token [tokens], table [vocab, width], out, gate, x, y [tokens, width], off [sequences + 1], states h
+    [sequences, width]; tokens and offsets int32, states float32, all others of one type; all on the handle's device, which has to be the
+    current one.  gate, x and their gradients may be rows of something wider (a distance from row to row of at least their width); everything else is
+    contiguous.  Outputs are tensors of the caller's, and nothing is recorded for torch's automatic differentiation: a gradient is a call of its own."""
+
+    _destroy = "gr_tokens_destroy"
+
+    def __init__(self, max_tokens: int, max_vocab: int, max_width: int):
+        self._create("gr_tokens_create", int(max_tokens), int(max_vocab), int(max_width))
+
+    def _rows(self, t, dtype, name: str, n: int, width: int):
+        """Address and distance of rows that need not be next to each other."""
+        self._shape(t, name, n, width)
+        if not t.is_cuda or t.dtype != dtype or (width > 1 and t.numel() and t.stride(1) != 1):
+            raise TypeError(f"{name}: need a {dtype} GPU tensor of contiguous rows, got {t.dtype} on {t.device}")
+        stride = t.stride(0) if n > 1 else width
+        if stride < width:
+            raise ValueError(f"{name}: rows {stride} elements apart, need {width}")
+        return self._dev(t[:1], dtype, name) if n else None, stride
+
+    def gr_token_embed(self, token, table, out, scale=1.0) -> None:
+        rc = self._m.token_embed(self._at, token, table, out, scale)
+        if rc is not None:
+            return _done(rc, "gr_token_embed")
+        import torch
+        V, W = self._shape(table, "table", None, None)
+        n, = self._shape(token, "token", None)
+        self._shape(out, "out", n, W)
+        _check(lib().gr_token_embed(self._h, n, V, W, _dtype(table, "table"), self._dev(token, torch.int32, "token"),
+                                    self._dev(table, table.dtype, "table"), float(scale), self._dev(out, table.dtype, "out"), self._stream()),
+               "gr_token_embed")
+
+    def gr_token_embed_backward(self, token, dout, out_dtable, scale=1.0) -> None:
+        rc = self._m.token_embed_backward(self._at, token, dout, out_dtable, scale)
+        if rc is not None:
+            return _done(rc, "gr_token_embed_backward")
+        import torch
+        V, W = self._shape(out_dtable, "out_dtable", None, None)
+        n, = self._shape(token, "token", None)
+        self._shape(dout, "dout", n, W)
+        _check(lib().gr_token_embed_backward(
+            self._h, n, V, W, _dtype(dout, "dout"), self._dev(token, torch.int32, "token"), self._dev(dout, dout.dtype, "dout"), float(scale),
+            self._dev(out_dtable, dout.dtype, "out_dtable"), self._stream()), "gr_token_embed_backward")
+
+    def _sequences(self, gate, off, states, name):
+        """Tokens, sequences and width; the sequences are those of `off`, without it the tokens."""
+        import torch
+        n, W = self._shape(gate, "gate", None, None)
+        S = n
+        if off is not None:
+            S = self._shape(off, "off", None)[0] - 1
+            if S < 0:
+                raise ValueError("off: 0 elements, need one at least")
+        for t, what in zip(states, name):
+            if t is not None:
+                self._shape(t, what, S, W)
+        return n, S, W, self._dev(off, torch.int32, "off")
+
+    def gr_gated_scan(self, gate, x, out_y=None, off=None, h0=None, out_h=None) -> None:
+        rc = self._m.gated_scan(self._at, gate, x, out_y, off, h0, out_h)
+        if rc is not None:
+            return _done(rc, "gr_gated_scan")
+        import torch
+        f32, t = torch.float32, gate.dtype
+        n, S, W, off = self._sequences(gate, off, (h0, out_h), ("h0", "out_h"))
+        if out_y is not None:
+            self._shape(out_y, "out_y", n, W)
+        _check(lib().gr_gated_scan(
+            self._h, n, S, W, _dtype(gate, "gate"), off, *self._rows(gate, t, "gate", n, W), *self._rows(x, t, "x", n, W),
+            self._dev(h0, f32, "h0"), self._dev(out_y, t, "out_y"), self._dev(out_h, f32, "out_h"), self._stream()), "gr_gated_scan")
+
+    def gr_gated_scan_backward(self, gate, x, y, out_dgate, out_dx, off=None, h0=None, dy=None, dh=None, out_dh0=None) -> None:
+        rc = self._m.gated_scan_backward(self._at, gate, x, y, out_dgate, out_dx, off, h0, dy, dh, out_dh0)
+        if rc is not None:
+            return _done(rc, "gr_gated_scan_backward")
+        import torch
+        f32, t = torch.float32, gate.dtype
+        n, S, W, off = self._sequences(gate, off, (h0, dh, out_dh0), ("h0", "dh", "out_dh0"))
+        for v, name in ((y, "y"), (dy, "dy")):
+            if v is not None:
+                self._shape(v, name, n, W)
+        _check(lib().gr_gated_scan_backward(
+            self._h, n, S, W, _dtype(gate, "gate"), off, *self._rows(gate, t, "gate", n, W), *self._rows(x, t, "x", n, W),
+            self._dev(y, t, "y"), self._dev(h0, f32, "h0"), self._dev(dy, t, "dy"), self._dev(dh, f32, "dh"),
+            *self._rows(out_dgate, t, "out_dgate", n, W), *self._rows(out_dx, t, "out_dx", n, W), self._dev(out_dh0, f32, "out_dh0"),
+            self._stream()), "gr_gated_scan_backward")
+
+    def gr_dropout(self, x, out, rate, seed, offset=0, residual=None, offset_add=None) -> None:
+        """seed, offset: in [0, 2^64); offset_add: an int64 tensor of one element, whose bits are added to offset when the kernel runs."""
+        rc = self._m.dropout(self._at, x, out, rate, seed, offset, residual, offset_add)
+        if rc is not None:
+            return _done(rc, "gr_dropout")
+        import torch
+        n, t = x.numel(), x.dtype
+        for v, name in ((out, "out"), (residual, "residual")):
+            if v is not None:
+                self._shape(v, name, *x.shape)
+        for v, name in ((seed, "seed"), (offset, "offset")):
+            if not 0 <= operator.index(v) < 1 << 64:
+                raise ValueError(f"{name}: {v}, need 64 bits without a sign")
+        _check(lib().gr_dropout(self._h, n, _dtype(x, "x"), self._dev(x, t, "x"), self._dev(residual, t, "residual"), float(rate), int(seed),
+                                int(offset), self._dev(offset_add, torch.int64, "offset_add", 1), self._dev(out, t, "out"), self._stream()),
+               "gr_dropout")

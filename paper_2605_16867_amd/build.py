@@ -10,7 +10,8 @@ _HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(_HERE)
 CSRC = os.path.join(_HERE, "csrc")
 LIB = os.path.join(CSRC, "libgoodroute.so")
-SOURCES = ["api.hip", "status.hip", "score.hip", "experts_api.hip", "experts.hip", "linear.hip", "clip.hip"]
+SOURCES = ["api.hip", "status.hip", "score.hip", "experts_api.hip", "experts.hip", "linear.hip", "clip.hip",
+           "tokens_api.hip", "embed.hip", "scan.hip", "dropout.hip"]
 
 
 def hipcc_command() -> list:

@@ -1,4 +1,4 @@
-// Argument marshalling of the calls of a serving loop, in native code: a call of a dozen tensors spends 7 to 9 us
+// Argument marshalling of the calls of a serving loop and of a length predictor, in native code: a call of a dozen tensors spends 7 to 9 us
 // in the interpreter when each of them is checked there (type, place, layout, size, address), several times what
 // the call itself takes to queue its kernels; here it is below one.  What is accepted and what is refused is the same: an
 // argument that is not plainly right (a subclass, a wrong type, too short) goes to the binding's own check,
@@ -44,6 +44,13 @@ struct Entries {
     int (*expert_combine_backward)(void*, int64_t, int32_t, int32_t, int32_t, const void*, const void*, const void*, const void*, void*, void*,
                                    void*);
     int (*clip_gradients)(void*, int32_t, const void* const*, void* const*, const int64_t*, const int32_t*, float, void*, void*);
+    int (*token_embed)(void*, int64_t, int32_t, int32_t, int32_t, const void*, const void*, float, void*, void*);
+    int (*token_embed_backward)(void*, int64_t, int32_t, int32_t, int32_t, const void*, const void*, float, void*, void*);
+    int (*gated_scan)(void*, int64_t, int64_t, int32_t, int32_t, const void*, const void*, int64_t, const void*, int64_t, const void*, void*, void*,
+                      void*);
+    int (*gated_scan_backward)(void*, int64_t, int64_t, int32_t, int32_t, const void*, const void*, int64_t, const void*, int64_t, const void*,
+                               const void*, const void*, const void*, void*, int64_t, void*, int64_t, void*, void*);
+    int (*dropout)(void*, int64_t, int32_t, const void*, const void*, double, uint64_t, uint64_t, const void*, void*, void*);
 } entries;
 
 PyObject* check_slowly = nullptr;      // (tensor, type code, name, elements or None) -> address or None, or raises
@@ -418,6 +425,133 @@ PyObject* clip_gradients(PyObject* const* a)
                 (const int32_t*)type.data(), real(a[2]), plain(a[3], at::kFloat, 1), stream());
 }
 
+// A whole number of 64 bits without a sign.
+uint64_t bits(PyObject* o)
+{
+    must(PyLong_CheckExact(o));
+    const unsigned long long v = PyLong_AsUnsignedLongLong(o);
+    if (v == (unsigned long long)-1 && PyErr_Occurred()) {
+        PyErr_Clear();
+        throw Unclear{};
+    }
+    return v;
+}
+
+int32_t size32(int64_t n)
+{
+    must(n <= INT32_MAX);
+    return (int32_t)n;
+}
+
+// A dense tensor of these sizes; None: null.
+void* sized(PyObject* o, at::ScalarType type, int64_t n, int64_t width)
+{
+    if (o == Py_None) return nullptr;
+    const at::TensorBase& t = plain(o, 2);
+    must(t.scalar_type() == type && t.size(0) == n && t.size(1) == width);
+    return t.data_ptr();
+}
+
+// token, rows of tokens, rows of the table, scale
+template <typename Entry>
+PyObject* embed(Entry entry, PyObject* handle_, PyObject* token_, PyObject* in_, PyObject* rows_, PyObject* table_, PyObject* out_, PyObject* scale)
+{
+    const at::TensorBase &token = plain(token_, 1), &table = plain(table_, 2);
+    const int64_t n = token.numel(), V = table.size(0), W = table.size(1);
+    must(token.scalar_type() == at::kInt);
+    (void)sized(rows_, table.scalar_type(), n, W);
+    const at::TensorBase &in = plain(in_, 2), &out = plain(out_, 2);
+    return call(entry, workspace(handle_), n, size32(V), size32(W), type_code(table), (const void*)token.data_ptr(), (const void*)in.data_ptr(),
+                real(scale), (void*)out.data_ptr(), stream());
+}
+
+// token, table, out, scale
+PyObject* token_embed(PyObject* const* a) { return embed(entries.token_embed, a[0], a[1], a[2], a[3], a[2], a[3], a[4]); }
+
+// token, dout, out_dtable, scale
+PyObject* token_embed_backward(PyObject* const* a) { return embed(entries.token_embed_backward, a[0], a[1], a[2], a[2], a[3], a[3], a[4]); }
+
+// Rows of one type that need not be next to each other.
+struct Rows {
+    void* at;
+    int64_t stride;
+
+    Rows(PyObject* o, at::ScalarType type, int64_t n, int64_t width)
+    {
+        must(THPVariable_CheckExact(o));
+        const at::TensorBase& t = THPVariable_Unpack(o);
+        must(t.is_cuda() && t.get_device() == here && t.dim() == 2 && t.scalar_type() == type && t.size(0) == n && t.size(1) == width);
+        must(n > 0 && width > 0 && (width == 1 || t.stride(1) == 1));
+        stride = n > 1 ? t.stride(0) : width;
+        must(stride >= width);
+        at = t.data_ptr();
+    }
+};
+
+struct Sequences {
+    int64_t n, W, S;
+    at::ScalarType scalar;
+    int32_t type;
+    const void* off;
+
+    // gate, off
+    Sequences(PyObject* gate_, PyObject* off_)
+    {
+        must(THPVariable_CheckExact(gate_));
+        const at::TensorBase& gate = THPVariable_Unpack(gate_);
+        must(gate.dim() == 2);
+        n = gate.size(0);
+        W = gate.size(1);
+        scalar = gate.scalar_type();
+        type = type_code(gate);
+        off = nullptr;
+        S = n;
+        if (off_ != Py_None) {
+            const at::TensorBase& t = plain(off_, 1);
+            must(t.scalar_type() == at::kInt && t.numel() > 0);
+            off = t.data_ptr();
+            S = t.numel() - 1;
+        }
+    }
+};
+
+// gate, x, out_y, off, h0, out_h
+PyObject* gated_scan(PyObject* const* a)
+{
+    const Sequences q(a[1], a[4]);
+    const Rows gate(a[1], q.scalar, q.n, q.W), x(a[2], q.scalar, q.n, q.W);
+    return call(entries.gated_scan, workspace(a[0]), q.n, q.S, size32(q.W), q.type, q.off, (const void*)gate.at, gate.stride, (const void*)x.at, x.stride,
+                (const void*)sized(a[5], at::kFloat, q.S, q.W), sized(a[3], q.scalar, q.n, q.W), sized(a[6], at::kFloat, q.S, q.W), stream());
+}
+
+// gate, x, y, out_dgate, out_dx, off, h0, dy, dh, out_dh0
+PyObject* gated_scan_backward(PyObject* const* a)
+{
+    const Sequences q(a[1], a[6]);
+    const Rows gate(a[1], q.scalar, q.n, q.W), x(a[2], q.scalar, q.n, q.W), dgate(a[4], q.scalar, q.n, q.W), dx(a[5], q.scalar, q.n, q.W);
+    return call(entries.gated_scan_backward, workspace(a[0]), q.n, q.S, size32(q.W), q.type, q.off, (const void*)gate.at, gate.stride, (const void*)x.at,
+                x.stride, (const void*)sized(a[3], q.scalar, q.n, q.W), (const void*)sized(a[7], at::kFloat, q.S, q.W),
+                (const void*)sized(a[8], q.scalar, q.n, q.W), (const void*)sized(a[9], at::kFloat, q.S, q.W), dgate.at, dgate.stride, dx.at, dx.stride,
+                sized(a[10], at::kFloat, q.S, q.W), stream());
+}
+
+// x, out, rate, seed, offset, residual, offset_add
+PyObject* dropout(PyObject* const* a)
+{
+    const at::TensorBase &x = plain(a[1]), &out = plain(a[2]);
+    must(out.sizes() == x.sizes() && out.scalar_type() == x.scalar_type());
+    const void* residual = nullptr;
+    if (a[6] != Py_None) {
+        const at::TensorBase& r = plain(a[6]);
+        must(r.sizes() == x.sizes() && r.scalar_type() == x.scalar_type());
+        residual = r.data_ptr();
+    }
+    const double rate = PyFloat_AsDouble(a[3]);
+    if (rate == -1 && PyErr_Occurred()) throw Raised{};
+    return call(entries.dropout, workspace(a[0]), (int64_t)x.numel(), type_code(x), (const void*)x.data_ptr(), residual, rate, bits(a[4]), bits(a[5]),
+                (const void*)plain(a[7], at::kLong, 1), (void*)out.data_ptr(), stream());
+}
+
 // check_slowly, then the addresses of the entry points in the order of Entries
 PyObject* connect(PyObject* const* a)
 {
@@ -435,7 +569,9 @@ PyMethodDef methods[] = {GR_METHOD(build_status, 13), GR_METHOD(score_route, 10)
                          GR_METHOD_HERE(expert_route, 14), GR_METHOD_HERE(expert_route_backward, 9), GR_METHOD_HERE(expert_plan, 6),
                          GR_METHOD_HERE(expert_linear, 10), GR_METHOD_HERE(expert_linear_backward, 13), GR_METHOD_HERE(expert_combine, 5),
                          GR_METHOD_HERE(expert_combine_backward, 7), GR_METHOD_HERE(clip_gradients, 5),
-                         GR_METHOD(connect, 15), {nullptr, nullptr, 0, nullptr}};
+                         GR_METHOD_HERE(token_embed, 5), GR_METHOD_HERE(token_embed_backward, 5), GR_METHOD_HERE(gated_scan, 7),
+                         GR_METHOD_HERE(gated_scan_backward, 11), GR_METHOD_HERE(dropout, 8),
+                         GR_METHOD(connect, 20), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "marshal", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

@@ -1,0 +1,43 @@
+// Internal declarations shared by the source files of the operators that read a request's tokens
+// (embed.hip, scan.hip, dropout.hip).  The public interface and the mathematics are in goodroute.h.
+#pragma once
+
+#include "experts.h"
+
+struct gr_tokens {
+    int64_t max_tokens = 0;
+    int max_vocab = 0, max_width = 0;
+    int* order = nullptr;      // [4][max_tokens] tokens and where they stood, before and after a pass of the sort (see embed.hip)
+    int* digits = nullptr;     // [kDigits][units] tokens of each digit in each unit, then those before; behind them those of all units
+};
+
+namespace gr {
+
+constexpr int kDigitBits = 9, kDigits = 1 << kDigitBits;      // of a pass of the sort
+constexpr int kSortUnit = 2048;                               // tokens that a workgroup puts in order
+inline int64_t sort_units(int64_t n) { return (n + kSortUnit - 1) / kSortUnit; }
+
+int launch_embed(int64_t n, int vocab, int width, int dtype, const int* token, const void* table, float scale, void* out, hipStream_t s);
+int launch_embed_backward(gr_tokens* h, int64_t n, int vocab, int width, int dtype, const int* token, const void* dout, float scale,
+                          void* dtable, hipStream_t s);
+
+struct ScanIn {
+    const int* off;      // null: every token is a sequence
+    const void *gate, *x, *y, *dy;
+    const float *h0, *dh;
+    int64_t n, n_seq, gate_stride, x_stride, dgate_stride, dx_stride;
+    int width;
+};
+int launch_scan(gr_tokens* h, const ScanIn& in, int dtype, void* y, float* last, hipStream_t s);
+int launch_scan_backward(gr_tokens* h, const ScanIn& in, int dtype, void* dgate, void* dx, float* dh0, hipStream_t s);
+
+struct DropoutIn {
+    const void *x, *residual;
+    const uint64_t* offset_add;
+    int64_t n;
+    uint64_t seed, offset;
+    int limit;      // of 65 536 elements so many are dropped
+};
+int launch_dropout(const DropoutIn& in, int dtype, void* out, hipStream_t s);
+
+}  // namespace gr

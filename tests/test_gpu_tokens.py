@@ -1,0 +1,641 @@
+"""The operators that read a request's tokens (rows by token, the gated recurrence, dropout) against their definitions in 64 bits: lengths of none, of
+one and of many units, odd widths, strides and addresses, padding, values that are no numbers; gradients against the formulas and
+against differences; recordings, other streams, refusals."""
+import numpy as np
+import pytest
+import torch
+
+from paper_2605_16867_amd import binding
+from tests import experts_reference, tokens_reference as ref
+from tests.test_gpu_experts import DEV, INF, NAN, TYPES, empty, f64_of, ints, put, shifted
+
+pytestmark = pytest.mark.gpu
+
+SCALE = 11.3125      # (16 bits hold it, as a float does)
+
+
+# ---- rows by token ----------------------------------------------------------------------------
+
+
+def some_tokens(rng, n, vocab, padded=True):
+    """Few tokens very often, most hardly ever, some that are none."""
+    t = np.minimum((vocab ** rng.random(n)).astype(np.int64) - 1, vocab - 1)
+    if padded and n:
+        t[rng.random(n) < 0.1] = -1
+        t[rng.random(n) < 0.05] = vocab
+        t[0] = np.iinfo(np.int32).max if n > 3 else t[0]
+        t[-1] = np.iinfo(np.int32).min if n > 3 else t[-1]
+    return t
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("n,vocab,width", [(0, 5, 8), (1, 1, 1), (1, 1, 16), (7, 3, 5), (64, 100, 4), (65, 100, 3), (300, 50, 33), (513, 1000, 256),
+                                           (1000, 700, 511), (129, 64, 1024), (33, 40, 1030), (20, 9, 4097)])
+def test_embed(n, vocab, width, dtype):
+    rng = np.random.default_rng(n + width)
+    h = binding.Tokens(n, vocab, width)
+    token, table = some_tokens(rng, n, vocab), f64_of(rng.normal(size=(vocab, width)), dtype)
+    want = np.where(((token >= 0) & (token < vocab))[:, None], table[np.clip(token, 0, vocab - 1)] * SCALE, 0) if n else np.zeros((0, width))
+    for shift in (False, True):
+        out = empty(n, width, dtype=dtype)
+        out = shifted(out) if shift else out
+        h.gr_token_embed(ints(token), shifted(put(table, dtype)) if shift else put(table, dtype), out, scale=SCALE)
+        experts_reference.close(out, want, dtype, magnitude=np.abs(want))
+
+
+def test_rows_that_are_no_numbers_stay_where_they_are():
+    table = torch.zeros(4, 9, device=DEV)
+    table[0], table[2, 3] = NAN, INF
+    out = empty(5, 9)
+    binding.Tokens(5, 4, 9).gr_token_embed(ints([1, -1, 2, 4, 0]), table, out, scale=2.0)
+    assert bool((out[[0, 1, 3]] == 0).all()) and float(out[2, 3]) == INF and int((out[2] == 0).sum()) == 8 and bool(out[4].isnan().all())
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("n,vocab,width", [(0, 5, 8), (1, 1, 1), (1, 9, 16), (7, 3, 5), (64, 100, 4), (65, 2, 3), (300, 513, 33), (2047, 512, 64),
+                                           (2049, 1000, 256), (5000, 300, 511), (4100, 64, 1024), (30000, 7, 40), (9000, 40000, 24),
+                                           (70000, 3000, 20), (12000, 300000, 8)])
+def test_embed_backward(n, vocab, width, dtype):
+    rng = np.random.default_rng(n + width)
+    h = binding.Tokens(max(n, 17), vocab, width)
+    token, dout = some_tokens(rng, n, vocab), f64_of(rng.normal(size=(n, width)), dtype)
+    want, size, count = ref.embed_backward(token, dout, vocab, SCALE)
+    seen = []
+    for shift in (False, True, False):
+        out, d = empty(vocab, width, dtype=dtype), put(dout, dtype)
+        out, d = (shifted(out), shifted(d)) if shift else (out, d)
+        h.gr_token_embed_backward(ints(token), d, out, scale=SCALE)
+        experts_reference.close(out, want, dtype, magnitude=size, n=count[:, None])
+        seen.append(out)
+    assert torch.equal(seen[0], seen[2])
+
+
+@pytest.mark.parametrize("n,vocab", [(5000, 40), (40000, 1)])
+def test_gradient_of_one_token_only(n, vocab):
+    """All tokens are the same, or none is one."""
+    rng = np.random.default_rng(5)
+    dout = f64_of(rng.normal(size=(n, 36)), torch.float32)
+    h = binding.Tokens(n, vocab, 36)
+    for token in (np.full(n, vocab - 1), np.full(n, -1), np.full(n, vocab), np.where(np.arange(n) % 4096 == 17, 0, -7)):
+        want, size, count = ref.embed_backward(token, dout, vocab, 1.0)
+        out = empty(vocab, 36)
+        h.gr_token_embed_backward(ints(token), put(dout, torch.float32), out)
+        experts_reference.close(out, want, torch.float32, magnitude=size, n=count[:, None])
+
+
+def test_rows_of_padding_are_not_read():
+    dout = torch.ones(3000, 12, device=DEV)
+    token = torch.arange(3000, device=DEV, dtype=torch.int32) % 50
+    token[::7] = -1
+    dout[::7] = NAN
+    dout[1] = NAN
+    out = empty(60, 12)
+    binding.Tokens(3000, 60, 12).gr_token_embed_backward(token, dout, out)
+    assert bool(out[1].isnan().all()) and not bool(out[2:].isnan().any()) and not bool(out[0].isnan().any()) and bool((out[50:] == 0).all())
+    want = torch.bincount(token[token >= 0].long(), minlength=60).float()
+    assert torch.equal(out[2:, 0], want[2:])
+
+
+def test_gradient_by_differences():
+    """A loss of every element of the result, moved in some weights: linear, so differences of any size are the gradient."""
+    rng = np.random.default_rng(3)
+    n, vocab, width = 200, 30, 12
+    h = binding.Tokens(n, vocab, width)
+    token, u = ints(some_tokens(rng, n, vocab)), put(rng.normal(size=(n, width)), torch.float32)
+    table, out, grad = put(rng.normal(size=(vocab, width)), torch.float32), empty(n, width), empty(vocab, width)
+    h.gr_token_embed_backward(token, u, grad, scale=0.5)
+    for v, c in [(0, 0), (0, 5), (1, 11), (3, 7), (vocab - 1, 2)]:
+        loss = []
+        for step in (1.0, -1.0):
+            moved = table.clone()
+            moved[v, c] += step
+            h.gr_token_embed(token, moved, out, scale=0.5)
+            loss.append(float((out.double() * u.double()).sum()))
+        # 200 terms of order 1 to 4, each of them rounded to 2^-24
+        assert abs((loss[0] - loss[1]) / 2 - float(grad[v, c])) < 200 * 4 * 2.0 ** -24
+
+
+# ---- the recurrence ---------------------------------------------------------------------------
+
+
+def some_offsets(rng, n, S):
+    """Sequences of all lengths, none among them; all of n."""
+    if S == 0:
+        return np.zeros(1, dtype=np.int64)
+    cut = np.sort(rng.integers(0, n + 1, S - 1))
+    if S > 3:
+        cut[0], cut[-1] = cut[1], cut[-2]      # (empty ones)
+        cut = np.sort(np.where(rng.random(S - 1) < 0.2, 0, cut))
+    return np.concatenate([[0], cut, [n]])
+
+
+def inputs(rng, n, width, dtype, far=6.0):
+    return f64_of(rng.normal(size=(n, width)) * 2 + rng.uniform(-1, far, width), dtype), f64_of(rng.normal(size=(n, width)), dtype)
+
+
+def halves(*arrays, dtype, shift=False):
+    """Arrays side by side in one tensor, its parts."""
+    both = put(np.concatenate(arrays, 1), dtype)
+    both = shifted(both) if shift else both
+    at = np.cumsum([0] + [a.shape[1] for a in arrays])
+    return [both[:, a:b] for a, b in zip(at, at[1:])]
+
+
+SIZES = [(0, 3, 8), (1, 1, 1), (1, 1, 64), (5, 2, 3), (16, 1, 8), (17, 3, 16), (64, 1, 65), (100, 100, 7), (130, 9, 33), (257, 1, 129), (600, 30, 256),
+         (333, 4, 515), (1025, 3, 40), (2500, 700, 24), (2100, 1, 8), (5000, 2, 5), (3000, 6, 130), (9000, 1, 16), (700, 2, 1024)]
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("n,S,width", SIZES)
+def test_scan(n, S, width, dtype):
+    rng = np.random.default_rng(n + width)
+    h = binding.Tokens(n, 1, width)
+    gate, x = inputs(rng, n, width, dtype)
+    off = some_offsets(rng, n, S)
+    h0 = f64_of(rng.normal(size=(S, width)), torch.float32)
+    for start in (False, True):
+        want_y, want, E_y, E = ref.scan(gate, x, off, h0 if start else None)
+        g, v = halves(gate, x, dtype=dtype, shift=start) if not start or width % 2 else (put(gate, dtype), put(x, dtype))
+        y, last = empty(n, width, dtype=dtype), empty(S, width)
+        y = shifted(y) if start else y
+        h.gr_gated_scan(g, v, out_y=y, off=ints(off), h0=put(h0, torch.float32) if start else None, out_h=last)
+        ref.near(y, want_y, E_y, dtype, np.abs(gate).max(initial=0), "y")
+        ref.near(last, want, E, dtype, np.abs(gate).max(initial=0), "last")
+        # one of the results alone; the states in place
+        alone, state = empty(n, width, dtype=dtype), put(h0, torch.float32)
+        h.gr_gated_scan(g, v, out_y=alone, off=ints(off), h0=state if start else None)
+        assert torch.equal(alone, y)
+        h.gr_gated_scan(g, v, off=ints(off), h0=state if start else None, out_h=state)
+        assert torch.equal(state, last)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("n,S,width", SIZES)
+def test_scan_backward(n, S, width, dtype):
+    rng = np.random.default_rng(n + width + 1)
+    h = binding.Tokens(n, 1, width)
+    gate, x = inputs(rng, n, width, dtype)
+    off = some_offsets(rng, n, S)
+    h0, dh = (f64_of(rng.normal(size=(S, width)), torch.float32) for _ in range(2))
+    dy = f64_of(rng.normal(size=(n, width)), dtype)
+    for start, every, last in ((False, True, False), (True, True, True), (True, False, True)):
+        y = f64_of(ref.scan(gate, x, off, h0 if start else None)[0], dtype)
+        want = ref.scan_backward(gate, x, y, off, h0 if start else None, dy if every else None, dh if last else None)
+        g, v = halves(gate, x, dtype=dtype, shift=every)
+        dg, dx = halves(np.full(gate.shape, 77.0), np.full(x.shape, 77.0), dtype=dtype, shift=not every)
+        dh0 = empty(S, width)
+        args = dict(off=ints(off), h0=put(h0, torch.float32) if start else None, dy=put(dy, dtype) if every else None)
+        state = put(dh, torch.float32) if last else None
+        h.gr_gated_scan_backward(g, v, put(y, dtype), dg, dx, dh=state, out_dh0=dh0, **args)
+        most = np.abs(gate).max(initial=0)
+        for got, (r, E), what in zip((dg, dx, dh0), want, ("dgate", "dx", "dh0")):
+            ref.near(got, r, E, dtype, most, what)
+        # dense, without the gradient of the first states; that in place
+        dense = [empty(n, width, dtype=dtype) for _ in range(2)]
+        h.gr_gated_scan_backward(put(gate, dtype), put(x, dtype), put(y, dtype), *dense, dh=state, **args)
+        assert torch.equal(dense[0], dg) and torch.equal(dense[1], dx)
+        if last:
+            h.gr_gated_scan_backward(g, v, put(y, dtype), dg, dx, dh=state, out_dh0=state, **args)
+            assert torch.equal(state, dh0)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("n,width", [(1, 1), (3, 5), (64, 24), (257, 130), (40, 1024), (1000, 33)])
+def test_scan_of_single_tokens(n, width, dtype):
+    """A token of every running request: as sequences of one, and the same bits."""
+    rng = np.random.default_rng(n)
+    h = binding.Tokens(n, 1, width)
+    gate, x = inputs(rng, n, width, dtype)
+    h0, dh, dy = (f64_of(rng.normal(size=(n, width)), t) for t in (torch.float32, torch.float32, dtype))
+    most = np.abs(gate).max()
+    for start in (False, True):
+        s0 = put(h0, torch.float32) if start else None
+        want_y, want, E_y, E = ref.scan(gate, x, None, h0 if start else None)
+        g, v = halves(gate, x, dtype=dtype, shift=start)
+        y, last = empty(n, width, dtype=dtype), empty(n, width)
+        h.gr_gated_scan(g, v, out_y=y, h0=s0, out_h=last)
+        ref.near(y, want_y, E_y, dtype, most, "y")
+        ref.near(last, want, E, dtype, most, "last")
+        y2, last2 = empty(n, width, dtype=dtype), s0.clone() if start else empty(n, width)
+        h.gr_gated_scan(g, v, out_y=y2, off=ints(np.arange(n + 1)), h0=last2 if start else None, out_h=last2)
+        assert torch.equal(y2, y) and torch.equal(last2, last)
+        if start:
+            state = s0.clone()
+            h.gr_gated_scan(g, v, h0=state, out_h=state)
+            assert torch.equal(state, last)
+        y0 = f64_of(want_y, dtype)
+        dg, dx, dh0 = empty(n, width, dtype=dtype), empty(n, width, dtype=dtype), empty(n, width)
+        h.gr_gated_scan_backward(g, v, put(y0, dtype), dg, dx, h0=s0, dy=put(dy, dtype), dh=put(dh, torch.float32), out_dh0=dh0)
+        want = ref.scan_backward(gate, x, y0, None, h0 if start else None, dy, dh)
+        for got, (r, E), what in zip((dg, dx, dh0), want, ("dgate", "dx", "dh0")):
+            ref.near(got, r, E, dtype, most, what)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("n,width", [(300, 40), (3000, 12), (2000, 520)])
+def test_rows_of_no_sequence_are_left_alone(n, width, dtype):
+    rng = np.random.default_rng(n)
+    h = binding.Tokens(n, 1, width)
+    gate, x = inputs(rng, n, width, dtype)
+    a, b = n // 5, n - n // 4
+    off = np.concatenate([[a, a], np.sort(rng.integers(a, b, 4)), [b, b]])
+    inside = np.arange(a, b)
+    gate[:a], x[b:] = np.nan, np.inf
+    h0 = f64_of(rng.normal(size=(7, width)), torch.float32)
+    with np.errstate(invalid="ignore"):
+        want_y, want, E_y, E = ref.scan(gate, x, off, h0)
+    y, last = empty(n, width, dtype=dtype), empty(7, width)
+    h.gr_gated_scan(put(gate, dtype), put(x, dtype), out_y=y, off=ints(off), h0=put(h0, torch.float32), out_h=last)
+    most = np.abs(gate[inside]).max()
+    assert bool((y[:a] == 77).all()) and bool((y[b:] == 77).all())
+    ref.near(y[a:b], want_y[inside], E_y[inside], dtype, most, "y")
+    ref.near(last, want, E, dtype, most, "last")
+    y0 = np.full((n, width), np.nan)
+    y0[inside] = f64_of(want_y[inside], dtype)
+    dy = f64_of(rng.normal(size=(n, width)), dtype)
+    dy[:a] = np.nan
+    want = ref.scan_backward(gate, x, y0, off, h0, dy, h0)
+    dg, dx, dh0 = empty(n, width, dtype=dtype), empty(n, width, dtype=dtype), empty(7, width)
+    h.gr_gated_scan_backward(put(gate, dtype), put(x, dtype), put(y0, dtype), dg, dx, off=ints(off), h0=put(h0, torch.float32), dy=put(dy, dtype),
+                             dh=put(h0, torch.float32), out_dh0=dh0)
+    for got, (r, E), what in zip((dg, dx), want, ("dgate", "dx")):
+        assert bool((got[:a] == 77).all()) and bool((got[b:] == 77).all())
+        ref.near(got[a:b], r[inside], E[inside], dtype, most, what)
+    ref.near(dh0, *want[2], dtype, most, "dh0")
+
+
+@pytest.mark.parametrize("n,width", [(400, 24), (4000, 9), (1500, 300)])
+def test_what_is_no_number_stays_in_its_sequence(n, width):
+    rng = np.random.default_rng(n)
+    h = binding.Tokens(n, 1, width)
+    gate, x = inputs(rng, n, width, torch.float32, far=2.0)
+    off = np.array([0, n // 10, n // 3, n // 3, n // 3 + 1, n - n // 4, n])
+    want_y, want, E_y, E = ref.scan(gate, x, off, None)
+    dy, y0 = f64_of(rng.normal(size=(n, width)), torch.float32), f64_of(want_y, torch.float32)
+    back = ref.scan_backward(gate, x, y0, off, None, dy, None)
+    at = n // 3 + 1 + n // 20      # in the last sequence but one
+    for bad in (NAN, INF, -INF):
+        x2, g2, d2 = x.copy(), gate.copy(), dy.copy()
+        x2[at, 1], g2[at, 2], d2[at, 3] = bad, NAN, bad
+        y, last = empty(n, width), empty(6, width)
+        h.gr_gated_scan(put(g2, torch.float32), put(x2, torch.float32), out_y=y, off=ints(off), out_h=last)
+        others = np.ones((n, width), dtype=bool)
+        others[at:off[5], 1:3] = False
+        got = y.cpu().numpy()
+        assert not np.isfinite(got[~others]).any() and not np.isfinite(last[4, 1:3].cpu().numpy()).any()
+        ref.near(torch.from_numpy(np.where(others, got, 0)), np.where(others, want_y, 0), E_y, torch.float32, 0, "y")
+        dg, dx, dh0 = empty(n, width), empty(n, width), empty(6, width)
+        h.gr_gated_scan_backward(put(g2, torch.float32), put(x, torch.float32), put(y0, torch.float32), dg, dx, off=ints(off), dy=put(d2, torch.float32),
+                                 out_dh0=dh0)
+        others = np.ones((n, width), dtype=bool)
+        others[off[4]:at + 1, 2:4] = False
+        for got, (r, E) in ((dg, back[0]), (dx, back[1])):
+            got = got.cpu().numpy()
+            ref.near(torch.from_numpy(np.where(others, got, 0)), np.where(others, r, 0), E, torch.float32, 0, "back")
+        assert not np.isfinite(dx.cpu().numpy()[~others]).any() and not np.isfinite(dh0[4, 2:4].cpu().numpy()).any()
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_gates_at_their_ends(dtype):
+    """Gates that keep everything or nothing, infinite ones and the type's largest among them."""
+    rng = np.random.default_rng(0)
+    big = float(torch.finfo(dtype).max)
+    ends = np.array([-INF, -big, -200, -100, -88.5, -87, -30, -1e-30, 0, 1e-30, 30, 87, 88.5, 100, 200, big, INF])
+    gate = f64_of(np.tile(ends, (200, 1)), dtype)
+    gate[::3] = f64_of(rng.choice(ends, gate[::3].shape), dtype)
+    x = f64_of(rng.normal(size=gate.shape), dtype)
+    h0 = f64_of(rng.normal(size=(2, len(ends))), torch.float32)
+    off = np.array([0, 90, 200])
+    want_y, want, E_y, E = ref.scan(gate, x, off, h0)
+    y, last = empty(*gate.shape, dtype=dtype), empty(2, len(ends))
+    h = binding.Tokens(200, 1, len(ends))
+    h.gr_gated_scan(put(gate, dtype), put(x, dtype), out_y=y, off=ints(off), h0=put(h0, torch.float32), out_h=last)
+    # (gates of up to 88 count: behind them both sigmoids are 0 and 1 to all digits)
+    ref.near(y, want_y, E_y, dtype, 89, "y")
+    ref.near(last, want, E, dtype, 89, "last")
+
+
+def test_scan_gradient_by_differences():
+    """Of a loss of all states and the last ones, in 64 bits, at some gates, values and first states."""
+    rng = np.random.default_rng(9)
+    n, S, width = 60, 4, 6
+    gate, x = inputs(rng, n, width, torch.float32, far=2.0)
+    off = np.array([0, 13, 13, 40, 60])
+    h0, dh = (f64_of(rng.normal(size=(S, width)), torch.float32) for _ in range(2))
+    dy = f64_of(rng.normal(size=(n, width)), torch.float32)
+
+    def loss():
+        y, last, _, _ = ref.scan(gate, x, off, h0)
+        return (y * dy).sum() + (last * dh).sum()
+
+    h, f32 = binding.Tokens(n, 1, width), torch.float32
+    y, dg, dx, dh0 = empty(n, width), empty(n, width), empty(n, width), empty(S, width)
+    h.gr_gated_scan(put(gate, f32), put(x, f32), out_y=y, off=ints(off), h0=put(h0, f32))
+    h.gr_gated_scan_backward(put(gate, f32), put(x, f32), y, dg, dx, off=ints(off), h0=put(h0, f32), dy=put(dy, f32), dh=put(dh, f32), out_dh0=dh0)
+    for a, g in ((gate, dg), (x, dx), (h0, dh0)):
+        g = g.double().cpu().numpy()
+        for i in rng.choice(a.size, min(40, a.size), replace=False):
+            at = np.unravel_index(i, a.shape)
+            keep, step, both = a[at], 1e-4, []
+            for s in (step, -step):
+                a[at] = keep + s
+                both.append(loss())
+            a[at] = keep
+            # third derivatives of order 10 at 1e-4: 1e-7; single precision over 47 tokens of order 1: 1e-5
+            assert abs((both[0] - both[1]) / (2 * step) - g[at]) < 3e-5 * max(1, abs(g[at])), at
+
+
+@pytest.mark.parametrize("dtype,n,width", [(torch.bfloat16, 40000, 64), (torch.float32, 20001, 35), (torch.float16, 6000, 300)])
+def test_a_long_sequence_and_many(dtype, n, width):
+    """Past every unit that work is split in; channels that remember thousands of tokens, and ones that forget at once."""
+    rng = np.random.default_rng(n)
+    h = binding.Tokens(n, 1, width)
+    gate = f64_of(rng.normal(size=(n, width)) + np.linspace(-4, 9, width), dtype)
+    x, dy = (f64_of(rng.normal(size=(n, width)), dtype) for _ in range(2))
+    most = np.abs(gate).max()
+    for off in (np.array([0, n]), some_offsets(rng, n, 30), np.array([0, 100, n - 70, n])):
+        S = len(off) - 1
+        h0, dh = (f64_of(rng.normal(size=(S, width)), torch.float32) for _ in range(2))
+        want_y, want, E_y, E = ref.scan(gate, x, off, h0)
+        outs = []
+        for _ in range(2):
+            y, last = empty(n, width, dtype=dtype), empty(S, width)
+            h.gr_gated_scan(put(gate, dtype), put(x, dtype), out_y=y, off=ints(off), h0=put(h0, torch.float32), out_h=last)
+            outs.append((y, last))
+        assert torch.equal(outs[0][0], outs[1][0]) and torch.equal(outs[0][1], outs[1][1])
+        ref.near(y, want_y, E_y, dtype, most, "y")
+        ref.near(last, want, E, dtype, most, "last")
+        y0 = f64_of(want_y, dtype)
+        want = ref.scan_backward(gate, x, y0, off, h0, dy, dh)
+        outs = []
+        for _ in range(2):
+            dg, dx, dh0 = empty(n, width, dtype=dtype), empty(n, width, dtype=dtype), empty(S, width)
+            h.gr_gated_scan_backward(put(gate, dtype), put(x, dtype), put(y0, dtype), dg, dx, off=ints(off), h0=put(h0, torch.float32), dy=put(dy, dtype),
+                                     dh=put(dh, torch.float32), out_dh0=dh0)
+            outs.append((dg, dx, dh0))
+        for a, b in zip(*outs):
+            assert torch.equal(a, b)
+        for got, (r, E), what in zip(outs[0], want, ("dgate", "dx", "dh0")):
+            ref.near(got, r, E, dtype, most, what)
+
+
+# ---- dropout ----------------------------------------------------------------------------------
+
+
+def test_random_words_are_the_published_ones():
+    """Known answers of Philox 4x32 with ten rounds."""
+    for counter, key, want in (((0,) * 4, (0,) * 2, (0x6627E8D5, 0xE169C58D, 0xBC57AC4C, 0x9B00DBD8)),
+                               ((0xFFFFFFFF,) * 4, (0xFFFFFFFF,) * 2, (0x408F276D, 0x41C83B0E, 0xA20BC7C6, 0x6D5451FD)),
+                               ((0x243F6A88, 0x85A308D3, 0x13198A2E, 0x03707344), (0xA4093822, 0x299F31D0),
+                                (0xD16CFE09, 0x94FDCCEB, 0x5001E420, 0x24126EA1))):
+        assert tuple(int(w) for w in ref.philox(counter, key)) == want
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("n", [0, 1, 7, 8, 9, 255, 2048, 2049, 40003])
+def test_dropout(n, dtype):
+    rng = np.random.default_rng(n)
+    h = binding.Tokens(1, 1, 1)
+    x, add = (f64_of(rng.normal(size=n) + 3, dtype) for _ in range(2))
+    for rate, seed, offset in ((0.1, 0, 0), (0.5, 2 ** 64 - 1, 2 ** 64 - 1), (0.25, 1 << 40, 7), (0.0, 5, 1), (0.99, 3, 1 << 33)):
+        m = round(rate * 65536)
+        kept = ref.random_bits(range(n), seed, offset) >= m if n else np.zeros(0, dtype=bool)
+        scale = 65536 / (65536 - m)
+        for shift in (False, True):
+            a, b, out = put(x, dtype), put(add, dtype), empty(n, dtype=dtype)
+            a, b, out = (shifted(t) for t in (a, b, out)) if shift else (a, b, out)
+            h.gr_dropout(a, out, rate, seed, offset=offset)
+            assert bool(((out != 0).cpu().numpy() == kept).all())
+            experts_reference.close(out, np.where(kept, x * scale, 0), dtype, magnitude=np.abs(x) * scale)
+            h.gr_dropout(a, out, rate, seed, offset=offset, residual=b)
+            experts_reference.close(out, np.where(kept, x * scale, 0) + add, dtype, magnitude=np.abs(x) * scale + np.abs(add))
+            # in the place of either; an offset that the kernel finds
+            more = torch.tensor([offset - 3 - (1 << 64) if offset - 3 >= 1 << 63 else offset - 3], dtype=torch.int64, device=DEV)
+            h.gr_dropout(a, b, rate, seed, offset=3, residual=b, offset_add=more)
+            assert torch.equal(b, out)
+            h.gr_dropout(a, a, rate, seed, offset=offset)
+            experts_reference.close(a, np.where(kept, x * scale, 0), dtype, magnitude=np.abs(x) * scale)
+
+
+def test_what_is_dropped_is_nothing():
+    """Values that are no numbers go where they are dropped; a share of the rate is, up to six standard deviations."""
+    n, h = 1 << 20, binding.Tokens(1, 1, 1)
+    x = torch.full((n,), NAN, device=DEV)
+    out = empty(n)
+    h.gr_dropout(x, out, 0.3, 11)
+    gone = out == 0
+    assert bool(out[~gone].isnan().all())
+    assert abs(int(gone.sum()) - 0.3 * n) < 6 * (n * 0.21) ** 0.5
+    again = empty(n)
+    h.gr_dropout(torch.ones_like(x), again, 0.3, 11)
+    assert torch.equal(again == 0, gone)
+    for other in (dict(seed=12), dict(seed=11, offset=1), dict(seed=11 + (1 << 32))):
+        h.gr_dropout(torch.ones_like(x), again, 0.3, **other)
+        # (independent: both dropped 0.09)
+        assert abs(int(((again == 0) & gone).sum()) - 0.09 * n) < 6 * (n * 0.09) ** 0.5
+
+
+def test_dropout_of_any_shape_and_many_elements():
+    h = binding.Tokens(1, 1, 1)
+    n = (1 << 28) + 11
+    x = torch.ones(n, dtype=torch.bfloat16, device=DEV)
+    h.gr_dropout(x, x, 0.5, 77, offset=5)
+    index = np.concatenate([np.arange(64), n // 2 + np.arange(64), n - 64 + np.arange(64)])
+    kept = ref.random_bits(index, 77, 5) >= 32768
+    assert np.array_equal((x[torch.from_numpy(index).to(DEV)] == 2).cpu().numpy(), kept)
+    y = torch.ones(3, 5, 7, device=DEV)
+    out = empty(3, 5, 7)
+    h.gr_dropout(y, out, 0.5, 77, offset=5)
+    assert np.array_equal((out.view(-1)[:64] == 2).cpu().numpy(), kept[:64])
+
+
+def test_gradient_of_dropout():
+    """The same call on the gradient: linear in its input, so differences of any size are the gradient."""
+    h, n = binding.Tokens(1, 1, 1), 1000
+    x, u = torch.randn(n, device=DEV), torch.randn(n, device=DEV)
+    g, lo, hi = empty(n), empty(n), empty(n)
+    h.gr_dropout(u, g, 0.2, 4, offset=9)
+    h.gr_dropout(x + 1, hi, 0.2, 4, offset=9, residual=x)
+    h.gr_dropout(x - 1, lo, 0.2, 4, offset=9, residual=x)
+    # values of up to 6, three roundings of each side
+    assert float(((hi - lo) / 2 * u - g).abs().max()) < 6 * 6 * 2.0 ** -23 * float(u.abs().max())
+
+
+# ---- together, recorded, on other streams ------------------------------------------------------
+
+
+def _chain(h, token, table, off, out):
+    """Tokens -> rows -> the recurrence (gates and values are halves of the rows) -> dropout, and back."""
+    W = table.shape[1] // 2
+    h.gr_token_embed(token, table, out["rows"], scale=1.5)
+    g, x = out["rows"][:, :W], out["rows"][:, W:]
+    h.gr_gated_scan(g, x, out_y=out["y"], off=off, out_h=out["h"])
+    h.gr_dropout(out["h"], out["f"], 0.25, 7, offset=1, offset_add=out["step"])
+    h.gr_dropout(out["f"], out["df"], 0.25, 7, offset=1, offset_add=out["step"])
+    d = out["drows"]
+    h.gr_gated_scan_backward(g, x, out["y"], d[:, :W], d[:, W:], off=off, dh=out["df"], out_dh0=out["dh0"])
+    h.gr_token_embed_backward(token, d, out["dtable"], scale=1.5)
+
+
+def _chain_buffers(rng, n, V, W, S, dtype):
+    off = ints(some_offsets(rng, n, S))
+    f = lambda *s: empty(*s)
+    out = dict(rows=empty(n, 2 * W, dtype=dtype), y=empty(n, W, dtype=dtype), h=f(S, W), f=f(S, W), df=f(S, W), drows=empty(n, 2 * W, dtype=dtype),
+               dh0=f(S, W), dtable=empty(V, 2 * W, dtype=dtype), step=torch.zeros(1, dtype=torch.int64, device=DEV))
+    return ints(some_tokens(rng, n, V)), put(rng.normal(size=(V, 2 * W)), dtype), off, out
+
+
+@pytest.mark.parametrize("n,V,W,S", [(50, 30, 12, 3), (5000, 700, 40, 9), (30000, 5000, 256, 40)])
+def test_a_run_of_them_recorded_and_replayed(n, V, W, S):
+    """Two recordings on one handle, replayed in turn with eager calls between, on new inputs: every replay gives the eager call's bits."""
+    rng = np.random.default_rng(n)
+    h = binding.Tokens(n, V, 2 * W)
+    sets = [_chain_buffers(rng, n, V, W, S, t) for t in (torch.float32, torch.bfloat16)]
+    side, graphs = torch.cuda.Stream(), []
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        for args in sets:
+            _chain(h, *args)
+    torch.cuda.current_stream().wait_stream(side)
+    torch.cuda.synchronize()
+    for args in sets:
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            _chain(h, *args)
+        graphs.append(g)
+    masks = []
+    for turn in range(3):
+        for args, g in zip(sets, graphs):
+            token, table, off, out = args
+            new_token, new_table, new_off, _ = _chain_buffers(rng, n, V, W, S, table.dtype)
+            token.copy_(new_token), table.copy_(new_table), off.copy_(new_off), out["step"].fill_(turn)
+            _chain(h, *args)
+            want = {k: v.clone() for k, v in out.items()}
+            for k, v in out.items():
+                if k != "step":
+                    v.fill_(77)
+            torch.cuda.synchronize()
+            g.replay()
+            for k, v in out.items():
+                assert torch.equal(v, want[k]) or bool(((v == want[k]) | (v.isnan() & want[k].isnan())).all()), (turn, k)
+            masks.append((out["f"] == 0).clone())
+    assert not torch.equal(masks[0], masks[2])
+
+
+def test_on_another_stream_behind_what_is_queued_there():
+    rng = np.random.default_rng(1)
+    n, V, W, S = 3000, 100, 24, 5
+    h = binding.Tokens(n, V, 2 * W)
+    token, table, off, out = _chain_buffers(rng, n, V, W, S, torch.float32)
+    later = token.flip(0).contiguous()
+    _chain(h, later, table, off, out)
+    want = {k: v.clone() for k, v in out.items()}
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side):
+        torch.cuda._sleep(20_000_000)
+        token.copy_(later)
+        _chain(h, token, table, off, out)
+    torch.cuda.synchronize()
+    for k, v in out.items():
+        assert torch.equal(v, want[k]), k
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_as_by_ctypes(dtype, monkeypatch):
+    """The native marshalling and the binding's own give the same bits."""
+    outs = []
+    for native in (True, False):
+        if not native:
+            monkeypatch.setattr(binding, "_marshal", binding._Ctypes)
+        rng = np.random.default_rng(4)
+        h = binding.Tokens(2000, 300, 64)
+        args = _chain_buffers(rng, 2000, 300, 32, 6, dtype)
+        _chain(h, *args)
+        outs.append(args[3])
+    for k in outs[0]:
+        assert torch.equal(outs[0][k], outs[1][k]), k
+
+
+# ---- refusals ---------------------------------------------------------------------------------
+
+
+@pytest.mark.parametrize("native", [True, False])
+def test_refusals(native, monkeypatch):
+    if not native:
+        monkeypatch.setattr(binding, "_marshal", binding._Ctypes)
+    n, V, W, S = 12, 7, 16, 3
+    h = binding.Tokens(n, V, W)
+    f, i = (lambda *s, t=torch.float32: torch.zeros(*s, dtype=t, device=DEV)), (lambda *s: torch.zeros(*s, dtype=torch.int32, device=DEV))
+    token, off, g, y, st = i(n), ints([0, 4, 4, n]), f(n, W), f(n, W), f(S, W)
+    both = f(n, 2 * W)
+
+    def refused(error, call, match=None):
+        with pytest.raises(error, match=match):
+            call()
+
+    def code(c, call):
+        with pytest.raises(binding.GoodRouteError) as e:
+            call()
+        assert e.value.code == c
+
+    # rows by token
+    refused(ValueError, lambda: h.gr_token_embed(token, f(V, W), f(n, W + 1)), "out: shape")
+    refused(ValueError, lambda: h.gr_token_embed(i(n, 1), f(V, W), f(n, W)), "token: shape")
+    refused(TypeError, lambda: h.gr_token_embed(token.long(), f(V, W), f(n, W)), "token: need a contiguous torch.int32")
+    refused(TypeError, lambda: h.gr_token_embed(token, f(V, W), f(n, W, t=torch.float16)), "out: need")
+    refused(TypeError, lambda: h.gr_token_embed(token, f(V, W, t=torch.float64), f(n, W, t=torch.float64)), "float32, bfloat16 or float16")
+    refused(TypeError, lambda: h.gr_token_embed(token, f(V, 2 * W)[:, :W], f(n, W)), "contiguous")
+    refused(TypeError, lambda: h.gr_token_embed(token.cpu(), f(V, W), f(n, W)), "token")
+    refused(ValueError, lambda: h.gr_token_embed_backward(token, f(n - 1, W), f(V, W)), "dout: shape")
+    for bad in (INF, NAN):
+        code(-1, lambda: h.gr_token_embed(token, f(V, W), f(n, W), scale=bad))
+        code(-1, lambda: h.gr_token_embed_backward(token, f(n, W), f(V, W), scale=bad))
+    code(-2, lambda: h.gr_token_embed(i(n + 1), f(V, W), f(n + 1, W)))
+    code(-2, lambda: h.gr_token_embed(token, f(V + 1, W), f(n, W)))
+    code(-2, lambda: h.gr_token_embed_backward(token, f(n, W + 1), f(V, W + 1)))
+    # the recurrence
+    refused(ValueError, lambda: h.gr_gated_scan(g, f(n, W + 1), out_y=y), "x: shape")
+    refused(ValueError, lambda: h.gr_gated_scan(g, g, out_y=f(n + 1, W)), "out_y: shape")
+    refused(ValueError, lambda: h.gr_gated_scan(g, g, off=off, out_h=f(S + 1, W)), "out_h: shape")
+    refused(ValueError, lambda: h.gr_gated_scan(g, g, off=off, h0=f(S - 1, W), out_y=y), "h0: shape")
+    refused(ValueError, lambda: h.gr_gated_scan(g, g, off=i(0), out_y=y), "off: 0 elements")
+    refused(ValueError, lambda: h.gr_gated_scan(g[:1].expand(n, W), g, out_y=y), "rows 0 elements apart")
+    refused(TypeError, lambda: h.gr_gated_scan(f(W, n).t(), g, out_y=y), "contiguous rows")
+    refused(TypeError, lambda: h.gr_gated_scan(g, g.half(), out_y=y), "x: need a torch.float32")
+    refused(TypeError, lambda: h.gr_gated_scan(g, g, off=off.long(), out_y=y), "off: need")
+    refused(TypeError, lambda: h.gr_gated_scan(g, g, off=off, out_y=y, h0=st.half()), "h0: need")
+    refused(TypeError, lambda: h.gr_gated_scan(g, g, out_y=both[:, :W]), "out_y: need a contiguous")
+    refused(TypeError, lambda: h.gr_gated_scan(g.double(), g.double(), out_y=y.double()), "float32, bfloat16 or float16")
+    code(-2, lambda: h.gr_gated_scan(f(n + 1, W), f(n + 1, W), out_y=f(n + 1, W)))
+    code(-2, lambda: h.gr_gated_scan(both, both, out_y=both))
+    refused(ValueError, lambda: h.gr_gated_scan_backward(g, g, f(n, W - 1), f(n, W), f(n, W), dy=y), "y: shape")
+    refused(ValueError, lambda: h.gr_gated_scan_backward(g, g, y, f(n, W), f(n, W), off=off, dh=f(n, W)), "dh: shape")
+    refused(TypeError, lambda: h.gr_gated_scan_backward(g, g, y, f(n, W).half(), f(n, W), dy=y), "out_dgate")
+    refused(TypeError, lambda: h.gr_gated_scan_backward(g, g, y, f(n, W), f(n, W), dy=y.half()), "dy: need")
+    code(-1, lambda: h.gr_gated_scan_backward(g, g, None, f(n, W), f(n, W), dy=y))
+    # dropout
+    refused(ValueError, lambda: h.gr_dropout(g, f(n, W + 1), 0.1, 1), "out: shape")
+    refused(ValueError, lambda: h.gr_dropout(g, f(n, W), 0.1, -1), "seed")
+    refused(ValueError, lambda: h.gr_dropout(g, f(n, W), 0.1, 1, offset=1 << 64), "offset")
+    refused(TypeError, lambda: h.gr_dropout(g, f(n, W), 0.1, 1.5))
+    refused(TypeError, lambda: h.gr_dropout(g, f(n, W), 0.1, 1, residual=g.half()), "residual: need")
+    refused(TypeError, lambda: h.gr_dropout(g, f(n, W), 0.1, 1, offset_add=i(1)), "offset_add: need")
+    refused(ValueError, lambda: h.gr_dropout(g, f(n, W), 0.1, 1, offset_add=i(0).long()), "offset_add: 0 elements")
+    refused(TypeError, lambda: h.gr_dropout(both[:, :W], f(n, W), 0.1, 1), "x: need a contiguous")
+    for rate in (-0.1, 1.0, 0.999999, NAN, INF):
+        code(-1, lambda: h.gr_dropout(g, f(n, W), rate, 1))
+    # nothing of that was queued; another device; a closed handle
+    torch.cuda.synchronize()
+    calls = (lambda: h.gr_token_embed(token, f(V, W), f(n, W)), lambda: h.gr_token_embed_backward(token, f(n, W), f(V, W)),
+             lambda: h.gr_gated_scan(g, g, out_y=y), lambda: h.gr_gated_scan_backward(g, g, y, f(n, W), f(n, W), dy=y),
+             lambda: h.gr_dropout(g, y, 0.1, 1))
+    for call in calls:
+        call()
+    h._device, h._at = 1, (h._at[0], 1)
+    for call in calls:
+        refused(ValueError, call, "need the handle's")
+    h._device = 0
+    h.close()
+    for call in calls:
+        code(-1, call)
