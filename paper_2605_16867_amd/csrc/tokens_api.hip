@@ -54,7 +54,10 @@ int gr_tokens_create(gr_tokens** out, int64_t max_tokens, int32_t max_vocab, int
     h->max_tokens = max_tokens;
     h->max_vocab = max_vocab;
     h->max_width = max_width;
-    if (!dev_alloc(&h->order, 4 * (size_t)max_tokens) || !dev_alloc(&h->digits, (size_t)(sort_units(max_tokens) + 1) * kDigits + 1)) {
+    h->n_words = scan_words(max_tokens, max_width);
+    const unsigned first_call[3] = {0, 0, 1};
+    if (!dev_alloc(&h->words, h->n_words) || hipMemset(h->words, 0, h->n_words * sizeof(uint64_t)) != hipSuccess || !dev_alloc(&h->control, 3) ||
+        hipMemcpy(h->control, first_call, sizeof first_call, hipMemcpyHostToDevice) != hipSuccess || !dev_alloc(&h->order, 4 * (size_t)max_tokens) || !dev_alloc(&h->digits, (size_t)(sort_units(max_tokens) + 1) * kDigits + 1)) {
         gr_tokens_destroy(h);
         return GR_ERR_NOMEM;
     }
@@ -67,7 +70,7 @@ int gr_tokens_destroy(gr_tokens* h)
     if (!h) return GR_OK;
     (void)hipDeviceSynchronize();
     int rc = GR_OK;
-    for (void* p : {(void*)h->order, (void*)h->digits})
+    for (void* p : {(void*)h->order, (void*)h->digits, (void*)h->words, (void*)h->control})
         if (p && hipFree(p) != hipSuccess) rc = GR_ERR_HIP;
     delete h;
     return rc;
