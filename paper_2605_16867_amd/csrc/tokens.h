@@ -10,7 +10,8 @@ struct gr_tokens {
     int* order = nullptr;      // [4][max_tokens] tokens and where they stood, before and after a pass of the sort (see embed.hip)
     uint64_t* words = nullptr;      // [n_words] what workgroups of a recurrence tell each other (see scan.hip)
     size_t n_words = 0;
-    unsigned* control = nullptr;      // ticket, workgroups that are done, number of the call
+    uint64_t* control = nullptr;      // its counters
+    int counters = 0;
     int* digits = nullptr;     // [kDigits][units] tokens of each digit in each unit, then those before; behind them those of all units
 };
 
@@ -31,7 +32,9 @@ struct ScanIn {
     int64_t n, n_seq, gate_stride, x_stride, dgate_stride, dx_stride;
     int width;
 };
-constexpr int kScanRun = 8, kScanChannels = 4;      // rows and channels that a lane takes of a tile
+constexpr int kScanRun = 8, kScanChannels = 4, kScanLanesLog = 5;      // rows and channels that a lane takes of a tile; log2 of lanes that share a row
+constexpr int kScanLine = 16;                                           // words from one counter to the next
+int scan_counters(int width);
 size_t scan_words(int64_t n, int width);
 int launch_scan(gr_tokens* h, const ScanIn& in, int dtype, void* y, float* last, hipStream_t s);
 int launch_scan_backward(gr_tokens* h, const ScanIn& in, int dtype, void* dgate, void* dx, float* dh0, hipStream_t s);

@@ -639,3 +639,47 @@ def test_refusals(native, monkeypatch):
     h.close()
     for call in calls:
         code(-1, call)
+
+
+class _Handle(binding.C.Structure):
+    """The first members of a handle."""
+    _fields_ = [("max_tokens", binding.C.c_int64), ("max_vocab", binding.C.c_int), ("max_width", binding.C.c_int), ("order", binding.C.c_void_p),
+                ("words", binding.C.c_void_p), ("n_words", binding.C.c_size_t), ("control", binding.C.c_void_p), ("counters", binding.C.c_int)]
+
+
+def test_the_last_number_of_a_call():
+    """Calls are numbered in 32 bits; after the last number all that they left in the handle is cleared and the first one follows."""
+    n, width, line = 3000, 300, 16
+    rng = np.random.default_rng(8)
+    h, hip = binding.Tokens(n, 1, width), binding.C.CDLL("libamdhip64.so")
+    gate, x = (put(a, torch.float32) for a in inputs(rng, n, width, torch.float32))
+    off = ints([0, 1000, n])
+    want, y = empty(n, width), empty(n, width)
+    h.gr_gated_scan(gate, x, out_y=want, off=off)
+    torch.cuda.synchronize()
+    inside = _Handle.from_address(h._h.value)
+    assert inside.max_tokens == n and inside.max_width == width and inside.counters == 3
+    size = 8 * line * (inside.counters + 1)
+    control = np.zeros(size // 8, dtype=np.uint64)
+
+    def copy(to, source, kind):
+        assert hip.hipMemcpy(binding.C.c_void_p(to), binding.C.c_void_p(source), binding.C.c_size_t(size), kind) == 0
+
+    def as_after(call):
+        """Every counter holds the next call's number and no draw; nothing else is left."""
+        expected = np.zeros_like(control)
+        expected[line::line] = np.uint64(call << 32)
+        return np.array_equal(control, expected)
+
+    copy(control.ctypes.data, inside.control, 2)
+    assert as_after(2)
+    control[line::line] = np.uint64((2 ** 32 - 2) << 32)
+    copy(inside.control, control.ctypes.data, 1)
+    for number in (2 ** 32 - 2, 2 ** 32 - 1, 1, 2):
+        y.fill_(77)
+        h.gr_gated_scan(gate, x, out_y=y, off=off)
+        torch.cuda.synchronize()
+        assert torch.equal(y, want)
+        copy(control.ctypes.data, inside.control, 2)
+        after = number % (2 ** 32 - 1) + 1
+        assert as_after(after)
