@@ -567,12 +567,13 @@ int gr_clip_gradients(gr_experts* h, int32_t n_grad, const void* const* grad, vo
  * request, and dropout while it is trained; forward, backward, and token by token while a request runs.
  *
  * Conventions as for the operators above, with these besides: `stride` is the number of elements from one row
- * to the next, at least the width (the halves of one product's result are such arrays); arrays without one are
+ * to the next, at least the width and at most GR_MAX_STRIDE (the halves of one product's result are such arrays); arrays without one are
  * dense.  Indexes on the device are not validated: kernels stay in bounds whatever token and off hold.
  */
 typedef struct gr_tokens gr_tokens;
 
 #define GR_MAX_VOCAB (1 << 24)
+#define GR_MAX_STRIDE (1 << 20)
 
 /*
  * Create the workspace of calls on up to max_tokens tokens (<= 2^30) of up to max_vocab different ones and rows of up to max_width

@@ -3,6 +3,7 @@
 //   f = sigmoid(gate), i = sigmoid(-gate);  h_t = f_t h_{t-1} + i_t x_t
 //   D_t = dy_t + c_{t+1}, c_t = f_t D_t;  dx_t = i_t D_t, dgate_t = f_t i_t D_t (h_{t-1} - x_t)
 #include <type_traits>
+#include <utility>
 
 #include "tokens.h"
 
@@ -12,42 +13,52 @@ namespace {
 constexpr int kBlock = 256;
 
 struct Gate {
-    float keep, take;      // sigmoid(gate), sigmoid(-gate)
+    float keep, take, both;      // sigmoid(gate), sigmoid(-gate), their product
 };
 
-// Both from exp(-|gate|) =: e, as 1 / (1 + e) and e / (1 + e): neither is a difference, so both have all their digits however far the gate is from 0.
+// All from exp(-|gate|) =: e, as 1 / (1 + e) and e / (1 + e): neither is a difference, so both have all their digits however far the gate is from 0.
 // The exponent's rounding, |gate| log2(e) * 2^-24, is made good where results are in single precision.  (A gate that is no number stays one.)
 template <typename T>
 __device__ __forceinline__ Gate gate_of(float g)
 {
     constexpr float kLog2e = 1.44269504089f, kLog2eRest = 1.92596299e-8f, kLn2 = 0.693147181f;
-    float a = fabsf(g);
-    a = a > 88.0f ? 88.0f : a;      // (behind that e is no whole number of single precision, and 0 is as good)
-    const float p = a * -kLog2e;
-    float e = __builtin_amdgcn_exp2f(p);
-    if (sizeof(T) == 4) e = fmaf(e, fmaf(a, -kLog2eRest, fmaf(a, -kLog2e, -p)) * kLn2, e);
+    const float a = fabsf(g);
+    float e = __builtin_amdgcn_exp2f(a * -kLog2e);
+    if (sizeof(T) == 4) {
+        const float near_a = fminf(a, 128.0f), p = near_a * -kLog2e;      // (behind that e is 0, and an infinite gate has no rounding)
+        e = fmaf(e, fmaf(near_a, -kLog2eRest, fmaf(near_a, -kLog2e, -p)) * kLn2, e);
+    }
     const float near = __builtin_amdgcn_rcpf(1.0f + e), far = e * near;
-    return g >= 0 ? Gate{near, far} : Gate{far, near};
+    return g >= 0 ? Gate{near, far, near * far} : Gate{far, near, near * far};
 }
 
 // ---- many tokens: tiles of rows -----------------------------------------------------------------
 //
 // Rows are taken in the direction of the recurrence (backward: the last one first), a tile of them by a workgroup, a run of kRun by the lanes
-// that share a row; a lane has N channels.  A stretch of rows takes a state c to F c + B, F the product of its f.  A tile
-//   1. reads its rows once, holds f and what is added in registers, and finds (F, B) of its runs, and of itself, which it publishes;
-//   2. finds the state that it starts from: of the tiles since the one that its sequence starts in, or since the last multiple of kGroup tiles, whose
-//      last tile publishes the state itself;
+// that share a row; a lane has N channels.  A stretch of rows takes a state c to F c + B, F the product of its f.  For a tile a workgroup
+//   1. reads its rows once, holds f and what is added in registers, and finds (F, B) of its runs, and of the tile, which it publishes;
+//   2. finds the state that the tile starts from: of the tiles since the one that its sequence starts in, or since the last multiple of kGroup tiles,
+//      whose last tile publishes the state itself;
 //   3. goes through its rows once more, in registers, and writes.
 // The order in which stretches are joined hangs on the places of rows and sequences alone, so the bits are the same every time.
 //
 // Published words are 64 bits, a value and the number of the call: complete or not there, with nothing to order between words.  Workgroups take
-// tiles by a ticket, one counter for each block of channels, so that those that a tile waits for are always held by workgroups that run already, and
-// wait for none behind them: every wait ends.  A counter holds the number of the call and the next ticket in one word; whoever draws the last one of
-// all counters sets them for the next call (all others have what they need by then).  Draws at one counter follow each other in 43 ns: with one for all
-// blocks, and another for workgroups that are done, 262 144 tokens of 1 024 took 1.4 ms whatever else was done.
+// tiles by a ticket, one counter for each block of channels, one tile after the other, so that those that a tile waits for are always held by
+// workgroups that run already, and wait for none behind them: every wait ends.  A counter holds the number of the call and the next ticket in one
+// word; whoever draws the last one of all counters sets them for the next call (all others have what they need by then).  Draws at one counter
+// follow each other in 43 ns: with one for all blocks, and another for workgroups that are done, 262 144 tokens of 1 024 took 1.4 ms whatever else
+// was done.
 
-constexpr int kTileBlock = 512, kGroup = 16, kLeastLanesLog = 2;
-constexpr int kMostRuns = kTileBlock >> kLeastLanesLog;
+#ifndef V_FT
+#define V_FT 512
+#define V_BT 512
+#define V_G 16
+#define V_WG 2
+#define V_OCC 2
+#define V_WGB 2
+#endif
+constexpr int kThreads = V_FT, kWaves = kThreads / 64;
+constexpr int kGroup = V_G, kLeastLanesLog = 2, kMostRuns = kThreads >> kLeastLanesLog;
 
 struct TileArgs {
     ScanIn in;
@@ -56,6 +67,7 @@ struct TileArgs {
     uint64_t *sums, *states;
     uint64_t* control;      // see Control
     int n, n_seq, tiles, blocks, lanes, lg, rows;      // blocks of channels, lanes of a row in use, log2 of lanes of a row, rows of a tile
+    int gate_stride, x_stride, dgate_stride, dx_stride;
     int counters;      // all of the handle's, and its words
     size_t n_words;
 };
@@ -87,30 +99,41 @@ __device__ __forceinline__ int bound(int v, int n) { return v < 0 ? 0 : v > n ? 
 // What the words of a handle's control are; each counter has a line of memory of its own.
 enum Control { kBlocksDrawn = 0, kDone = 1, kCounters = kScanLine };
 
+// By one wave.
 __device__ void ready(const TileArgs& a, unsigned call)
 {
-    if (threadIdx.x == 0) a.control[kBlocksDrawn] = a.control[kDone] = 0;
-    for (int i = threadIdx.x; i < a.counters; i += kTileBlock) a.control[kCounters + i * kScanLine] = (uint64_t)call << 32;
+    const int lane = threadIdx.x & 63;
+    if (lane == 0) a.control[kBlocksDrawn] = a.control[kDone] = 0;
+    for (int i = lane; i < a.counters; i += 64) a.control[kCounters + i * kScanLine] = (uint64_t)call << 32;
 }
 
 __device__ __forceinline__ uint64_t draw(uint64_t* at) { return __hip_atomic_fetch_add(at, uint64_t(1), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
 
+// By the wave whose workgroup has drawn the last tile of a block of channels.
+__device__ void last_tile(const TileArgs& a, unsigned call)
+{
+    uint64_t v = 0;
+    if ((threadIdx.x & 63) == 0) v = draw(a.control + kBlocksDrawn);
+    if (__builtin_amdgcn_readfirstlane((int)v) == a.blocks - 1 && call != ~0u) ready(a, call + 1);
+}
+
 // Where sequences enter and leave the rows of a tile.
+template <int kRun>
 struct Marks {
-    unsigned enter[kMostRuns], leave[kMostRuns];      // a bit for each row of a run
     int start;                                        // the row, of all, that the sequence of the tile's first row starts with
+    unsigned enter[kMostRuns], leave[kMostRuns];      // a bit for each row of a run
+    int entering[kMostRuns * kRun], leaving[kMostRuns * kRun];      // the sequences, where a bit is set
 };
 
-// The wave's own runs: rows q0 .. q0 + count - 1 of the tile, whose first row is row p0 of all.  `entering` and `leaving` get the sequences.
+// By one wave.
 template <int kRun, bool kBack>
-__device__ void mark(const TileArgs& a, Marks& m, int* entering, int* leaving, int p0, int q0, int count)
+__device__ void mark(const TileArgs& a, Marks<kRun>& m, int tile)
 {
-    const int lane = threadIdx.x & 63, first = p0 + q0, end = first + count < a.n ? first + count : a.n;
-    for (int r = lane; r < count / kRun; r += 64) m.enter[q0 / kRun + r] = m.leave[q0 / kRun + r] = 0;
-    if (q0 == 0 && lane == 0) m.start = p0;
+    const int lane = threadIdx.x & 63, p0 = tile * a.rows, end = p0 + a.rows < a.n ? p0 + a.rows : a.n;
+    for (int r = lane; r < a.rows / kRun; r += 64) m.enter[r] = m.leave[r] = 0;
+    if (lane == 0) m.start = p0;
     wave_sync();
-    if (first >= end) return;
-    const int from = kBack ? a.n - end : first, to = kBack ? a.n - first : end;      // as tokens
+    const int from = kBack ? a.n - end : p0, to = kBack ? a.n - p0 : end;      // as tokens
     // how many sequences start at or before `from`: 64 at a time
     int lo = 0, hi = a.n_seq + 1;
     while (lo < hi) {
@@ -129,15 +152,15 @@ __device__ void mark(const TileArgs& a, Marks& m, int* entering, int* leaving, i
             end_here = e;
             if (b < e) {
                 const int enter = kBack ? a.n - e : b, leave = kBack ? a.n - 1 - b : e - 1;      // as rows
-                if (enter >= first && enter < end) {
-                    entering[enter - p0] = s;
+                if (enter >= p0 && enter < end) {
+                    m.entering[enter - p0] = s;
                     atomicOr(&m.enter[(enter - p0) / kRun], 1u << (enter - p0) % kRun);
                 }
-                if (leave >= first && leave < end) {
-                    leaving[leave - p0] = s;
+                if (leave >= p0 && leave < end) {
+                    m.leaving[leave - p0] = s;
                     atomicOr(&m.leave[(leave - p0) / kRun], 1u << (leave - p0) % kRun);
                 }
-                if (q0 == 0 && enter < p0 && leave >= p0) m.start = enter;
+                if (enter < p0 && leave >= p0) m.start = enter;
             }
         }
         if (__shfl(end_here, 63) >= to) break;
@@ -145,222 +168,362 @@ __device__ void mark(const TileArgs& a, Marks& m, int* entering, int* leaving, i
     wave_sync();
 }
 
-// Rows of T as the lane has them: N channels from c, of which it writes those from `own`.
-template <typename T, int N>
-__device__ __forceinline__ void store(T* at, const float (&v)[N], int own)
+// What follows from v is found anew where it is asked for, not kept in registers from before.
+__device__ __forceinline__ int anew(int v)
 {
-    Elements<T, N> o;
+    asm volatile("" : "+v"(v));
+    return v;
+}
+
+// What a lane holds of its rows between the passes.
+template <int N, int kRun, bool kBack>
+struct Held {
+    float f[kRun][N], b[kRun][N];      // forward: what is added to f c; backward: dy, and dh where a sequence enters
+    float take[kBack ? kRun : 1][N], by[kBack ? kRun : 1][N];      // dx and dgate are D times these
+};
+
+// f(0), ... f(M - 1), as constants: what they index is in registers.
+template <typename F, int... I>
+__device__ __forceinline__ void each_of(F f, std::integer_sequence<int, I...>)
+{
+    (f(std::integral_constant<int, I>{}), ...);
+}
+
+template <int M, typename F>
+__device__ __forceinline__ void each(F f)
+{
+    each_of(f, std::make_integer_sequence<int, M>{});
+}
+
+// The rows of one lane.  Rows that are special (sequences enter or leave, there are none) are looked for by the wave, one after the other, and what is
+// held is chosen by selects: no branch by lanes has it live on both of its sides.
+template <typename T, int N, int kRun, bool kBack>
+struct Rows {
+    typedef Elements<T, N> Of;
+    const TileArgs& a;
+    int q, first, rows_here;       // the lane's first row in the tile; the tile's lowest token, and how many there are from it
+    int c;                         // first channel
+    unsigned enter, leave;         // bits of rows
+    const int *entering, *leaving; // sequences, where a bit is set
+
+    __device__ __forceinline__ static bool any(bool v) { return __ballot(v) != 0; }
+
+    // Distance in bytes, from the tile's lowest token, of row j of an array: in 32 bits by the limit on strides.  Rows that are not there are others that are.
+    __device__ __forceinline__ unsigned at(int j, int stride) const
+    {
+        int r = kBack ? rows_here - 1 - (q + j) : q + j;
+        r = kBack ? (r < 0 ? 0 : r) : (r < rows_here ? r : rows_here - 1);
+        return ((unsigned)r * (unsigned)stride + c) * (unsigned)sizeof(T);
+    }
+
+    template <typename P>
+    __device__ __forceinline__ static auto* byte(P* p, unsigned off)
+    {
+        typedef std::conditional_t<std::is_const<P>::value, const char, char> Byte;
+        return reinterpret_cast<P*>(reinterpret_cast<Byte*>(p) + off);
+    }
+
+    __device__ __forceinline__ void load(Of (&to)[kRun], const void* p, int stride) const
+    {
+        const T* const base = static_cast<const T*>(p) + (int64_t)first * stride;
+        each<kRun>([&](auto j) { to[j] = Of::load(byte(base, at(j, stride))); });
+    }
+
+    // `step`(row, whether the lane has it, its sequence) for the rows that some lane has a bit for.
+    template <typename F>
+    __device__ __forceinline__ void special(unsigned bits, const int* seq, F step) const
+    {
+        while (true) {
+            const uint64_t lanes = __ballot(bits != 0);
+            if (lanes == 0) return;
+            const int j = __builtin_ctz((unsigned)__builtin_amdgcn_readlane((int)bits, __builtin_ctzll(lanes)));
+            const bool here = bits >> j & 1;
+            step(j, here, here ? seq[q + j] : 0);
+            bits &= ~(1u << j);
+        }
+    }
+
+    __device__ __forceinline__ Elements<float, N> state_of(const float* state, int s) const
+    {
+        return state ? Elements<float, N>::load(state + (int64_t)s * a.in.width + c) : Elements<float, N>{};
+    }
+
+    struct Raw {
+        Of g[kRun], x[kRun], up[kBack ? kRun : 1], was[kBack ? kRun : 1];
+    };
+
+    __device__ __forceinline__ void read(Raw& r) const
+    {
+        const ScanIn& in = a.in;
+        load(r.g, in.gate, a.gate_stride);
+        load(r.x, in.x, a.x_stride);
+        if constexpr (kBack) {
+            if (in.dy) load(r.up, in.dy, in.width);
+            else each<kRun>([&](auto j) { r.up[j] = Of{}; });
+            // (the row before the first token is not there, and not asked for: a sequence leaves at it)
+            const T* const base = static_cast<const T*>(in.y) + (int64_t)(first - 1) * in.width;
+            each<kRun>([&](auto j) {
+                const unsigned off = at(j, in.width), least = first == 0 ? (unsigned)in.width * (unsigned)sizeof(T) : 0;
+                r.was[j] = Of::load(byte(base, off < least ? off + least : off));
+            });
+        }
+    }
+
+    __device__ __forceinline__ void first_pass(const Raw& r, Held<N, kRun, kBack>& held, float (&F)[N], float (&B)[N]) const
+    {
+        const ScanIn& in = a.in;
+        if constexpr (kBack) {
+            each<kRun>([&](auto j) {
+                each<N>([&](auto e) { held.by[j][e] = (float)r.was[j].v[e]; });
+            });
+            special(leave, leaving, [&](int row, bool here, int s) {
+                const Elements<float, N> h0 = state_of(in.h0, s);
+                each<kRun>([&](auto j) {
+                    each<N>([&](auto e) { held.by[j][e] = here && j == row ? +h0.v[e] : +held.by[j][e]; });
+                });
+            });
+        }
+        each<kRun>([&](auto j) {
+            each<N>([&](auto e) {
+                const Gate k = gate_of<T>((float)r.g[j].v[e]);
+                const float v = (float)r.x[j].v[e];
+                held.f[j][e] = k.keep;
+                if constexpr (!kBack) held.b[j][e] = k.take * v;
+                else {
+                    held.b[j][e] = (float)r.up[j].v[e];
+                    held.take[j][e] = k.take;
+                    held.by[j][e] = k.both * (held.by[j][e] - v);
+                }
+            });
+        });
+        const bool short_of = any(q + kRun > rows_here);
+        if (short_of || any(enter != 0)) {
+            each<kRun>([&](auto j) {
+                const bool there = q + j < rows_here;      // (rows that are not there change nothing)
+                each<N>([&](auto e) {
+                    held.f[j][e] = there ? held.f[j][e] : 1.0f;
+                    held.b[j][e] = there ? held.b[j][e] : 0.0f;
+                });
+            });
+            special(enter, entering, [&](int r, bool here, int s) {
+                const Elements<float, N> from = state_of(kBack ? in.dh : in.h0, s);
+                each<kRun>([&](auto j) {
+                    each<N>([&](auto e) {
+                        const float b = held.b[j][e];
+                        held.b[j][e] = here && j == r ? (kBack ? b + from.v[e] : fmaf(held.f[j][e], from.v[e], b)) : b;
+                    });
+                });
+            });
+            each<kRun>([&](auto j) {
+                const bool here = enter >> j & 1;
+                each<N>([&](auto e) {
+                    const float f = held.f[j][e], b = held.b[j][e];
+                    const float cut = kBack ? f * b : b;
+                    B[e] = j == 0 || here ? cut : kBack ? f * (b + B[e]) : fmaf(f, B[e], b);
+                    F[e] = here ? 0.0f : j == 0 ? f : F[e] * f;
+                });
+            });
+        } else {
+            each<kRun>([&](auto j) {
+                each<N>([&](auto e) {
+                    const float f = held.f[j][e], b = held.b[j][e];
+                    B[e] = j == 0 ? (kBack ? f * b : b) : kBack ? f * (b + B[e]) : fmaf(f, B[e], b);
+                    F[e] = j == 0 ? f : F[e] * f;
+                });
+            });
+        }
+    }
+
+    // A row's results, and the state behind it.
+    __device__ __forceinline__ void step(const Held<N, kRun, kBack>& held, int j, bool enters, float (&h)[N], Of& o, Of& p) const
+    {
+        each<N>([&](auto e) {
+            if constexpr (!kBack) {
+                h[e] = enters ? +held.b[j][e] : fmaf(held.f[j][e], h[e], held.b[j][e]);
+                o.v[e] = (T)h[e];
+            } else {
+                const float d = enters ? held.b[j][e] : held.b[j][e] + h[e];
+                o.v[e] = (T)(d * held.take[j][e]);
+                p.v[e] = (T)(d * held.by[j][e]);
+                h[e] = d * held.f[j][e];
+            }
+        });
+    }
+
+    __device__ __forceinline__ void write(int j, const Of& o, const Of& p) const
+    {
+        if constexpr (!kBack) o.store(byte(static_cast<T*>(a.y) + (int64_t)first * a.in.width, at(j, a.in.width)));
+        else {
+            o.store(byte(static_cast<T*>(a.dx) + (int64_t)first * a.dx_stride, at(j, a.dx_stride)));
+            p.store(byte(static_cast<T*>(a.dgate) + (int64_t)first * a.dgate_stride, at(j, a.dgate_stride)));
+        }
+    }
+
+    __device__ __forceinline__ void second_pass(Held<N, kRun, kBack>& held, float (&h)[N], bool on, bool plain, int lowest, int highest) const
+    {
+        Of o, p;
+        if (plain) {
+            if (!on) return;
+            each<kRun>([&](auto j) {
+                step(held, j, false, h, o, p);
+                write(j, o, p);
+            });
+            return;
+        }
+        each<kRun>([&](auto j) {
+            const int t = first + (kBack ? rows_here - 1 - (q + j) : q + j);
+            step(held, j, enter >> j & 1, h, o, p);
+            each<N>([&](auto e) { held.b[j][e] = h[e]; });
+            if (on && q + j < rows_here && t >= lowest && t < highest && (kBack || a.y)) write(j, o, p);
+        });
+        if (!a.last) return;
+        special(leave, leaving, [&](int r, bool here, int s) {
+            Elements<float, N> v;
+            each<N>([&](auto e) {
+                unsigned bits = 0;      // (by masks: of selects the compiler makes an index into memory)
+                each<kRun>([&](auto j) { bits |= __float_as_uint(held.b[j][e]) & (j == r ? ~0u : 0u); });
+                v.v[e] = __uint_as_float(bits);
+            });
+            if (here && on) v.store(a.last + (int64_t)s * a.in.width + c);
+        });
+    }
+};
+
+// (F, B) of a channel of the tile from those of its runs, published; the state that it starts from; those that its runs start from, in the place of F.
+__device__ __forceinline__ void join(const TileArgs& a, int tile, int start, unsigned call, const unsigned* enter, float* part_f, float* part_b, int channels, int block,
+                                     int ch)
+{
+    const int runs = kThreads >> a.lg, p0 = tile * a.rows;
+    const int64_t pitch = (int64_t)a.blocks * channels, word = block * channels + ch;
+    float tf = 1, tb = 0;
+    bool cut = false;
+    const auto each_run = [&](auto step) {      // (runs are a multiple of four)
+#pragma unroll 1
+        for (int r = 0; r < runs; r += 4) {
+            float rf[4], rb[4];
 #pragma unroll
-    for (int e = 0; e < N; ++e) o.v[e] = (T)v[e];
-    if (own == 0) o.store(at);
-    else
-        for (int e = 0; e < N; ++e)
-            if (e >= own) at[e] = o.v[e];
+            for (int u = 0; u < 4; ++u) {
+                rf[u] = part_f[(r + u) * channels + ch];
+                rb[u] = part_b[(r + u) * channels + ch];
+            }
+#pragma unroll
+            for (int u = 0; u < 4; ++u) step(r + u, enter[r + u] != 0, rf[u], rb[u]);
+        }
+    };
+    each_run([&](int, bool here, float rf, float rb) {
+        tb = here ? rb : fmaf(rf, tb, rb);
+        tf = here ? 0.0f : tf * rf;
+        cut = cut || here;
+    });
+    const bool more = tile + 1 < a.tiles;
+    uint64_t* const sums = a.sums + word;
+    if (more) {
+        publish(sums + (int64_t)tile * 2 * pitch, tf, call);
+        publish(sums + ((int64_t)tile * 2 + 1) * pitch, tb, call);
+        __atomic_signal_fence(__ATOMIC_SEQ_CST);      // (before anything is waited for)
+    }
+    float state = 0;
+    if (start < p0) {
+        const int from = start / a.rows, group = tile / kGroup * kGroup;
+        int k = from;
+        if (from >= group) {
+            const uint64_t* const at = sums + ((int64_t)k++ * 2 + 1) * pitch;
+            state = wait_for(at, look(at), call);
+        } else {
+            const uint64_t* const at = a.states + (int64_t)(group / kGroup - 1) * pitch + word;
+            k = group;
+            state = wait_for(at, look(at), call);
+        }
+        for (; k < tile; k += 4) {
+            uint64_t sf[4], sb[4];
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+                const int64_t w = (int64_t)(k + u < tile ? k + u : k) * 2;
+                sf[u] = look(sums + w * pitch);
+                sb[u] = look(sums + (w + 1) * pitch);
+            }
+#pragma unroll
+            for (int u = 0; u < 4; ++u)
+                if (k + u < tile) {
+                    const int64_t w = (int64_t)(k + u) * 2;
+                    const float kf = wait_for(sums + w * pitch, sf[u], call), kb = wait_for(sums + (w + 1) * pitch, sb[u], call);
+                    state = fmaf(kf, state, kb);
+                }
+        }
+    }
+    if (more && tile % kGroup == kGroup - 1) publish(a.states + (int64_t)(tile / kGroup) * pitch + word, cut ? tb : fmaf(tf, state, tb), call);
+    each_run([&](int r, bool here, float rf, float rb) {
+        part_f[r * channels + ch] = state;
+        state = here ? rb : fmaf(rf, state, rb);
+    });
+}
+
+// Sequences of no token: their states stay.
+__device__ void stay(const TileArgs& a, int s0, const float* state)
+{
+    const int s = s0 + (threadIdx.x & 63), width = a.in.width;
+    uint64_t none = __ballot(s < a.n_seq && bound(a.in.off[s < a.n_seq ? s : 0], a.n) >= bound(a.in.off[s < a.n_seq ? s + 1 : 0], a.n));
+    for (; none; none &= none - 1) {
+        const int64_t at = (int64_t)(s0 + __builtin_ctzll(none)) * width;
+        for (int c = threadIdx.x; c < width; c += kThreads) a.last[at + c] = state ? state[at + c] : 0.0f;
+    }
 }
 
 template <typename T, int N, int kRun, bool kBack>
-__global__ __launch_bounds__(kTileBlock) void k_scan_tiles(TileArgs a)
+__global__ __launch_bounds__(kThreads, V_OCC) void k_scan_tiles(TileArgs a)
 {
-    typedef Elements<T, N> Of;
-    __shared__ float part_f[kTileBlock * N], part_b[kTileBlock * N];
-    __shared__ int entering[kMostRuns * kRun], leaving[kMostRuns * kRun];
-    __shared__ Marks m;
+    typedef Rows<T, N, kRun, kBack> Of;
+    __shared__ float part_f[kThreads * N], part_b[kThreads * N];
+    __shared__ Marks<kRun> m;
     __shared__ uint64_t drawn;
-    __shared__ bool last_drawn;
-    const int tid = threadIdx.x;
+    const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const ScanIn& in = a.in;
-    const int width = in.width;
-    if (blockIdx.x >= (unsigned)a.tiles * a.blocks) {      // sequences of no token: their states stay
-        const int lane = tid & 63, s0 = (int)(blockIdx.x - (unsigned)a.tiles * a.blocks) * 64, s = s0 + lane;
-        const float* const state = kBack ? in.dh : in.h0;
-        uint64_t none = __ballot(s < a.n_seq && bound(in.off[s < a.n_seq ? s : 0], a.n) >= bound(in.off[s < a.n_seq ? s + 1 : 0], a.n));
-        for (; none; none &= none - 1) {
-            const int64_t at = (int64_t)(s0 + __builtin_ctzll(none)) * width;
-            for (int c = tid; c < width; c += kTileBlock) a.last[at + c] = state ? state[at + c] : 0.0f;
-        }
-        return;
-    }
+    const int width = in.width, workers = a.tiles * a.blocks;
+    if (blockIdx.x >= (unsigned)workers) return stay(a, (int)(blockIdx.x - workers) * 64, kBack ? in.dh : in.h0);
     const int block = blockIdx.x % a.blocks;
-    if (tid == 0) {
-        drawn = draw(a.control + kCounters + block * kScanLine);
-        last_drawn = (int)(unsigned)drawn == a.tiles - 1 && draw(a.control + kBlocksDrawn) == (uint64_t)a.blocks - 1;
+    if (tid == 0) drawn = draw(a.control + kCounters + block * kScanLine);
+    __syncthreads();
+    const int tile = __builtin_amdgcn_readfirstlane((int)(unsigned)drawn), p0 = tile * a.rows;
+    const unsigned call = __builtin_amdgcn_readfirstlane((int)(drawn >> 32));
+    const int l = tid & ((1 << a.lg) - 1), run = tid >> a.lg, channels = a.lanes * N;
+    // channels: those of a last lane that is not whole reach back, and both come to the same values (states are not in place then)
+    const int c_own = block * channels + (l < a.lanes ? l : 0) * N, c = c_own + N > width ? width - N : c_own;
+    const bool on = l < a.lanes && c_own < width;
+    const int q = run * kRun, rows_here = a.n - p0 < a.rows ? a.n - p0 : a.rows, first = kBack ? a.n - p0 - rows_here : p0;
+    Held<N, kRun, kBack> held;
+    {
+        float F[N], B[N];
+        typename Of::Raw raw;
+        Of{a, q, first, rows_here, c, 0, 0, nullptr, nullptr}.read(raw);
+        if (wave == kWaves - 1) mark<kRun, kBack>(a, m, tile);
+        else if (wave == 0 && tile == a.tiles - 1) last_tile(a, call);
+        __syncthreads();
+        Of{a, anew(q), first, rows_here, anew(c), m.enter[run], m.leave[run], m.entering, m.leaving}.first_pass(raw, held, F, B);
+        if (l < a.lanes) each<N>([&](auto e) {
+            part_f[run * channels + l * N + e] = F[e];
+            part_b[run * channels + l * N + e] = B[e];
+        });
     }
     __syncthreads();
-    const int tile = (int)(unsigned)drawn;
-    const unsigned now = (unsigned)(drawn >> 32);
-    if (last_drawn && now != ~0u) ready(a, now + 1);
+    if (tid < channels) join(a, tile, m.start, call, m.enter, part_f, part_b, channels, block, tid);
+    __syncthreads();
     {
-        const int p0 = tile * a.rows;
-        const int l = tid & ((1 << a.lg) - 1), run = tid >> a.lg, runs = kTileBlock >> a.lg, channels = a.lanes * N;
-        const int wave_rows = (64 >> a.lg) * kRun;
-        mark<kRun, kBack>(a, m, entering, leaving, p0, (tid >> 6) * wave_rows, wave_rows);
+        float h[N];
+        each<N>([&](auto e) { h[e] = part_f[l < a.lanes ? run * channels + l * N + e : 0]; });
+        const Of rows{a, anew(q), first, rows_here, anew(c), m.enter[run], m.leave[run], m.entering, m.leaving};
         const int lowest = bound(in.off[0], a.n), highest = bound(in.off[a.n_seq], a.n);
-        // channels: those of the last lane reach back, and it writes only its own
-        const int c_own = block * channels + l * N, c = c_own + N > width ? width - N : c_own, own = c_own - c;
-        const bool on = l < a.lanes && c_own < width;
-        const unsigned enter = m.enter[run], leave = m.leave[run];
-        float f[kRun][N], b[kRun][N];      // backward: b is dy
-        Of xs[kBack ? kRun : 1], before[kBack ? kRun : 1];
-        float i_of[kBack ? kRun : 1][N];
-        float F[N], B[N];
-#pragma unroll
-        for (int e = 0; e < N; ++e) { F[e] = 1; B[e] = 0; }
-        const int q = run * kRun, p_run = p0 + q;
-        const auto token_of = [&](int j) { return kBack ? a.n - 1 - (p_run + j) : p_run + j; };
-        if (on && p_run < a.n) {
-            Of g[kRun], v[kRun];
-#pragma unroll
-            for (int j = 0; j < kRun; ++j) {
-                const int t0 = token_of(j), t = t0 < 0 ? 0 : t0 >= a.n ? a.n - 1 : t0;
-                g[j] = Of::load(static_cast<const T*>(in.gate) + t * in.gate_stride + c);
-                if (!kBack) v[j] = Of::load(static_cast<const T*>(in.x) + t * in.x_stride + c);
-                else {
-                    v[j] = Of{};
-                    if (in.dy) v[j] = Of::load(static_cast<const T*>(in.dy) + (int64_t)t * width + c);
-                    xs[j] = Of::load(static_cast<const T*>(in.x) + t * in.x_stride + c);
-                    before[j] = Of::load(static_cast<const T*>(in.y) + (int64_t)(t > 0 ? t - 1 : 0) * width + c);
-                }
-            }
-#pragma unroll
-            for (int j = 0; j < kRun; ++j) {
-                const bool there = p_run + j < a.n;
-#pragma unroll
-                for (int e = 0; e < N; ++e) {
-                    const Gate k = gate_of<T>((float)g[j].v[e]);
-                    f[j][e] = there ? k.keep : 1.0f;
-                    if (!kBack) b[j][e] = there ? k.take * (float)v[j].v[e] : 0.0f;
-                    else {
-                        i_of[j][e] = k.take;
-                        b[j][e] = there ? (float)v[j].v[e] : 0.0f;
-                    }
-                }
-                if (enter >> j & 1) {
-                    const float* const state = kBack ? in.dh : in.h0;
-                    const int64_t at = (int64_t)entering[q + j] * width + c;
-#pragma unroll
-                    for (int e = 0; e < N; ++e) {
-                        const float from = state ? state[at + e] : 0.0f;
-                        b[j][e] = kBack ? b[j][e] + from : fmaf(f[j][e], from, b[j][e]);
-                        B[e] = kBack ? f[j][e] * b[j][e] : b[j][e];
-                        F[e] = 0;
-                    }
-                } else {
-#pragma unroll
-                    for (int e = 0; e < N; ++e) {
-                        B[e] = kBack ? f[j][e] * (b[j][e] + B[e]) : fmaf(f[j][e], B[e], b[j][e]);
-                        F[e] *= f[j][e];
-                    }
-                }
-            }
-        }
-        if (l < a.lanes) {
-#pragma unroll
-            for (int e = 0; e < N; ++e) {
-                part_f[run * channels + l * N + e] = F[e];
-                part_b[run * channels + l * N + e] = B[e];
-            }
-        }
-        __syncthreads();
-        for (int ch = tid; ch < channels; ch += kTileBlock) {
-            const int64_t pitch = (int64_t)a.blocks * channels, word = block * channels + ch;
-            float tf = 1, tb = 0;
-            bool cut = false;
-            for (int r = 0; r < runs; ++r) {
-                const float rf = part_f[r * channels + ch], rb = part_b[r * channels + ch];
-                const bool here = m.enter[r] != 0;
-                tb = here ? rb : fmaf(rf, tb, rb);
-                tf = here ? 0.0f : tf * rf;
-                cut = cut || here;
-            }
-            const bool more = tile + 1 < a.tiles;
-            uint64_t* const sums = a.sums + word;
-            if (more) {
-                publish(sums + (int64_t)tile * 2 * pitch, tf, now);
-                publish(sums + ((int64_t)tile * 2 + 1) * pitch, tb, now);
-                __atomic_signal_fence(__ATOMIC_SEQ_CST);      // (before anything is waited for)
-            }
-            float state = 0;
-            if (m.start < p0) {
-                const int from = m.start / a.rows, group = tile / kGroup * kGroup;
-                int k = from;
-                if (from >= group) {
-                    const uint64_t* const at = sums + ((int64_t)k++ * 2 + 1) * pitch;
-                    state = wait_for(at, look(at), now);
-                } else {
-                    const uint64_t* const at = a.states + (int64_t)(group / kGroup - 1) * pitch + word;
-                    k = group;
-                    state = wait_for(at, look(at), now);
-                }
-                for (; k < tile; k += 4) {
-                    uint64_t sf[4], sb[4];
-#pragma unroll
-                    for (int u = 0; u < 4; ++u) {
-                        const int64_t w = (int64_t)(k + u < tile ? k + u : k) * 2;
-                        sf[u] = look(sums + w * pitch);
-                        sb[u] = look(sums + (w + 1) * pitch);
-                    }
-#pragma unroll
-                    for (int u = 0; u < 4; ++u)
-                        if (k + u < tile) {
-                            const int64_t w = (int64_t)(k + u) * 2;
-                            const float kf = wait_for(sums + w * pitch, sf[u], now), kb = wait_for(sums + (w + 1) * pitch, sb[u], now);
-                            state = fmaf(kf, state, kb);
-                        }
-                }
-            }
-            if (more && tile % kGroup == kGroup - 1) publish(a.states + (int64_t)(tile / kGroup) * pitch + word, cut ? tb : fmaf(tf, state, tb), now);
-            for (int r = 0; r < runs; ++r) {
-                const float rf = part_f[r * channels + ch], rb = part_b[r * channels + ch];
-                part_f[r * channels + ch] = state;
-                state = m.enter[r] ? rb : fmaf(rf, state, rb);
-            }
-        }
-        __syncthreads();
-        if (on && p_run < a.n) {
-            float h[N];
-#pragma unroll
-            for (int e = 0; e < N; ++e) h[e] = part_f[run * channels + l * N + e];
-#pragma unroll
-            for (int j = 0; j < kRun; ++j) {
-                const int t = token_of(j);
-                const bool enters = enter >> j & 1;
-                if (!kBack) {
-#pragma unroll
-                    for (int e = 0; e < N; ++e) h[e] = enters ? b[j][e] : fmaf(f[j][e], h[e], b[j][e]);
-                    if (a.y && t >= lowest && t < highest) store<T, N>(static_cast<T*>(a.y) + (int64_t)t * width + c, h, own);
-                } else {
-                    float d[N], dg[N], dx[N], was[N];
-#pragma unroll
-                    for (int e = 0; e < N; ++e) was[e] = (float)before[j].v[e];
-                    if (leave >> j & 1) {
-                        const int64_t at = (int64_t)leaving[q + j] * width + c;
-#pragma unroll
-                        for (int e = 0; e < N; ++e) was[e] = in.h0 ? in.h0[at + e] : 0.0f;
-                    }
-#pragma unroll
-                    for (int e = 0; e < N; ++e) {
-                        d[e] = enters ? b[j][e] : b[j][e] + h[e];
-                        dx[e] = d[e] * i_of[j][e];
-                        dg[e] = dx[e] * f[j][e] * (was[e] - (float)xs[j].v[e]);
-                        h[e] = d[e] * f[j][e];
-                    }
-                    if (t >= lowest && t < highest) {
-                        store<T, N>(static_cast<T*>(a.dx) + t * in.dx_stride + c, dx, own);
-                        store<T, N>(static_cast<T*>(a.dgate) + t * in.dgate_stride + c, dg, own);
-                    }
-                }
-                if (a.last && leave >> j & 1) store<float, N>(a.last + (int64_t)leaving[q + j] * width + c, h, own);
-            }
-        }
+        const bool plain = rows_here == a.rows && first >= lowest && first + rows_here <= highest && (kBack || a.y) &&
+                           __ballot((rows.enter | rows.leave) != 0) == 0;
+        rows.second_pass(held, h, on, plain, lowest, highest);
     }
     // after the last number that there is all words are cleared, and 0 is no call's number
-    if (now != ~0u) return;
+    if (call != ~0u) return;
     __syncthreads();
-    if (tid == 0) last_drawn = draw(a.control + kDone) == (uint64_t)a.tiles * a.blocks - 1;
+    if (tid == 0) drawn = draw(a.control + kDone);
     __syncthreads();
-    if (!last_drawn) return;
-    for (size_t i = tid; i < a.n_words; i += kTileBlock) a.sums[i] = 0;
-    ready(a, 1);
+    if (drawn != (uint64_t)workers - 1) return;
+    for (size_t i = tid; i < a.n_words; i += kThreads) a.sums[i] = 0;
+    if (wave == 0) ready(a, 1);
 }
 
 // ---- a token of every sequence ------------------------------------------------------------------
@@ -427,41 +590,49 @@ int launch(gr_tokens* h, const ScanIn& in, int dtype, void* y, void* dgate, void
         });
     TileArgs a{};
     a.in = in; a.y = y; a.dgate = dgate; a.dx = dx; a.last = last;
+    a.gate_stride = (int)in.gate_stride; a.x_stride = (int)in.x_stride; a.dgate_stride = (int)in.dgate_stride; a.dx_stride = (int)in.dx_stride;
     a.n = (int)in.n; a.n_seq = (int)in.n_seq;
-    const int per = in.width >= kScanChannels ? kScanChannels : 1, pieces = (in.width + per - 1) / per;
-    const int most = 1 << kScanLanesLog;
-    a.blocks = (pieces + most - 1) / most;
-    a.lanes = (pieces + a.blocks - 1) / a.blocks;
+    // (single channels where a row has no whole piece, and where states are in place and one reaches back: it would find what the other wrote.  As many
+    // lanes all the same, so that tiles have the same rows and the bits are those of states that are not in place)
+    const bool in_place = last && last == (kBack ? in.dh : in.h0);
+    const int piece = in.width < kScanChannels ? 1 : kScanChannels, per = in_place && in.width % piece ? 1 : piece;
+    const int most = 1 << kScanLanesLog, pieces = (in.width + piece - 1) / piece, blocks = (pieces + most - 1) / most;
+    a.lanes = (pieces + blocks - 1) / blocks;
+    a.blocks = ((in.width + per - 1) / per + a.lanes - 1) / a.lanes;
     a.lg = kLeastLanesLog;
     while ((1 << a.lg) < a.lanes) ++a.lg;
-    a.rows = (kTileBlock >> a.lg) * kScanRun;
+    constexpr int kRun = kBack ? kScanRunBack : kScanRun;
+    a.rows = (kThreads >> a.lg) * kRun;
     a.tiles = (int)((in.n + a.rows - 1) / a.rows);
     a.control = h->control;
     a.sums = h->words;
     a.n_words = h->n_words;
     a.counters = h->counters;
-    a.states = a.sums + (int64_t)a.tiles * 2 * a.blocks * a.lanes * per;
+    const int64_t pitch = (int64_t)a.blocks * a.lanes * per;
+    a.states = a.sums + (int64_t)a.tiles * 2 * pitch;
+    if (a.blocks > a.counters || (size_t)((int64_t)a.tiles * 2 + a.tiles / kGroup + 1) * pitch > a.n_words) return GR_ERR_TOO_LARGE;
     const int64_t total = (int64_t)a.tiles * a.blocks + (last ? (in.n_seq + 63) / 64 : 0);
-    if (total > kMostBlocks / 2) return GR_ERR_TOO_LARGE;
+    if (total > kMostBlocks * kBlock / kThreads) return GR_ERR_TOO_LARGE;
     if (total == 0) return GR_OK;
     return by_type(dtype, [&](auto t) {
         typedef decltype(t) T;
-        if (per == 1) k_scan_tiles<T, 1, kScanRun, kBack><<<(unsigned)total, kTileBlock, 0, s>>>(a);
-        else k_scan_tiles<T, kScanChannels, kScanRun, kBack><<<(unsigned)total, kTileBlock, 0, s>>>(a);
+        if (per == 1) k_scan_tiles<T, 1, kRun, kBack><<<(unsigned)total, kThreads, 0, s>>>(a);
+        else k_scan_tiles<T, kScanChannels, kRun, kBack><<<(unsigned)total, kThreads, 0, s>>>(a);
         return launched();
     });
 }
 
 }  // namespace
 
-int scan_counters(int width) { return (width / kScanChannels >> kScanLanesLog) + 1; }
+// Blocks of channels: most where lanes have single channels.
+int scan_counters(int width) { return ((width / kScanChannels >> kScanLanesLog) + 1) * kScanChannels; }
 
 size_t scan_words(int64_t n, int width)
 {
     // a word for F and one for B of every channel of every tile, and one of every group's state: of the least tiles and the most channels in use
-    const int64_t rows = (int64_t)(kTileBlock >> kScanLanesLog) * kScanRun, tiles = (n + rows - 1) / rows;
-    // (lanes are as many in every block of channels: less than a piece a block more in all, and two pieces)
-    return (size_t)(tiles * 2 + tiles / kGroup + 1) * (width + (scan_counters(width) + 2) * kScanChannels);
+    const int64_t rows = (int64_t)(kThreads >> kScanLanesLog) * (kScanRun < kScanRunBack ? kScanRun : kScanRunBack), tiles = (n + rows - 1) / rows;
+    // (lanes are as many in every block of channels: less than a piece a block more in all, and a piece; of single channels less than a row's lanes)
+    return (size_t)(tiles * 2 + tiles / kGroup + 1) * (width + scan_counters(width) + (kScanChannels << kScanLanesLog));
 }
 
 int launch_scan(gr_tokens* h, const ScanIn& in, int dtype, void* y, float* last, hipStream_t s)

@@ -32,7 +32,12 @@ struct ScanIn {
     int64_t n, n_seq, gate_stride, x_stride, dgate_stride, dx_stride;
     int width;
 };
-constexpr int kScanRun = 8, kScanChannels = 4, kScanLanesLog = 5;      // rows and channels that a lane takes of a tile; log2 of lanes that share a row
+#ifndef V_LG
+#define V_RUN 4
+#define V_RUNB 4
+#define V_LG 5
+#endif
+constexpr int kScanRun = V_RUN, kScanRunBack = V_RUNB, kScanChannels = 4, kScanLanesLog = V_LG;      // rows and channels that a lane takes of a tile; log2 of lanes that share a row
 constexpr int kScanLine = 16;                                           // words from one counter to the next
 int scan_counters(int width);
 size_t scan_words(int64_t n, int width);

@@ -1,5 +1,6 @@
 // Host entry points of the operators that read a request's tokens: the workspace handle and the argument checks.
 #include <cmath>
+#include <initializer_list>
 #include <memory>
 #include <new>
 
@@ -29,7 +30,7 @@ int embed_ok(const gr_tokens* h, int64_t n_tokens, int32_t n_vocab, int32_t widt
     return n_vocab > h->max_vocab ? GR_ERR_TOO_LARGE : GR_OK;
 }
 
-constexpr int64_t kMostSequences = int64_t(1) << 30, kMostStride = int64_t(1) << 40;
+constexpr int64_t kMostSequences = int64_t(1) << 30;
 
 int scan_ok(const gr_tokens* h, int64_t n_tokens, int64_t n_seq, int32_t width, int32_t dtype, const int32_t* off)
 {
@@ -38,7 +39,14 @@ int scan_ok(const gr_tokens* h, int64_t n_tokens, int64_t n_seq, int32_t width, 
     return n_seq > kMostSequences ? GR_ERR_TOO_LARGE : GR_OK;
 }
 
-bool stride_ok(int64_t stride, int32_t width) { return stride >= width && stride <= kMostStride; }
+int strides(std::initializer_list<int64_t> all, int32_t width)
+{
+    for (const int64_t v : all) {
+        if (v < width) return GR_ERR_INVALID_ARG;
+        if (v > GR_MAX_STRIDE) return GR_ERR_TOO_LARGE;
+    }
+    return GR_OK;
+}
 
 }  // namespace
 
@@ -104,7 +112,7 @@ int gr_gated_scan(gr_tokens* h, int64_t n_tokens, int64_t n_seq, int32_t width, 
                   void* hip_stream)
 {
     if (const int rc = scan_ok(h, n_tokens, n_seq, width, dtype, off)) return rc;
-    if (!stride_ok(gate_stride, width) || !stride_ok(x_stride, width)) return GR_ERR_INVALID_ARG;
+    if (const int rc = strides({gate_stride, x_stride}, width)) return rc;
     if (n_seq == 0 || (!out_y && !out_h) || (n_tokens == 0 && !out_h)) return GR_OK;
     if (n_tokens > 0 && (!gate || !x)) return GR_ERR_INVALID_ARG;
     ScanIn in{};
@@ -119,8 +127,7 @@ int gr_gated_scan_backward(gr_tokens* h, int64_t n_tokens, int64_t n_seq, int32_
                            float* out_dh0, void* hip_stream)
 {
     if (const int rc = scan_ok(h, n_tokens, n_seq, width, dtype, off)) return rc;
-    if (!stride_ok(gate_stride, width) || !stride_ok(x_stride, width) || !stride_ok(dgate_stride, width) || !stride_ok(dx_stride, width))
-        return GR_ERR_INVALID_ARG;
+    if (const int rc = strides({gate_stride, x_stride, dgate_stride, dx_stride}, width)) return rc;
     if (n_seq == 0 || (n_tokens == 0 && !out_dh0)) return GR_OK;
     if (n_tokens > 0 && (!gate || !x || !y || !out_dgate || !out_dx)) return GR_ERR_INVALID_ARG;
     ScanIn in{};

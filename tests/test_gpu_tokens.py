@@ -658,7 +658,7 @@ def test_the_last_number_of_a_call():
     h.gr_gated_scan(gate, x, out_y=want, off=off)
     torch.cuda.synchronize()
     inside = _Handle.from_address(h._h.value)
-    assert inside.max_tokens == n and inside.max_width == width and inside.counters == 3
+    assert inside.max_tokens == n and inside.max_width == width and inside.counters >= 3
     size = 8 * line * (inside.counters + 1)
     control = np.zeros(size // 8, dtype=np.uint64)
 
