@@ -608,7 +608,8 @@ int gr_token_embed_backward(gr_tokens* h, int64_t n_tokens, int32_t n_vocab, int
  *   gate, x     DEVICE dtype[n_tokens, width], rows gate_stride and x_stride apart
  *   h0          DEVICE float[n_seq, width], the states that sequences start from; NULL: 0
  *   out_y       DEVICE dtype[n_tokens, width]; rows of no sequence are left as they are.  May be NULL
- *   out_h       DEVICE float[n_seq, width], the states after the last tokens, h0 for a sequence of none.  May be NULL, may be h0 itself
+ *   out_h       DEVICE float[n_seq, width], the states after the last tokens, h0 for a sequence of none.  May be NULL; may be h0 itself
+ *               where off is NULL
  */
 int gr_gated_scan(gr_tokens* h, int64_t n_tokens, int64_t n_seq, int32_t width, int32_t dtype, const int32_t* off,
                   const void* gate, int64_t gate_stride, const void* x, int64_t x_stride, const float* h0, void* out_y, float* out_h,
@@ -621,7 +622,7 @@ int gr_gated_scan(gr_tokens* h, int64_t n_tokens, int64_t n_seq, int32_t width, 
  *   y           DEVICE dtype[n_tokens, width], as gr_gated_scan gave it; h_{t-1} is taken from it as it was rounded
  *   dy          DEVICE dtype[n_tokens, width];  dh DEVICE float[n_seq, width]
  *   out_dgate, out_dx   DEVICE dtype[n_tokens, width], rows dgate_stride and dx_stride apart; rows of no sequence are left as they are
- *   out_dh0     DEVICE float[n_seq, width]; may be NULL, may be dh itself
+ *   out_dh0     DEVICE float[n_seq, width]; may be NULL; may be dh itself where off is NULL
  */
 int gr_gated_scan_backward(gr_tokens* h, int64_t n_tokens, int64_t n_seq, int32_t width, int32_t dtype, const int32_t* off,
                            const void* gate, int64_t gate_stride, const void* x, int64_t x_stride, const void* y, const float* h0,

@@ -13,13 +13,14 @@ namespace {
 constexpr int kBlock = 256;
 
 struct Gate {
-    float keep, take, both;      // sigmoid(gate), sigmoid(-gate), their product
+    float keep, take;      // sigmoid(gate), sigmoid(-gate)
 };
 
-// All from exp(-|gate|) =: e, as 1 / (1 + e) and e / (1 + e): neither is a difference, so both have all their digits however far the gate is from 0.
-// The exponent's rounding, |gate| log2(e) * 2^-24, is made good where results are in single precision.  (A gate that is no number stays one.)
+// The smaller of a gate's two sigmoids, with the gate's sign: from exp(-|gate|) =: e as e / (1 + e), no difference, so it has all its digits however far
+// the gate is from 0; the larger one is what it leaves of 1.  The exponent's rounding, |gate| log2(e) * 2^-24, is made good where results are in
+// single precision.  (A gate that is no number stays one.)
 template <typename T>
-__device__ __forceinline__ Gate gate_of(float g)
+__device__ __forceinline__ float smaller_of(float g)
 {
     constexpr float kLog2e = 1.44269504089f, kLog2eRest = 1.92596299e-8f, kLn2 = 0.693147181f;
     const float a = fabsf(g);
@@ -28,8 +29,13 @@ __device__ __forceinline__ Gate gate_of(float g)
         const float near_a = fminf(a, 128.0f), p = near_a * -kLog2e;      // (behind that e is 0, and an infinite gate has no rounding)
         e = fmaf(e, fmaf(near_a, -kLog2eRest, fmaf(near_a, -kLog2e, -p)) * kLn2, e);
     }
-    const float near = __builtin_amdgcn_rcpf(1.0f + e), far = e * near;
-    return g >= 0 ? Gate{near, far, near * far} : Gate{far, near, near * far};
+    return copysignf(e * __builtin_amdgcn_rcpf(1.0f + e), g);
+}
+
+__device__ __forceinline__ Gate gate_of(float smaller)
+{
+    const float s = fabsf(smaller), rest = 1.0f - s;
+    return __float_as_int(smaller) >= 0 ? Gate{rest, s} : Gate{s, rest};
 }
 
 // ---- many tokens: tiles of rows -----------------------------------------------------------------
@@ -178,8 +184,8 @@ __device__ __forceinline__ int anew(int v)
 // What a lane holds of its rows between the passes.
 template <int N, int kRun, bool kBack>
 struct Held {
-    float f[kRun][N], b[kRun][N];      // forward: what is added to f c; backward: dy, and dh where a sequence enters
-    float take[kBack ? kRun : 1][N], by[kBack ? kRun : 1][N];      // dx and dgate are D times these
+    float f[kRun][N], b[kRun][N];           // forward: what the state is multiplied with, and what is added; backward: the smaller sigmoid, and dy
+    float by[kBack ? kRun : 1][N];          // dgate is D times this
 };
 
 // f(0), ... f(M - 1), as constants: what they index is in registers.
@@ -195,11 +201,12 @@ __device__ __forceinline__ void each(F f)
     each_of(f, std::make_integer_sequence<int, M>{});
 }
 
-// The rows of one lane.  Rows that are special (sequences enter or leave, there are none) are looked for by the wave, one after the other, and what is
-// held is chosen by selects: no branch by lanes has it live on both of its sides.
+// The rows of one lane.  Whether sequences enter or leave at a row, or rows are not there, is asked for the wave; lanes choose by selects: no branch by
+// lanes has what is held live on both of its sides.
 template <typename T, int N, int kRun, bool kBack>
 struct Rows {
     typedef Elements<T, N> Of;
+    typedef Elements<float, N> State;
     const TileArgs& a;
     int q, first, rows_here;       // the lane's first row in the tile; the tile's lowest token, and how many there are from it
     int c;                         // first channel
@@ -229,23 +236,10 @@ struct Rows {
         each<kRun>([&](auto j) { to[j] = Of::load(byte(base, at(j, stride))); });
     }
 
-    // `step`(row, whether the lane has it, its sequence) for the rows that some lane has a bit for.
-    template <typename F>
-    __device__ __forceinline__ void special(unsigned bits, const int* seq, F step) const
+    // The state of row j's sequence; the first one's for lanes that have no mark there.
+    __device__ __forceinline__ State state_of(const float* state, const int* seq, bool here, int j) const
     {
-        while (true) {
-            const uint64_t lanes = __ballot(bits != 0);
-            if (lanes == 0) return;
-            const int j = __builtin_ctz((unsigned)__builtin_amdgcn_readlane((int)bits, __builtin_ctzll(lanes)));
-            const bool here = bits >> j & 1;
-            step(j, here, here ? seq[q + j] : 0);
-            bits &= ~(1u << j);
-        }
-    }
-
-    __device__ __forceinline__ Elements<float, N> state_of(const float* state, int s) const
-    {
-        return state ? Elements<float, N>::load(state + (int64_t)s * a.in.width + c) : Elements<float, N>{};
+        return state ? State::load(state + (int64_t)(here ? seq[q + j] : 0) * a.in.width + c) : State{};
     }
 
     struct Raw {
@@ -272,119 +266,92 @@ struct Rows {
     __device__ __forceinline__ void first_pass(const Raw& r, Held<N, kRun, kBack>& held, float (&F)[N], float (&B)[N]) const
     {
         const ScanIn& in = a.in;
-        if constexpr (kBack) {
-            each<kRun>([&](auto j) {
-                each<N>([&](auto e) { held.by[j][e] = (float)r.was[j].v[e]; });
-            });
-            special(leave, leaving, [&](int row, bool here, int s) {
-                const Elements<float, N> h0 = state_of(in.h0, s);
-                each<kRun>([&](auto j) {
-                    each<N>([&](auto e) { held.by[j][e] = here && j == row ? +h0.v[e] : +held.by[j][e]; });
-                });
-            });
-        }
+        const bool some_missing = rows_here < a.rows;
         each<kRun>([&](auto j) {
+            float before[N] = {};
+            if constexpr (kBack) {
+                const bool here = leave >> j & 1;
+                each<N>([&](auto e) { before[e] = (float)r.was[j].v[e]; });
+                if (any(here)) {
+                    const State h0 = state_of(in.h0, leaving, here, j);
+                    each<N>([&](auto e) { before[e] = here ? +h0.v[e] : +before[e]; });
+                }
+            }
+            float f[N];
+            const bool there = !some_missing || q + j < rows_here;
             each<N>([&](auto e) {
-                const Gate k = gate_of<T>((float)r.g[j].v[e]);
-                const float v = (float)r.x[j].v[e];
-                held.f[j][e] = k.keep;
+                const float smaller = smaller_of<T>((float)r.g[j].v[e]), v = (float)r.x[j].v[e];
+                const Gate k = gate_of(smaller);
+                f[e] = k.keep;
                 if constexpr (!kBack) held.b[j][e] = k.take * v;
                 else {
+                    held.f[j][e] = smaller;
                     held.b[j][e] = (float)r.up[j].v[e];
-                    held.take[j][e] = k.take;
-                    held.by[j][e] = k.both * (held.by[j][e] - v);
+                    held.by[j][e] = k.keep * k.take * (before[e] - v);
                 }
             });
-        });
-        const bool short_of = any(q + kRun > rows_here);
-        if (short_of || any(enter != 0)) {
-            each<kRun>([&](auto j) {
-                const bool there = q + j < rows_here;      // (rows that are not there change nothing)
+            if (some_missing)      // rows that are not there change nothing (and nothing is written for them)
                 each<N>([&](auto e) {
-                    held.f[j][e] = there ? held.f[j][e] : 1.0f;
-                    held.b[j][e] = there ? held.b[j][e] : 0.0f;
+                    f[e] = there ? +f[e] : 1.0f;
+                    held.b[j][e] = there ? +held.b[j][e] : 0.0f;
                 });
-            });
-            special(enter, entering, [&](int r, bool here, int s) {
-                const Elements<float, N> from = state_of(kBack ? in.dh : in.h0, s);
-                each<kRun>([&](auto j) {
-                    each<N>([&](auto e) {
-                        const float b = held.b[j][e];
-                        held.b[j][e] = here && j == r ? (kBack ? b + from.v[e] : fmaf(held.f[j][e], from.v[e], b)) : b;
-                    });
-                });
-            });
-            each<kRun>([&](auto j) {
-                const bool here = enter >> j & 1;
+            if constexpr (!kBack) each<N>([&](auto e) { held.f[j][e] = f[e]; });
+            if (j == 0) each<N>([&](auto e) { F[e] = 1.0f; B[e] = 0.0f; });
+            const bool here = enter >> j & 1;
+            if (any(here)) {
+                const State from = state_of(kBack ? in.dh : in.h0, entering, here, j);
                 each<N>([&](auto e) {
-                    const float f = held.f[j][e], b = held.b[j][e];
-                    const float cut = kBack ? f * b : b;
-                    B[e] = j == 0 || here ? cut : kBack ? f * (b + B[e]) : fmaf(f, B[e], b);
-                    F[e] = here ? 0.0f : j == 0 ? f : F[e] * f;
+                    B[e] = here ? +from.v[e] : +B[e];
+                    F[e] = here ? 0.0f : +F[e];
                 });
-            });
-        } else {
-            each<kRun>([&](auto j) {
-                each<N>([&](auto e) {
-                    const float f = held.f[j][e], b = held.b[j][e];
-                    B[e] = j == 0 ? (kBack ? f * b : b) : kBack ? f * (b + B[e]) : fmaf(f, B[e], b);
-                    F[e] = j == 0 ? f : F[e] * f;
-                });
-            });
-        }
-    }
-
-    // A row's results, and the state behind it.
-    __device__ __forceinline__ void step(const Held<N, kRun, kBack>& held, int j, bool enters, float (&h)[N], Of& o, Of& p) const
-    {
-        each<N>([&](auto e) {
-            if constexpr (!kBack) {
-                h[e] = enters ? +held.b[j][e] : fmaf(held.f[j][e], h[e], held.b[j][e]);
-                o.v[e] = (T)h[e];
-            } else {
-                const float d = enters ? held.b[j][e] : held.b[j][e] + h[e];
-                o.v[e] = (T)(d * held.take[j][e]);
-                p.v[e] = (T)(d * held.by[j][e]);
-                h[e] = d * held.f[j][e];
             }
-        });
-    }
-
-    __device__ __forceinline__ void write(int j, const Of& o, const Of& p) const
-    {
-        if constexpr (!kBack) o.store(byte(static_cast<T*>(a.y) + (int64_t)first * a.in.width, at(j, a.in.width)));
-        else {
-            o.store(byte(static_cast<T*>(a.dx) + (int64_t)first * a.dx_stride, at(j, a.dx_stride)));
-            p.store(byte(static_cast<T*>(a.dgate) + (int64_t)first * a.dgate_stride, at(j, a.dgate_stride)));
-        }
-    }
-
-    __device__ __forceinline__ void second_pass(Held<N, kRun, kBack>& held, float (&h)[N], bool on, bool plain, int lowest, int highest) const
-    {
-        Of o, p;
-        if (plain) {
-            if (!on) return;
-            each<kRun>([&](auto j) {
-                step(held, j, false, h, o, p);
-                write(j, o, p);
-            });
-            return;
-        }
-        each<kRun>([&](auto j) {
-            const int t = first + (kBack ? rows_here - 1 - (q + j) : q + j);
-            step(held, j, enter >> j & 1, h, o, p);
-            each<N>([&](auto e) { held.b[j][e] = h[e]; });
-            if (on && q + j < rows_here && t >= lowest && t < highest && (kBack || a.y)) write(j, o, p);
-        });
-        if (!a.last) return;
-        special(leave, leaving, [&](int r, bool here, int s) {
-            Elements<float, N> v;
             each<N>([&](auto e) {
-                unsigned bits = 0;      // (by masks: of selects the compiler makes an index into memory)
-                each<kRun>([&](auto j) { bits |= __float_as_uint(held.b[j][e]) & (j == r ? ~0u : 0u); });
-                v.v[e] = __uint_as_float(bits);
+                B[e] = kBack ? f[e] * (held.b[j][e] + B[e]) : fmaf(f[e], B[e], held.b[j][e]);
+                F[e] *= f[e];
             });
-            if (here && on) v.store(a.last + (int64_t)s * a.in.width + c);
+        });
+    }
+
+    __device__ __forceinline__ void second_pass(const Held<N, kRun, kBack>& held, float (&h)[N], bool on, int lowest, int highest) const
+    {
+        const bool edge = rows_here < a.rows || first < lowest || first + rows_here > highest;      // some rows are not there, or of no sequence
+        each<kRun>([&](auto j) {
+            const bool here = enter >> j & 1, leaves = leave >> j & 1;
+            if (any(here)) {
+                const State from = state_of(kBack ? a.in.dh : a.in.h0, entering, here, j);
+                each<N>([&](auto e) { h[e] = here ? +from.v[e] : +h[e]; });
+            }
+            Of o, p;
+            each<N>([&](auto e) {
+                if constexpr (kBack) {
+                    const Gate k = gate_of(held.f[j][e]);
+                    const float d = held.b[j][e] + h[e];
+                    o.v[e] = (T)(d * k.take);
+                    p.v[e] = (T)(d * held.by[j][e]);
+                    h[e] = k.keep * d;
+                } else {
+                    h[e] = fmaf(held.f[j][e], h[e], held.b[j][e]);
+                    o.v[e] = (T)h[e];
+                }
+            });
+            bool write = on;
+            if (edge) {
+                const int t = first + (kBack ? rows_here - 1 - (q + j) : q + j);
+                write = on && q + j < rows_here && t >= lowest && t < highest;
+            }
+            if (write) {
+                if constexpr (!kBack) {
+                    if (a.y) o.store(byte(static_cast<T*>(a.y) + (int64_t)first * a.in.width, at(j, a.in.width)));
+                } else {
+                    o.store(byte(static_cast<T*>(a.dx) + (int64_t)first * a.dx_stride, at(j, a.dx_stride)));
+                    p.store(byte(static_cast<T*>(a.dgate) + (int64_t)first * a.dgate_stride, at(j, a.dgate_stride)));
+                }
+            }
+            if (a.last && any(leaves)) {
+                State v;
+                each<N>([&](auto e) { v.v[e] = h[e]; });
+                if (leaves && on) v.store(a.last + (int64_t)leaving[q + j] * a.in.width + c);
+            }
         });
     }
 };
@@ -425,23 +392,20 @@ __device__ __forceinline__ void join(const TileArgs& a, int tile, int start, uns
     float state = 0;
     if (start < p0) {
         const int from = start / a.rows, group = tile / kGroup * kGroup;
-        int k = from;
-        if (from >= group) {
-            const uint64_t* const at = sums + ((int64_t)k++ * 2 + 1) * pitch;
-            state = wait_for(at, look(at), call);
-        } else {
-            const uint64_t* const at = a.states + (int64_t)(group / kGroup - 1) * pitch + word;
-            k = group;
-            state = wait_for(at, look(at), call);
-        }
-        for (; k < tile; k += 4) {
+        // what it starts from: the end of the tile that the sequence starts in, or the state at a group's end; then the tiles since
+        const uint64_t* const begin = from >= group ? sums + ((int64_t)from * 2 + 1) * pitch : a.states + (int64_t)(group / kGroup - 1) * pitch + word;
+        uint64_t seen = look(begin);
+        bool begun = false;
+        for (int k = from >= group ? from + 1 : group; k < tile || !begun; k += 4) {
             uint64_t sf[4], sb[4];
 #pragma unroll
             for (int u = 0; u < 4; ++u) {
-                const int64_t w = (int64_t)(k + u < tile ? k + u : k) * 2;
+                const int64_t w = (int64_t)(k + u < tile ? k + u : tile - 1) * 2;
                 sf[u] = look(sums + w * pitch);
                 sb[u] = look(sums + (w + 1) * pitch);
             }
+            if (!begun) state = wait_for(begin, seen, call);
+            begun = true;
 #pragma unroll
             for (int u = 0; u < 4; ++u)
                 if (k + u < tile) {
@@ -486,7 +450,7 @@ __global__ __launch_bounds__(kThreads, V_OCC) void k_scan_tiles(TileArgs a)
     const int tile = __builtin_amdgcn_readfirstlane((int)(unsigned)drawn), p0 = tile * a.rows;
     const unsigned call = __builtin_amdgcn_readfirstlane((int)(drawn >> 32));
     const int l = tid & ((1 << a.lg) - 1), run = tid >> a.lg, channels = a.lanes * N;
-    // channels: those of a last lane that is not whole reach back, and both come to the same values (states are not in place then)
+    // channels: those of a last lane that is not whole reach back, and both come to the same values
     const int c_own = block * channels + (l < a.lanes ? l : 0) * N, c = c_own + N > width ? width - N : c_own;
     const bool on = l < a.lanes && c_own < width;
     const int q = run * kRun, rows_here = a.n - p0 < a.rows ? a.n - p0 : a.rows, first = kBack ? a.n - p0 - rows_here : p0;
@@ -512,9 +476,7 @@ __global__ __launch_bounds__(kThreads, V_OCC) void k_scan_tiles(TileArgs a)
         each<N>([&](auto e) { h[e] = part_f[l < a.lanes ? run * channels + l * N + e : 0]; });
         const Of rows{a, anew(q), first, rows_here, anew(c), m.enter[run], m.leave[run], m.entering, m.leaving};
         const int lowest = bound(in.off[0], a.n), highest = bound(in.off[a.n_seq], a.n);
-        const bool plain = rows_here == a.rows && first >= lowest && first + rows_here <= highest && (kBack || a.y) &&
-                           __ballot((rows.enter | rows.leave) != 0) == 0;
-        rows.second_pass(held, h, on, plain, lowest, highest);
+        rows.second_pass(held, h, on, lowest, highest);
     }
     // after the last number that there is all words are cleared, and 0 is no call's number
     if (call != ~0u) return;
@@ -547,7 +509,7 @@ __global__ __launch_bounds__(kBlock) void k_scan_step(ScanIn in, T* y, T* dgate,
             Of o;
 #pragma unroll
             for (int e = 0; e < M; ++e) {
-                const Gate k = gate_of<T>((float)g.v[e]);
+                const Gate k = gate_of(smaller_of<T>((float)g.v[e]));
                 h.v[e] = fmaf(k.keep, h0.v[e], k.take * (float)x.v[e]);
                 o.v[e] = (T)h.v[e];
             }
@@ -559,7 +521,7 @@ __global__ __launch_bounds__(kBlock) void k_scan_step(ScanIn in, T* y, T* dgate,
             if (in.dh) dh = State::load(in.dh + at);
 #pragma unroll
             for (int e = 0; e < M; ++e) {
-                const Gate k = gate_of<T>((float)g.v[e]);
+                const Gate k = gate_of(smaller_of<T>((float)g.v[e]));
                 const float d = (float)up.v[e] + dh.v[e], by = d * k.take;
                 ox.v[e] = (T)by;
                 og.v[e] = (T)(by * k.keep * (h0.v[e] - (float)x.v[e]));
@@ -592,13 +554,9 @@ int launch(gr_tokens* h, const ScanIn& in, int dtype, void* y, void* dgate, void
     a.in = in; a.y = y; a.dgate = dgate; a.dx = dx; a.last = last;
     a.gate_stride = (int)in.gate_stride; a.x_stride = (int)in.x_stride; a.dgate_stride = (int)in.dgate_stride; a.dx_stride = (int)in.dx_stride;
     a.n = (int)in.n; a.n_seq = (int)in.n_seq;
-    // (single channels where a row has no whole piece, and where states are in place and one reaches back: it would find what the other wrote.  As many
-    // lanes all the same, so that tiles have the same rows and the bits are those of states that are not in place)
-    const bool in_place = last && last == (kBack ? in.dh : in.h0);
-    const int piece = in.width < kScanChannels ? 1 : kScanChannels, per = in_place && in.width % piece ? 1 : piece;
-    const int most = 1 << kScanLanesLog, pieces = (in.width + piece - 1) / piece, blocks = (pieces + most - 1) / most;
-    a.lanes = (pieces + blocks - 1) / blocks;
-    a.blocks = ((in.width + per - 1) / per + a.lanes - 1) / a.lanes;
+    const int per = in.width < kScanChannels ? 1 : kScanChannels, pieces = (in.width + per - 1) / per, most = 1 << kScanLanesLog;
+    a.blocks = (pieces + most - 1) / most;
+    a.lanes = (pieces + a.blocks - 1) / a.blocks;
     a.lg = kLeastLanesLog;
     while ((1 << a.lg) < a.lanes) ++a.lg;
     constexpr int kRun = kBack ? kScanRunBack : kScanRun;
@@ -624,15 +582,14 @@ int launch(gr_tokens* h, const ScanIn& in, int dtype, void* y, void* dgate, void
 
 }  // namespace
 
-// Blocks of channels: most where lanes have single channels.
-int scan_counters(int width) { return ((width / kScanChannels >> kScanLanesLog) + 1) * kScanChannels; }
+int scan_counters(int width) { return (width / kScanChannels >> kScanLanesLog) + 1; }
 
 size_t scan_words(int64_t n, int width)
 {
     // a word for F and one for B of every channel of every tile, and one of every group's state: of the least tiles and the most channels in use
     const int64_t rows = (int64_t)(kThreads >> kScanLanesLog) * (kScanRun < kScanRunBack ? kScanRun : kScanRunBack), tiles = (n + rows - 1) / rows;
-    // (lanes are as many in every block of channels: less than a piece a block more in all, and a piece; of single channels less than a row's lanes)
-    return (size_t)(tiles * 2 + tiles / kGroup + 1) * (width + scan_counters(width) + (kScanChannels << kScanLanesLog));
+    // (lanes are as many in every block of channels: less than a piece a block more in all, and a piece)
+    return (size_t)(tiles * 2 + tiles / kGroup + 1) * (width + (scan_counters(width) + 1) * kScanChannels);
 }
 
 int launch_scan(gr_tokens* h, const ScanIn& in, int dtype, void* y, float* last, hipStream_t s)

@@ -113,6 +113,7 @@ int gr_gated_scan(gr_tokens* h, int64_t n_tokens, int64_t n_seq, int32_t width, 
 {
     if (const int rc = scan_ok(h, n_tokens, n_seq, width, dtype, off)) return rc;
     if (const int rc = strides({gate_stride, x_stride}, width)) return rc;
+    if (off && out_h && out_h == h0) return GR_ERR_INVALID_ARG;
     if (n_seq == 0 || (!out_y && !out_h) || (n_tokens == 0 && !out_h)) return GR_OK;
     if (n_tokens > 0 && (!gate || !x)) return GR_ERR_INVALID_ARG;
     ScanIn in{};
@@ -128,6 +129,7 @@ int gr_gated_scan_backward(gr_tokens* h, int64_t n_tokens, int64_t n_seq, int32_
 {
     if (const int rc = scan_ok(h, n_tokens, n_seq, width, dtype, off)) return rc;
     if (const int rc = strides({gate_stride, x_stride, dgate_stride, dx_stride}, width)) return rc;
+    if (off && out_dh0 && out_dh0 == dh) return GR_ERR_INVALID_ARG;
     if (n_seq == 0 || (n_tokens == 0 && !out_dh0)) return GR_OK;
     if (n_tokens > 0 && (!gate || !x || !y || !out_dgate || !out_dx)) return GR_ERR_INVALID_ARG;
     ScanIn in{};

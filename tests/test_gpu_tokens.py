@@ -161,11 +161,11 @@ def test_scan(n, S, width, dtype):
         h.gr_gated_scan(g, v, out_y=y, off=ints(off), h0=put(h0, torch.float32) if start else None, out_h=last)
         ref.near(y, want_y, E_y, dtype, np.abs(gate).max(initial=0), "y")
         ref.near(last, want, E, dtype, np.abs(gate).max(initial=0), "last")
-        # one of the results alone; the states in place
-        alone, state = empty(n, width, dtype=dtype), put(h0, torch.float32)
-        h.gr_gated_scan(g, v, out_y=alone, off=ints(off), h0=state if start else None)
+        # one of the results alone
+        alone, state = empty(n, width, dtype=dtype), empty(S, width)
+        h.gr_gated_scan(g, v, out_y=alone, off=ints(off), h0=put(h0, torch.float32) if start else None)
         assert torch.equal(alone, y)
-        h.gr_gated_scan(g, v, off=ints(off), h0=state if start else None, out_h=state)
+        h.gr_gated_scan(g, v, off=ints(off), h0=put(h0, torch.float32) if start else None, out_h=state)
         assert torch.equal(state, last)
 
 
@@ -190,13 +190,10 @@ def test_scan_backward(n, S, width, dtype):
         most = np.abs(gate).max(initial=0)
         for got, (r, E), what in zip((dg, dx, dh0), want, ("dgate", "dx", "dh0")):
             ref.near(got, r, E, dtype, most, what)
-        # dense, without the gradient of the first states; that in place
+        # dense, without the gradient of the first states
         dense = [empty(n, width, dtype=dtype) for _ in range(2)]
         h.gr_gated_scan_backward(put(gate, dtype), put(x, dtype), put(y, dtype), *dense, dh=state, **args)
         assert torch.equal(dense[0], dg) and torch.equal(dense[1], dx)
-        if last:
-            h.gr_gated_scan_backward(g, v, put(y, dtype), dg, dx, dh=state, out_dh0=state, **args)
-            assert torch.equal(state, dh0)
 
 
 @pytest.mark.parametrize("dtype", TYPES)
@@ -216,8 +213,8 @@ def test_scan_of_single_tokens(n, width, dtype):
         h.gr_gated_scan(g, v, out_y=y, h0=s0, out_h=last)
         ref.near(y, want_y, E_y, dtype, most, "y")
         ref.near(last, want, E, dtype, most, "last")
-        y2, last2 = empty(n, width, dtype=dtype), s0.clone() if start else empty(n, width)
-        h.gr_gated_scan(g, v, out_y=y2, off=ints(np.arange(n + 1)), h0=last2 if start else None, out_h=last2)
+        y2, last2 = empty(n, width, dtype=dtype), empty(n, width)
+        h.gr_gated_scan(g, v, out_y=y2, off=ints(np.arange(n + 1)), h0=s0, out_h=last2)
         assert torch.equal(y2, y) and torch.equal(last2, last)
         if start:
             state = s0.clone()
@@ -229,6 +226,9 @@ def test_scan_of_single_tokens(n, width, dtype):
         want = ref.scan_backward(gate, x, y0, None, h0 if start else None, dy, dh)
         for got, (r, E), what in zip((dg, dx, dh0), want, ("dgate", "dx", "dh0")):
             ref.near(got, r, E, dtype, most, what)
+        state = put(dh, torch.float32)
+        h.gr_gated_scan_backward(g, v, put(y0, dtype), dg, dx, h0=s0, dy=put(dy, dtype), dh=state, out_dh0=state)
+        assert torch.equal(state, dh0)
 
 
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
@@ -613,6 +613,9 @@ def test_refusals(native, monkeypatch):
     refused(ValueError, lambda: h.gr_gated_scan_backward(g, g, y, f(n, W), f(n, W), off=off, dh=f(n, W)), "dh: shape")
     refused(TypeError, lambda: h.gr_gated_scan_backward(g, g, y, f(n, W).half(), f(n, W), dy=y), "out_dgate")
     refused(TypeError, lambda: h.gr_gated_scan_backward(g, g, y, f(n, W), f(n, W), dy=y.half()), "dy: need")
+    code(-1, lambda: h.gr_gated_scan(g, g, off=off, h0=st, out_h=st))
+    code(-1, lambda: h.gr_gated_scan_backward(g, g, y, f(n, W), f(n, W), off=off, dh=st, out_dh0=st))
+    refused(ValueError, lambda: h.gr_gated_scan(g, g, off=off, out_h=st.t()), "out_h: shape")
     code(-1, lambda: h.gr_gated_scan_backward(g, g, None, f(n, W), f(n, W), dy=y))
     # dropout
     refused(ValueError, lambda: h.gr_dropout(g, f(n, W + 1), 0.1, 1), "out: shape")
