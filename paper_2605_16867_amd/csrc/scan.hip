@@ -16,11 +16,10 @@ struct Gate {
     float keep, take;      // sigmoid(gate), sigmoid(-gate)
 };
 
-// The smaller of a gate's two sigmoids, with the gate's sign: from exp(-|gate|) =: e as e / (1 + e), no difference, so it has all its digits however far
-// the gate is from 0; the larger one is what it leaves of 1.  The exponent's rounding, |gate| log2(e) * 2^-24, is made good where results are in
-// single precision.  (A gate that is no number stays one.)
+// Both from exp(-|gate|) =: e, as 1 / (1 + e) and e / (1 + e): neither is a difference, so both have all their digits however far the gate is from 0.
+// The exponent's rounding, |gate| log2(e) * 2^-24, is made good where results are in single precision.  (A gate that is no number stays one.)
 template <typename T>
-__device__ __forceinline__ float smaller_of(float g)
+__device__ __forceinline__ Gate gate_of(float g)
 {
     constexpr float kLog2e = 1.44269504089f, kLog2eRest = 1.92596299e-8f, kLn2 = 0.693147181f;
     const float a = fabsf(g);
@@ -29,13 +28,17 @@ __device__ __forceinline__ float smaller_of(float g)
         const float near_a = fminf(a, 128.0f), p = near_a * -kLog2e;      // (behind that e is 0, and an infinite gate has no rounding)
         e = fmaf(e, fmaf(near_a, -kLog2eRest, fmaf(near_a, -kLog2e, -p)) * kLn2, e);
     }
-    return copysignf(e * __builtin_amdgcn_rcpf(1.0f + e), g);
+    const float near = __builtin_amdgcn_rcpf(1.0f + e), far = e * near;
+    return g >= 0 ? Gate{near, far} : Gate{far, near};
 }
 
-__device__ __forceinline__ Gate gate_of(float smaller)
+// Both in one word: the smaller one, negative where it is the first; the other is what it leaves of 1.
+__device__ __forceinline__ float packed(Gate g) { return g.keep < g.take ? -g.keep : g.take; }
+
+__device__ __forceinline__ Gate unpacked(float v)
 {
-    const float s = fabsf(smaller), rest = 1.0f - s;
-    return __float_as_int(smaller) >= 0 ? Gate{rest, s} : Gate{s, rest};
+    const float s = fabsf(v), rest = 1.0f - s;
+    return __float_as_int(v) >= 0 ? Gate{rest, s} : Gate{s, rest};
 }
 
 // ---- many tokens: tiles of rows -----------------------------------------------------------------
@@ -61,6 +64,7 @@ __device__ __forceinline__ Gate gate_of(float smaller)
 #define V_G 16
 #define V_WG 2
 #define V_OCC 2
+#define V_SB 1
 #define V_WGB 2
 #endif
 constexpr int kThreads = V_FT, kWaves = kThreads / 64;
@@ -175,7 +179,8 @@ __device__ void mark(const TileArgs& a, Marks<kRun>& m, int tile)
 }
 
 // What follows from v is found anew where it is asked for, not kept in registers from before.
-__device__ __forceinline__ int anew(int v)
+template <typename V>
+__device__ __forceinline__ V anew(V v)
 {
     asm volatile("" : "+v"(v));
     return v;
@@ -184,7 +189,7 @@ __device__ __forceinline__ int anew(int v)
 // What a lane holds of its rows between the passes.
 template <int N, int kRun, bool kBack>
 struct Held {
-    float f[kRun][N], b[kRun][N];           // forward: what the state is multiplied with, and what is added; backward: the smaller sigmoid, and dy
+    float f[kRun][N], b[kRun][N];           // forward: what the state is multiplied with, and what is added; backward: both sigmoids, and dy
     float by[kBack ? kRun : 1][N];          // dgate is D times this
 };
 
@@ -213,14 +218,30 @@ struct Rows {
     unsigned enter, leave;         // bits of rows
     const int *entering, *leaving; // sequences, where a bit is set
 
-    __device__ __forceinline__ static bool any(bool v) { return __ballot(v) != 0; }
-
-    // Distance in bytes, from the tile's lowest token, of row j of an array: in 32 bits by the limit on strides.  Rows that are not there are others that are.
-    __device__ __forceinline__ unsigned at(int j, int stride) const
+    // The bits that any lane has.
+    __device__ __forceinline__ static unsigned of_wave(unsigned bits)
     {
-        int r = kBack ? rows_here - 1 - (q + j) : q + j;
-        r = kBack ? (r < 0 ? 0 : r) : (r < rows_here ? r : rows_here - 1);
-        return ((unsigned)r * (unsigned)stride + c) * (unsigned)sizeof(T);
+        unsigned all = 0;
+        for (uint64_t lanes = __ballot(bits != 0); lanes; lanes = __ballot((bits & ~all) != 0))
+            all |= (unsigned)__builtin_amdgcn_readlane((int)bits, __builtin_ctzll(lanes));
+        return all;
+    }
+
+    // Distances in bytes, from the tile's lowest token, of the lane's rows of an array, in 32 bits by the limit on strides: row j is `step` from the one
+    // before.  Rows that are not there (past the last, or wrapped round) are the highest one that is, or lie between rows that are.
+    struct Lines {
+        unsigned from, step, most;
+        __device__ __forceinline__ unsigned operator[](int j) const
+        {
+            const unsigned off = kBack ? from - j * step : from + j * step;
+            return off < most ? off : most;
+        }
+    };
+
+    __device__ __forceinline__ Lines lines(int stride) const
+    {
+        const unsigned step = (unsigned)stride * (unsigned)sizeof(T), at = (unsigned)c * (unsigned)sizeof(T);
+        return {(unsigned)(kBack ? rows_here - 1 - q : q) * step + at, step, (unsigned)(rows_here - 1) * step + at};
     }
 
     template <typename P>
@@ -233,7 +254,8 @@ struct Rows {
     __device__ __forceinline__ void load(Of (&to)[kRun], const void* p, int stride) const
     {
         const T* const base = static_cast<const T*>(p) + (int64_t)first * stride;
-        each<kRun>([&](auto j) { to[j] = Of::load(byte(base, at(j, stride))); });
+        const Lines at = lines(stride);
+        each<kRun>([&](auto j) { to[j] = Of::load(byte(base, at[j])); });
     }
 
     // The state of row j's sequence; the first one's for lanes that have no mark there.
@@ -256,8 +278,10 @@ struct Rows {
             else each<kRun>([&](auto j) { r.up[j] = Of{}; });
             // (the row before the first token is not there, and not asked for: a sequence leaves at it)
             const T* const base = static_cast<const T*>(in.y) + (int64_t)(first - 1) * in.width;
+            const Lines at = lines(in.width);
+            const unsigned least = first == 0 ? at.step : 0;
             each<kRun>([&](auto j) {
-                const unsigned off = at(j, in.width), least = first == 0 ? (unsigned)in.width * (unsigned)sizeof(T) : 0;
+                const unsigned off = at[j];
                 r.was[j] = Of::load(byte(base, off < least ? off + least : off));
             });
         }
@@ -267,12 +291,13 @@ struct Rows {
     {
         const ScanIn& in = a.in;
         const bool some_missing = rows_here < a.rows;
+        const unsigned any_enter = of_wave(enter), any_leave = kBack ? of_wave(leave) : 0;
         each<kRun>([&](auto j) {
             float before[N] = {};
             if constexpr (kBack) {
                 const bool here = leave >> j & 1;
                 each<N>([&](auto e) { before[e] = (float)r.was[j].v[e]; });
-                if (any(here)) {
+                if (any_leave >> j & 1) {
                     const State h0 = state_of(in.h0, leaving, here, j);
                     each<N>([&](auto e) { before[e] = here ? +h0.v[e] : +before[e]; });
                 }
@@ -280,14 +305,14 @@ struct Rows {
             float f[N];
             const bool there = !some_missing || q + j < rows_here;
             each<N>([&](auto e) {
-                const float smaller = smaller_of<T>((float)r.g[j].v[e]), v = (float)r.x[j].v[e];
-                const Gate k = gate_of(smaller);
+                const float v = (float)r.x[j].v[e];
+                const Gate k = gate_of<T>((float)r.g[j].v[e]);
                 f[e] = k.keep;
                 if constexpr (!kBack) held.b[j][e] = k.take * v;
                 else {
-                    held.f[j][e] = smaller;
+                    held.f[j][e] = anew(packed(k));
                     held.b[j][e] = (float)r.up[j].v[e];
-                    held.by[j][e] = k.keep * k.take * (before[e] - v);
+                    held.by[j][e] = anew(k.keep * k.take * (before[e] - v));
                 }
             });
             if (some_missing)      // rows that are not there change nothing (and nothing is written for them)
@@ -298,13 +323,14 @@ struct Rows {
             if constexpr (!kBack) each<N>([&](auto e) { held.f[j][e] = f[e]; });
             if (j == 0) each<N>([&](auto e) { F[e] = 1.0f; B[e] = 0.0f; });
             const bool here = enter >> j & 1;
-            if (any(here)) {
+            if (any_enter >> j & 1) {
                 const State from = state_of(kBack ? in.dh : in.h0, entering, here, j);
                 each<N>([&](auto e) {
                     B[e] = here ? +from.v[e] : +B[e];
                     F[e] = here ? 0.0f : +F[e];
                 });
             }
+            if (V_SB) __builtin_amdgcn_sched_barrier(0);
             each<N>([&](auto e) {
                 B[e] = kBack ? f[e] * (held.b[j][e] + B[e]) : fmaf(f[e], B[e], held.b[j][e]);
                 F[e] *= f[e];
@@ -314,17 +340,20 @@ struct Rows {
 
     __device__ __forceinline__ void second_pass(const Held<N, kRun, kBack>& held, float (&h)[N], bool on, int lowest, int highest) const
     {
+        const unsigned any_enter = of_wave(enter), any_leave = of_wave(leave);
+        const Lines at_y = lines(kBack ? a.dx_stride : a.in.width), at_g = lines(a.dgate_stride);
         const bool edge = rows_here < a.rows || first < lowest || first + rows_here > highest;      // some rows are not there, or of no sequence
         each<kRun>([&](auto j) {
             const bool here = enter >> j & 1, leaves = leave >> j & 1;
-            if (any(here)) {
+            if (V_SB) __builtin_amdgcn_sched_barrier(0);
+            if (any_enter >> j & 1) {
                 const State from = state_of(kBack ? a.in.dh : a.in.h0, entering, here, j);
                 each<N>([&](auto e) { h[e] = here ? +from.v[e] : +h[e]; });
             }
             Of o, p;
             each<N>([&](auto e) {
                 if constexpr (kBack) {
-                    const Gate k = gate_of(held.f[j][e]);
+                    const Gate k = unpacked(held.f[j][e]);
                     const float d = held.b[j][e] + h[e];
                     o.v[e] = (T)(d * k.take);
                     p.v[e] = (T)(d * held.by[j][e]);
@@ -341,13 +370,13 @@ struct Rows {
             }
             if (write) {
                 if constexpr (!kBack) {
-                    if (a.y) o.store(byte(static_cast<T*>(a.y) + (int64_t)first * a.in.width, at(j, a.in.width)));
+                    if (a.y) o.store(byte(static_cast<T*>(a.y) + (int64_t)first * a.in.width, at_y[j]));
                 } else {
-                    o.store(byte(static_cast<T*>(a.dx) + (int64_t)first * a.dx_stride, at(j, a.dx_stride)));
-                    p.store(byte(static_cast<T*>(a.dgate) + (int64_t)first * a.dgate_stride, at(j, a.dgate_stride)));
+                    o.store(byte(static_cast<T*>(a.dx) + (int64_t)first * a.dx_stride, at_y[j]));
+                    p.store(byte(static_cast<T*>(a.dgate) + (int64_t)first * a.dgate_stride, at_g[j]));
                 }
             }
-            if (a.last && any(leaves)) {
+            if (a.last && any_leave >> j & 1) {
                 State v;
                 each<N>([&](auto e) { v.v[e] = h[e]; });
                 if (leaves && on) v.store(a.last + (int64_t)leaving[q + j] * a.in.width + c);
@@ -509,7 +538,7 @@ __global__ __launch_bounds__(kBlock) void k_scan_step(ScanIn in, T* y, T* dgate,
             Of o;
 #pragma unroll
             for (int e = 0; e < M; ++e) {
-                const Gate k = gate_of(smaller_of<T>((float)g.v[e]));
+                const Gate k = gate_of<T>((float)g.v[e]);
                 h.v[e] = fmaf(k.keep, h0.v[e], k.take * (float)x.v[e]);
                 o.v[e] = (T)h.v[e];
             }
@@ -521,7 +550,7 @@ __global__ __launch_bounds__(kBlock) void k_scan_step(ScanIn in, T* y, T* dgate,
             if (in.dh) dh = State::load(in.dh + at);
 #pragma unroll
             for (int e = 0; e < M; ++e) {
-                const Gate k = gate_of(smaller_of<T>((float)g.v[e]));
+                const Gate k = gate_of<T>((float)g.v[e]);
                 const float d = (float)up.v[e] + dh.v[e], by = d * k.take;
                 ox.v[e] = (T)by;
                 og.v[e] = (T)(by * k.keep * (h0.v[e] - (float)x.v[e]));

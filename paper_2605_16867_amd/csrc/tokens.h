@@ -33,8 +33,8 @@ struct ScanIn {
     int width;
 };
 #ifndef V_LG
-#define V_RUN 4
-#define V_RUNB 4
+#define V_RUN 8
+#define V_RUNB 6
 #define V_LG 5
 #endif
 constexpr int kScanRun = V_RUN, kScanRunBack = V_RUNB, kScanChannels = 4, kScanLanesLog = V_LG;      // rows and channels that a lane takes of a tile; log2 of lanes that share a row
