@@ -45,6 +45,27 @@ def check_spills(remarks: str) -> None:
         raise RuntimeError(f"the compiler said nothing of {sorted(set(NOTHING_SPILLED) - seen)}")
 
 
+# Kernels that hold most of their registers across branches.  With scalar registers spilled too, the compiler has put copies of vector registers before
+# the end of a branch gave its lanes back: the others had something else there afterwards.
+NEVER_SPILLED = ("k_scan_tiles",)
+
+
+def check_held(remarks: str) -> None:
+    """Raises where the compiler's remarks say that one of those kernels spills any register or uses scratch memory, or say nothing of it."""
+    seen = set()
+    for part in remarks.split("remark: Function Name: ")[1:]:
+        name = part.split()[0]
+        for kernel in NEVER_SPILLED:
+            if kernel in name:
+                seen.add(kernel)
+                for what in (r"SGPRs Spill", r"VGPRs Spill", r"ScratchSize \[bytes/lane\]"):
+                    m = re.search(what + r": (\d+)", part)
+                    if m is None or int(m.group(1)):
+                        raise RuntimeError(f"{name}: {m.group(0) if m else 'no word of ' + what}, and what its lanes hold may be lost")
+    if seen != set(NEVER_SPILLED):
+        raise RuntimeError(f"the compiler said nothing of {sorted(set(NEVER_SPILLED) - seen)}")
+
+
 def build_library(verbose: bool = False) -> str:
     cmd = hipcc_command()
     if verbose:
@@ -56,6 +77,7 @@ def build_library(verbose: bool = False) -> str:
     made.check_returncode()
     try:
         check_spills(made.stderr)
+        check_held(made.stderr)
     except RuntimeError:
         os.remove(LIB)
         raise

@@ -58,17 +58,12 @@ __device__ __forceinline__ Gate unpacked(float v)
 // follow each other in 43 ns: with one for all blocks, and another for workgroups that are done, 262 144 tokens of 1 024 took 1.4 ms whatever else
 // was done.
 
-#ifndef V_FT
-#define V_FT 512
-#define V_BT 512
-#define V_G 16
-#define V_WG 2
-#define V_OCC 2
-#define V_SB 1
-#define V_WGB 2
-#endif
-constexpr int kThreads = V_FT, kWaves = kThreads / 64;
-constexpr int kGroup = V_G, kLeastLanesLog = 2, kMostRuns = kThreads >> kLeastLanesLog;
+constexpr int kThreads = 512, kWaves = kThreads / 64;
+constexpr int kGroup = 16, kLeastLanesLog = 2, kNearOffsets = 2048, kMostRuns = kThreads >> kLeastLanesLog;
+// Rows of a run: as many as leave a unit two workgroups (forward 105 registers, backward 115); few where there would not be a tile a unit: 3 000 x 256 in
+// single precision 8.9 us with four (9.8 with two, 9.9 with eight), but 16 000 x 512, 504 tiles of eight, 20 us (24 with four, 33 with two).
+constexpr int kRunForward = 8, kRunBackward = 6, kRunFew = 4;
+constexpr int64_t kFewTiles = 256;
 
 struct TileArgs {
     ScanIn in;
@@ -135,9 +130,9 @@ struct Marks {
     int entering[kMostRuns * kRun], leaving[kMostRuns * kRun];      // the sequences, where a bit is set
 };
 
-// By one wave.
+// By one wave; `off` is in shared memory where there are few enough sequences.
 template <int kRun, bool kBack>
-__device__ void mark(const TileArgs& a, Marks<kRun>& m, int tile)
+__device__ __forceinline__ void mark(const TileArgs& a, Marks<kRun>& m, int tile, const int* off)
 {
     const int lane = threadIdx.x & 63, p0 = tile * a.rows, end = p0 + a.rows < a.n ? p0 + a.rows : a.n;
     for (int r = lane; r < a.rows / kRun; r += 64) m.enter[r] = m.leave[r] = 0;
@@ -148,7 +143,7 @@ __device__ void mark(const TileArgs& a, Marks<kRun>& m, int tile)
     int lo = 0, hi = a.n_seq + 1;
     while (lo < hi) {
         const int step = (hi - lo + 63) / 64, at = lo + lane * step;
-        const uint64_t not_yet = ~__ballot(at < hi && a.in.off[at < hi ? at : 0] <= from);
+        const uint64_t not_yet = ~__ballot(at < hi && off[at < hi ? at : 0] <= from);
         const int c = not_yet ? __builtin_ctzll(not_yet) : 64;
         if (c == 0) break;
         hi = lo + c * step < hi ? lo + c * step : hi;
@@ -158,7 +153,7 @@ __device__ void mark(const TileArgs& a, Marks<kRun>& m, int tile)
         const int s = base + lane;
         int end_here = a.n;
         if (s < a.n_seq) {
-            const int b = bound(a.in.off[s], a.n), e = bound(a.in.off[s + 1], a.n);
+            const int b = bound(off[s], a.n), e = bound(off[s + 1], a.n);
             end_here = e;
             if (b < e) {
                 const int enter = kBack ? a.n - e : b, leave = kBack ? a.n - 1 - b : e - 1;      // as rows
@@ -330,7 +325,6 @@ struct Rows {
                     F[e] = here ? 0.0f : +F[e];
                 });
             }
-            if (V_SB) __builtin_amdgcn_sched_barrier(0);
             each<N>([&](auto e) {
                 B[e] = kBack ? f[e] * (held.b[j][e] + B[e]) : fmaf(f[e], B[e], held.b[j][e]);
                 F[e] *= f[e];
@@ -345,7 +339,6 @@ struct Rows {
         const bool edge = rows_here < a.rows || first < lowest || first + rows_here > highest;      // some rows are not there, or of no sequence
         each<kRun>([&](auto j) {
             const bool here = enter >> j & 1, leaves = leave >> j & 1;
-            if (V_SB) __builtin_amdgcn_sched_barrier(0);
             if (any_enter >> j & 1) {
                 const State from = state_of(kBack ? a.in.dh : a.in.h0, entering, here, j);
                 each<N>([&](auto e) { h[e] = here ? +from.v[e] : +h[e]; });
@@ -463,17 +456,21 @@ __device__ void stay(const TileArgs& a, int s0, const float* state)
 }
 
 template <typename T, int N, int kRun, bool kBack>
-__global__ __launch_bounds__(kThreads, V_OCC) void k_scan_tiles(TileArgs a)
+__global__ __launch_bounds__(kThreads) void k_scan_tiles(TileArgs a)
 {
     typedef Rows<T, N, kRun, kBack> Of;
     __shared__ float part_f[kThreads * N], part_b[kThreads * N];
     __shared__ Marks<kRun> m;
     __shared__ uint64_t drawn;
+    __shared__ int near_off[kNearOffsets];
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const ScanIn& in = a.in;
     const int width = in.width, workers = a.tiles * a.blocks;
     if (blockIdx.x >= (unsigned)workers) return stay(a, (int)(blockIdx.x - workers) * 64, kBack ? in.dh : in.h0);
     const int block = blockIdx.x % a.blocks;
+    const bool few = a.n_seq < kNearOffsets;
+    if (few)
+        for (int i = tid; i <= a.n_seq; i += kThreads) near_off[i] = in.off[i];
     if (tid == 0) drawn = draw(a.control + kCounters + block * kScanLine);
     __syncthreads();
     const int tile = __builtin_amdgcn_readfirstlane((int)(unsigned)drawn), p0 = tile * a.rows;
@@ -488,8 +485,10 @@ __global__ __launch_bounds__(kThreads, V_OCC) void k_scan_tiles(TileArgs a)
         float F[N], B[N];
         typename Of::Raw raw;
         Of{a, q, first, rows_here, c, 0, 0, nullptr, nullptr}.read(raw);
-        if (wave == kWaves - 1) mark<kRun, kBack>(a, m, tile);
-        else if (wave == 0 && tile == a.tiles - 1) last_tile(a, call);
+        if (wave == kWaves - 1) {
+            if (few) mark<kRun, kBack>(a, m, tile, near_off);
+            else mark<kRun, kBack>(a, m, tile, in.off);
+        } else if (wave == 0 && tile == a.tiles - 1) last_tile(a, call);
         __syncthreads();
         Of{a, anew(q), first, rows_here, anew(c), m.enter[run], m.leave[run], m.entering, m.leaving}.first_pass(raw, held, F, B);
         if (l < a.lanes) each<N>([&](auto e) {
@@ -566,6 +565,22 @@ __global__ __launch_bounds__(kBlock) void k_scan_step(ScanIn in, T* y, T* dgate,
         for (int one = c; one < in.width; ++one) go(std::integral_constant<int, 1>{}, one);
 }
 
+template <typename T, int N, int kRun, bool kBack>
+int launch_tiles(gr_tokens* h, TileArgs a, hipStream_t s)
+{
+    static_assert((int64_t)kMostRuns * kRun * GR_MAX_STRIDE <= int64_t(1) << 30, "distances within a tile are in 32 bits, in bytes");
+    a.rows = (kThreads >> a.lg) * kRun;
+    a.tiles = (int)(((int64_t)a.n + a.rows - 1) / a.rows);
+    const int64_t pitch = (int64_t)a.blocks * a.lanes * N;
+    a.states = a.sums + (int64_t)a.tiles * 2 * pitch;
+    if (a.blocks > a.counters || (size_t)(((int64_t)a.tiles * 2 + a.tiles / kGroup + 1) * pitch) > a.n_words) return GR_ERR_TOO_LARGE;
+    const int64_t total = (int64_t)a.tiles * a.blocks + (a.last ? ((int64_t)a.n_seq + 63) / 64 : 0);
+    if (total > kMostBlocks * kBlock / kThreads) return GR_ERR_TOO_LARGE;
+    if (total == 0) return GR_OK;
+    k_scan_tiles<T, N, kRun, kBack><<<(unsigned)total, kThreads, 0, s>>>(a);
+    return launched();
+}
+
 template <bool kBack>
 int launch(gr_tokens* h, const ScanIn& in, int dtype, void* y, void* dgate, void* dx, float* last, hipStream_t s)
 {
@@ -583,29 +598,19 @@ int launch(gr_tokens* h, const ScanIn& in, int dtype, void* y, void* dgate, void
     a.in = in; a.y = y; a.dgate = dgate; a.dx = dx; a.last = last;
     a.gate_stride = (int)in.gate_stride; a.x_stride = (int)in.x_stride; a.dgate_stride = (int)in.dgate_stride; a.dx_stride = (int)in.dx_stride;
     a.n = (int)in.n; a.n_seq = (int)in.n_seq;
+    a.control = h->control; a.counters = h->counters; a.sums = h->words; a.n_words = h->n_words;
     const int per = in.width < kScanChannels ? 1 : kScanChannels, pieces = (in.width + per - 1) / per, most = 1 << kScanLanesLog;
     a.blocks = (pieces + most - 1) / most;
     a.lanes = (pieces + a.blocks - 1) / a.blocks;
     a.lg = kLeastLanesLog;
     while ((1 << a.lg) < a.lanes) ++a.lg;
-    constexpr int kRun = kBack ? kScanRunBack : kScanRun;
-    a.rows = (kThreads >> a.lg) * kRun;
-    a.tiles = (int)((in.n + a.rows - 1) / a.rows);
-    a.control = h->control;
-    a.sums = h->words;
-    a.n_words = h->n_words;
-    a.counters = h->counters;
-    const int64_t pitch = (int64_t)a.blocks * a.lanes * per;
-    a.states = a.sums + (int64_t)a.tiles * 2 * pitch;
-    if (a.blocks > a.counters || (size_t)((int64_t)a.tiles * 2 + a.tiles / kGroup + 1) * pitch > a.n_words) return GR_ERR_TOO_LARGE;
-    const int64_t total = (int64_t)a.tiles * a.blocks + (last ? (in.n_seq + 63) / 64 : 0);
-    if (total > kMostBlocks * kBlock / kThreads) return GR_ERR_TOO_LARGE;
-    if (total == 0) return GR_OK;
+    constexpr int kRun = kBack ? kRunBackward : kRunForward;
+    const int rows = (kThreads >> a.lg) * kRun;
+    const bool few = (in.n + rows - 1) / rows * a.blocks <= kFewTiles;
     return by_type(dtype, [&](auto t) {
         typedef decltype(t) T;
-        if (per == 1) k_scan_tiles<T, 1, kRun, kBack><<<(unsigned)total, kThreads, 0, s>>>(a);
-        else k_scan_tiles<T, kScanChannels, kRun, kBack><<<(unsigned)total, kThreads, 0, s>>>(a);
-        return launched();
+        if (per == 1) return launch_tiles<T, 1, kRun, kBack>(h, a, s);
+        return few ? launch_tiles<T, kScanChannels, kRunFew, kBack>(h, a, s) : launch_tiles<T, kScanChannels, kRun, kBack>(h, a, s);
     });
 }
 
@@ -616,9 +621,17 @@ int scan_counters(int width) { return (width / kScanChannels >> kScanLanesLog) +
 size_t scan_words(int64_t n, int width)
 {
     // a word for F and one for B of every channel of every tile, and one of every group's state: of the least tiles and the most channels in use
-    const int64_t rows = (int64_t)(kThreads >> kScanLanesLog) * (kScanRun < kScanRunBack ? kScanRun : kScanRunBack), tiles = (n + rows - 1) / rows;
     // (lanes are as many in every block of channels: less than a piece a block more in all, and a piece)
-    return (size_t)(tiles * 2 + tiles / kGroup + 1) * (width + (scan_counters(width) + 1) * kScanChannels);
+    const auto words = [&](int64_t tiles) { return (size_t)(tiles * 2 + tiles / kGroup + 1) * (width + (scan_counters(width) + 1) * kScanChannels); };
+    const auto tiles = [&](int run) {
+        const int64_t rows = (int64_t)(kThreads >> kScanLanesLog) * run;
+        return (n + rows - 1) / rows;
+    };
+    constexpr int kMost = kRunForward > kRunBackward ? kRunForward : kRunBackward, kLeast = kRunForward < kRunBackward ? kRunForward : kRunBackward;
+    // runs of few rows are for few tiles
+    const int64_t few = tiles(kRunFew), of_few = kFewTiles * ((kMost + kRunFew - 1) / kRunFew);
+    const size_t a = words(tiles(kLeast)), b = words(few < of_few ? few : of_few);
+    return a > b ? a : b;
 }
 
 int launch_scan(gr_tokens* h, const ScanIn& in, int dtype, void* y, float* last, hipStream_t s)

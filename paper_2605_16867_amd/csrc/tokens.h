@@ -32,12 +32,7 @@ struct ScanIn {
     int64_t n, n_seq, gate_stride, x_stride, dgate_stride, dx_stride;
     int width;
 };
-#ifndef V_LG
-#define V_RUN 8
-#define V_RUNB 6
-#define V_LG 5
-#endif
-constexpr int kScanRun = V_RUN, kScanRunBack = V_RUNB, kScanChannels = 4, kScanLanesLog = V_LG;      // rows and channels that a lane takes of a tile; log2 of lanes that share a row
+constexpr int kScanChannels = 4, kScanLanesLog = 5;      // channels that a lane takes of a row; log2 of lanes that share one
 constexpr int kScanLine = 16;                                           // words from one counter to the next
 int scan_counters(int width);
 size_t scan_words(int64_t n, int width);
