@@ -4,12 +4,14 @@
 //
 // Forward: the rows that are written, and those of the tokens that occur.  Backward: the tokens are sorted first, in passes of up to nine bits, each
 // stable, so that the rows of a token are summed in the order in which they stand, in single precision: no atomics, the same bits every time.
+#include <type_traits>
+
 #include "tokens.h"
 
 namespace gr {
 namespace {
 
-constexpr int kBlock = 256, kWave = 64, kWaves = kBlock / kWave;
+constexpr int kBlock = 256, kWave = 64, kWaves = kBlock / kWave, kSumWaves = 16384;
 
 // log2 of the lanes that share a row of so many pieces
 int lanes_log(int pieces)
@@ -19,24 +21,48 @@ int lanes_log(int pieces)
     return lg;
 }
 
-// Pieces of 16 bytes at any address of an element; the last one of a row reaches back into the one before.
+// N elements, past the cache.
+template <typename T, int N>
+__device__ __forceinline__ void store_past(T* at, const Elements<T, N>& e)
+{
+    typedef T Vec __attribute__((ext_vector_type(N), aligned(sizeof(T))));
+    Vec v;
+    __builtin_memcpy(&v, &e, sizeof e);
+    __builtin_nontemporal_store(v, reinterpret_cast<Vec*>(at));
+}
+
+constexpr int kRowsAtOnce = 4;      // rows of a group of lanes whose loads are under way together
+
+// Pieces of 16 bytes at any address of an element; the last one of a row reaches back into the one before.  What is written is not asked for again soon:
+// it goes past the cache, which the rows of frequent tokens then stay in.
 template <typename T, int N>
 __global__ __launch_bounds__(kBlock) void k_embed(const int* token, const T* table, float scale, T* out, int64_t n, int vocab, int width, int lg)
 {
     typedef Elements<T, N> Of;
-    const int64_t row = ((int64_t)blockIdx.x * kBlock + threadIdx.x) >> lg;
-    if (row >= n) return;
-    const int v = token[row];
-    const bool there = v >= 0 && v < vocab;
-    const T* const from = table + (int64_t)(there ? v : 0) * width;
+    const int groups = kBlock >> lg, group = threadIdx.x >> lg;
+    const int64_t first = (int64_t)blockIdx.x * groups * kRowsAtOnce + group;
+    const T* from[kRowsAtOnce];
+#pragma unroll
+    for (int u = 0; u < kRowsAtOnce; ++u) {
+        const int64_t row = first + u * groups;
+        const int v = row < n ? token[row] : -1;
+        from[u] = v >= 0 && v < vocab ? table + (int64_t)v * width : nullptr;
+    }
     for (int p = (threadIdx.x & ((1 << lg) - 1)) * N; p < width; p += N << lg) {
         const int c = p + N > width ? width - N : p;
-        Of e{};
-        if (there) e = Of::load(from + c);
+        Of e[kRowsAtOnce];
 #pragma unroll
-        for (int j = 0; j < N; ++j) e.v[j] = (T)((float)e.v[j] * scale);
-        if (!there) e = Of{};
-        e.store(out + row * width + c);
+        for (int u = 0; u < kRowsAtOnce; ++u) {
+            e[u] = Of{};
+            if (from[u]) e[u] = Of::load(from[u] + c);
+        }
+#pragma unroll
+        for (int u = 0; u < kRowsAtOnce; ++u) {
+            const int64_t row = first + u * groups;
+#pragma unroll
+            for (int j = 0; j < N; ++j) e[u].v[j] = from[u] ? (T)((float)e[u].v[j] * scale) : (T)0.0f;
+            if (row < n) store_past(out + row * width + c, e[u]);
+        }
     }
 }
 
@@ -171,39 +197,171 @@ __global__ __launch_bounds__(kBlock) void k_digit_place(SortArgs a, int bits, in
     }
 }
 
-// The place of the first key that is at least v.
-__device__ __forceinline__ int64_t first_of(const int* key, int64_t n, int v)
+// ---- the sums ----------------------------------------------------------------------------------
+//
+// Sorted places and rows of the table are one line of work: the places of a row, then the row itself, which is written.  A wave takes kPiece items
+// of it and a block of channels, and finds its first place by the line's order: that of place p is p + key[p], of row v the places up to its last plus v.
+// A row of at most kPiece places is summed where its first place is, as far as it goes; a longer one in every piece that it has places in, whose
+// sums a second launch adds up in their order.
+
+struct SumArgs {
+    const int *key, *slot, *left;      // left: how many there are; null: none
+    const void* dout;
+    void* dtable;
+    float *head, *trail;      // [pieces][width] of long rows: of the piece that has the row's end, of the others
+    float scale;
+    int vocab, width, piece, pieces, blocks;
+};
+
+// How many of [lo, hi) are before the first that `before` is not true for; by a wave.
+template <typename F>
+__device__ __forceinline__ int first_not(int lo, int hi, F before)
 {
-    int64_t lo = 0, hi = n;
+    const int lane = threadIdx.x % kWave;
     while (lo < hi) {
-        const int64_t mid = (lo + hi) / 2;
-        if (key[mid] < v) lo = mid + 1;
-        else hi = mid;
+        const int step = (hi - lo + kWave - 1) / kWave, at = lo + lane * step;
+        const uint64_t not_yet = ~__ballot(at < hi && before(at < hi ? at : lo));
+        const int c = not_yet ? __builtin_ctzll(not_yet) : kWave;
+        if (c == 0) break;
+        hi = lo + c * step < hi ? lo + c * step : hi;
+        lo += (c - 1) * step + 1;
     }
     return lo;
 }
 
+__device__ __forceinline__ int place_at(const SumArgs& a, int n, int64_t item)
+{
+    return first_not(0, n, [&](int p) { return (int64_t)p + a.key[p] < item; });
+}
+
+// More than kPiece places, from the first one.
+__device__ __forceinline__ bool is_long(const SumArgs& a, int n, int first, int v) { return first + a.piece < n && a.key[first + a.piece] == v; }
+
 template <typename T, int N>
-__global__ __launch_bounds__(kBlock) void k_embed_sums(const int* key, const int* slot, const int* left, const T* dout, float scale, T* dtable,
-                                                       int vocab, int width, int lg)
+__global__ __launch_bounds__(kBlock) void k_embed_sums(SumArgs a)
 {
     typedef Elements<T, N> Of;
-    const int64_t v = ((int64_t)blockIdx.x * kBlock + threadIdx.x) >> lg;
-    if (v >= vocab) return;
-    const int64_t n = left ? *left : 0, from = first_of(key, n, (int)v), to = first_of(key, n, (int)v + 1);
-    for (int p = (threadIdx.x & ((1 << lg) - 1)) * N; p < width; p += N << lg) {
-        const int c = p + N > width ? width - N : p;
-        float sum[N] = {};
-        for (int64_t i = from; i < to; ++i) {
-            const Of e = Of::load(dout + (int64_t)slot[i] * width + c);
+    constexpr int kAtOnce = 8;
+    const int lane = threadIdx.x % kWave;
+    const int64_t id = (int64_t)blockIdx.x * kWaves + __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+    const int piece = (int)(id / a.blocks), block = (int)(id - (int64_t)piece * a.blocks);
+    if (piece >= a.pieces) return;
+    const int n = a.left ? *a.left : 0;
+    const int64_t item = (int64_t)piece * a.piece, all = (int64_t)a.vocab + n, end = item + a.piece < all ? item + a.piece : all;
+    if (item >= end) return;
+    const int c_own = (block * kWave + lane) * N, c = c_own + N > a.width ? a.width - N : c_own;
+    const bool on = c_own < a.width;
+    const T* const dout = static_cast<const T*>(a.dout) + c;
+    T* const dtable = static_cast<T*>(a.dtable) + c;
+    float sum[N] = {};
+    const auto put = [&](float* to) {
+        if (on) reinterpret_cast<Elements<float, N>*>(sum)->store(to + (int64_t)piece * a.width + c);
+    };
+    const auto clear = [&] {
 #pragma unroll
-            for (int j = 0; j < N; ++j) sum[j] += (float)e.v[j];
+        for (int e = 0; e < N; ++e) sum[e] = 0;
+    };
+    int p = place_at(a, n, item), v = (int)(item - p);
+    int ends = first_not(p, n, [&](int q) { return (int64_t)q + a.key[q] < end; });      // places up to the piece's end
+    const int v_end = (int)(end - ends);
+    // a row from before: long, or not this piece's
+    bool headed = p > 0 && a.key[p - 1] == v;
+    if (headed) {
+        const int back = p > a.piece ? p - a.piece : 0, first = first_not(back, p, [&](int q) { return a.key[q] < v; });
+        if (!((first == back && back > 0 && a.key[back - 1] == v) || is_long(a, n, first, v))) {
+            headed = false;
+            p = first_not(p, n < first + a.piece ? n : first + a.piece, [&](int q) { return a.key[q] == v; });
+            ++v;
         }
-        Of o;
-#pragma unroll
-        for (int j = 0; j < N; ++j) o.v[j] = (T)(sum[j] * scale);
-        o.store(dtable + v * width + c);
     }
+    // a row that has places here and does not end here: to its last place, where it is not long
+    const bool open = ends > p && a.key[ends - 1] == v_end;
+    bool trailing = open;
+    if (open && !(headed && v == v_end)) {
+        const int first = first_not(p, ends, [&](int q) { return a.key[q] < v_end; });
+        if (!is_long(a, n, first, v_end)) {
+            trailing = false;
+            ends = first_not(ends, n < first + a.piece ? n : first + a.piece, [&](int q) { return a.key[q] == v_end; });
+        }
+    }
+    const int last = open && !trailing ? v_end + 1 : v_end;      // rows before it are ended here
+    const auto finish = [&] {
+        if (headed) put(a.head);
+        else if (on) {
+            Of o;
+#pragma unroll
+            for (int e = 0; e < N; ++e) o.v[e] = (T)(sum[e] * a.scale);
+            o.store(dtable + (int64_t)v * a.width);
+        }
+        headed = false;
+        ++v;
+        clear();
+    };
+    for (; p < ends; p += kWave) {
+        const int here = ends - p < kWave ? ends - p : kWave, at = p + (lane < here ? lane : here - 1);
+        const int key = a.key[at], slot = a.slot[at];
+        for (int j0 = 0; j0 < here; j0 += kAtOnce) {
+            Of row[kAtOnce];
+#pragma unroll
+            for (int u = 0; u < kAtOnce; ++u) {
+                const int j = j0 + u < here ? j0 + u : here - 1;
+                row[u] = Of::load(dout + (int64_t)__builtin_amdgcn_readlane(slot, j) * a.width);
+            }
+#pragma unroll
+            for (int u = 0; u < kAtOnce; ++u) {
+                if (j0 + u >= here) break;
+                const int k = __builtin_amdgcn_readlane(key, j0 + u);
+                while (v < k) finish();
+#pragma unroll
+                for (int e = 0; e < N; ++e) sum[e] += (float)row[u].v[e];
+            }
+        }
+    }
+    while (v < last) finish();
+    if (trailing) put(a.trail);
+}
+
+// A wave for each piece and block of channels: what a long row has, in the piece that it ends in.
+template <typename T, int N>
+__global__ __launch_bounds__(kBlock) void k_embed_join(SumArgs a)
+{
+    const int lane = threadIdx.x % kWave;
+    const int64_t id = (int64_t)blockIdx.x * kWaves + __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+    const int piece = (int)(id / a.blocks), block = (int)(id - (int64_t)piece * a.blocks);
+    if (piece >= a.pieces) return;
+    const int n = *a.left;
+    const int64_t item = (int64_t)piece * a.piece, all = (int64_t)a.vocab + n, end = item + a.piece < all ? item + a.piece : all;
+    if (item >= end) return;
+    const int p = place_at(a, n, item), v = (int)(item - p);
+    if (p == 0 || a.key[p - 1] != v) return;
+    const int ends = first_not(p, n, [&](int q) { return (int64_t)q + a.key[q] < end; });
+    if (v == (int)(end - ends)) return;      // the row does not end here
+    const int first = first_not(0, p, [&](int q) { return a.key[q] < v; });
+    if (!is_long(a, n, first, v)) return;
+    const int c_own = (block * kWave + lane) * N, c = c_own + N > a.width ? a.width - N : c_own;
+    if (c_own >= a.width) return;
+    typedef Elements<float, N> Sum;
+    float sum[N] = {};
+    const auto add = [&](const Sum& s) {
+#pragma unroll
+        for (int e = 0; e < N; ++e) sum[e] += s.v[e];
+    };
+    constexpr int kAtOnce = 8;
+    const float* const trail = a.trail + c;
+    int i = (int)(((int64_t)first + v) / a.piece);
+    for (; i + kAtOnce <= piece; i += kAtOnce) {
+        Sum s[kAtOnce];
+#pragma unroll
+        for (int u = 0; u < kAtOnce; ++u) s[u] = Sum::load(trail + (int64_t)(i + u) * a.width);
+#pragma unroll
+        for (int u = 0; u < kAtOnce; ++u) add(s[u]);
+    }
+    for (; i < piece; ++i) add(Sum::load(trail + (int64_t)i * a.width));
+    add(Sum::load(a.head + (int64_t)piece * a.width + c));
+    Elements<T, N> o;
+#pragma unroll
+    for (int e = 0; e < N; ++e) o.v[e] = (T)(sum[e] * a.scale);
+    o.store(static_cast<T*>(a.dtable) + (int64_t)v * a.width + c);
 }
 
 }  // namespace
@@ -214,7 +372,7 @@ int launch_embed(int64_t n, int vocab, int width, int dtype, const int* token, c
         typedef decltype(t) T;
         const auto go = [&](auto kernel, int per) -> int {
             const int lg = lanes_log((width + per - 1) / per);
-            const int64_t blocks = ((n << lg) + kBlock - 1) / kBlock;
+            const int64_t rows = (int64_t)(kBlock >> lg) * kRowsAtOnce, blocks = (n + rows - 1) / rows;
             if (blocks > kMostBlocks) return GR_ERR_TOO_LARGE;
             kernel<<<(unsigned)blocks, kBlock, 0, s>>>(token, static_cast<const T*>(table), scale, static_cast<T*>(out), n, vocab, width, lg);
             return launched();
@@ -248,16 +406,38 @@ int launch_embed_backward(gr_tokens* h, int64_t n, int vocab, int width, int dty
     }
     return by_type(dtype, [&](auto t) {
         typedef decltype(t) T;
-        const auto go = [&](auto kernel, int per) -> int {
-            const int lg = lanes_log((width + per - 1) / per);
-            const int64_t blocks = (((int64_t)vocab << lg) + kBlock - 1) / kBlock;
-            if (blocks > kMostBlocks) return GR_ERR_TOO_LARGE;
-            kernel<<<(unsigned)blocks, kBlock, 0, s>>>(key[at], slot[at], n > 0 ? left : nullptr, static_cast<const T*>(dout), scale,
-                                                       static_cast<T*>(dtable), vocab, width, lg);
+        const auto go = [&](auto count) -> int {
+            constexpr int N = decltype(count)::value;
+            SumArgs b{};
+            b.key = key[at]; b.slot = slot[at]; b.left = n > 0 ? left : nullptr; b.dout = dout; b.dtable = dtable; b.scale = scale; b.vocab = vocab;
+            b.width = width;
+            b.blocks = (width + kWave * N - 1) / (kWave * N);
+            // as many pieces as there are waves in a few rounds; no less than 64 items each
+            const int64_t items = vocab + n, most = kSumWaves / b.blocks > 1 ? kSumWaves / b.blocks : 1;
+            const int64_t piece = (items + most - 1) / most > 64 ? (items + most - 1) / most : 64;
+            b.piece = (int)piece;
+            b.pieces = (int)((items + piece - 1) / piece);
+            b.head = h->parts;
+            b.trail = h->parts + (int64_t)b.pieces * width;
+            if (2 * (int64_t)b.pieces * width > h->n_parts) return GR_ERR_TOO_LARGE;
+            const int64_t waves = (int64_t)b.pieces * b.blocks, blocks = (waves + kWaves - 1) / kWaves;
+            k_embed_sums<T, N><<<(unsigned)blocks, kBlock, 0, s>>>(b);
+            if (n > piece) k_embed_join<T, N><<<(unsigned)blocks, kBlock, 0, s>>>(b);
             return launched();
         };
-        return width >= Chunk<T>::n ? go(k_embed_sums<T, Chunk<T>::n>, Chunk<T>::n) : go(k_embed_sums<T, 1>, 1);
+        // 16 bytes a lane, fewer where a row has not as many for all lanes
+        constexpr int kMost = Chunk<T>::n;
+        if (width >= kWave * kMost) return go(std::integral_constant<int, kMost>{});
+        if (width >= kWave * kMost / 2) return go(std::integral_constant<int, kMost / 2>{});
+        return go(std::integral_constant<int, 1>{});
     });
+}
+
+// (blocks of channels of 64 lanes: a wave's sums are 64 * 8 channels at most, and there are kSumWaves or one a block)
+int64_t embed_parts(int width)
+{
+    const int64_t most = 2 * (int64_t)kWave * 8 * kSumWaves, one = 2 * (int64_t)width;
+    return most > one ? most : one;
 }
 
 }  // namespace gr

@@ -647,7 +647,7 @@ def test_refusals(native, monkeypatch):
 class _Handle(binding.C.Structure):
     """The first members of a handle."""
     _fields_ = [("max_tokens", binding.C.c_int64), ("max_vocab", binding.C.c_int), ("max_width", binding.C.c_int), ("order", binding.C.c_void_p),
-                ("words", binding.C.c_void_p), ("n_words", binding.C.c_size_t), ("control", binding.C.c_void_p), ("counters", binding.C.c_int)]
+                ("parts", binding.C.c_void_p), ("n_parts", binding.C.c_int64), ("words", binding.C.c_void_p), ("n_words", binding.C.c_size_t), ("control", binding.C.c_void_p), ("counters", binding.C.c_int)]
 
 
 def test_the_last_number_of_a_call():
