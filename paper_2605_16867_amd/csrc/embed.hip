@@ -11,7 +11,7 @@
 namespace gr {
 namespace {
 
-constexpr int kBlock = 256, kWave = 64, kWaves = kBlock / kWave, kSumWaves = 16384;
+constexpr int kBlock = 256, kWave = 64, kWaves = kBlock / kWave;
 
 // log2 of the lanes that share a row of so many pieces
 int lanes_log(int pieces)
@@ -70,6 +70,8 @@ __global__ __launch_bounds__(kBlock) void k_embed(const int* token, const T* tab
 //
 // A pass: how many tokens of each digit every unit of 2 048 has; for each digit the sums over units; the places.
 
+constexpr int kFewUnits = 64;      // up to so many each workgroup of the places adds them up itself, one launch less
+
 struct SortArgs {
     const int *key, *slot;      // slot: null in the first pass, where they are the places themselves
     int *to_key, *to_slot;
@@ -77,6 +79,7 @@ struct SortArgs {
     int64_t n;      // tokens (in later passes: most)
     const int* left;      // null in the first pass: how many there are
     int units, vocab, shift, mask;
+    int summed;      // digits holds what is before a unit, and those of all; else each unit's own
 };
 
 __device__ __forceinline__ int64_t count_of(const SortArgs& a) { return a.left ? *a.left : a.n; }
@@ -101,7 +104,7 @@ __global__ __launch_bounds__(kBlock) void k_digit_count(SortArgs a)
         if (d >= 0) atomicAdd(&hist[d], 1);
     }
     __syncthreads();
-    for (int d = threadIdx.x; d <= a.mask; d += kBlock) a.digits[(int64_t)d * a.units + blockIdx.x] = hist[d];
+    for (int d = threadIdx.x; d <= a.mask; d += kBlock) a.digits[a.summed ? (int64_t)d * a.units + blockIdx.x : (int64_t)blockIdx.x * kDigits + d] = hist[d];
 }
 
 // Over a workgroup: the sum of the values of lower threads, and that of all.
@@ -166,10 +169,21 @@ __global__ __launch_bounds__(kBlock) void k_digit_place(SortArgs a, int bits, in
     for (int d0 = 0; d0 <= a.mask; d0 += kBlock) {
         const int d = d0 + threadIdx.x;
         int all;
-        int at = before + before_me(d <= a.mask ? a.digits[(int64_t)kDigits * a.units + d] : 0, part, &all);
+        int earlier = 0, whole = 0;
+        if (d <= a.mask) {
+            if (a.summed) {
+                earlier = a.digits[(int64_t)d * a.units + blockIdx.x];
+                whole = a.digits[(int64_t)kDigits * a.units + d];
+            } else
+                for (int u = 0; u < a.units; ++u) {
+                    const int own = a.digits[(int64_t)u * kDigits + d];
+                    earlier += u < (int)blockIdx.x ? own : 0;
+                    whole += own;
+                }
+        }
+        int at = before + before_me(whole, part, &all) + earlier;
         before += all;
         if (d > a.mask) continue;
-        at += a.digits[(int64_t)d * a.units + blockIdx.x];
         for (int w = 0; w < kWaves; ++w) {
             const int own = next[w][d];
             next[w][d] = at;
@@ -197,6 +211,88 @@ __global__ __launch_bounds__(kBlock) void k_digit_place(SortArgs a, int bits, in
     }
 }
 
+// Few tokens are sorted by one workgroup in one launch, in shared memory, eight bits a pass: 512 of 32 000 in 5 us where six launches take 16.
+constexpr int kFewTokens = 8192, kFewThreads = 1024, kFewWaves = kFewThreads / kWave, kFewBits = 8, kFewDigits = 1 << kFewBits;
+
+__global__ __launch_bounds__(kFewThreads) void k_sort_few(const int* token, int n, int vocab, int bits, int* to_key, int* to_slot, int* left)
+{
+    __shared__ int keys[2][kFewTokens];
+    __shared__ uint16_t slots[2][kFewTokens];
+    __shared__ int next[kFewWaves][kFewDigits], part[kFewDigits / kWave];
+    const int tid = threadIdx.x, lane = tid % kWave, wave = tid / kWave;
+    for (int i = tid; i < n; i += kFewThreads) {
+        keys[0][i] = token[i];
+        slots[0][i] = (uint16_t)i;
+    }
+    const int passes = (bits + kFewBits - 1) / kFewBits;
+    int at = 0;
+    for (int pass = 0; pass < passes; ++pass, at ^= 1) {
+        const int shift = bits * pass / passes, width = bits * (pass + 1) / passes - shift, mask = (1 << width) - 1;
+        const int per = (n + kFewWaves * kWave - 1) / (kFewWaves * kWave) * kWave, from = wave * per, to = from + per < n ? from + per : n;
+        for (int i = tid; i < kFewWaves * kFewDigits; i += kFewThreads) (&next[0][0])[i] = 0;
+        __syncthreads();
+        const auto digit_at = [&](int i) {
+            const int k = i < to ? keys[at][i] : -1;
+            return k < 0 || k >= vocab ? -1 : k >> shift & mask;
+        };
+        for (int i = from + lane; i < to; i += kWave) {
+            const int d = digit_at(i);
+            if (d >= 0) atomicAdd(&next[wave][d], 1);
+        }
+        __syncthreads();
+        int before = 0, own = 0;
+        if (tid < kFewDigits) {
+            for (int w = 0; w < kFewWaves; ++w) own += next[w][tid];
+            before = own;
+            for (int d = 1; d < kWave; d *= 2) {
+                const int o = __shfl_up(before, d);
+                if (lane >= d) before += o;
+            }
+            if (lane == kWave - 1) part[wave] = before;
+        }
+        __syncthreads();
+        int all = 0;
+        for (int w = 0; w < kFewDigits / kWave; ++w) {
+            if (w < wave) before += part[w];
+            all += part[w];
+        }
+        if (tid < kFewDigits) {
+            before -= own;
+            for (int w = 0; w < kFewWaves; ++w) {
+                const int mine = next[w][tid];
+                next[w][tid] = before;
+                before += mine;
+            }
+        }
+        __syncthreads();
+        const bool last = pass + 1 == passes;
+        for (int i0 = from; i0 < to; i0 += kWave) {
+            const int i = i0 + lane, d = digit_at(i);
+            uint64_t same = __ballot(d >= 0);
+            for (int b = 0; b < width; ++b) {
+                const uint64_t set = __ballot(d >> b & 1);
+                same &= d >> b & 1 ? set : ~set;
+            }
+            if (d >= 0) {
+                const int place = next[wave][d] + __popcll(same & ((uint64_t(1) << lane) - 1));
+                if (last) {
+                    to_key[place] = keys[at][i];
+                    to_slot[place] = slots[at][i];
+                } else {
+                    keys[at ^ 1][place] = keys[at][i];
+                    slots[at ^ 1][place] = slots[at][i];
+                }
+            }
+            wave_sync();
+            if (d >= 0 && (same >> lane) == 1) next[wave][d] += __popcll(same);
+            wave_sync();
+        }
+        n = all;
+        __syncthreads();
+    }
+    if (tid == 0) *left = n;
+}
+
 // ---- the sums ----------------------------------------------------------------------------------
 //
 // Sorted places and rows of the table are one line of work: the places of a row, then the row itself, which is written.  A wave takes kPiece items
@@ -209,6 +305,7 @@ struct SumArgs {
     const void* dout;
     void* dtable;
     float *head, *trail;      // [pieces][width] of long rows: of the piece that has the row's end, of the others
+    int2* ended;              // [pieces] a long row that ends there and the piece that it starts in; -1
     float scale;
     int vocab, width, piece, pieces, blocks;
 };
@@ -274,6 +371,11 @@ __global__ __launch_bounds__(kBlock) void k_embed_sums(SumArgs a)
             ++v;
         }
     }
+    if (block == 0) {
+        int2 e = {-1, 0};
+        if (headed && v < v_end) e = {v, (int)(((int64_t)first_not(0, p, [&](int q) { return a.key[q] < v; }) + v) / a.piece)};
+        if (lane == 0) a.ended[piece] = e;
+    }
     // a row that has places here and does not end here: to its last place, where it is not long
     const bool open = ends > p && a.key[ends - 1] == v_end;
     bool trailing = open;
@@ -321,47 +423,51 @@ __global__ __launch_bounds__(kBlock) void k_embed_sums(SumArgs a)
     if (trailing) put(a.trail);
 }
 
-// A wave for each piece and block of channels: what a long row has, in the piece that it ends in.
+// Of kJoined pieces and a block of channels: the parts of long rows that end there, a quarter of them by each wave, and those in order.
+constexpr int kJoined = 32, kJoinChannels = 4;
+
 template <typename T, int N>
 __global__ __launch_bounds__(kBlock) void k_embed_join(SumArgs a)
 {
-    const int lane = threadIdx.x % kWave;
-    const int64_t id = (int64_t)blockIdx.x * kWaves + __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
-    const int piece = (int)(id / a.blocks), block = (int)(id - (int64_t)piece * a.blocks);
-    if (piece >= a.pieces) return;
-    const int n = *a.left;
-    const int64_t item = (int64_t)piece * a.piece, all = (int64_t)a.vocab + n, end = item + a.piece < all ? item + a.piece : all;
-    if (item >= end) return;
-    const int p = place_at(a, n, item), v = (int)(item - p);
-    if (p == 0 || a.key[p - 1] != v) return;
-    const int ends = first_not(p, n, [&](int q) { return (int64_t)q + a.key[q] < end; });
-    if (v == (int)(end - ends)) return;      // the row does not end here
-    const int first = first_not(0, p, [&](int q) { return a.key[q] < v; });
-    if (!is_long(a, n, first, v)) return;
-    const int c_own = (block * kWave + lane) * N, c = c_own + N > a.width ? a.width - N : c_own;
-    if (c_own >= a.width) return;
     typedef Elements<float, N> Sum;
-    float sum[N] = {};
-    const auto add = [&](const Sum& s) {
+    __shared__ float part[kWaves][kWave * N];
+    const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave, piece0 = blockIdx.y * kJoined;
+    const int c_own = (blockIdx.x * kWave + lane) * N, c = c_own + N > a.width ? a.width - N : c_own;
+    const int64_t items = (int64_t)a.vocab + *a.left;
+    int2 ended = {-1, 0};
+    // (behind the last item there may be pieces that nothing was written for)
+    if (lane < kJoined && piece0 + lane < a.pieces && (int64_t)(piece0 + lane) * a.piece < items) ended = a.ended[piece0 + lane];
+    for (uint64_t some = __ballot(ended.x >= 0); some; some &= some - 1) {
+        const int at = __builtin_ctzll(some), piece = piece0 + at, v = __builtin_amdgcn_readlane(ended.x, at), i0 = __builtin_amdgcn_readlane(ended.y, at);
+        const int per = (piece - i0 + kWaves - 1) / kWaves, from = i0 + wave * per, to = from + per < piece ? from + per : piece;
+        float sum[N] = {};
+        constexpr int kAtOnce = 8;
+        for (int i = from; i < to; i += kAtOnce) {
+            Sum s[kAtOnce];
 #pragma unroll
-        for (int e = 0; e < N; ++e) sum[e] += s.v[e];
-    };
-    constexpr int kAtOnce = 8;
-    const float* const trail = a.trail + c;
-    int i = (int)(((int64_t)first + v) / a.piece);
-    for (; i + kAtOnce <= piece; i += kAtOnce) {
-        Sum s[kAtOnce];
+            for (int u = 0; u < kAtOnce; ++u) s[u] = Sum::load(a.trail + (int64_t)(i + u < to ? i + u : i) * a.width + c);
 #pragma unroll
-        for (int u = 0; u < kAtOnce; ++u) s[u] = Sum::load(trail + (int64_t)(i + u) * a.width);
+            for (int u = 0; u < kAtOnce; ++u)
 #pragma unroll
-        for (int u = 0; u < kAtOnce; ++u) add(s[u]);
+                for (int e = 0; e < N; ++e) sum[e] += i + u < to ? s[u].v[e] : 0.0f;
+        }
+#pragma unroll
+        for (int e = 0; e < N; ++e) part[wave][lane * N + e] = sum[e];
+        __syncthreads();
+        if (wave == 0 && c_own < a.width) {
+            const Sum head = Sum::load(a.head + (int64_t)piece * a.width + c);
+            Elements<T, N> o;
+#pragma unroll
+            for (int e = 0; e < N; ++e) {
+                float all = part[0][lane * N + e];
+#pragma unroll
+                for (int w = 1; w < kWaves; ++w) all += part[w][lane * N + e];
+                o.v[e] = (T)((all + head.v[e]) * a.scale);
+            }
+            o.store(static_cast<T*>(a.dtable) + (int64_t)v * a.width + c);
+        }
+        __syncthreads();
     }
-    for (; i < piece; ++i) add(Sum::load(trail + (int64_t)i * a.width));
-    add(Sum::load(a.head + (int64_t)piece * a.width + c));
-    Elements<T, N> o;
-#pragma unroll
-    for (int e = 0; e < N; ++e) o.v[e] = (T)(sum[e] * a.scale);
-    o.store(static_cast<T*>(a.dtable) + (int64_t)v * a.width + c);
 }
 
 }  // namespace
@@ -389,10 +495,11 @@ int launch_embed_backward(gr_tokens* h, int64_t n, int vocab, int width, int dty
     const int passes = (bits + kDigitBits - 1) / kDigitBits;
     int *const key[2] = {h->order, h->order + h->max_tokens}, *const slot[2] = {h->order + 2 * h->max_tokens, h->order + 3 * h->max_tokens};
     SortArgs a{};
-    a.digits = h->digits; a.n = n; a.units = (int)sort_units(n); a.vocab = vocab;
+    a.digits = h->digits; a.n = n; a.units = (int)sort_units(n); a.vocab = vocab; a.summed = a.units > kFewUnits;
     int* const left = h->digits + (sort_units(h->max_tokens) + 1) * kDigits;
     int at = 0;
-    for (int p = 0; p < passes && n > 0; ++p) {
+    if (n > 0 && n <= kFewTokens) k_sort_few<<<1, kFewThreads, 0, s>>>(token, (int)n, vocab, bits, key[0], slot[0], left);
+    for (int p = 0; p < passes && n > kFewTokens; ++p) {
         const int from = bits * p / passes, to = bits * (p + 1) / passes;
         a.key = p ? key[at] : token;
         a.slot = p ? slot[at] : nullptr;
@@ -401,7 +508,7 @@ int launch_embed_backward(gr_tokens* h, int64_t n, int vocab, int width, int dty
         a.to_key = key[at]; a.to_slot = slot[at];
         a.shift = from; a.mask = (1 << (to - from)) - 1;
         k_digit_count<<<a.units, kBlock, 0, s>>>(a);
-        k_digit_sum<<<a.mask + 1, kBlock, 0, s>>>(a);
+        if (a.summed) k_digit_sum<<<a.mask + 1, kBlock, 0, s>>>(a);
         k_digit_place<<<a.units, kBlock, 0, s>>>(a, to - from, p ? nullptr : left);
     }
     return by_type(dtype, [&](auto t) {
@@ -418,11 +525,16 @@ int launch_embed_backward(gr_tokens* h, int64_t n, int vocab, int width, int dty
             b.piece = (int)piece;
             b.pieces = (int)((items + piece - 1) / piece);
             b.head = h->parts;
+            b.ended = h->ended;
             b.trail = h->parts + (int64_t)b.pieces * width;
             if (2 * (int64_t)b.pieces * width > h->n_parts) return GR_ERR_TOO_LARGE;
             const int64_t waves = (int64_t)b.pieces * b.blocks, blocks = (waves + kWaves - 1) / kWaves;
             k_embed_sums<T, N><<<(unsigned)blocks, kBlock, 0, s>>>(b);
-            if (n > piece) k_embed_join<T, N><<<(unsigned)blocks, kBlock, 0, s>>>(b);
+            if (n > piece) {      // (a row has more places than that, or there is nothing to join)
+                constexpr int J = N < kJoinChannels ? N : kJoinChannels;
+                const dim3 grid((width + kWave * J - 1) / (kWave * J), (b.pieces + kJoined - 1) / kJoined);
+                k_embed_join<T, J><<<grid, kBlock, 0, s>>>(b);
+            }
             return launched();
         };
         // 16 bytes a lane, fewer where a row has not as many for all lanes

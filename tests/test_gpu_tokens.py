@@ -54,7 +54,8 @@ def test_rows_that_are_no_numbers_stay_where_they_are():
 @pytest.mark.parametrize("dtype", TYPES)
 @pytest.mark.parametrize("n,vocab,width", [(0, 5, 8), (1, 1, 1), (1, 9, 16), (7, 3, 5), (64, 100, 4), (65, 2, 3), (300, 513, 33), (2047, 512, 64),
                                            (2049, 1000, 256), (5000, 300, 511), (4100, 64, 1024), (30000, 7, 40), (9000, 40000, 24),
-                                           (70000, 3000, 20), (12000, 300000, 8)])
+                                           (70000, 3000, 20), (12000, 300000, 8), (8192, 70000, 4), (8193, 70000, 4), (150000, 5, 9),
+                                           (500, 2000000, 1), (140000, 300, 6)])
 def test_embed_backward(n, vocab, width, dtype):
     rng = np.random.default_rng(n + width)
     h = binding.Tokens(max(n, 17), vocab, width)
@@ -647,7 +648,8 @@ def test_refusals(native, monkeypatch):
 class _Handle(binding.C.Structure):
     """The first members of a handle."""
     _fields_ = [("max_tokens", binding.C.c_int64), ("max_vocab", binding.C.c_int), ("max_width", binding.C.c_int), ("order", binding.C.c_void_p),
-                ("parts", binding.C.c_void_p), ("n_parts", binding.C.c_int64), ("words", binding.C.c_void_p), ("n_words", binding.C.c_size_t), ("control", binding.C.c_void_p), ("counters", binding.C.c_int)]
+                ("parts", binding.C.c_void_p), ("n_parts", binding.C.c_int64), ("ended", binding.C.c_void_p),
+                ("words", binding.C.c_void_p), ("n_words", binding.C.c_size_t), ("control", binding.C.c_void_p), ("counters", binding.C.c_int)]
 
 
 def test_the_last_number_of_a_call():
