@@ -12,6 +12,7 @@ namespace gr {
 namespace {
 
 constexpr int kBlock = 256, kWave = 64, kWaves = kBlock / kWave;
+constexpr int64_t kCacheBytes = 256 << 20;      // of the device's last-level cache
 
 // log2 of the lanes that share a row of so many pieces
 int lanes_log(int pieces)
@@ -29,6 +30,16 @@ __device__ __forceinline__ void store_past(T* at, const Elements<T, N>& e)
     Vec v;
     __builtin_memcpy(&v, &e, sizeof e);
     __builtin_nontemporal_store(v, reinterpret_cast<Vec*>(at));
+}
+
+template <typename T, int N>
+__device__ __forceinline__ Elements<T, N> load_past(const T* at)
+{
+    typedef T Vec __attribute__((ext_vector_type(N), aligned(sizeof(T))));
+    const Vec v = __builtin_nontemporal_load(reinterpret_cast<const Vec*>(at));
+    Elements<T, N> e;
+    __builtin_memcpy(&e, &v, sizeof e);
+    return e;
 }
 
 constexpr int kRowsAtOnce = 4;      // rows of a group of lanes whose loads are under way together
@@ -92,53 +103,54 @@ __device__ __forceinline__ int digit_of(const SortArgs& a, int64_t i, int64_t n,
     return *key < 0 || *key >= a.vocab ? -1 : *key >> a.shift & a.mask;
 }
 
-__global__ __launch_bounds__(kBlock) void k_digit_count(SortArgs a)
+constexpr int kSortThreads = 1024, kSortWaves = kSortThreads / kWave, kSortRounds = kSortUnit / kSortThreads;
+
+__global__ __launch_bounds__(kSortThreads) void k_digit_count(SortArgs a)
 {
     __shared__ int hist[kDigits];
-    for (int d = threadIdx.x; d <= a.mask; d += kBlock) hist[d] = 0;
+    if (threadIdx.x < kDigits) hist[threadIdx.x] = 0;
+    const int64_t from = (int64_t)blockIdx.x * kSortUnit + threadIdx.x, n = count_of(a);
+    int d[kSortRounds], key;
+#pragma unroll
+    for (int r = 0; r < kSortRounds; ++r) d[r] = digit_of(a, from + r * kSortThreads, n, &key);
     __syncthreads();
-    const int64_t from = (int64_t)blockIdx.x * kSortUnit, n = count_of(a);
-    for (int i = threadIdx.x; i < kSortUnit; i += kBlock) {
-        int key;
-        const int d = digit_of(a, from + i, n, &key);
-        if (d >= 0) atomicAdd(&hist[d], 1);
-    }
+#pragma unroll
+    for (int r = 0; r < kSortRounds; ++r)
+        if (d[r] >= 0) atomicAdd(&hist[d[r]], 1);
     __syncthreads();
-    for (int d = threadIdx.x; d <= a.mask; d += kBlock) a.digits[a.summed ? (int64_t)d * a.units + blockIdx.x : (int64_t)blockIdx.x * kDigits + d] = hist[d];
+    const int t = threadIdx.x;
+    if (t <= a.mask) a.digits[a.summed ? (int64_t)t * a.units + blockIdx.x : (int64_t)blockIdx.x * kDigits + t] = hist[t];
 }
 
-// Over a workgroup: the sum of the values of lower threads, and that of all.
-__device__ __forceinline__ int before_me(int own, int* part, int* all)
+// The sum over the lanes up to this one.
+__device__ __forceinline__ int up_to_me(int v)
 {
-    const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
-    int v = own;
+    const int lane = threadIdx.x % kWave;
     for (int d = 1; d < kWave; d *= 2) {
         const int o = __shfl_up(v, d);
         if (lane >= d) v += o;
     }
-    if (lane == kWave - 1) part[wave] = v;
-    __syncthreads();
-    int base = 0, sum = 0;
-    for (int w = 0; w < kWaves; ++w) {
-        if (w < wave) base += part[w];
-        sum += part[w];
-    }
-    __syncthreads();
-    *all = sum;
-    return base + v - own;
+    return v;
 }
 
+// Of a digit: what is before each unit, and the sum of all.
 __global__ __launch_bounds__(kBlock) void k_digit_sum(SortArgs a)
 {
     __shared__ int part[kWaves];
+    const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
     int* const at = a.digits + (int64_t)blockIdx.x * a.units;
     int before = 0;
     for (int u0 = 0; u0 < a.units; u0 += kBlock) {
-        const int u = u0 + threadIdx.x, own = u < a.units ? at[u] : 0;
-        int all;
-        const int b = before_me(own, part, &all);
-        if (u < a.units) at[u] = before + b;
-        before += all;
+        const int u = u0 + threadIdx.x, own = u < a.units ? at[u] : 0, upto = up_to_me(own);
+        if (lane == kWave - 1) part[wave] = upto;
+        __syncthreads();
+        int base = before;
+        for (int w = 0; w < kWaves; ++w) {
+            if (w < wave) base += part[w];
+            before += part[w];
+        }
+        if (u < a.units) at[u] = base + upto - own;
+        __syncthreads();
     }
     if (threadIdx.x == 0) a.digits[(int64_t)kDigits * a.units + blockIdx.x] = before;
 }
@@ -150,69 +162,85 @@ __device__ __forceinline__ void wave_sync()
     __builtin_amdgcn_wave_barrier();
 }
 
-// Waves take 512 tokens each, 64 at a time; lanes of one digit find each other bit by bit.
-__global__ __launch_bounds__(kBlock) void k_digit_place(SortArgs a, int bits, int* left)
+// The lanes of a wave that have the same digit, of so many bits; none for a digit of -1.
+__device__ __forceinline__ uint64_t lanes_of(int digit, int bits)
 {
-    __shared__ int part[kWaves], next[kWaves][kDigits];
-    constexpr int kPer = kSortUnit / kWaves;
-    const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
-    for (int i = threadIdx.x; i < kWaves * kDigits; i += kBlock) (&next[0][0])[i] = 0;
-    __syncthreads();
-    const int64_t from = (int64_t)blockIdx.x * kSortUnit + wave * kPer, n = count_of(a);
-    for (int i = lane; i < kPer; i += kWave) {
-        int key;
-        const int d = digit_of(a, from + i, n, &key);
-        if (d >= 0) atomicAdd(&next[wave][d], 1);
+    uint64_t same = __ballot(digit >= 0);
+    for (int b = 0; b < bits; ++b) {
+        const uint64_t set = __ballot(digit >> b & 1);
+        same &= digit >> b & 1 ? set : ~set;
     }
-    __syncthreads();
-    int before = 0;
-    for (int d0 = 0; d0 <= a.mask; d0 += kBlock) {
-        const int d = d0 + threadIdx.x;
-        int all;
-        int earlier = 0, whole = 0;
-        if (d <= a.mask) {
-            if (a.summed) {
-                earlier = a.digits[(int64_t)d * a.units + blockIdx.x];
-                whole = a.digits[(int64_t)kDigits * a.units + d];
-            } else
-                for (int u = 0; u < a.units; ++u) {
-                    const int own = a.digits[(int64_t)u * kDigits + d];
-                    earlier += u < (int)blockIdx.x ? own : 0;
-                    whole += own;
+    return same;
+}
+
+// Waves take 128 tokens each, 64 at a time; lanes of one digit find each other bit by bit.
+__global__ __launch_bounds__(kSortThreads) void k_digit_place(SortArgs a, int bits, int* left)
+{
+    __shared__ int part[kDigits / kWave], next[kSortWaves][kDigits];
+    const int tid = threadIdx.x, lane = tid % kWave, wave = tid / kWave;
+    const int64_t from = (int64_t)blockIdx.x * kSortUnit + wave * (kSortUnit / kSortWaves) + lane, n = count_of(a);
+    int key[kSortRounds], slot[kSortRounds], d[kSortRounds];
+#pragma unroll
+    for (int r = 0; r < kSortRounds; ++r) {
+        const int64_t i = from + r * kWave;
+        d[r] = digit_of(a, i, n, &key[r]);
+        slot[r] = a.slot && i < n ? a.slot[i] : (int)i;
+    }
+    int earlier = 0, whole = 0;
+    if (tid <= a.mask) {
+        if (a.summed) {
+            earlier = a.digits[(int64_t)tid * a.units + blockIdx.x];
+            whole = a.digits[(int64_t)kDigits * a.units + tid];
+        } else
+            for (int u0 = 0; u0 < a.units; u0 += 16) {
+                int own[16];
+#pragma unroll
+                for (int u = 0; u < 16; ++u) own[u] = a.digits[(int64_t)(u0 + u < a.units ? u0 + u : u0) * kDigits + tid];
+#pragma unroll
+                for (int u = 0; u < 16; ++u) {
+                    earlier += u0 + u < (int)blockIdx.x ? own[u] : 0;
+                    whole += u0 + u < a.units ? own[u] : 0;
                 }
+            }
+    }
+    for (int i = tid; i < kSortWaves * kDigits; i += kSortThreads) (&next[0][0])[i] = 0;
+    const int upto = up_to_me(whole);
+    if (tid < kDigits && lane == kWave - 1) part[wave] = upto;
+    __syncthreads();
+#pragma unroll
+    for (int r = 0; r < kSortRounds; ++r)
+        if (d[r] >= 0) atomicAdd(&next[wave][d[r]], 1);
+    __syncthreads();
+    if (tid < kDigits) {
+        int at = earlier + upto - whole, all = 0;
+        for (int w = 0; w < kDigits / kWave; ++w) {
+            if (w < wave) at += part[w];
+            all += part[w];
         }
-        int at = before + before_me(whole, part, &all) + earlier;
-        before += all;
-        if (d > a.mask) continue;
-        for (int w = 0; w < kWaves; ++w) {
-            const int own = next[w][d];
-            next[w][d] = at;
+        if (left && blockIdx.x == 0 && tid == 0) *left = all;
+        for (int w = 0; w < kSortWaves; ++w) {
+            const int own = next[w][tid];
+            next[w][tid] = at;
             at += own;
         }
     }
-    if (left && blockIdx.x == 0 && threadIdx.x == 0) *left = before;
     __syncthreads();
-    for (int i = lane; i < kPer; i += kWave) {
-        int key = 0;
-        const int d = digit_of(a, from + i, n, &key);
-        uint64_t same = __ballot(d >= 0);
-        for (int b = 0; b < bits; ++b) {
-            const uint64_t set = __ballot(d >> b & 1);
-            same &= d >> b & 1 ? set : ~set;
-        }
-        if (d >= 0) {
-            const int rank = __popcll(same & ((uint64_t(1) << lane) - 1)), at = next[wave][d] + rank;
-            a.to_key[at] = key;
-            a.to_slot[at] = a.slot ? a.slot[from + i] : (int)(from + i);
+#pragma unroll
+    for (int r = 0; r < kSortRounds; ++r) {
+        const uint64_t same = lanes_of(d[r], bits);
+        if (d[r] >= 0) {
+            const int at = next[wave][d[r]] + __popcll(same & ((uint64_t(1) << lane) - 1));
+            a.to_key[at] = key[r];
+            a.to_slot[at] = slot[r];
         }
         wave_sync();
-        if (d >= 0 && (same >> lane) == 1) next[wave][d] += __popcll(same);
+        if (d[r] >= 0 && (same >> lane) == 1) next[wave][d[r]] += __popcll(same);
         wave_sync();
     }
 }
 
 // Few tokens are sorted by one workgroup in one launch, in shared memory, eight bits a pass: 512 of 32 000 in 5 us where six launches take 16.
-constexpr int kFewTokens = 8192, kFewThreads = 1024, kFewWaves = kFewThreads / kWave, kFewBits = 8, kFewDigits = 1 << kFewBits;
+constexpr int kFewTokens = 4096, kFewThreads = 1024, kFewWaves = kFewThreads / kWave, kFewBits = 8, kFewDigits = 1 << kFewBits;
 
 __global__ __launch_bounds__(kFewThreads) void k_sort_few(const int* token, int n, int vocab, int bits, int* to_key, int* to_slot, int* left)
 {
@@ -243,11 +271,7 @@ __global__ __launch_bounds__(kFewThreads) void k_sort_few(const int* token, int 
         int before = 0, own = 0;
         if (tid < kFewDigits) {
             for (int w = 0; w < kFewWaves; ++w) own += next[w][tid];
-            before = own;
-            for (int d = 1; d < kWave; d *= 2) {
-                const int o = __shfl_up(before, d);
-                if (lane >= d) before += o;
-            }
+            before = up_to_me(own);
             if (lane == kWave - 1) part[wave] = before;
         }
         __syncthreads();
@@ -268,11 +292,7 @@ __global__ __launch_bounds__(kFewThreads) void k_sort_few(const int* token, int 
         const bool last = pass + 1 == passes;
         for (int i0 = from; i0 < to; i0 += kWave) {
             const int i = i0 + lane, d = digit_at(i);
-            uint64_t same = __ballot(d >= 0);
-            for (int b = 0; b < width; ++b) {
-                const uint64_t set = __ballot(d >> b & 1);
-                same &= d >> b & 1 ? set : ~set;
-            }
+            const uint64_t same = lanes_of(d, width);
             if (d >= 0) {
                 const int place = next[wave][d] + __popcll(same & ((uint64_t(1) << lane) - 1));
                 if (last) {
@@ -334,7 +354,8 @@ __device__ __forceinline__ int place_at(const SumArgs& a, int n, int64_t item)
 // More than kPiece places, from the first one.
 __device__ __forceinline__ bool is_long(const SumArgs& a, int n, int first, int v) { return first + a.piece < n && a.key[first + a.piece] == v; }
 
-template <typename T, int N>
+// kPast: rows are read past the cache.
+template <typename T, int N, bool kPast>
 __global__ __launch_bounds__(kBlock) void k_embed_sums(SumArgs a)
 {
     typedef Elements<T, N> Of;
@@ -407,7 +428,8 @@ __global__ __launch_bounds__(kBlock) void k_embed_sums(SumArgs a)
 #pragma unroll
             for (int u = 0; u < kAtOnce; ++u) {
                 const int j = j0 + u < here ? j0 + u : here - 1;
-                row[u] = Of::load(dout + (int64_t)__builtin_amdgcn_readlane(slot, j) * a.width);
+                const T* const from = dout + (int64_t)__builtin_amdgcn_readlane(slot, j) * a.width;
+                row[u] = kPast ? load_past<T, N>(from) : Of::load(from);
             }
 #pragma unroll
             for (int u = 0; u < kAtOnce; ++u) {
@@ -507,9 +529,9 @@ int launch_embed_backward(gr_tokens* h, int64_t n, int vocab, int width, int dty
         at = p & 1;
         a.to_key = key[at]; a.to_slot = slot[at];
         a.shift = from; a.mask = (1 << (to - from)) - 1;
-        k_digit_count<<<a.units, kBlock, 0, s>>>(a);
+        k_digit_count<<<a.units, kSortThreads, 0, s>>>(a);
         if (a.summed) k_digit_sum<<<a.mask + 1, kBlock, 0, s>>>(a);
-        k_digit_place<<<a.units, kBlock, 0, s>>>(a, to - from, p ? nullptr : left);
+        k_digit_place<<<a.units, kSortThreads, 0, s>>>(a, to - from, p ? nullptr : left);
     }
     return by_type(dtype, [&](auto t) {
         typedef decltype(t) T;
@@ -529,7 +551,11 @@ int launch_embed_backward(gr_tokens* h, int64_t n, int vocab, int width, int dty
             b.trail = h->parts + (int64_t)b.pieces * width;
             if (2 * (int64_t)b.pieces * width > h->n_parts) return GR_ERR_TOO_LARGE;
             const int64_t waves = (int64_t)b.pieces * b.blocks, blocks = (waves + kWaves - 1) / kWaves;
-            k_embed_sums<T, N><<<(unsigned)blocks, kBlock, 0, s>>>(b);
+            // rows of more than the cache holds would only push the table's and the sums out of it: 524 288 rows of 1 024 in bfloat16 295 us past it, 308
+            // else; 16 000 of 512 in single precision, which the last kernel may have left there, 43 and 37
+            const bool past = n * width * (int64_t)sizeof(T) > kCacheBytes;
+            if (past) k_embed_sums<T, N, true><<<(unsigned)blocks, kBlock, 0, s>>>(b);
+            else k_embed_sums<T, N, false><<<(unsigned)blocks, kBlock, 0, s>>>(b);
             if (n > piece) {      // (a row has more places than that, or there is nothing to join)
                 constexpr int J = N < kJoinChannels ? N : kJoinChannels;
                 const dim3 grid((width + kWave * J - 1) / (kWave * J), (b.pieces + kJoined - 1) / kJoined);
