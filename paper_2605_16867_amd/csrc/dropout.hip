@@ -41,7 +41,7 @@ __device__ __forceinline__ T kept(float x, uint32_t bits, uint32_t limit, float 
     return (T)(add ? fmaf(x, scale, residual) : x * scale);
 }
 
-template <typename T>
+template <typename T, bool kPast>
 __global__ __launch_bounds__(kBlock) void k_dropout(DropoutIn in, float scale, T* out)
 {
     typedef Elements<T, kPer> Of;
@@ -52,13 +52,13 @@ __global__ __launch_bounds__(kBlock) void k_dropout(DropoutIn in, float scale, T
         const Words r = philox((uint64_t)b, offset, in.seed);
         const int64_t at = b * kPer;
         if (at + kPer <= in.n) {
-            const Of v = Of::load(x + at);
+            const Of v = load_of<kPast, T, kPer>(x + at);
             Of o, add{};
-            if (residual) add = Of::load(residual + at);
+            if (residual) add = load_of<kPast, T, kPer>(residual + at);
 #pragma unroll
             for (int j = 0; j < kPer; ++j)
                 o.v[j] = kept<T>((float)v.v[j], r.w[j / 2] >> (j % 2 * 16) & 0xFFFF, in.limit, scale, (float)add.v[j], residual != nullptr);
-            o.store(out + at);
+            store_of<kPast>(out + at, o);
         } else {
 #pragma unroll
             for (int j = 0; j < kPer; ++j)
@@ -77,7 +77,9 @@ int launch_dropout(const DropoutIn& in, int dtype, void* out, hipStream_t s)
     const float scale = 65536.0f / (float)(65536 - in.limit);
     return by_type(dtype, [&](auto t) {
         typedef decltype(t) T;
-        k_dropout<T><<<(unsigned)(blocks < kMostBlocks ? blocks : kMostBlocks), kBlock, 0, s>>>(in, scale, static_cast<T*>(out));
+        const unsigned grid = (unsigned)(blocks < kMostBlocks ? blocks : kMostBlocks);
+        if (past_cache(in.n * (int64_t)sizeof(T) * (in.residual ? 3 : 2))) k_dropout<T, true><<<grid, kBlock, 0, s>>>(in, scale, static_cast<T*>(out));
+        else k_dropout<T, false><<<grid, kBlock, 0, s>>>(in, scale, static_cast<T*>(out));
         return launched();
     });
 }

@@ -12,7 +12,6 @@ namespace gr {
 namespace {
 
 constexpr int kBlock = 256, kWave = 64, kWaves = kBlock / kWave;
-constexpr int64_t kCacheBytes = 256 << 20;      // of the device's last-level cache
 
 // log2 of the lanes that share a row of so many pieces
 int lanes_log(int pieces)
@@ -20,26 +19,6 @@ int lanes_log(int pieces)
     int lg = 0;
     while (lg < 6 && (1 << lg) < pieces) ++lg;
     return lg;
-}
-
-// N elements, past the cache.
-template <typename T, int N>
-__device__ __forceinline__ void store_past(T* at, const Elements<T, N>& e)
-{
-    typedef T Vec __attribute__((ext_vector_type(N), aligned(sizeof(T))));
-    Vec v;
-    __builtin_memcpy(&v, &e, sizeof e);
-    __builtin_nontemporal_store(v, reinterpret_cast<Vec*>(at));
-}
-
-template <typename T, int N>
-__device__ __forceinline__ Elements<T, N> load_past(const T* at)
-{
-    typedef T Vec __attribute__((ext_vector_type(N), aligned(sizeof(T))));
-    const Vec v = __builtin_nontemporal_load(reinterpret_cast<const Vec*>(at));
-    Elements<T, N> e;
-    __builtin_memcpy(&e, &v, sizeof e);
-    return e;
 }
 
 constexpr int kRowsAtOnce = 4;      // rows of a group of lanes whose loads are under way together
@@ -72,7 +51,7 @@ __global__ __launch_bounds__(kBlock) void k_embed(const int* token, const T* tab
             const int64_t row = first + u * groups;
 #pragma unroll
             for (int j = 0; j < N; ++j) e[u].v[j] = from[u] ? (T)((float)e[u].v[j] * scale) : (T)0.0f;
-            if (row < n) store_past(out + row * width + c, e[u]);
+            if (row < n) store_of<true>(out + row * width + c, e[u]);
         }
     }
 }
@@ -429,7 +408,7 @@ __global__ __launch_bounds__(kBlock) void k_embed_sums(SumArgs a)
             for (int u = 0; u < kAtOnce; ++u) {
                 const int j = j0 + u < here ? j0 + u : here - 1;
                 const T* const from = dout + (int64_t)__builtin_amdgcn_readlane(slot, j) * a.width;
-                row[u] = kPast ? load_past<T, N>(from) : Of::load(from);
+                row[u] = load_of<kPast, T, N>(from);
             }
 #pragma unroll
             for (int u = 0; u < kAtOnce; ++u) {
@@ -551,9 +530,7 @@ int launch_embed_backward(gr_tokens* h, int64_t n, int vocab, int width, int dty
             b.trail = h->parts + (int64_t)b.pieces * width;
             if (2 * (int64_t)b.pieces * width > h->n_parts) return GR_ERR_TOO_LARGE;
             const int64_t waves = (int64_t)b.pieces * b.blocks, blocks = (waves + kWaves - 1) / kWaves;
-            // rows of more than the cache holds would only push the table's and the sums out of it: 524 288 rows of 1 024 in bfloat16 295 us past it, 308
-            // else; 16 000 of 512 in single precision, which the last kernel may have left there, 43 and 37
-            const bool past = n * width * (int64_t)sizeof(T) > kCacheBytes;
+            const bool past = past_cache((n + vocab) * width * (int64_t)sizeof(T));
             if (past) k_embed_sums<T, N, true><<<(unsigned)blocks, kBlock, 0, s>>>(b);
             else k_embed_sums<T, N, false><<<(unsigned)blocks, kBlock, 0, s>>>(b);
             if (n > piece) {      // (a row has more places than that, or there is nothing to join)

@@ -203,7 +203,7 @@ __device__ __forceinline__ void each(F f)
 
 // The rows of one lane.  Whether sequences enter or leave at a row, or rows are not there, is asked for the wave; lanes choose by selects: no branch by
 // lanes has what is held live on both of its sides.
-template <typename T, int N, int kRun, bool kBack>
+template <typename T, int N, int kRun, bool kBack, bool kPast>
 struct Rows {
     typedef Elements<T, N> Of;
     typedef Elements<float, N> State;
@@ -250,7 +250,7 @@ struct Rows {
     {
         const T* const base = static_cast<const T*>(p) + (int64_t)first * stride;
         const Lines at = lines(stride);
-        each<kRun>([&](auto j) { to[j] = Of::load(byte(base, at[j])); });
+        each<kRun>([&](auto j) { to[j] = load_of<kPast, T, N>(byte(base, at[j])); });
     }
 
     // The state of row j's sequence; the first one's for lanes that have no mark there.
@@ -277,7 +277,7 @@ struct Rows {
             const unsigned least = first == 0 ? at.step : 0;
             each<kRun>([&](auto j) {
                 const unsigned off = at[j];
-                r.was[j] = Of::load(byte(base, off < least ? off + least : off));
+                r.was[j] = load_of<kPast, T, N>(byte(base, off < least ? off + least : off));
             });
         }
     }
@@ -363,10 +363,10 @@ struct Rows {
             }
             if (write) {
                 if constexpr (!kBack) {
-                    if (a.y) o.store(byte(static_cast<T*>(a.y) + (int64_t)first * a.in.width, at_y[j]));
+                    if (a.y) store_of<kPast>(byte(static_cast<T*>(a.y) + (int64_t)first * a.in.width, at_y[j]), o);
                 } else {
-                    o.store(byte(static_cast<T*>(a.dx) + (int64_t)first * a.dx_stride, at_y[j]));
-                    p.store(byte(static_cast<T*>(a.dgate) + (int64_t)first * a.dgate_stride, at_g[j]));
+                    store_of<kPast>(byte(static_cast<T*>(a.dx) + (int64_t)first * a.dx_stride, at_y[j]), o);
+                    store_of<kPast>(byte(static_cast<T*>(a.dgate) + (int64_t)first * a.dgate_stride, at_g[j]), p);
                 }
             }
             if (a.last && any_leave >> j & 1) {
@@ -455,10 +455,10 @@ __device__ void stay(const TileArgs& a, int s0, const float* state)
     }
 }
 
-template <typename T, int N, int kRun, bool kBack>
+template <typename T, int N, int kRun, bool kBack, bool kPast>
 __global__ __launch_bounds__(kThreads) void k_scan_tiles(TileArgs a)
 {
-    typedef Rows<T, N, kRun, kBack> Of;
+    typedef Rows<T, N, kRun, kBack, kPast> Of;
     __shared__ float part_f[kThreads * N], part_b[kThreads * N];
     __shared__ Marks<kRun> m;
     __shared__ uint64_t drawn;
@@ -565,7 +565,7 @@ __global__ __launch_bounds__(kBlock) void k_scan_step(ScanIn in, T* y, T* dgate,
         for (int one = c; one < in.width; ++one) go(std::integral_constant<int, 1>{}, one);
 }
 
-template <typename T, int N, int kRun, bool kBack>
+template <typename T, int N, int kRun, bool kBack, bool kPast>
 int launch_tiles(gr_tokens* h, TileArgs a, hipStream_t s)
 {
     static_assert((int64_t)kMostRuns * kRun * GR_MAX_STRIDE <= int64_t(1) << 30, "distances within a tile are in 32 bits, in bytes");
@@ -577,7 +577,7 @@ int launch_tiles(gr_tokens* h, TileArgs a, hipStream_t s)
     const int64_t total = (int64_t)a.tiles * a.blocks + (a.last ? ((int64_t)a.n_seq + 63) / 64 : 0);
     if (total > kMostBlocks * kBlock / kThreads) return GR_ERR_TOO_LARGE;
     if (total == 0) return GR_OK;
-    k_scan_tiles<T, N, kRun, kBack><<<(unsigned)total, kThreads, 0, s>>>(a);
+    k_scan_tiles<T, N, kRun, kBack, kPast><<<(unsigned)total, kThreads, 0, s>>>(a);
     return launched();
 }
 
@@ -609,8 +609,10 @@ int launch(gr_tokens* h, const ScanIn& in, int dtype, void* y, void* dgate, void
     const bool few = (in.n + rows - 1) / rows * a.blocks <= kFewTiles;
     return by_type(dtype, [&](auto t) {
         typedef decltype(t) T;
-        if (per == 1) return launch_tiles<T, 1, kRun, kBack>(h, a, s);
-        return few ? launch_tiles<T, kScanChannels, kRunFew, kBack>(h, a, s) : launch_tiles<T, kScanChannels, kRun, kBack>(h, a, s);
+        if (per == 1) return launch_tiles<T, 1, kRun, kBack, false>(h, a, s);
+        if (few) return launch_tiles<T, kScanChannels, kRunFew, kBack, false>(h, a, s);
+        return past_cache(in.n * in.width * (int64_t)sizeof(T) * (kBack ? 6 : 3)) ? launch_tiles<T, kScanChannels, kRun, kBack, true>(h, a, s)
+                                                                                 : launch_tiles<T, kScanChannels, kRun, kBack, false>(h, a, s);
     });
 }
 
