@@ -16,19 +16,18 @@ struct Gate {
     float keep, take;      // sigmoid(gate), sigmoid(-gate)
 };
 
-// Both from exp(-|gate|) =: e, as 1 / (1 + e) and e / (1 + e): neither is a difference, so both have all their digits however far the gate is from 0.
-// The exponent's rounding, |gate| log2(e) * 2^-24, is made good where results are in single precision.  (A gate that is no number stays one.)
-template <typename T>
+// With e = exp(-|gate|) the smaller one is e / (1 + e), which is no difference and has all its digits however far the gate is from 0; the larger one is
+// what it leaves of 1, rounded once: states pass through thousands of those.  The exponent's rounding, |gate| log2(e) * 2^-24, is made good, as states
+// are in single precision whatever the type.  (A gate that is no number stays one; behind 128 e is 0.)
 __device__ __forceinline__ Gate gate_of(float g)
 {
     constexpr float kLog2e = 1.44269504089f, kLog2eRest = 1.92596299e-8f, kLn2 = 0.693147181f;
-    const float a = fabsf(g);
-    float e = __builtin_amdgcn_exp2f(a * -kLog2e);
-    if (sizeof(T) == 4) {
-        const float near_a = fminf(a, 128.0f), p = near_a * -kLog2e;      // (behind that e is 0, and an infinite gate has no rounding)
-        e = fmaf(e, fmaf(near_a, -kLog2eRest, fmaf(near_a, -kLog2e, -p)) * kLn2, e);
-    }
-    const float near = __builtin_amdgcn_rcpf(1.0f + e), far = e * near;
+    float a = fabsf(g);
+    a = a > 128.0f ? 128.0f : a;
+    const float p = a * -kLog2e, rest = fmaf(fmaf(a, -kLog2e, -p), kLn2, a * (-kLog2eRest * kLn2));
+    float e = __builtin_amdgcn_exp2f(p);
+    e = fmaf(e, rest, e);
+    const float far = e * __builtin_amdgcn_rcpf(1.0f + e), near = 1.0f - far;
     return g >= 0 ? Gate{near, far} : Gate{far, near};
 }
 
@@ -301,7 +300,7 @@ struct Rows {
             const bool there = !some_missing || q + j < rows_here;
             each<N>([&](auto e) {
                 const float v = (float)r.x[j].v[e];
-                const Gate k = gate_of<T>((float)r.g[j].v[e]);
+                const Gate k = gate_of((float)r.g[j].v[e]);
                 f[e] = k.keep;
                 if constexpr (!kBack) held.b[j][e] = k.take * v;
                 else {
@@ -537,7 +536,7 @@ __global__ __launch_bounds__(kBlock) void k_scan_step(ScanIn in, T* y, T* dgate,
             Of o;
 #pragma unroll
             for (int e = 0; e < M; ++e) {
-                const Gate k = gate_of<T>((float)g.v[e]);
+                const Gate k = gate_of((float)g.v[e]);
                 h.v[e] = fmaf(k.keep, h0.v[e], k.take * (float)x.v[e]);
                 o.v[e] = (T)h.v[e];
             }
@@ -549,7 +548,7 @@ __global__ __launch_bounds__(kBlock) void k_scan_step(ScanIn in, T* y, T* dgate,
             if (in.dh) dh = State::load(in.dh + at);
 #pragma unroll
             for (int e = 0; e < M; ++e) {
-                const Gate k = gate_of<T>((float)g.v[e]);
+                const Gate k = gate_of((float)g.v[e]);
                 const float d = (float)up.v[e] + dh.v[e], by = d * k.take;
                 ox.v[e] = (T)by;
                 og.v[e] = (T)(by * k.keep * (h0.v[e] - (float)x.v[e]));

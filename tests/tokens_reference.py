@@ -1,9 +1,9 @@
 """The operators that read a request's tokens from their definitions, in 64 bits on the CPU (numpy), and how far results in fewer bits may be
 off.  Shares no code with the library.
 
-Tolerances of the recurrence.  In single precision a gate's two sigmoids are off by at most 4 units of 2^-23 each, relative (an exponential's unit
-and its correction's half, the sum's half, a reciprocal's unit, a product's half); in a call of 16-bit types the exponent is not corrected and its
-own rounding, |gate| * 2^-24, comes on top.  A step adds two roundings.  With M_t = f_t M_{t-1} + i_t |x_t| the sum of magnitudes behind a state, a step
+Tolerances of the recurrence.  A gate's smaller sigmoid is off by at most 4 units of 2^-23, relative (an exponential's unit and its
+correction's half, the sum's half, a reciprocal's unit, a product's half), the larger one, what it leaves of 1, by no more.  A step adds two
+roundings.  With M_t = f_t M_{t-1} + i_t |x_t| the sum of magnitudes behind a state, a step
 puts an error of at most k M_t there, and it goes on as the state does: in all k E_t with E_t = f_t E_{t-1} + M_t.  Stretches that are joined (a state
 times a product of f) have the roundings of the product besides, one a step and one a join: twice as many at most.  k = 2 * (4 + 4 + 2) * 2^-23, which is 20 units.
 Gradients likewise, backward, with one more product or three."""
@@ -65,15 +65,14 @@ def scan_backward(gate, x, y, off, h0, dy, dh):
     return (dgate, E_dgate), (dx, E_dx), (dh0, E_dh0)
 
 
-def near(got, ref, E, dtype, gate_most, what):
+def near(got, ref, E, dtype, what):
     """|got - ref| within k E and one rounding; the same places not finite."""
     import torch
     g = f64(got)
     assert g.shape == ref.shape, (what, g.shape, ref.shape)
-    k = K + (0 if dtype == torch.float32 else 2 * gate_most)
     out = torch.float32 if got.dtype == torch.float32 else dtype
-    # (behind a gate of 88 a sigmoid is held as 0 or as what is left at 88, 2^-126)
-    tol = k * 2.0 ** -23 * E + UNIT[out] * np.abs(ref) * (1 + 1e-3) + LEAST[out] + 2.0 ** -120
+    # (behind a gate of 87 the smaller sigmoid is past single precision's range of full digits, 2^-126)
+    tol = K * 2.0 ** -23 * E + UNIT[out] * np.abs(ref) * (1 + 1e-3) + LEAST[out] + 2.0 ** -120
     bad = ~(np.abs(g - ref) <= tol)
     assert not bad.any(), (what, int(bad.sum()), np.argwhere(bad)[:3].tolist(), g[bad][:3], ref[bad][:3], tol[bad][:3])
 
