@@ -107,21 +107,26 @@ class LengthPredictor:
         for p, g in zip(parameters, gradients):
             p.add_(g, alpha=-rate)
 
-    def train_experts(self, x: torch.Tensor, target: torch.Tensor, expert: torch.Tensor, rate: float) -> torch.Tensor:
+    def train_experts(self, x: torch.Tensor, target: torch.Tensor, expert: torch.Tensor, rate: float,
+                      out_dx: Optional[torch.Tensor] = None) -> torch.Tensor:
         """A step of the first phase: requests x with logarithms of lengths `target` [rows], each given to expert [rows] (int32; a request
-        whose expert there is not is left out).  Returns the loss."""
+        whose expert there is not is left out).  out_dx, as x: the gradient by the features, for what makes them.  Returns the loss."""
         T = x.shape[0]
         off, slot, h = self.off, self.slot[:T], self.h
-        h.gr_expert_plan(expert.view(T, 1), off, slot, self.pos.view(-1)[:T].view(T, 1))
+        pos = self.pos.view(-1)[:T].view(T, 1)
+        h.gr_expert_plan(expert.view(T, 1), off, slot, pos)
+        by_position = None if out_dx is None else torch.empty_like(out_dx)
         y = self._experts(x, T, 1)
         loss, d = self._loss(y, target[torch.where(slot < 0, -1 - slot, slot).long()], self.dy[-1][:T], counts=slot >= 0)
         for i in range(len(self.w) - 1, -1, -1):
             relu = i < len(self.w) - 1
             source = x if i == 0 else self.y[i - 1][:T]
-            h.gr_expert_linear_backward(source, self.w[i], d, out_dx=self.dy[i - 1][:T] if i else None, out_dw=self.dw[i], out_db=self.db[i],
+            h.gr_expert_linear_backward(source, self.w[i], d, out_dx=self.dy[i - 1][:T] if i else by_position, out_dw=self.dw[i], out_db=self.db[i],
                                         y=self.y[i][:T] if relu else None, out_dz=d if relu else None, off=off,
                                         slot=slot if i == 0 else None)
             d = self.dy[i - 1][:T]
+        if out_dx is not None:
+            h.gr_expert_combine(by_position, pos, out_dx)
         self._update(self.w + self.b, self.dw + self.db, rate)
         return loss
 
