@@ -21,7 +21,7 @@ int lanes_log(int pieces)
     return lg;
 }
 
-constexpr int kRowsAtOnce = 4;      // rows of a group of lanes whose loads are under way together
+constexpr int kRowsAtOnce = 2;      // rows of a group of lanes whose loads are under way together
 
 // Pieces of 16 bytes at any address of an element; the last one of a row reaches back into the one before.  What is written is not asked for again soon:
 // it goes past the cache, which the rows of frequent tokens then stay in.

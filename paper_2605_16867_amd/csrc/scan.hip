@@ -413,28 +413,29 @@ __device__ __forceinline__ void join(const TileArgs& a, int tile, int start, uns
     float state = 0;
     if (start < p0) {
         const int from = start / a.rows, group = tile / kGroup * kGroup;
-        // what it starts from: the end of the tile that the sequence starts in, or the state at a group's end; then the tiles since
+        // what it starts from: the end of the tile that the sequence starts in, or the state at a group's end; then the tiles since, which are joined
+        // first: nothing but a word and a product is between the state at a group's end and that at the next
         const uint64_t* const begin = from >= group ? sums + ((int64_t)from * 2 + 1) * pitch : a.states + (int64_t)(group / kGroup - 1) * pitch + word;
-        uint64_t seen = look(begin);
-        bool begun = false;
-        for (int k = from >= group ? from + 1 : group; k < tile || !begun; k += 4) {
+        const uint64_t seen = look(begin);
+        float cf = 1, cb = 0;
+        for (int k = from >= group ? from + 1 : group; k < tile; k += 4) {
             uint64_t sf[4], sb[4];
 #pragma unroll
             for (int u = 0; u < 4; ++u) {
-                const int64_t w = (int64_t)(k + u < tile ? k + u : tile - 1) * 2;
+                const int64_t w = (int64_t)(k + u < tile ? k + u : k) * 2;
                 sf[u] = look(sums + w * pitch);
                 sb[u] = look(sums + (w + 1) * pitch);
             }
-            if (!begun) state = wait_for(begin, seen, call);
-            begun = true;
 #pragma unroll
             for (int u = 0; u < 4; ++u)
                 if (k + u < tile) {
                     const int64_t w = (int64_t)(k + u) * 2;
                     const float kf = wait_for(sums + w * pitch, sf[u], call), kb = wait_for(sums + (w + 1) * pitch, sb[u], call);
-                    state = fmaf(kf, state, kb);
+                    cb = fmaf(kf, cb, kb);
+                    cf *= kf;
                 }
         }
+        state = fmaf(cf, wait_for(begin, seen, call), cb);
     }
     if (more && tile % kGroup == kGroup - 1) publish(a.states + (int64_t)(tile / kGroup) * pitch + word, cut ? tb : fmaf(tf, state, tb), call);
     each_run([&](int r, bool here, float rf, float rb) {
