@@ -573,7 +573,7 @@ int gr_clip_gradients(gr_experts* h, int32_t n_grad, const void* const* grad, vo
 typedef struct gr_tokens gr_tokens;
 
 #define GR_MAX_VOCAB (1 << 24)
-#define GR_MAX_STRIDE (1 << 20)
+#define GR_MAX_STRIDE (1 << 18)
 
 /*
  * Create the workspace of calls on up to max_tokens tokens (<= 2^30) of up to max_vocab different ones and rows of up to max_width

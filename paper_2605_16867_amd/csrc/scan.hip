@@ -387,28 +387,34 @@ struct Rows {
     }
 };
 
-// (F, B) of a channel of the tile from those of its runs, published; the state that it starts from; those that its runs start from, in the place of F.
-__device__ __forceinline__ void join(const TileArgs& a, int tile, int start, unsigned call, const unsigned* enter, float* part_f, float* part_b, int channels, int block,
+constexpr int kJoined = 4;      // runs that a thread joins for a channel
+
+// Stretches one after the other, kJoined at a time: `step`(which, whether a sequence enters in it, F, B).
+template <typename F>
+__device__ __forceinline__ void each_stretch(int n, int channels, int ch, const bool* cut, const float* f, const float* b, F step)
+{
+#pragma unroll 1
+    for (int r = 0; r < n; r += kJoined) {
+        float rf[kJoined], rb[kJoined];
+#pragma unroll
+        for (int u = 0; u < kJoined; ++u) {
+            rf[u] = f[(r + u) * channels + ch];
+            rb[u] = b[(r + u) * channels + ch];
+        }
+#pragma unroll
+        for (int u = 0; u < kJoined; ++u) step(r + u, cut[r + u], rf[u], rb[u]);
+    }
+}
+
+// (F, B) of a channel of the tile from those of its stretches, published; the state that it starts from; those that its stretches start from, in the place of F.
+__device__ __forceinline__ void join(const TileArgs& a, int tile, int start, unsigned call, const bool* cuts, float* f, const float* b, int n, int channels, int block,
                                      int ch)
 {
-    const int runs = kThreads >> a.lg, p0 = tile * a.rows;
+    const int p0 = tile * a.rows;
     const int64_t pitch = (int64_t)a.blocks * channels, word = block * channels + ch;
     float tf = 1, tb = 0;
     bool cut = false;
-    const auto each_run = [&](auto step) {      // (runs are a multiple of four)
-#pragma unroll 1
-        for (int r = 0; r < runs; r += 4) {
-            float rf[4], rb[4];
-#pragma unroll
-            for (int u = 0; u < 4; ++u) {
-                rf[u] = part_f[(r + u) * channels + ch];
-                rb[u] = part_b[(r + u) * channels + ch];
-            }
-#pragma unroll
-            for (int u = 0; u < 4; ++u) step(r + u, enter[r + u] != 0, rf[u], rb[u]);
-        }
-    };
-    each_run([&](int, bool here, float rf, float rb) {
+    each_stretch(n, channels, ch, cuts, f, b, [&](int, bool here, float rf, float rb) {
         tb = here ? rb : fmaf(rf, tb, rb);
         tf = here ? 0.0f : tf * rf;
         cut = cut || here;
@@ -448,8 +454,8 @@ __device__ __forceinline__ void join(const TileArgs& a, int tile, int start, uns
         state = fmaf(cf, wait_for(begin, seen, call), cb);
     }
     if (more && tile % kGroup == kGroup - 1) publish(a.states + (int64_t)(tile / kGroup) * pitch + word, cut ? tb : fmaf(tf, state, tb), call);
-    each_run([&](int r, bool here, float rf, float rb) {
-        part_f[r * channels + ch] = state;
+    each_stretch(n, channels, ch, cuts, f, b, [&](int r, bool here, float rf, float rb) {
+        f[r * channels + ch] = state;
         state = here ? rb : fmaf(rf, state, rb);
     });
 }
@@ -469,7 +475,8 @@ template <typename T, int N, int kRun, bool kBack, bool kPast>
 __global__ __launch_bounds__(kThreads) void k_scan_tiles(TileArgs a)
 {
     typedef Rows<T, N, kRun, kBack, kPast> Of;
-    __shared__ float part_f[kThreads * N], part_b[kThreads * N];
+    __shared__ float part_f[kThreads * N], part_b[kThreads * N], stretch_f[kThreads], stretch_b[kThreads];
+    __shared__ bool cuts[kMostRuns / kJoined];
     __shared__ Marks<kRun> m;
     __shared__ uint64_t drawn;
     __shared__ int near_off[kNearOffsets];
@@ -507,7 +514,38 @@ __global__ __launch_bounds__(kThreads) void k_scan_tiles(TileArgs a)
         });
     }
     __syncthreads();
-    if (tid < channels) join(a, tile, m.start, call, m.enter, part_f, part_b, channels, block, tid);
+    {
+        // four runs of a channel by each thread, then those by a thread for each channel, and back
+        const int stretch = tid / channels, ch = tid - stretch * channels, stretches = (kThreads >> a.lg) / kJoined;
+        float rf[kJoined], rb[kJoined], f = 1, b = 0;
+        bool enters[kJoined], cut = false;
+        if (stretch < stretches) {
+#pragma unroll
+            for (int u = 0; u < kJoined; ++u) {
+                const int r = stretch * kJoined + u;
+                rf[u] = part_f[r * channels + ch];
+                rb[u] = part_b[r * channels + ch];
+                enters[u] = m.enter[r] != 0;
+                b = enters[u] ? rb[u] : fmaf(rf[u], b, rb[u]);
+                f = enters[u] ? 0.0f : f * rf[u];
+                cut = cut || enters[u];
+            }
+            stretch_f[tid] = f;
+            stretch_b[tid] = b;
+            if (ch == 0) cuts[stretch] = cut;
+        }
+        __syncthreads();
+        if (tid < channels) join(a, tile, m.start, call, cuts, stretch_f, stretch_b, stretches, channels, block, tid);
+        __syncthreads();
+        if (stretch < stretches) {
+            float state = stretch_f[tid];
+#pragma unroll
+            for (int u = 0; u < kJoined; ++u) {
+                part_f[(stretch * kJoined + u) * channels + ch] = state;
+                state = enters[u] ? rb[u] : fmaf(rf[u], state, rb[u]);
+            }
+        }
+    }
     __syncthreads();
     {
         float h[N];
@@ -579,6 +617,7 @@ __global__ __launch_bounds__(kBlock) void k_scan_step(ScanIn in, T* y, T* dgate,
 template <typename T, int N, int kRun, bool kBack, bool kPast>
 int launch_tiles(gr_tokens* h, TileArgs a, hipStream_t s)
 {
+    static_assert((kThreads >> kScanLanesLog) % (kJoined * kJoined) == 0, "runs and stretches are joined four at a time");
     static_assert((int64_t)kMostRuns * kRun * GR_MAX_STRIDE <= int64_t(1) << 30, "distances within a tile are in 32 bits, in bytes");
     a.rows = (kThreads >> a.lg) * kRun;
     a.tiles = (int)(((int64_t)a.n + a.rows - 1) / a.rows);
