@@ -525,9 +525,9 @@ int launch_embed_backward(gr_tokens* h, int64_t n, int vocab, int width, int dty
             b.key = key[at]; b.slot = slot[at]; b.left = n > 0 ? left : nullptr; b.dout = dout; b.dtable = dtable; b.scale = scale; b.vocab = vocab;
             b.width = width;
             b.blocks = (width + kWave * N - 1) / (kWave * N);
-            // as many pieces as there are waves in a few rounds; no less than 64 items each
+            // as many pieces as there are waves in a few rounds; no less than 32 items each (49 999 rows of 511 64 us with 64 or 16)
             const int64_t items = vocab + n, most = kSumWaves / b.blocks > 1 ? kSumWaves / b.blocks : 1;
-            const int64_t piece = (items + most - 1) / most > 64 ? (items + most - 1) / most : 64;
+            const int64_t piece = (items + most - 1) / most > 32 ? (items + most - 1) / most : 32;
             b.piece = (int)piece;
             b.pieces = (int)((items + piece - 1) / piece);
             b.head = h->parts;
