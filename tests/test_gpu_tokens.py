@@ -696,3 +696,113 @@ def test_more_rows_than_the_cache_holds():
     ok = (token >= 0) & (token < V)
     want = torch.zeros(V, W, device=DEV).index_add_(0, token[ok].long(), dout[ok])
     assert n * W * 4 > 256 << 20 and torch.equal(out, want * 0.5)
+
+
+@pytest.mark.parametrize("dtype,n,S,width", [(torch.float32, 9000, 3000, 24), (torch.bfloat16, 6000, 20000, 40), (torch.float16, 5000, 2047, 9),
+                                             (torch.float32, 5000, 2048, 9), (torch.float32, 300, 5000, 130)])
+def test_more_sequences_than_shared_memory_has_room_for(dtype, n, S, width):
+    """Offsets looked up where they lie, hundreds of empty sequences between two tokens."""
+    rng = np.random.default_rng(S)
+    h = binding.Tokens(n, 1, width)
+    gate, x = inputs(rng, n, width, dtype)
+    off = np.sort(np.concatenate([[0, n], rng.integers(0, n + 1, S // 2), np.full(S - 1 - S // 2, n // 3)]))
+    h0, dh = (f64_of(rng.normal(size=(S, width)), torch.float32) for _ in range(2))
+    dy = f64_of(rng.normal(size=(n, width)), dtype)
+    want_y, want, E_y, E = ref.scan(gate, x, off, h0)
+    y, last = empty(n, width, dtype=dtype), empty(S, width)
+    h.gr_gated_scan(put(gate, dtype), put(x, dtype), out_y=y, off=ints(off), h0=put(h0, torch.float32), out_h=last)
+    ref.near(y, want_y, E_y, dtype, "y")
+    ref.near(last, want, E, dtype, "last")
+    y0 = f64_of(want_y, dtype)
+    dg, dx, dh0 = empty(n, width, dtype=dtype), empty(n, width, dtype=dtype), empty(S, width)
+    h.gr_gated_scan_backward(put(gate, dtype), put(x, dtype), put(y0, dtype), dg, dx, off=ints(off), h0=put(h0, torch.float32), dy=put(dy, dtype),
+                             dh=put(dh, torch.float32), out_dh0=dh0)
+    for got, (r, E), what in zip((dg, dx, dh0), ref.scan_backward(gate, x, y0, off, h0, dy, dh), ("dgate", "dx", "dh0")):
+        ref.near(got, r, E, dtype, what)
+
+
+@pytest.mark.parametrize("off", [[0, 0, 0], [7, 7], [0], [50, 50, 50, 50]])
+def test_tokens_of_no_sequence_at_all(off):
+    h, S = binding.Tokens(50, 1, 20), len(off) - 1
+    g, y, dg, dx = (empty(50, 20) for _ in range(4))
+    state, last, dh0 = torch.randn(S, 20, device=DEV), empty(S, 20), empty(S, 20)
+    h.gr_gated_scan(g, g, out_y=y, off=ints(off), h0=state, out_h=last)
+    h.gr_gated_scan_backward(g, g, y, dg, dx, off=ints(off), dh=state, out_dh0=dh0)
+    assert torch.equal(last, state) and torch.equal(dh0, state)
+    for t in (y, dg, dx):
+        assert bool((t == 77).all())
+
+
+def test_past_2_31_elements():
+    """Tokens, rows of a table and their gradients behind the first 2^31 elements of an array."""
+    n, width, tail = 2_200_000, 1024, 96
+    dt = torch.bfloat16
+    rng = np.random.default_rng(6)
+    gate, x = inputs(rng, tail, width, dt)
+    off = ints([0, 1_000_000, n - tail, n - 30, n])
+    h = binding.Tokens(n, n, width)
+    big, value = torch.zeros(n, width, dtype=dt, device=DEV), torch.zeros(n, width, dtype=dt, device=DEV)
+    big[-tail:], value[-tail:] = put(gate, dt), put(x, dt)
+    y, last = torch.zeros_like(big), empty(4, width)
+    h.gr_gated_scan(big, value, out_y=y, off=off, out_h=last)
+    want_y, want, E_y, E = ref.scan(gate, x, np.array([0, tail - 30, tail]), None)
+    ref.near(y[-tail:], want_y, E_y, dt, "y")
+    ref.near(last[2:], want, E, dt, "last")
+    dy = f64_of(rng.normal(size=(tail, width)), dt)
+    up, y0 = torch.zeros_like(big), f64_of(want_y, dt)
+    up[-tail:], y[-tail:] = put(dy, dt), put(y0, dt)
+    dg, dx = torch.empty_like(big), torch.empty_like(big)
+    h.gr_gated_scan_backward(big, value, y, dg, dx, off=off, dy=up)
+    back = ref.scan_backward(gate, x, y0, np.array([0, tail - 30, tail]), None, dy, None)
+    for got, (r, E), what in zip((dg, dx), back, ("dgate", "dx")):
+        ref.near(got[-tail:], r, E, dt, what)
+        assert bool((got[:tail] == 0).all())
+    del up, dg, y
+    # rows of a table: the last ones, and their gradient; the same rows as the results
+    token = torch.full((n,), -1, dtype=torch.int32, device=DEV)
+    token[-tail:] = torch.arange(n - tail, n, device=DEV, dtype=torch.int32).flip(0)
+    h.gr_token_embed(token, value, dx, scale=2.0)
+    assert torch.equal(dx[-tail:], (value[-tail:].float() * 2).to(dt).flip(0)) and bool((dx[:-tail] == 0).all())
+    h.gr_token_embed_backward(token, dx, big, scale=0.5)
+    assert torch.equal(big[-tail:], value[-tail:]) and bool((big[:-tail] == 0).all())
+
+
+def test_two_handles_at_once():
+    """Long recurrences on two streams, each with a handle of its own: as one after the other."""
+    n, width = 40_000, 256
+    sides, outs, args = [torch.cuda.Stream() for _ in range(2)], [], []
+    for k in range(2):
+        g = torch.Generator(device=DEV).manual_seed(k)
+        a = torch.randn(n, 2 * width, generator=g, device=DEV).to(torch.bfloat16)
+        args.append((binding.Tokens(n, 1, width), a[:, :width], a[:, width:], ints([0, n // 3, n])))
+    want = []
+    for h, gate, x, off in args:
+        y = empty(n, width, dtype=torch.bfloat16)
+        h.gr_gated_scan(gate, x, out_y=y, off=off)
+        want.append(y)
+    torch.cuda.synchronize()
+    for side, (h, gate, x, off) in zip(sides, args):
+        with torch.cuda.stream(side):
+            got = [empty(n, width, dtype=torch.bfloat16) for _ in range(8)]
+            for y in got:
+                h.gr_gated_scan(gate, x, out_y=y, off=off)
+            outs.append(got)
+    torch.cuda.synchronize()
+    for got, y in zip(outs, want):
+        assert all(torch.equal(g, y) for g in got)
+
+
+@pytest.mark.parametrize("native", [True, False])
+def test_rows_too_far_apart(native, monkeypatch):
+    if not native:
+        monkeypatch.setattr(binding, "_marshal", binding._Ctypes)
+    h, far = binding.Tokens(2, 1, 8), 1 << 18
+    a = torch.randn(far + 1 + 8, device=DEV)
+    at = lambda stride: torch.as_strided(a, (2, 8), (stride, 1))
+    y, ok = empty(2, 8), empty(2, 8)
+    h.gr_gated_scan(at(far), at(far), out_y=y, off=ints([0, 2]))
+    h.gr_gated_scan(at(far).contiguous(), at(far).contiguous(), out_y=ok, off=ints([0, 2]))
+    assert torch.equal(y, ok)
+    with pytest.raises(binding.GoodRouteError) as e:
+        h.gr_gated_scan(at(far + 1), at(far), out_y=y)
+    assert e.value.code == -2
