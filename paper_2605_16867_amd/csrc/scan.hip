@@ -22,17 +22,16 @@ struct Gate {
     float keep, take;      // sigmoid(gate), sigmoid(-gate)
 };
 
-// With e = exp(-|gate|) the smaller one is e / (1 + e), which is no difference and has all its digits however far the gate is from 0; the larger one is
-// what it leaves of 1, rounded once: states pass through thousands of those.  The exponent's rounding, |gate| log2(e) * 2^-24, is made good, as states
-// are in single precision whatever the type.  (A gate that is no number stays one; behind 128 e is 0.)
+// With e = exp(-|gate|) the smaller one is e / (1 + e), which is no difference and has its digits however far the gate is from 0; the larger one is
+// what it leaves of 1, rounded once: states pass through thousands of those.  The exponent is |gate| log2(e) in single precision, rounded to |gate| * 2^-24:
+// what the product lost is made good, as states are in single precision whatever the type (what the constant lost, |gate| * 2^-26, is not).  An infinite
+// gate's product has lost what is no number; the median of three makes a number of it, and e is 0.  A gate that is no number stays one.
 __device__ __forceinline__ Gate gate_of(float g)
 {
-    constexpr float kLog2e = 1.44269504089f, kLog2eRest = 1.92596299e-8f, kLn2 = 0.693147181f;
-    float a = fabsf(g);
-    a = a > 128.0f ? 128.0f : a;
-    const float p = a * -kLog2e, rest = fmaf(fmaf(a, -kLog2e, -p), kLn2, a * (-kLog2eRest * kLn2));
+    constexpr float kLog2e = 1.44269504089f, kLn2 = 0.693147181f;
+    const float a = fabsf(g), p = a * -kLog2e, lost = __builtin_amdgcn_fmed3f(fmaf(a, -kLog2e, -p) * kLn2, -1.0f, 1.0f);
     float e = __builtin_amdgcn_exp2f(p);
-    e = fmaf(e, rest, e);
+    e = fmaf(e, lost, e);
     const float far = e * __builtin_amdgcn_rcpf(1.0f + e), near = 1.0f - far;
     return g >= 0 ? Gate{near, far} : Gate{far, near};
 }
