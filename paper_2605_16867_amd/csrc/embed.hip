@@ -13,7 +13,7 @@
 namespace gr {
 namespace {
 
-constexpr int kBlock = 256, kWave = 64, kWaves = kBlock / kWave;
+constexpr int kBlock = 256, kWave = 64, kWaves = kBlock / kWave, kDies = 8;
 
 // log2 of the lanes that share a row of so many pieces
 int lanes_log(int pieces)
@@ -299,19 +299,22 @@ __global__ __launch_bounds__(kFewThreads) void k_sort_few(const int* token, int 
 
 // ---- the sums ----------------------------------------------------------------------------------
 //
-// Sorted places and rows of the table are one line of work: the places of a row, then the row itself, which is written.  A wave takes a piece's items
-// of it and a block of channels, and finds its first place by the line's order: that of place p is p + key[p], of row v the places up to its last plus v.
-// A row of at most a piece's places is summed where its first place is, as far as it goes; a longer one in every piece that it has places in, whose
-// sums a second launch adds up in their order.  So a token that is 4 % of all tokens, 20 000 rows, is shared by 280 waves (a wave a row: 19.9 ms).
+// Sorted places and rows of the table are one line of work: the places of a row, then the row itself, which is written.  A workgroup takes a piece's items
+// of it, 64 to 1 024, and a block of channels, and finds its first place by the line's order: that of place p is p + key[p], of row v the places up
+// to its last plus v.  Its places stand in shared memory.  As many lanes as a row has chunks are a team, up to a wave; a team takes places that follow each
+// other, eight rows under way at a time, and writes the rows that it has all of.  What it has of one that goes on behind it is passed on from team to team
+// by a scan, whose order hangs on places alone, and what a piece has of one that goes on behind the piece by a second launch.  So it does not matter how the
+// places are shared out among rows: 1 000 000 of 16 channels, where a token is 4 % of all of them, 26 us.
 
 struct SumArgs {
     const int *key, *slot, *left;      // left: how many there are; null: none
     const void* dout;
     void* dtable;
-    float *head, *trail;      // [pieces][width] of long rows: of the piece that has the row's end, of the others
-    int2* ended;              // [pieces] a long row that ends there and the piece that it starts in; -1
+    float *head, *trail;      // [pieces][width] of rows that pieces share: of the piece that has the row's end, of the others
+    int2* ended;              // [pieces] such a row that ends there, or -1; whether one goes through
     float scale;
     int vocab, width, piece, pieces, blocks;
+    int lg;      // log2 of the lanes of a team
 };
 
 // How many of [lo, hi) are before the first that `before` is not true for; by a wave.
@@ -335,145 +338,179 @@ __device__ __forceinline__ int place_at(const SumArgs& a, int n, int64_t item)
     return first_not(0, n, [&](int p) { return (int64_t)p + a.key[p] < item; });
 }
 
-// More places than a piece has items, from the first one.
-__device__ __forceinline__ bool is_long(const SumArgs& a, int n, int first, int v) { return first + a.piece < n && a.key[first + a.piece] == v; }
+// The sum of a row that goes on behind these places; of all of them, the row having begun before them?
+template <int N>
+struct Open {
+    Elements<float, N> sum;
+    bool through;
+    __device__ __forceinline__ void behind(const Open& o)      // o is what stands before
+    {
+#pragma unroll
+        for (int e = 0; e < N; ++e) sum.v[e] = through ? o.sum.v[e] + sum.v[e] : sum.v[e];
+        through = through && o.through;
+    }
+    __device__ __forceinline__ Open up(int lanes) const
+    {
+        Open o;
+#pragma unroll
+        for (int e = 0; e < N; ++e) o.sum.v[e] = __shfl_up(sum.v[e], lanes);
+        o.through = __shfl_up((int)through, lanes);
+        return o;
+    }
+};
 
 // kPast: rows are read past the cache.
 template <typename T, int N, bool kPast>
 __global__ __launch_bounds__(kBlock) void k_embed_sums(SumArgs a)
 {
     typedef Elements<T, N> Of;
+    typedef Elements<float, N> Sum;
     constexpr int kAtOnce = 8;
-    const int lane = threadIdx.x % kWave;
-    const int64_t id = (int64_t)blockIdx.x * kWaves + __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
-    const int piece = (int)(id / a.blocks), block = (int)(id - (int64_t)piece * a.blocks);
-    if (piece >= a.pieces) return;
-    const int n = a.left ? *a.left : 0;
+    __shared__ int keys[kPieceItems], slots[kPieceItems], occurs[kPieceItems], bound[2];
+    __shared__ Open<N> of_wave[kWaves][kWave];
+    const int tid = threadIdx.x, lane = tid % kWave, wave = __builtin_amdgcn_readfirstlane(tid / kWave), lg = a.lg, teams = kBlock >> lg, team = tid >> lg;
+    // (the blocks of a piece share lines at their edges: one die's workgroups, every eighth, take them one after the other)
+    const int block = (int)(blockIdx.x / kDies % a.blocks), piece = (int)(blockIdx.x / (kDies * a.blocks) * kDies + blockIdx.x % kDies), mine = tid & ((1 << lg) - 1), n = a.left ? *a.left : 0;
     const int64_t item = (int64_t)piece * a.piece, all = (int64_t)a.vocab + n, end = item + a.piece < all ? item + a.piece : all;
     if (item >= end) return;
-    const int c_own = (block * kWave + lane) * N, c = c_own + N > a.width ? a.width - N : c_own;
-    const bool on = c_own < a.width;
+    for (int i = tid; i < kPieceItems; i += kBlock) occurs[i] = 0;
+    if (wave < 2) {
+        const int p = place_at(a, n, wave ? end : item);
+        if (lane == 0) bound[wave] = p;
+    }
+    __syncthreads();
+    const int p0 = bound[0], count = bound[1] - p0, v0 = (int)(item - p0), v1 = (int)(end - bound[1]);      // rows from v0 to v1 end here
+    const bool headed = p0 > 0 && a.key[p0 - 1] == v0;
+    for (int i = tid; i < count; i += kBlock) {
+        const int k = a.key[p0 + i];
+        keys[i] = k;
+        slots[i] = a.slot[p0 + i];
+        if (k < v1) occurs[k - v0] = 1;
+    }
+    __syncthreads();
+    const int per = (count + teams - 1) / teams, from = team * per, to = from + per < count ? from + per : count;
+    bool before = false, after = false;      // the first row began before this team's places, the last goes on behind them
+    if (from < to) {
+        before = from > 0 ? keys[from - 1] == keys[from] : headed && keys[0] == v0;
+        after = keys[to - 1] == (to < count ? keys[to] : v1);
+    }
+    const int c0 = (block * kWave + mine) * N, c = c0 + N > a.width ? a.width - N : c0;
+    const bool on = c0 < a.width;
     const T* const dout = static_cast<const T*>(a.dout) + c;
     T* const dtable = static_cast<T*>(a.dtable) + c;
-    float sum[N] = {};
-    const auto put = [&](float* to) {
-        if (on) reinterpret_cast<Elements<float, N>*>(sum)->store(to + (int64_t)piece * a.width + c);
+    const auto write = [&](int v, const Sum& sum) {
+        Of o;
+#pragma unroll
+        for (int e = 0; e < N; ++e) o.v[e] = (T)(sum.v[e] * a.scale);
+        if (on) o.store(dtable + (int64_t)v * a.width);
     };
-    const auto clear = [&] {
-#pragma unroll
-        for (int e = 0; e < N; ++e) sum[e] = 0;
+    const auto keep = [&](float* to, const Sum& sum) {
+        if (on) sum.store(to + (int64_t)piece * a.width + c);
     };
-    int p = place_at(a, n, item), v = (int)(item - p);
-    int ends = first_not(p, n, [&](int q) { return (int64_t)q + a.key[q] < end; });      // places up to the piece's end
-    const int v_end = (int)(end - ends);
-    // a row from before: long, or not this piece's
-    bool headed = p > 0 && a.key[p - 1] == v;
-    if (headed) {
-        const int back = p > a.piece ? p - a.piece : 0, first = first_not(back, p, [&](int q) { return a.key[q] < v; });
-        if (!((first == back && back > 0 && a.key[back - 1] == v) || is_long(a, n, first, v))) {
-            headed = false;
-            p = first_not(p, n < first + a.piece ? n : first + a.piece, [&](int q) { return a.key[q] == v; });
-            ++v;
+    int ended = -1;      // a row that began before and ends here, and what this team has of it
+    Sum head{}, sum{};
+    for (int i0 = from; i0 < to; i0 += kAtOnce) {
+        Of row[kAtOnce];
+#pragma unroll
+        for (int u = 0; u < kAtOnce; ++u) row[u] = load_of<kPast, T, N>(dout + (int64_t)slots[i0 + u < to ? i0 + u : to - 1] * a.width);
+#pragma unroll
+        for (int u = 0; u < kAtOnce; ++u) {
+            const int i = i0 + u;
+            if (i >= to) break;
+#pragma unroll
+            for (int e = 0; e < N; ++e) sum.v[e] += (float)row[u].v[e];
+            if (i + 1 < to ? keys[i + 1] == keys[i] : after) continue;
+            if (before) {
+                ended = keys[i];
+                head = sum;
+            } else write(keys[i], sum);
+            before = false;
+            sum = Sum{};
         }
     }
-    if (block == 0) {
-        int2 e = {-1, 0};
-        if (headed && v < v_end) e = {v, (int)(((int64_t)first_not(0, p, [&](int q) { return a.key[q] < v; }) + v) / a.piece)};
-        if (lane == 0) a.ended[piece] = e;
+    Open<N> open{sum, after && before};
+    for (int d = 1 << lg; d < kWave; d *= 2) {
+        const Open<N> o = open.up(d);
+        if (lane >= d) open.behind(o);
     }
-    // a row that has places here and does not end here: to its last place, where it is not long
-    const bool open = ends > p && a.key[ends - 1] == v_end;
-    bool trailing = open;
-    if (open && !(headed && v == v_end)) {
-        const int first = first_not(p, ends, [&](int q) { return a.key[q] < v_end; });
-        if (!is_long(a, n, first, v_end)) {
-            trailing = false;
-            ends = first_not(ends, n < first + a.piece ? n : first + a.piece, [&](int q) { return a.key[q] == v_end; });
-        }
+    if (lane >= kWave - (1 << lg)) of_wave[wave][mine] = open;
+    Open<N> earlier = open.up(1 << lg);      // before this team
+    __syncthreads();
+    Open<N> first{Sum{}, true};      // before this wave
+    for (int w = 0; w < wave; ++w) {
+        Open<N> o = of_wave[w][mine];
+        o.behind(first);
+        first = o;
     }
-    const int last = open && !trailing ? v_end + 1 : v_end;      // rows before it are ended here
-    const auto finish = [&] {
-        if (headed) put(a.head);
-        else if (on) {
-            Of o;
+    if (lane < 1 << lg) earlier = first;
+    else earlier.behind(first);
+    if (ended >= 0) {
 #pragma unroll
-            for (int e = 0; e < N; ++e) o.v[e] = (T)(sum[e] * a.scale);
-            o.store(dtable + (int64_t)v * a.width);
-        }
-        headed = false;
-        ++v;
-        clear();
-    };
-    for (; p < ends; p += kWave) {
-        const int here = ends - p < kWave ? ends - p : kWave, at = p + (lane < here ? lane : here - 1);
-        const int key = a.key[at], slot = a.slot[at];
-        for (int j0 = 0; j0 < here; j0 += kAtOnce) {
-            Of row[kAtOnce];
-#pragma unroll
-            for (int u = 0; u < kAtOnce; ++u) {
-                const int j = j0 + u < here ? j0 + u : here - 1;
-                const T* const from = dout + (int64_t)__builtin_amdgcn_readlane(slot, j) * a.width;
-                row[u] = load_of<kPast, T, N>(from);
-            }
-#pragma unroll
-            for (int u = 0; u < kAtOnce; ++u) {
-                if (j0 + u >= here) break;
-                const int k = __builtin_amdgcn_readlane(key, j0 + u);
-                while (v < k) finish();
-#pragma unroll
-                for (int e = 0; e < N; ++e) sum[e] += (float)row[u].v[e];
-            }
-        }
+        for (int e = 0; e < N; ++e) head.v[e] += earlier.sum.v[e];
+        if (earlier.through) keep(a.head, head);
+        else write(ended, head);
     }
-    while (v < last) finish();
-    if (trailing) put(a.trail);
+    if (to == count && from < to && after) {
+        open.behind(first);
+        keep(a.trail, open.sum);
+    }
+    if (team == 0 && headed && v0 < v1 && (count == 0 || keys[0] != v0)) keep(a.head, Sum{});
+    for (int r = team * a.blocks + block; r < v1 - v0; r += teams * a.blocks)
+        if (!occurs[r] && !(r == 0 && headed)) {
+            T* const row = static_cast<T*>(a.dtable) + (int64_t)(v0 + r) * a.width;
+            for (int c0 = mine * N; c0 < a.width; c0 += kWave * N) Of{}.store(row + (c0 + N > a.width ? a.width - N : c0));
+        }
+    // (a row that goes through this piece: no place of another is in it, and it does not end here)
+    if (tid == 0 && block == 0) a.ended[piece] = int2{headed && v0 < v1 ? v0 : -1, headed && v0 == v1};
 }
 
-// Of kJoined pieces and a block of channels: the parts of long rows that end there, a quarter of them by each wave, and those in order.
-constexpr int kJoined = 32, kJoinChannels = 4;
-
+// A workgroup a piece that a row from before ends in: the parts of it, shared by the teams.
 template <typename T, int N>
 __global__ __launch_bounds__(kBlock) void k_embed_join(SumArgs a)
 {
     typedef Elements<float, N> Sum;
-    __shared__ float part[kWaves][kWave * N];
-    const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave, piece0 = blockIdx.y * kJoined;
-    const int c_own = (blockIdx.x * kWave + lane) * N, c = c_own + N > a.width ? a.width - N : c_own;
-    const int64_t items = (int64_t)a.vocab + *a.left;
-    int2 ended = {-1, 0};
+    __shared__ Sum of_wave[kWaves][kWave];
+    const int tid = threadIdx.x, lane = tid % kWave, wave = tid / kWave, lg = a.lg, teams = kBlock >> lg, team = tid >> lg, mine = tid & ((1 << lg) - 1);
+    const int piece = blockIdx.x;
     // (behind the last item there may be pieces that nothing was written for)
-    if (lane < kJoined && piece0 + lane < a.pieces && (int64_t)(piece0 + lane) * a.piece < items) ended = a.ended[piece0 + lane];
-    for (uint64_t some = __ballot(ended.x >= 0); some; some &= some - 1) {
-        const int at = __builtin_ctzll(some), piece = piece0 + at, v = __builtin_amdgcn_readlane(ended.x, at), i0 = __builtin_amdgcn_readlane(ended.y, at);
-        const int per = (piece - i0 + kWaves - 1) / kWaves, from = i0 + wave * per, to = from + per < piece ? from + per : piece;
-        float sum[N] = {};
-        constexpr int kAtOnce = 8;
-        for (int i = from; i < to; i += kAtOnce) {
-            Sum s[kAtOnce];
-#pragma unroll
-            for (int u = 0; u < kAtOnce; ++u) s[u] = Sum::load(a.trail + (int64_t)(i + u < to ? i + u : i) * a.width + c);
-#pragma unroll
-            for (int u = 0; u < kAtOnce; ++u)
-#pragma unroll
-                for (int e = 0; e < N; ++e) sum[e] += i + u < to ? s[u].v[e] : 0.0f;
-        }
-#pragma unroll
-        for (int e = 0; e < N; ++e) part[wave][lane * N + e] = sum[e];
-        __syncthreads();
-        if (wave == 0 && c_own < a.width) {
-            const Sum head = Sum::load(a.head + (int64_t)piece * a.width + c);
-            Elements<T, N> o;
-#pragma unroll
-            for (int e = 0; e < N; ++e) {
-                float all = part[0][lane * N + e];
-#pragma unroll
-                for (int w = 1; w < kWaves; ++w) all += part[w][lane * N + e];
-                o.v[e] = (T)((all + head.v[e]) * a.scale);
-            }
-            o.store(static_cast<T*>(a.dtable) + (int64_t)v * a.width + c);
-        }
-        __syncthreads();
+    if ((int64_t)piece * a.piece >= (int64_t)a.vocab + *a.left) return;
+    const int v = a.ended[piece].x;
+    if (v < 0) return;
+    int start = piece - 1;      // the piece that it begins in: the last before this one that it does not go through
+    for (;;) {
+        const uint64_t not_through = __ballot(start - lane <= 0 || !a.ended[start - lane > 0 ? start - lane : 0].y);
+        start -= not_through ? __builtin_ctzll(not_through) : kWave;
+        if (not_through) break;
     }
+    const int c_own = (blockIdx.y * kWave + mine) * N, c = c_own + N > a.width ? a.width - N : c_own, parts = piece - start, per = (parts + teams - 1) / teams;
+    const int from = start + team * per, to = from + per < piece ? from + per : piece;
+    Sum sum{};
+    constexpr int kAtOnce = 8;
+    for (int i = from; i < to; i += kAtOnce) {
+        Sum s[kAtOnce];
+#pragma unroll
+        for (int u = 0; u < kAtOnce; ++u) s[u] = Sum::load(a.trail + (int64_t)(i + u < to ? i + u : i) * a.width + c);
+#pragma unroll
+        for (int u = 0; u < kAtOnce; ++u)
+#pragma unroll
+            for (int e = 0; e < N; ++e) sum.v[e] += i + u < to ? s[u].v[e] : 0.0f;
+    }
+    for (int d = 1 << lg; d < kWave; d *= 2)
+#pragma unroll
+        for (int e = 0; e < N; ++e) sum.v[e] += __shfl_xor(sum.v[e], d);
+    if (lane < 1 << lg) of_wave[wave][mine] = sum;
+    __syncthreads();
+    if (tid >= 1 << lg || c_own >= a.width) return;
+    const Sum head = Sum::load(a.head + (int64_t)piece * a.width + c);
+    Elements<T, N> o;
+#pragma unroll
+    for (int e = 0; e < N; ++e) {
+        float all = of_wave[0][mine].v[e];
+#pragma unroll
+        for (int w = 1; w < kWaves; ++w) all += of_wave[w][mine].v[e];
+        o.v[e] = (T)((all + head.v[e]) * a.scale);
+    }
+    o.store(static_cast<T*>(a.dtable) + (int64_t)v * a.width + c);
 }
 
 }  // namespace
@@ -491,6 +528,17 @@ int launch_embed(int64_t n, int vocab, int width, int dtype, const int* token, c
         };
         return width >= Chunk<T>::n ? go(k_embed<T, Chunk<T>::n>, Chunk<T>::n) : go(k_embed<T, 1>, 1);
     });
+}
+
+// How many pieces there are, as long as they have 64 items at least and 1 024 at most.  1 000 000 rows of 16 channels in bfloat16 with 1 024 pieces 81 us, with 2 048 83,
+// with 4 096 87; 300 000 of 400 with 2 048 95, with 4 096 100; 524 288 of 1 024, two blocks, with 1 024 295, with 2 048 286, with 4 096 289; 50 000 of 2 000, four
+// blocks, with 1 024 91, with 2 048 96.  At least 32 items: 49 999 of 511 in single precision 61 us for 57; at least 128: 16 000 of 512 33 for 31.
+constexpr int kTeamPieces = 1024, kMostPieces = 2048, kBlockPieces = 4096, kLeastItems = 64;
+
+int pieces_of(int lg, int blocks)
+{
+    const int most = lg < 6 ? kTeamPieces : kBlockPieces / blocks;
+    return most > kMostPieces ? kMostPieces : most < 1 ? 1 : most;
 }
 
 int launch_embed_backward(gr_tokens* h, int64_t n, int vocab, int width, int dtype, const int* token, const void* dout, float scale,
@@ -525,39 +573,36 @@ int launch_embed_backward(gr_tokens* h, int64_t n, int vocab, int width, int dty
             b.key = key[at]; b.slot = slot[at]; b.left = n > 0 ? left : nullptr; b.dout = dout; b.dtable = dtable; b.scale = scale; b.vocab = vocab;
             b.width = width;
             b.blocks = (width + kWave * N - 1) / (kWave * N);
-            // as many pieces as there are waves in a few rounds; no less than 32 items each (49 999 rows of 511 64 us with 64 or 16)
-            const int64_t items = vocab + n, most = kSumWaves / b.blocks > 1 ? kSumWaves / b.blocks : 1;
-            const int64_t piece = (items + most - 1) / most > 32 ? (items + most - 1) / most : 32;
-            b.piece = (int)piece;
-            b.pieces = (int)((items + piece - 1) / piece);
+            b.lg = lanes_log((width + N - 1) / N);
+            const int64_t items = vocab + n, least = (items + pieces_of(b.lg, b.blocks) - 1) / pieces_of(b.lg, b.blocks);
+            b.piece = (int)(least < kLeastItems ? kLeastItems : least > kPieceItems ? kPieceItems : least);
+            b.pieces = (int)((items + b.piece - 1) / b.piece);
             b.head = h->parts;
             b.ended = h->ended;
             b.trail = h->parts + (int64_t)b.pieces * width;
             if (2 * (int64_t)b.pieces * width > h->n_parts) return GR_ERR_TOO_LARGE;
-            const int64_t waves = (int64_t)b.pieces * b.blocks, blocks = (waves + kWaves - 1) / kWaves;
-            const bool past = past_cache((n + vocab) * width * (int64_t)sizeof(T));
-            if (past) k_embed_sums<T, N, true><<<(unsigned)blocks, kBlock, 0, s>>>(b);
+            const int64_t blocks = (int64_t)(b.pieces + kDies - 1) / kDies * kDies * b.blocks;
+            if (blocks > kMostBlocks) return GR_ERR_TOO_LARGE;
+            if (past_cache((n + vocab) * width * (int64_t)sizeof(T))) k_embed_sums<T, N, true><<<(unsigned)blocks, kBlock, 0, s>>>(b);
             else k_embed_sums<T, N, false><<<(unsigned)blocks, kBlock, 0, s>>>(b);
-            if (n > piece) {      // (a row has more places than that, or there is nothing to join)
-                constexpr int J = N < kJoinChannels ? N : kJoinChannels;
-                const dim3 grid((width + kWave * J - 1) / (kWave * J), (b.pieces + kJoined - 1) / kJoined);
-                k_embed_join<T, J><<<grid, kBlock, 0, s>>>(b);
-            }
+            if (n > 0 && b.pieces > 1) k_embed_join<T, N><<<dim3(b.pieces, b.blocks), kBlock, 0, s>>>(b);
             return launched();
         };
-        // 16 bytes a lane, fewer where a row has not as many for all lanes
-        constexpr int kMost = Chunk<T>::n;
-        if (width >= kWave * kMost) return go(std::integral_constant<int, kMost>{});
-        if (width >= kWave * kMost / 2) return go(std::integral_constant<int, kMost / 2>{});
-        return go(std::integral_constant<int, 1>{});
+        return width >= Chunk<T>::n ? go(std::integral_constant<int, Chunk<T>::n>{}) : go(std::integral_constant<int, 1>{});
     });
 }
 
-// (blocks of channels of 64 lanes: a wave's sums are 64 * 8 channels at most, and there are kSumWaves or one a block)
-int64_t embed_parts(int width)
+int64_t embed_pieces(int64_t n, int vocab)
 {
-    const int64_t most = 2 * (int64_t)kWave * 8 * kSumWaves, one = 2 * (int64_t)width;
-    return most > one ? most : one;
+    const int64_t whole = (n + vocab + kPieceItems - 1) / kPieceItems;
+    return whole > kMostPieces ? whole : kMostPieces;
+}
+
+// (pieces of less than kPieceItems are no more than pieces_of)
+int64_t embed_parts(int64_t n, int vocab, int width)
+{
+    const int64_t less = 2 * (int64_t)kWave * 8 * kBlockPieces, whole = 2 * (int64_t)width * ((n + vocab + kPieceItems - 1) / kPieceItems);
+    return less > whole ? less : whole;
 }
 
 }  // namespace gr

@@ -10,7 +10,7 @@ struct gr_tokens {
     int* order = nullptr;      // [4][max_tokens] tokens and where they stood, before and after a pass of the sort (see embed.hip)
     float* parts = nullptr;    // [n_parts] parts of long sums (see embed.hip)
     int64_t n_parts = 0;
-    int2* ended = nullptr;     // [kSumWaves] long rows that end in a piece
+    int2* ended = nullptr;     // [embed_pieces] rows that pieces share
     uint64_t* words = nullptr;      // [n_words] what workgroups of a recurrence tell each other (see scan.hip)
     size_t n_words = 0;
     uint64_t* control = nullptr;      // its counters
@@ -50,11 +50,12 @@ __device__ __forceinline__ void store_of(T* at, const Elements<T, N>& e)
 }
 
 constexpr int kDigitBits = 9, kDigits = 1 << kDigitBits;      // of a pass of the sort
-constexpr int kSumWaves = 16384;                              // waves of the sums, at most, or one for each block of channels
 constexpr int kSortUnit = 2048;                               // tokens that a workgroup puts in order
 inline int64_t sort_units(int64_t n) { return (n + kSortUnit - 1) / kSortUnit; }
 
-int64_t embed_parts(int width);
+constexpr int kPieceItems = 1024;                             // of a piece of the sums, at most
+int64_t embed_pieces(int64_t n, int vocab);
+int64_t embed_parts(int64_t n, int vocab, int width);
 int launch_embed(int64_t n, int vocab, int width, int dtype, const int* token, const void* table, float scale, void* out, hipStream_t s);
 int launch_embed_backward(gr_tokens* h, int64_t n, int vocab, int width, int dtype, const int* token, const void* dout, float scale,
                           void* dtable, hipStream_t s);

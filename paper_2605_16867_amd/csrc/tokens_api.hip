@@ -64,14 +64,14 @@ int gr_tokens_create(gr_tokens** out, int64_t max_tokens, int32_t max_vocab, int
     h->max_vocab = max_vocab;
     h->max_width = max_width;
     h->n_words = scan_words(max_tokens, max_width);
-    h->n_parts = embed_parts(max_width);
+    h->n_parts = embed_parts(max_tokens, max_vocab, max_width);
     h->counters = scan_counters(max_width);
     const size_t n_control = (size_t)(h->counters + 1) * kScanLine;
     std::unique_ptr<uint64_t[]> first(new (std::nothrow) uint64_t[n_control]());      // (the first call is number 1)
     for (int i = 0; first && i < h->counters; ++i) first[(i + 1) * kScanLine] = uint64_t(1) << 32;
     if (!first || !dev_alloc(&h->words, h->n_words) || hipMemset(h->words, 0, h->n_words * sizeof(uint64_t)) != hipSuccess ||
         !dev_alloc(&h->control, n_control) || hipMemcpy(h->control, first.get(), n_control * sizeof(uint64_t), hipMemcpyHostToDevice) != hipSuccess ||
-        !dev_alloc(&h->parts, h->n_parts) || !dev_alloc(&h->ended, kSumWaves) || !dev_alloc(&h->order, 4 * (size_t)max_tokens) || !dev_alloc(&h->digits, (size_t)(sort_units(max_tokens) + 1) * kDigits + 1)) {
+        !dev_alloc(&h->parts, h->n_parts) || !dev_alloc(&h->ended, (size_t)embed_pieces(max_tokens, max_vocab)) || !dev_alloc(&h->order, 4 * (size_t)max_tokens) || !dev_alloc(&h->digits, (size_t)(sort_units(max_tokens) + 1) * kDigits + 1)) {
         gr_tokens_destroy(h);
         return GR_ERR_NOMEM;
     }

@@ -698,6 +698,26 @@ def test_more_rows_than_the_cache_holds():
     assert n * W * 4 > 256 << 20 and torch.equal(out, want * 0.5)
 
 
+@pytest.mark.parametrize("width", [1, 8, 16, 40, 100, 129, 256, 300, 513, 1040])
+@pytest.mark.parametrize("each", [(63,), (64,), (62, 64), (1,), (0, 0, 127), (5000, 0, 1), (300, 20, 1, 0), (0,) * 500 + (70,)])
+def test_gradient_of_rows_that_end_where_the_work_is_split(each, width):
+    """So many rows of each token: sums of whole numbers, which single precision holds; what is no number stays with its token."""
+    rng = np.random.default_rng(width + len(each))
+    count = np.resize(each, 900 if sum(each) < 100 else 40 if len(each) < 100 else 20_000)
+    token = rng.permutation(np.repeat(np.arange(len(count)), count))
+    dout = rng.integers(-4, 5, (len(token), width)).astype(np.float64)
+    want = np.zeros((len(count), width))
+    np.add.at(want, token, dout)
+    bad = int(token[0])
+    dout[np.flatnonzero(token == bad)[-1], width // 2] = NAN
+    want[bad, width // 2] = NAN
+    h = binding.Tokens(len(token), len(count), width)
+    for dtype in (torch.float32, torch.bfloat16):
+        out = empty(len(count), width, dtype=dtype)
+        h.gr_token_embed_backward(ints(token), put(dout, dtype), out, scale=2.0)
+        assert torch.equal(out.nan_to_num(nan=1e30), put(np.nan_to_num(want * 2, nan=1e30), torch.float32).to(dtype))
+
+
 @pytest.mark.parametrize("dtype,n,S,width", [(torch.float32, 9000, 3000, 24), (torch.bfloat16, 6000, 20000, 40), (torch.float16, 5000, 2047, 9),
                                              (torch.float32, 5000, 2048, 9), (torch.float32, 300, 5000, 130)])
 def test_more_sequences_than_shared_memory_has_room_for(dtype, n, S, width):
