@@ -4,8 +4,8 @@
 //
 // Bound by memory.  Forward: the rows that are written, and those of the tokens that occur: 524 288 rows of 1 024 in bfloat16 1.2 GB, 227 us while the table
 // stands in the cache, 290 where it does not.  Backward: the tokens are sorted first, in passes of up to nine bits, each stable, so that the rows of a
-// token are summed in the order in which they stand, in single precision: no atomics, the same bits every time.  Of 298 us at the same sizes
-// 244 are the sums (1.2 GB, 5 TB/s), 8 the joining of long ones, 38 the sort; of 64 at 49 999 of 511 in single precision 41, 5 and 18.
+// token are summed in single precision in an order that hangs on where they stand alone: no atomics, the same bits every time.  Of 283 us at the same
+// sizes 234 are the sums (1.2 GB, 5.2 TB/s), 7 the joining of those that pieces share, 33 the sort; of 57 at 49 999 of 511 in single precision 35, 5 and 18.
 #include <type_traits>
 
 #include "tokens.h"
@@ -60,15 +60,16 @@ __global__ __launch_bounds__(kBlock) void k_embed(const int* token, const T* tab
 
 // ---- the sort ----------------------------------------------------------------------------------
 //
-// A pass: how many tokens of each digit every unit of 2 048 has; for each digit the sums over units; the places.  2 MB of tokens are in the cache
-// throughout: what counts is launches and the loads that wait for each other, 5, 5 and 9 us at 524 288 tokens.  A unit is 16 waves of 128 tokens (four of 512: 13 us
-// for the places).
+// A pass: how many tokens of each digit every unit of 2 048 has; for each digit the sums over units; the places.  4 MB of tokens and places are in the cache
+// throughout: what counts is launches and the loads that wait for each other, 4, 3 and 7 us at 524 288 tokens.  A unit is 16 waves of 128 tokens (four of 512: 13 us
+// for the places).  Token and place are a pair: as two arrays, in two stores, 9.
 
 constexpr int kFewUnits = 64;      // up to so many each workgroup of the places adds them up itself, one launch less
 
 struct SortArgs {
-    const int *key, *slot;      // slot: null in the first pass, where they are the places themselves
-    int *to_key, *to_slot;
+    const int* token;      // the first pass's, which stand at their places
+    const int2* from;      // later ones': token and place
+    int2* to;
     int* digits;
     int64_t n;      // tokens (in later passes: most)
     const int* left;      // null in the first pass: how many there are
@@ -78,12 +79,19 @@ struct SortArgs {
 
 __device__ __forceinline__ int64_t count_of(const SortArgs& a) { return a.left ? *a.left : a.n; }
 
+// A die's workgroups, every eighth, take units that follow each other: what they write is side by side in its cache (the places of 1 000 000 tokens 13.6 us for 15.5).
+__device__ __forceinline__ int unit_of(const SortArgs& a)
+{
+    return (int)(a.summed ? blockIdx.x % kDies * (gridDim.x / kDies) + blockIdx.x / kDies : blockIdx.x);
+}
+
 // The digit of the token at i, -1 if there is none or it has no row.
-__device__ __forceinline__ int digit_of(const SortArgs& a, int64_t i, int64_t n, int* key)
+__device__ __forceinline__ int digit_of(const SortArgs& a, int64_t i, int64_t n, int2* pair)
 {
     if (i >= n) return -1;
-    *key = a.key[i];
-    return *key < 0 || *key >= a.vocab ? -1 : *key >> a.shift & a.mask;
+    *pair = a.from ? a.from[i] : int2{a.token[i], (int)i};
+    const int key = pair->x;
+    return key < 0 || key >= a.vocab ? -1 : key >> a.shift & a.mask;
 }
 
 constexpr int kSortThreads = 1024, kSortWaves = kSortThreads / kWave, kSortRounds = kSortUnit / kSortThreads;
@@ -91,18 +99,21 @@ constexpr int kSortThreads = 1024, kSortWaves = kSortThreads / kWave, kSortRound
 __global__ __launch_bounds__(kSortThreads) void k_digit_count(SortArgs a)
 {
     __shared__ int hist[kDigits];
+    const int unit = unit_of(a);
+    if (unit >= a.units) return;
     if (threadIdx.x < kDigits) hist[threadIdx.x] = 0;
-    const int64_t from = (int64_t)blockIdx.x * kSortUnit + threadIdx.x, n = count_of(a);
-    int d[kSortRounds], key;
+    const int64_t from = (int64_t)unit * kSortUnit + threadIdx.x, n = count_of(a);
+    int d[kSortRounds];
+    int2 pair;
 #pragma unroll
-    for (int r = 0; r < kSortRounds; ++r) d[r] = digit_of(a, from + r * kSortThreads, n, &key);
+    for (int r = 0; r < kSortRounds; ++r) d[r] = digit_of(a, from + r * kSortThreads, n, &pair);
     __syncthreads();
 #pragma unroll
     for (int r = 0; r < kSortRounds; ++r)
         if (d[r] >= 0) atomicAdd(&hist[d[r]], 1);
     __syncthreads();
     const int t = threadIdx.x;
-    if (t <= a.mask) a.digits[a.summed ? (int64_t)t * a.units + blockIdx.x : (int64_t)blockIdx.x * kDigits + t] = hist[t];
+    if (t <= a.mask) a.digits[a.summed ? (int64_t)t * a.units + unit : (int64_t)unit * kDigits + t] = hist[t];
 }
 
 // The sum over the lanes up to this one.
@@ -160,19 +171,17 @@ __device__ __forceinline__ uint64_t lanes_of(int digit, int bits)
 __global__ __launch_bounds__(kSortThreads) void k_digit_place(SortArgs a, int bits, int* left)
 {
     __shared__ int part[kDigits / kWave], next[kSortWaves][kDigits];
-    const int tid = threadIdx.x, lane = tid % kWave, wave = tid / kWave;
-    const int64_t from = (int64_t)blockIdx.x * kSortUnit + wave * (kSortUnit / kSortWaves) + lane, n = count_of(a);
-    int key[kSortRounds], slot[kSortRounds], d[kSortRounds];
+    const int tid = threadIdx.x, lane = tid % kWave, wave = tid / kWave, unit = unit_of(a);
+    if (unit >= a.units) return;
+    const int64_t from = (int64_t)unit * kSortUnit + wave * (kSortUnit / kSortWaves) + lane, n = count_of(a);
+    int2 pair[kSortRounds];
+    int d[kSortRounds];
 #pragma unroll
-    for (int r = 0; r < kSortRounds; ++r) {
-        const int64_t i = from + r * kWave;
-        d[r] = digit_of(a, i, n, &key[r]);
-        slot[r] = a.slot && i < n ? a.slot[i] : (int)i;
-    }
+    for (int r = 0; r < kSortRounds; ++r) d[r] = digit_of(a, from + r * kWave, n, &pair[r]);
     int earlier = 0, whole = 0;
     if (tid <= a.mask) {
         if (a.summed) {
-            earlier = a.digits[(int64_t)tid * a.units + blockIdx.x];
+            earlier = a.digits[(int64_t)tid * a.units + unit];
             whole = a.digits[(int64_t)kDigits * a.units + tid];
         } else
             for (int u0 = 0; u0 < a.units; u0 += 16) {
@@ -181,7 +190,7 @@ __global__ __launch_bounds__(kSortThreads) void k_digit_place(SortArgs a, int bi
                 for (int u = 0; u < 16; ++u) own[u] = a.digits[(int64_t)(u0 + u < a.units ? u0 + u : u0) * kDigits + tid];
 #pragma unroll
                 for (int u = 0; u < 16; ++u) {
-                    earlier += u0 + u < (int)blockIdx.x ? own[u] : 0;
+                    earlier += u0 + u < unit ? own[u] : 0;
                     whole += u0 + u < a.units ? own[u] : 0;
                 }
             }
@@ -200,7 +209,7 @@ __global__ __launch_bounds__(kSortThreads) void k_digit_place(SortArgs a, int bi
             if (w < wave) at += part[w];
             all += part[w];
         }
-        if (left && blockIdx.x == 0 && tid == 0) *left = all;
+        if (left && unit == 0 && tid == 0) *left = all;
         for (int w = 0; w < kSortWaves; ++w) {
             const int own = next[w][tid];
             next[w][tid] = at;
@@ -213,8 +222,7 @@ __global__ __launch_bounds__(kSortThreads) void k_digit_place(SortArgs a, int bi
         const uint64_t same = lanes_of(d[r], bits);
         if (d[r] >= 0) {
             const int at = next[wave][d[r]] + __popcll(same & ((uint64_t(1) << lane) - 1));
-            a.to_key[at] = key[r];
-            a.to_slot[at] = slot[r];
+            a.to[at] = pair[r];
         }
         wave_sync();
         if (d[r] >= 0 && (same >> lane) == 1) next[wave][d[r]] += __popcll(same);
@@ -226,7 +234,7 @@ __global__ __launch_bounds__(kSortThreads) void k_digit_place(SortArgs a, int bi
 // 22, where four launches take 18.
 constexpr int kFewTokens = 4096, kFewThreads = 1024, kFewWaves = kFewThreads / kWave, kFewBits = 8, kFewDigits = 1 << kFewBits;
 
-__global__ __launch_bounds__(kFewThreads) void k_sort_few(const int* token, int n, int vocab, int bits, int* to_key, int* to_slot, int* left)
+__global__ __launch_bounds__(kFewThreads) void k_sort_few(const int* token, int n, int vocab, int bits, int2* to, int* left)
 {
     __shared__ int keys[2][kFewTokens];
     __shared__ uint16_t slots[2][kFewTokens];
@@ -240,14 +248,14 @@ __global__ __launch_bounds__(kFewThreads) void k_sort_few(const int* token, int 
     int at = 0;
     for (int pass = 0; pass < passes; ++pass, at ^= 1) {
         const int shift = bits * pass / passes, width = bits * (pass + 1) / passes - shift, mask = (1 << width) - 1;
-        const int per = (n + kFewWaves * kWave - 1) / (kFewWaves * kWave) * kWave, from = wave * per, to = from + per < n ? from + per : n;
+        const int per = (n + kFewWaves * kWave - 1) / (kFewWaves * kWave) * kWave, from = wave * per, end = from + per < n ? from + per : n;
         for (int i = tid; i < kFewWaves * kFewDigits; i += kFewThreads) (&next[0][0])[i] = 0;
         __syncthreads();
         const auto digit_at = [&](int i) {
-            const int k = i < to ? keys[at][i] : -1;
+            const int k = i < end ? keys[at][i] : -1;
             return k < 0 || k >= vocab ? -1 : k >> shift & mask;
         };
-        for (int i = from + lane; i < to; i += kWave) {
+        for (int i = from + lane; i < end; i += kWave) {
             const int d = digit_at(i);
             if (d >= 0) atomicAdd(&next[wave][d], 1);
         }
@@ -274,15 +282,13 @@ __global__ __launch_bounds__(kFewThreads) void k_sort_few(const int* token, int 
         }
         __syncthreads();
         const bool last = pass + 1 == passes;
-        for (int i0 = from; i0 < to; i0 += kWave) {
+        for (int i0 = from; i0 < end; i0 += kWave) {
             const int i = i0 + lane, d = digit_at(i);
             const uint64_t same = lanes_of(d, width);
             if (d >= 0) {
                 const int place = next[wave][d] + __popcll(same & ((uint64_t(1) << lane) - 1));
-                if (last) {
-                    to_key[place] = keys[at][i];
-                    to_slot[place] = slots[at][i];
-                } else {
+                if (last) to[place] = int2{keys[at][i], (int)slots[at][i]};
+                else {
                     keys[at ^ 1][place] = keys[at][i];
                     slots[at ^ 1][place] = slots[at][i];
                 }
@@ -307,7 +313,8 @@ __global__ __launch_bounds__(kFewThreads) void k_sort_few(const int* token, int 
 // places are shared out among rows: 1 000 000 of 16 channels, where a token is 4 % of all of them, 26 us.
 
 struct SumArgs {
-    const int *key, *slot, *left;      // left: how many there are; null: none
+    const int2* place;      // tokens in order, and where each stood
+    const int* left;        // how many there are; null: none
     const void* dout;
     void* dtable;
     float *head, *trail;      // [pieces][width] of rows that pieces share: of the piece that has the row's end, of the others
@@ -335,7 +342,7 @@ __device__ __forceinline__ int first_not(int lo, int hi, F before)
 
 __device__ __forceinline__ int place_at(const SumArgs& a, int n, int64_t item)
 {
-    return first_not(0, n, [&](int p) { return (int64_t)p + a.key[p] < item; });
+    return first_not(0, n, [&](int p) { return (int64_t)p + a.place[p].x < item; });
 }
 
 // The sum of a row that goes on behind these places; of all of them, the row having begun before them?
@@ -380,12 +387,12 @@ __global__ __launch_bounds__(kBlock) void k_embed_sums(SumArgs a)
     }
     __syncthreads();
     const int p0 = bound[0], count = bound[1] - p0, v0 = (int)(item - p0), v1 = (int)(end - bound[1]);      // rows from v0 to v1 end here
-    const bool headed = p0 > 0 && a.key[p0 - 1] == v0;
+    const bool headed = p0 > 0 && a.place[p0 - 1].x == v0;
     for (int i = tid; i < count; i += kBlock) {
-        const int k = a.key[p0 + i];
-        keys[i] = k;
-        slots[i] = a.slot[p0 + i];
-        if (k < v1) occurs[k - v0] = 1;
+        const int2 at = a.place[p0 + i];
+        keys[i] = at.x;
+        slots[i] = at.y;
+        if (at.x < v1) occurs[at.x - v0] = 1;
     }
     __syncthreads();
     const int per = (count + teams - 1) / teams, from = team * per, to = from + per < count ? from + per : count;
@@ -547,30 +554,31 @@ int launch_embed_backward(gr_tokens* h, int64_t n, int vocab, int width, int dty
     int bits = 1;
     while ((int64_t(1) << bits) < vocab) ++bits;
     const int passes = (bits + kDigitBits - 1) / kDigitBits;
-    int *const key[2] = {h->order, h->order + h->max_tokens}, *const slot[2] = {h->order + 2 * h->max_tokens, h->order + 3 * h->max_tokens};
+    int2* const order[2] = {h->order, h->order + h->max_tokens};
     SortArgs a{};
     a.digits = h->digits; a.n = n; a.units = (int)sort_units(n); a.vocab = vocab; a.summed = a.units > kFewUnits;
     int* const left = h->digits + (sort_units(h->max_tokens) + 1) * kDigits;
+    const int grid = a.summed ? (a.units + kDies - 1) / kDies * kDies : a.units;
     int at = 0;
-    if (n > 0 && n <= kFewTokens) k_sort_few<<<1, kFewThreads, 0, s>>>(token, (int)n, vocab, bits, key[0], slot[0], left);
+    if (n > 0 && n <= kFewTokens) k_sort_few<<<1, kFewThreads, 0, s>>>(token, (int)n, vocab, bits, order[0], left);
     for (int p = 0; p < passes && n > kFewTokens; ++p) {
         const int from = bits * p / passes, to = bits * (p + 1) / passes;
-        a.key = p ? key[at] : token;
-        a.slot = p ? slot[at] : nullptr;
+        a.token = token;
+        a.from = p ? order[at] : nullptr;
         a.left = p ? left : nullptr;
         at = p & 1;
-        a.to_key = key[at]; a.to_slot = slot[at];
+        a.to = order[at];
         a.shift = from; a.mask = (1 << (to - from)) - 1;
-        k_digit_count<<<a.units, kSortThreads, 0, s>>>(a);
+        k_digit_count<<<grid, kSortThreads, 0, s>>>(a);
         if (a.summed) k_digit_sum<<<a.mask + 1, kBlock, 0, s>>>(a);
-        k_digit_place<<<a.units, kSortThreads, 0, s>>>(a, to - from, p ? nullptr : left);
+        k_digit_place<<<grid, kSortThreads, 0, s>>>(a, to - from, p ? nullptr : left);
     }
     return by_type(dtype, [&](auto t) {
         typedef decltype(t) T;
         const auto go = [&](auto count) -> int {
             constexpr int N = decltype(count)::value;
             SumArgs b{};
-            b.key = key[at]; b.slot = slot[at]; b.left = n > 0 ? left : nullptr; b.dout = dout; b.dtable = dtable; b.scale = scale; b.vocab = vocab;
+            b.place = order[at]; b.left = n > 0 ? left : nullptr; b.dout = dout; b.dtable = dtable; b.scale = scale; b.vocab = vocab;
             b.width = width;
             b.blocks = (width + kWave * N - 1) / (kWave * N);
             b.lg = lanes_log((width + N - 1) / N);

@@ -7,7 +7,7 @@
 struct gr_tokens {
     int64_t max_tokens = 0;
     int max_vocab = 0, max_width = 0;
-    int* order = nullptr;      // [4][max_tokens] tokens and where they stood, before and after a pass of the sort (see embed.hip)
+    int2* order = nullptr;     // [2][max_tokens] tokens and where they stood, before and after a pass of the sort (see embed.hip)
     float* parts = nullptr;    // [n_parts] parts of long sums (see embed.hip)
     int64_t n_parts = 0;
     int2* ended = nullptr;     // [embed_pieces] rows that pieces share

@@ -71,7 +71,7 @@ int gr_tokens_create(gr_tokens** out, int64_t max_tokens, int32_t max_vocab, int
     for (int i = 0; first && i < h->counters; ++i) first[(i + 1) * kScanLine] = uint64_t(1) << 32;
     if (!first || !dev_alloc(&h->words, h->n_words) || hipMemset(h->words, 0, h->n_words * sizeof(uint64_t)) != hipSuccess ||
         !dev_alloc(&h->control, n_control) || hipMemcpy(h->control, first.get(), n_control * sizeof(uint64_t), hipMemcpyHostToDevice) != hipSuccess ||
-        !dev_alloc(&h->parts, h->n_parts) || !dev_alloc(&h->ended, (size_t)embed_pieces(max_tokens, max_vocab)) || !dev_alloc(&h->order, 4 * (size_t)max_tokens) || !dev_alloc(&h->digits, (size_t)(sort_units(max_tokens) + 1) * kDigits + 1)) {
+        !dev_alloc(&h->parts, h->n_parts) || !dev_alloc(&h->ended, (size_t)embed_pieces(max_tokens, max_vocab)) || !dev_alloc(&h->order, 2 * (size_t)max_tokens) || !dev_alloc(&h->digits, (size_t)(sort_units(max_tokens) + 1) * kDigits + 1)) {
         gr_tokens_destroy(h);
         return GR_ERR_NOMEM;
     }
