@@ -5,7 +5,7 @@
 // Bound by memory.  Forward: the rows that are written, and those of the tokens that occur: 524 288 rows of 1 024 in bfloat16 1.2 GB, 227 us while the table
 // stands in the cache, 290 where it does not.  Backward: the tokens are sorted first, in passes of up to nine bits, each stable, so that the rows of a
 // token are summed in single precision in an order that hangs on where they stand alone: no atomics, the same bits every time.  Of 283 us at the same
-// sizes 234 are the sums (1.2 GB, 5.2 TB/s), 7 the joining of those that pieces share, 33 the sort; of 57 at 49 999 of 511 in single precision 35, 5 and 18.
+// sizes 234 are the sums (1.2 GB, 5.2 TB/s), 7 the joining of those that pieces share, 33 the sort; of 56 at 49 999 of 511 in single precision 35, 5 and 17.
 #include <type_traits>
 
 #include "tokens.h"
@@ -167,7 +167,30 @@ __device__ __forceinline__ uint64_t lanes_of(int digit, int bits)
     return same;
 }
 
-// Waves take 128 tokens each, 64 at a time; lanes of one digit find each other bit by bit.
+// Each lane's place among its wave's tokens of the same digit, 64 tokens at a time, lanes of one digit finding each other bit by bit; `next`, the wave's own,
+// is left with how many there are.
+template <int kRounds>
+__device__ __forceinline__ void ranks(const int (&d)[kRounds], int rounds, int bits, int* next, int digits, int (&rank)[kRounds])
+{
+    const int lane = threadIdx.x % kWave;
+    for (int i = lane; i < digits; i += kWave) next[i] = 0;
+    uint64_t same[kRounds];
+#pragma unroll
+    for (int r = 0; r < kRounds; ++r)
+        if (r < rounds) same[r] = lanes_of(d[r], bits);
+    wave_sync();
+#pragma unroll
+    for (int r = 0; r < kRounds; ++r) {
+        if (r >= rounds) break;
+        const int before = d[r] >= 0 ? next[d[r]] : 0;
+        rank[r] = before + __popcll(same[r] & ((uint64_t(1) << lane) - 1));
+        wave_sync();
+        if (d[r] >= 0 && (same[r] >> lane) == 1) next[d[r]] = rank[r] + 1;
+        wave_sync();
+    }
+}
+
+// Waves take 128 tokens each.
 __global__ __launch_bounds__(kSortThreads) void k_digit_place(SortArgs a, int bits, int* left)
 {
     __shared__ int part[kDigits / kWave], next[kSortWaves][kDigits];
@@ -175,7 +198,7 @@ __global__ __launch_bounds__(kSortThreads) void k_digit_place(SortArgs a, int bi
     if (unit >= a.units) return;
     const int64_t from = (int64_t)unit * kSortUnit + wave * (kSortUnit / kSortWaves) + lane, n = count_of(a);
     int2 pair[kSortRounds];
-    int d[kSortRounds];
+    int d[kSortRounds], rank[kSortRounds];
 #pragma unroll
     for (int r = 0; r < kSortRounds; ++r) d[r] = digit_of(a, from + r * kWave, n, &pair[r]);
     int earlier = 0, whole = 0;
@@ -195,108 +218,81 @@ __global__ __launch_bounds__(kSortThreads) void k_digit_place(SortArgs a, int bi
                 }
             }
     }
-    for (int i = tid; i < kSortWaves * kDigits; i += kSortThreads) (&next[0][0])[i] = 0;
+    ranks(d, kSortRounds, bits, next[wave], kDigits, rank);
     const int upto = up_to_me(whole);
     if (tid < kDigits && lane == kWave - 1) part[wave] = upto;
     __syncthreads();
-#pragma unroll
-    for (int r = 0; r < kSortRounds; ++r)
-        if (d[r] >= 0) atomicAdd(&next[wave][d[r]], 1);
-    __syncthreads();
     if (tid < kDigits) {
-        int at = earlier + upto - whole, all = 0;
+        int at = earlier + upto - whole, all = 0, own[kSortWaves];
+#pragma unroll
+        for (int w = 0; w < kSortWaves; ++w) own[w] = next[w][tid];
         for (int w = 0; w < kDigits / kWave; ++w) {
             if (w < wave) at += part[w];
             all += part[w];
         }
         if (left && unit == 0 && tid == 0) *left = all;
+#pragma unroll
         for (int w = 0; w < kSortWaves; ++w) {
-            const int own = next[w][tid];
             next[w][tid] = at;
-            at += own;
+            at += own[w];
         }
     }
     __syncthreads();
 #pragma unroll
-    for (int r = 0; r < kSortRounds; ++r) {
-        const uint64_t same = lanes_of(d[r], bits);
-        if (d[r] >= 0) {
-            const int at = next[wave][d[r]] + __popcll(same & ((uint64_t(1) << lane) - 1));
-            a.to[at] = pair[r];
-        }
-        wave_sync();
-        if (d[r] >= 0 && (same >> lane) == 1) next[wave][d[r]] += __popcll(same);
-        wave_sync();
-    }
+    for (int r = 0; r < kSortRounds; ++r)
+        if (d[r] >= 0) a.to[next[wave][d[r]] + rank[r]] = pair[r];
 }
 
-// Few tokens are sorted by one workgroup in one launch, in shared memory, eight bits a pass: 512 of 32 000 in 5 us where six launches take 16; 8 192 of them
+// Few tokens are sorted by one workgroup in one launch, in shared memory between the passes: 512 of 32 000 in 5 us where six launches take 16; 8 192 of them
 // 22, where four launches take 18.
-constexpr int kFewTokens = 4096, kFewThreads = 1024, kFewWaves = kFewThreads / kWave, kFewBits = 8, kFewDigits = 1 << kFewBits;
+constexpr int kFewTokens = 4096, kFewThreads = 1024, kFewWaves = kFewThreads / kWave, kFewRounds = kFewTokens / kFewThreads;
 
 __global__ __launch_bounds__(kFewThreads) void k_sort_few(const int* token, int n, int vocab, int bits, int2* to, int* left)
 {
-    __shared__ int keys[2][kFewTokens];
-    __shared__ uint16_t slots[2][kFewTokens];
-    __shared__ int next[kFewWaves][kFewDigits], part[kFewDigits / kWave];
-    const int tid = threadIdx.x, lane = tid % kWave, wave = tid / kWave;
-    for (int i = tid; i < n; i += kFewThreads) {
-        keys[0][i] = token[i];
-        slots[0][i] = (uint16_t)i;
-    }
-    const int passes = (bits + kFewBits - 1) / kFewBits;
-    int at = 0;
-    for (int pass = 0; pass < passes; ++pass, at ^= 1) {
+    __shared__ int2 order[kFewTokens];
+    __shared__ int next[kFewWaves][kDigits], part[kDigits / kWave];
+    const int tid = threadIdx.x, lane = tid % kWave, wave = __builtin_amdgcn_readfirstlane(tid / kWave), passes = (bits + kDigitBits - 1) / kDigitBits;
+    for (int pass = 0; pass < passes; ++pass) {
         const int shift = bits * pass / passes, width = bits * (pass + 1) / passes - shift, mask = (1 << width) - 1;
-        const int per = (n + kFewWaves * kWave - 1) / (kFewWaves * kWave) * kWave, from = wave * per, end = from + per < n ? from + per : n;
-        for (int i = tid; i < kFewWaves * kFewDigits; i += kFewThreads) (&next[0][0])[i] = 0;
+        const int most = (n + kFewThreads - 1) / kFewThreads, first = wave * most * kWave, from = first + lane, rounds = first < n ? most : 0;
+        int2 pair[kFewRounds];
+        int d[kFewRounds], rank[kFewRounds];
+#pragma unroll
+        for (int r = 0; r < kFewRounds; ++r) {
+            const int i = from + r * kWave;
+            pair[r] = int2{-1, 0};
+            if (r < rounds && i < n) pair[r] = pass ? order[i] : int2{token[i], i};
+            d[r] = pair[r].x < 0 || pair[r].x >= vocab ? -1 : pair[r].x >> shift & mask;
+        }
+        ranks(d, rounds, width, next[wave], mask + 1, rank);
         __syncthreads();
-        const auto digit_at = [&](int i) {
-            const int k = i < end ? keys[at][i] : -1;
-            return k < 0 || k >= vocab ? -1 : k >> shift & mask;
-        };
-        for (int i = from + lane; i < end; i += kWave) {
-            const int d = digit_at(i);
-            if (d >= 0) atomicAdd(&next[wave][d], 1);
+        int before = 0, own[kFewWaves], upto = 0, all = 0;
+        if (tid < kDigits) {
+#pragma unroll
+            for (int w = 0; w < kFewWaves; ++w) {
+                own[w] = tid <= mask ? next[w][tid] : 0;
+                before += own[w];
+            }
+            upto = up_to_me(before);
+            if (lane == kWave - 1) part[wave] = upto;
         }
         __syncthreads();
-        int before = 0, own = 0;
-        if (tid < kFewDigits) {
-            for (int w = 0; w < kFewWaves; ++w) own += next[w][tid];
-            before = up_to_me(own);
-            if (lane == kWave - 1) part[wave] = before;
-        }
-        __syncthreads();
-        int all = 0;
-        for (int w = 0; w < kFewDigits / kWave; ++w) {
+        before = upto - before;
+        for (int w = 0; w < kDigits / kWave; ++w) {
             if (w < wave) before += part[w];
             all += part[w];
         }
-        if (tid < kFewDigits) {
-            before -= own;
+        if (tid <= mask) {
+#pragma unroll
             for (int w = 0; w < kFewWaves; ++w) {
-                const int mine = next[w][tid];
                 next[w][tid] = before;
-                before += mine;
+                before += own[w];
             }
         }
         __syncthreads();
-        const bool last = pass + 1 == passes;
-        for (int i0 = from; i0 < end; i0 += kWave) {
-            const int i = i0 + lane, d = digit_at(i);
-            const uint64_t same = lanes_of(d, width);
-            if (d >= 0) {
-                const int place = next[wave][d] + __popcll(same & ((uint64_t(1) << lane) - 1));
-                if (last) to[place] = int2{keys[at][i], (int)slots[at][i]};
-                else {
-                    keys[at ^ 1][place] = keys[at][i];
-                    slots[at ^ 1][place] = slots[at][i];
-                }
-            }
-            wave_sync();
-            if (d >= 0 && (same >> lane) == 1) next[wave][d] += __popcll(same);
-            wave_sync();
-        }
+#pragma unroll
+        for (int r = 0; r < kFewRounds; ++r)
+            if (d[r] >= 0) (pass + 1 == passes ? to : order)[next[wave][d[r]] + rank[r]] = pair[r];
         n = all;
         __syncthreads();
     }
