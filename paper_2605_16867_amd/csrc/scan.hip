@@ -72,6 +72,14 @@ constexpr int kGroup = 16, kLeastLanesLog = 2, kNearOffsets = 2048, kMostRuns = 
 // single precision 8.9 us with four (9.8 with two, 9.9 with eight), but 16 000 x 512, 504 tiles of eight, 20 us (24 with four, 33 with two).
 constexpr int kRunForward = 8, kRunBackward = 6, kRunFew = 4;
 constexpr int64_t kFewTiles = 256;
+// Blocks of channels.  A row is split into as few as 32 lanes allow, all with as many lanes, or, where it is whole sixteens of lanes, into those: if the
+// others would not be whole (bfloat16, 300 000 x 192 96 us for 131, 100 000 x 1 088 156 for 194, backward 262 for 346), with rows of 512 bytes at most (a
+// block has a counter, and 300 000 x 128 are 2 300 draws: 69 us for 76), and with a round of tiles (16 000 x 512 17.3 for 18.5, 3 000 x 256 in single precision
+// 7.7 for 8.3); elsewhere 32 are faster (200 000 x 512 152 for 154, 262 144 x 1 024 380 for 390).  Blocks start at lines, or halves of lines, where rows do: two
+// that share a line both ask for it (200 000 x 224 86 for 89, 100 000 x 352 backward 107 for 120, single precision 100 000 x 416 106 for 118).  Half as many
+// lanes, blocks of 64 bytes, are slower everywhere.
+constexpr int kFewLanesLog = 4, kFewLanesBytes = 512;
+constexpr int64_t kFewLanesTiles = 512;
 
 struct TileArgs {
     ScanIn in;
@@ -648,14 +656,22 @@ int launch(gr_tokens* h, const ScanIn& in, int dtype, void* y, void* dgate, void
     a.gate_stride = (int)in.gate_stride; a.x_stride = (int)in.x_stride; a.dgate_stride = (int)in.dgate_stride; a.dx_stride = (int)in.dx_stride;
     a.n = (int)in.n; a.n_seq = (int)in.n_seq;
     a.control = h->control; a.counters = h->counters; a.sums = h->words; a.n_words = h->n_words;
-    const int per = in.width < kScanChannels ? 1 : kScanChannels, pieces = (in.width + per - 1) / per, most = 1 << kScanLanesLog;
-    a.blocks = (pieces + most - 1) / most;
-    a.lanes = (pieces + a.blocks - 1) / a.blocks;
-    a.lg = kLeastLanesLog;
-    while ((1 << a.lg) < a.lanes) ++a.lg;
+    const int per = in.width < kScanChannels ? 1 : kScanChannels, pieces = (in.width + per - 1) / per;
     constexpr int kRun = kBack ? kRunBackward : kRunForward;
-    const int rows = (kThreads >> a.lg) * kRun;
-    const bool few = (in.n + rows - 1) / rows * a.blocks <= kFewTiles;
+    const auto split = [&](int most) {
+        a.blocks = (pieces + most - 1) / most;
+        a.lanes = (pieces + a.blocks - 1) / a.blocks;
+        a.lg = kLeastLanesLog;
+        while ((1 << a.lg) < a.lanes) ++a.lg;
+        const int rows = (kThreads >> a.lg) * kRun;
+        return (in.n + rows - 1) / rows * a.blocks;
+    };
+    const int64_t tiles = split(1 << kScanLanesLog);
+    const bool few = tiles <= kFewTiles;
+    const int bytes = in.width * (int)size_of(dtype), wide = kScanChannels << kScanLanesLog, narrow = kScanChannels << kFewLanesLog;
+    if (in.width % narrow == 0 && (bytes <= kFewLanesBytes || tiles <= kFewLanesTiles || in.width % wide != 0)) split(1 << kFewLanesLog);
+    const int line = bytes % 128 == 0 ? 128 : bytes % 64 == 0 ? 64 : 1, per_line = line / (kScanChannels * (int)size_of(dtype));
+    if (a.blocks > 1 && per_line > 1) a.lanes = (a.lanes + per_line - 1) / per_line * per_line;
     return by_type(dtype, [&](auto t) {
         typedef decltype(t) T;
         if (per == 1) return launch_tiles<T, 1, kRun, kBack, false>(h, a, s);
@@ -667,13 +683,15 @@ int launch(gr_tokens* h, const ScanIn& in, int dtype, void* y, void* dgate, void
 
 }  // namespace
 
-int scan_counters(int width) { return (width / kScanChannels >> kScanLanesLog) + 1; }
+int scan_counters(int width) { return (width / kScanChannels >> kFewLanesLog) + 1; }
 
 size_t scan_words(int64_t n, int width)
 {
     // a word for F and one for B of every channel of every tile, and one of every group's state: of the least tiles and the most channels in use
-    // (lanes are as many in every block of channels: less than a piece a block more in all, and a piece)
-    const auto words = [&](int64_t tiles) { return (size_t)(tiles * 2 + tiles / kGroup + 1) * (width + (scan_counters(width) + 1) * kScanChannels); };
+    // (all blocks have as many lanes, and a block that is not the only one 32 at most)
+    constexpr int kWide = kScanChannels << kScanLanesLog;
+    const int64_t channels = width > kWide ? (width + (int64_t)kWide - 1) / kWide * kWide : width + kScanChannels - 1;
+    const auto words = [&](int64_t tiles) { return (size_t)((tiles * 2 + tiles / kGroup + 1) * channels); };
     const auto tiles = [&](int run) {
         const int64_t rows = (int64_t)(kThreads >> kScanLanesLog) * run;
         return (n + rows - 1) / rows;

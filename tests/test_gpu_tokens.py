@@ -698,6 +698,31 @@ def test_more_rows_than_the_cache_holds():
     assert n * W * 4 > 256 << 20 and torch.equal(out, want * 0.5)
 
 
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("n,S,width", [(700, 5, 64), (700, 5, 128), (1300, 7, 192), (900, 3, 160), (700, 2, 288), (600, 40, 320), (400, 3, 352), (300, 2, 544), (500, 3, 416),
+                                       (40000, 9, 96), (20000, 3, 512), (90, 4, 1088), (64, 1, 1300)])
+def test_blocks_of_channels(n, S, width, dtype):
+    """Rows split at lines and elsewhere, few tiles and many; a handle of just these sizes; every channel is one of a row that is alone."""
+    rng = np.random.default_rng(n + width)
+    h = binding.Tokens(n, 1, width)
+    gate, x = (put(a, dtype) for a in inputs(rng, n, width, dtype))
+    off = ints(some_offsets(rng, n, S))
+    h0, dh = (torch.randn(S, width, device=DEV) for _ in range(2))
+    y, last = empty(n, width, dtype=dtype), empty(S, width)
+    h.gr_gated_scan(gate, x, out_y=y, off=off, h0=h0, out_h=last)
+    dy = put(f64_of(rng.normal(size=(n, width)), dtype), dtype)
+    dg, dx, dh0 = empty(n, width, dtype=dtype), empty(n, width, dtype=dtype), empty(S, width)
+    h.gr_gated_scan_backward(gate, x, y, dg, dx, off=off, h0=h0, dy=dy, dh=dh, out_dh0=dh0)
+    channels = sorted({0, 1, width // 2, width - 1} | {c + d for c in (16, 32, 64, 96, 128, 256, 512) for d in (-1, 0) if c + d < width})
+    part = lambda a: a[:, channels].double().cpu().numpy()
+    offsets, names = off.cpu().numpy(), ("dgate", "dx", "dh0")
+    want_y, want, E_y, E = ref.scan(part(gate), part(x), offsets, part(h0))
+    ref.near(y[:, channels], want_y, E_y, dtype, "y")
+    ref.near(last[:, channels], want, E, dtype, "last")
+    for got, (r, E), what in zip((dg, dx, dh0), ref.scan_backward(part(gate), part(x), part(y), offsets, part(h0), part(dy), part(dh)), names):
+        ref.near(got[:, channels], r, E, dtype, what)
+
+
 @pytest.mark.parametrize("width", [1, 8, 16, 40, 100, 129, 256, 300, 513, 1040])
 @pytest.mark.parametrize("each", [(63,), (64,), (62, 64), (1,), (0, 0, 127), (5000, 0, 1), (300, 20, 1, 0), (0,) * 500 + (70,)])
 def test_gradient_of_rows_that_end_where_the_work_is_split(each, width):
