@@ -371,9 +371,10 @@ __global__ __launch_bounds__(kBlock) void k_embed_sums(SumArgs a)
     constexpr int kAtOnce = 8;
     __shared__ int keys[kPieceItems], slots[kPieceItems], occurs[kPieceItems], bound[2];
     __shared__ Open<N> of_wave[kWaves][kWave];
-    const int tid = threadIdx.x, lane = tid % kWave, wave = __builtin_amdgcn_readfirstlane(tid / kWave), lg = a.lg, teams = kBlock >> lg, team = tid >> lg;
+    const int tid = threadIdx.x, lane = tid % kWave, wave = __builtin_amdgcn_readfirstlane(tid / kWave);
+    const int lg = a.lg, teams = kBlock >> lg, team = tid >> lg, mine = tid & ((1 << lg) - 1), n = a.left ? *a.left : 0;
     // (the blocks of a piece share lines at their edges: one die's workgroups, every eighth, take them one after the other)
-    const int block = (int)(blockIdx.x / kDies % a.blocks), piece = (int)(blockIdx.x / (kDies * a.blocks) * kDies + blockIdx.x % kDies), mine = tid & ((1 << lg) - 1), n = a.left ? *a.left : 0;
+    const int block = (int)(blockIdx.x / kDies % a.blocks), piece = (int)(blockIdx.x / (kDies * a.blocks) * kDies + blockIdx.x % kDies);
     const int64_t item = (int64_t)piece * a.piece, all = (int64_t)a.vocab + n, end = item + a.piece < all ? item + a.piece : all;
     if (item >= end) return;
     for (int i = tid; i < kPieceItems; i += kBlock) occurs[i] = 0;

@@ -22,7 +22,7 @@ namespace gr {
 
 // A call whose arrays are more than half of the device's last-level cache (256 MB) goes past it: what it reads and writes once would only push itself
 // out.  With 6 to 40 times that: the recurrence of 262 144 x 1 024 in bfloat16 379 us for 406, backward 692 for 722, dropout of 2^28 elements 257 for
-// 272, the gradient of 524 288 rows of 1 024 295 for 308; with 33 MB that the last kernel may have left there, 43 us for 37 (16 000 rows of 512).
+// 272, the gradient of 524 288 rows of 1 024 285 for 300; with 33 MB that the last kernel may have left there, 34 us for 30 (16 000 rows of 512).
 inline bool past_cache(int64_t bytes) { return bytes > int64_t(128) << 20; }
 
 // N neighbouring elements at any address of one, past the cache or not.
