@@ -72,12 +72,12 @@ constexpr int kGroup = 16, kLeastLanesLog = 2, kNearOffsets = 2048, kMostRuns = 
 // single precision 8.9 us with four (9.8 with two, 9.9 with eight), but 16 000 x 512, 504 tiles of eight, 20 us (24 with four, 33 with two).
 constexpr int kRunForward = 8, kRunBackward = 6, kRunFew = 4;
 constexpr int64_t kFewTiles = 256;
-// Blocks of channels.  A row is split into as few as 32 lanes allow, all with as many lanes, or, where it is whole sixteens of lanes, into those: if the
-// others would not be whole (bfloat16, 300 000 x 192 96 us for 131, 100 000 x 1 088 156 for 194, backward 262 for 346), with rows of 512 bytes at most (a
-// block has a counter, and 300 000 x 128 are 2 300 draws: 69 us for 76), and with a round of tiles (16 000 x 512 17.3 for 18.5, 3 000 x 256 in single precision
-// 7.7 for 8.3); elsewhere 32 are faster (200 000 x 512 152 for 154, 262 144 x 1 024 380 for 390).  Blocks start at lines, or halves of lines, where rows do: two
-// that share a line both ask for it (200 000 x 224 86 for 89, 100 000 x 352 backward 107 for 120, single precision 100 000 x 416 106 for 118).  Half as many
-// lanes, blocks of 64 bytes, are slower everywhere.
+// Blocks of channels.  A row is split into as few as 32 lanes allow, all with as many lanes.  Where rows lie on lines, or halves of lines, blocks start there as well:
+// two that share a line both ask for it (200 000 x 224 in bfloat16 86 us for 89, 100 000 x 352 backward 107 for 120, single precision 100 000 x 416 106 for
+// 118).  There 16 lanes are taken if that leaves fewer without a piece (bfloat16, 300 000 x 192 96 us for 131, 200 000 x 160 67 for 82, 100 000 x 1 088 156 for 194,
+// backward 262 for 346; elsewhere 200 000 x 270 128 for 124, backward 244 for 215), and, where rows are whole sixteens, with rows of 512 bytes at most
+// (a block has a counter, and 300 000 x 128 are 2 300 draws: 69 us for 76) and with a round of tiles (16 000 x 512 17.3 for 18.5, 3 000 x 256 in single
+// precision 7.7 for 8.3); other rows are faster by 32 (200 000 x 512 152 for 154, 262 144 x 1 024 380 for 390).  Eight lanes, blocks of 64 bytes, are slower.
 constexpr int kFewLanesLog = 4, kFewLanesBytes = 512;
 constexpr int64_t kFewLanesTiles = 512;
 
@@ -668,9 +668,11 @@ int launch(gr_tokens* h, const ScanIn& in, int dtype, void* y, void* dgate, void
     };
     const int64_t tiles = split(1 << kScanLanesLog);
     const bool few = tiles <= kFewTiles;
-    const int bytes = in.width * (int)size_of(dtype), wide = kScanChannels << kScanLanesLog, narrow = kScanChannels << kFewLanesLog;
-    if (in.width % narrow == 0 && (bytes <= kFewLanesBytes || tiles <= kFewLanesTiles || in.width % wide != 0)) split(1 << kFewLanesLog);
-    const int line = bytes % 128 == 0 ? 128 : bytes % 64 == 0 ? 64 : 1, per_line = line / (kScanChannels * (int)size_of(dtype));
+    const int bytes = in.width * (int)size_of(dtype), line = bytes % 128 == 0 ? 128 : bytes % 64 == 0 ? 64 : 1;
+    const auto lanes_of = [&](int most) { return (pieces + most - 1) / most * most; };
+    const bool fewer = lanes_of(1 << kFewLanesLog) < lanes_of(1 << kScanLanesLog), whole = in.width % (kScanChannels << kFewLanesLog) == 0;
+    if ((line > 1 && fewer) || (whole && (bytes <= kFewLanesBytes || tiles <= kFewLanesTiles))) split(1 << kFewLanesLog);
+    const int per_line = line / (kScanChannels * (int)size_of(dtype));
     if (a.blocks > 1 && per_line > 1) a.lanes = (a.lanes + per_line - 1) / per_line * per_line;
     return by_type(dtype, [&](auto t) {
         typedef decltype(t) T;
