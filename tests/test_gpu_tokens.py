@@ -312,6 +312,41 @@ def test_gates_at_their_ends(dtype):
     ref.near(last, want, E, dtype, "last")
 
 
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("single", [True, False])
+def test_a_far_gates_smaller_sigmoid(single, dtype):
+    """As exact at a gate of 80 as at one of 1: states and gradients that are the sigmoid itself.
+
+    It is off by at most 3.5 units of 2^-23, relative: an exponential's unit, the half of its correction's rounding, the half of the sum's, a reciprocal's
+    unit, the half of the product's; less than 4 with products of those.  dgate, both sigmoids' product, has the larger one's rounding and two products'
+    besides, a half each.  What is written in 16 bits is rounded to them."""
+    rng = np.random.default_rng(12)
+    n, width = 2000, 40
+    ends = np.array([0, 1, 4, 9, 16, 30, 45, 60, 75, 86])
+    lo = rng.integers(0, len(ends) - 1, (n, width))
+    gate = f64_of(rng.uniform(ends[lo], ends[lo + 1]) * rng.choice([-1, 1], (n, width)), dtype)
+    with np.errstate(over="ignore"):
+        keep, take = 1 / (1 + np.exp(-gate)), 1 / (1 + np.exp(gate))
+    h, off, one, none = binding.Tokens(n, 1, width), None if single else ints(np.arange(n + 1)), np.ones((n, width)), np.zeros((n, width))
+    g, f32 = put(gate, dtype), torch.float32
+
+    def check(got, want, units, at, what):
+        err = np.abs(experts_reference.f64(got) - want)
+        bad = at & ~(err <= units * 2.0 ** -23 * want + (0 if got.dtype == f32 else experts_reference.UNIT[dtype] * want * (1 + 1e-3) + experts_reference.LEAST[dtype]))
+        i = tuple(np.argwhere(bad)[0]) if bad.any() else None
+        assert i is None, (what, int(bad.sum()), gate[i], err[i] / want[i] * 2 ** 23)
+
+    y, last = empty(n, width, dtype=dtype), empty(n, width)
+    h.gr_gated_scan(g, put(one, dtype), out_y=y, off=off, out_h=last)
+    check(last, take, 4, gate > 0, "states")
+    check(y, take, 4, gate > 0, "y")
+    dg, dx, dh0 = empty(n, width, dtype=dtype), empty(n, width, dtype=dtype), empty(n, width)
+    h.gr_gated_scan_backward(g, put(none, dtype), put(none, dtype), dg, dx, off=off, h0=put(one, f32), dy=put(one, dtype), out_dh0=dh0)
+    check(dx, take, 4, gate > 0, "dx")
+    check(dh0, keep, 4, gate < 0, "dh0")
+    check(dg, keep * take, 6, np.abs(gate) < 86, "dgate")
+
+
 def test_scan_gradient_by_differences():
     """Of a loss of all states and the last ones, in 64 bits, at some gates, values and first states."""
     rng = np.random.default_rng(9)
