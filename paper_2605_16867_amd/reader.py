@@ -38,7 +38,9 @@ class PromptReader:
         self.b = torch.cat([torch.log(far - 1 + 1e-3), torch.zeros(n_out, device=self.dev)]).to(dtype)
         self.dtable, self.dw, self.db = (torch.empty_like(t) for t in (self.table, self.w, self.b))
         T, R, f32 = max_tokens, max_rows, torch.float32
-        self.rows, self.both, self.y = self._empty(T, width), self._empty(T, 2 * n_out), self._empty(T, n_out)
+        self.rows, self.both = self._empty(T, width), self._empty(T, 2 * n_out)
+        # a batch's own, which wait for its gradient while others are read
+        self.batch_rows, self.batch_both, self.y = self._empty(T, width), self._empty(T, 2 * n_out), self._empty(T, n_out)
         self.drows, self.dboth = self._empty(T, width), self._empty(T, 2 * n_out)
         self.last, self.dlast, self.features = self._empty(R, n_out, of=f32), self._empty(R, n_out, of=f32), self._empty(R, n_out)
         self.norm = self._empty(1, of=f32)
@@ -47,12 +49,12 @@ class PromptReader:
     def _empty(self, *shape, of=None):
         return torch.empty(*shape, dtype=of or self.dtype, device=self.dev)
 
-    def _gates(self, token: torch.Tensor) -> Tuple[torch.Tensor, torch.Tensor]:
+    def _gates(self, token: torch.Tensor, rows: torch.Tensor, both: torch.Tensor) -> Tuple[torch.Tensor, torch.Tensor]:
         """Gates and values of tokens, the halves of one product's result."""
         n = token.numel()
-        self.h.gr_token_embed(token, self.table, self.rows[:n], scale=self.scale)
-        self.products.gr_expert_linear(self.rows[:n], self.w, self.both[:n], bias=self.b)
-        return self.both[:n, :self.n_out], self.both[:n, self.n_out:]
+        self.h.gr_token_embed(token, self.table, rows[:n], scale=self.scale)
+        self.products.gr_expert_linear(rows[:n], self.w, both[:n], bias=self.b)
+        return both[:n, :self.n_out], both[:n, self.n_out:]
 
     # ---- reading ------------------------------------------------------------------------------
 
@@ -60,12 +62,12 @@ class PromptReader:
         """States [requests, n_out] (float32) after the tokens of every request: token int32 [tokens], request r's at off[r] .. off[r+1]-1.  start:
         the states that they go on from (of what was read of them before).  The caller's to keep."""
         out = self._empty(off.numel() - 1, self.n_out, of=torch.float32)
-        self.h.gr_gated_scan(*self._gates(token), off=off, h0=start, out_h=out)
+        self.h.gr_gated_scan(*self._gates(token, self.rows, self.both), off=off, h0=start, out_h=out)
         return out
 
     def advance(self, token: torch.Tensor, state: torch.Tensor) -> None:
         """A generated token of every running request: states [requests, n_out] move on in place."""
-        self.h.gr_gated_scan(*self._gates(token), h0=state, out_h=state)
+        self.h.gr_gated_scan(*self._gates(token, self.rows, self.both), h0=state, out_h=state)
 
     def features_of(self, state: torch.Tensor) -> torch.Tensor:
         """What a length predictor takes of states."""
@@ -74,22 +76,22 @@ class PromptReader:
     # ---- training -----------------------------------------------------------------------------
 
     def train_forward(self, token: torch.Tensor, off: torch.Tensor) -> torch.Tensor:
-        """Features [requests, n_out] of a batch, some of them dropped; valid until the next call."""
+        """Features [requests, n_out] of a batch, some of them dropped; valid until the next batch's."""
         n, R = token.numel(), off.numel() - 1
         self.step.add_(1)
-        self.h.gr_gated_scan(*self._gates(token), out_y=self.y[:n], off=off, out_h=self.last[:R])
+        self.h.gr_gated_scan(*self._gates(token, self.batch_rows, self.batch_both), out_y=self.y[:n], off=off, out_h=self.last[:R])
         self.features[:R].copy_(self.last[:R])
         self.h.gr_dropout(self.features[:R], self.features[:R], self.drop, self.seed, offset_add=self.step)
         return self.features[:R]
 
     def backward(self, token: torch.Tensor, off: torch.Tensor, dfeatures: torch.Tensor) -> None:
-        """Gradients of the weights from that of the features of the last `train_forward`, which is overwritten."""
+        """Gradients of the weights from that of the features of the last `train_forward`, which is overwritten.  What was read since does not matter."""
         n, R, C = token.numel(), off.numel() - 1, self.n_out
         self.h.gr_dropout(dfeatures, dfeatures, self.drop, self.seed, offset_add=self.step)
         self.dlast[:R].copy_(dfeatures)
-        both, d = self.both[:n], self.dboth[:n]
+        both, d = self.batch_both[:n], self.dboth[:n]
         self.h.gr_gated_scan_backward(both[:, :C], both[:, C:], self.y[:n], d[:, :C], d[:, C:], off=off, dh=self.dlast[:R])
-        self.products.gr_expert_linear_backward(self.rows[:n], self.w, d, out_dx=self.drows[:n], out_dw=self.dw, out_db=self.db)
+        self.products.gr_expert_linear_backward(self.batch_rows[:n], self.w, d, out_dx=self.drows[:n], out_dw=self.dw, out_db=self.db)
         self.h.gr_token_embed_backward(token, self.drows[:n], self.dtable, scale=self.scale)
 
     def update(self, rate: float) -> None:

@@ -56,6 +56,25 @@ def test_token_by_token_as_at_once():
     assert float((state - whole).abs().max()) < 1e-5
 
 
+def test_reading_between_a_batch_and_its_gradient():
+    """Arrivals are read, what runs moves on, while a batch waits for its gradient: the gradient is the batch's all the same."""
+    token, off, _, _ = _prompts(12, seed=4)
+    others, their_off, _, _ = _prompts(30, seed=77)
+    grads = []
+    for reads in (False, True):
+        r = _small(drop=0.3)
+        x = r.train_forward(token, off)
+        kept = x.clone()
+        if reads:
+            state = r.read(others, their_off)
+            r.advance(others[:30].contiguous(), state)
+        assert torch.equal(x, kept)
+        r.backward(token, off, torch.ones_like(x))
+        grads.append([t.clone() for t in (r.dtable, r.dw, r.db)])
+    for a, b in zip(*grads):
+        assert torch.equal(a, b)
+
+
 @pytest.mark.parametrize("drop", [0.0, 0.3])
 def test_gradients_through_all_operators(drop):
     """The gradient of a loss by table, product and bias: against differences of the loss in 64 bits, the same elements dropped."""
