@@ -720,6 +720,50 @@ def test_the_last_number_of_a_call():
         assert as_after(after)
 
 
+def test_what_calls_leave_is_cleared_before_their_numbers_come_again():
+    """A word that is left with a call's number would be taken for one of the call that has the number next: after the last number there is none, and the
+    next call number 1, of as many tokens as the first but other inputs, gives what a new handle gives."""
+    n, few, width, line = 6000, 700, 300, 16
+    rng = np.random.default_rng(21)
+    first, second = [[put(a, torch.float32) for a in inputs(rng, n, width, torch.float32)] for _ in range(2)]
+    off, short = ints([0, n]), ints([0, few])
+    fresh, want = binding.Tokens(n, 1, width), empty(n, width)
+    fresh.gr_gated_scan(*second, out_y=want, off=off)
+    h, hip, y = binding.Tokens(n, 1, width), binding.C.CDLL("libamdhip64.so"), empty(n, width)
+    inside = _Handle.from_address(h._h.value)
+
+    def copy(to, source, size, kind):
+        torch.cuda.synchronize()
+        assert hip.hipMemcpy(binding.C.c_void_p(to), binding.C.c_void_p(source), binding.C.c_size_t(size), kind) == 0
+
+    def words():
+        a = np.ones(inside.n_words, dtype=np.uint64)
+        copy(a.ctypes.data, inside.words, a.nbytes, 2)
+        return a
+
+    def number(call):
+        control = np.zeros(line * (inside.counters + 1), dtype=np.uint64)
+        control[line::line] = np.uint64(call << 32)
+        copy(inside.control, control.ctypes.data, control.nbytes, 1)
+
+    h.gr_gated_scan(*first, out_y=y, off=off)
+    of_first = words()
+    assert ((of_first >> 32) <= 1).all() and (of_first >> 32 == 1).sum() > 3 * width
+    number(2 ** 32 - 1)
+    h.gr_gated_scan(first[0][:few], first[1][:few], out_y=y[:few], off=short)
+    assert (words() == 0).all()
+    h.gr_gated_scan(*second, out_y=y, off=off)
+    assert torch.equal(y, want)
+    # the last number by a call of many tiles, backward; then a forward one
+    dg, dx = empty(n, width), empty(n, width)
+    number(2 ** 32 - 1)
+    h.gr_gated_scan_backward(*second, want, dg, dx, off=off, dy=want)
+    assert (words() == 0).all()
+    y.fill_(77)
+    h.gr_gated_scan(*second, out_y=y, off=off)
+    assert torch.equal(y, want)
+
+
 def test_more_rows_than_the_cache_holds():
     """Their gradient, 300 MB of rows, some read past the cache: sums of whole numbers, which single precision holds."""
     n, V, W = 150_000, 9000, 513
