@@ -577,8 +577,15 @@ typedef struct gr_tokens gr_tokens;
 
 /*
  * Create the workspace of calls on up to max_tokens tokens (<= 2^30) of up to max_vocab different ones and rows of up to max_width
- * elements, on the current HIP device (not inside a capture).  Device memory held until gr_tokens_destroy: for the sort 16 bytes a token and
- * 2 KB for each 2 048; 64 MB for the parts of long sums; for the recurrence 16 bytes for each channel of each 96 tokens and 2 MB.
+ * elements, on the current HIP device (not inside a capture).  All of it is allocated here, whichever of the calls follow, and held until
+ * gr_tokens_destroy; in bytes, with quotients rounded up, p = (max_tokens + max_vocab) / 1 024, and t = max_tokens / 96, or max_tokens / 64 up to 512
+ * of those if that is more:
+ *   16 * max_tokens + 2 048 * (max_tokens / 2 048 + 1)   the sort,
+ *   8 * max_width * p, 2^24 at least                     parts of long sums (570 MB for 2^20 tokens of 2^24 and rows of 4 096),
+ *   8 * p, 16 384 at least                               the rows whose sums have parts,
+ *   8 * (2 * t + t / 16) * [max_width + 3, rounded up to a multiple of 128 if max_width is more than that]
+ *                                                        what the recurrence's tiles tell each other (738 MB there),
+ * and its counters, 2 * max_width + 400.
  */
 int gr_tokens_create(gr_tokens** out, int64_t max_tokens, int32_t max_vocab, int32_t max_width);
 int gr_tokens_destroy(gr_tokens* h);         /* waits for the device first; NULL is allowed */

@@ -39,3 +39,18 @@ def test_feedback_sums_only_where_waves_share_an_instance():
     whose 18 bytes an entry and 8 a request double."""
     small, large = _held(512, 3, 64, 64, 1, 32), _held(512, 3, 128, 64, 1, 32)
     assert large - small >= 0.9 * 512 * ((50 * 128 + 1200) + 64 * 26)
+
+
+@pytest.mark.parametrize("tokens,vocab,width", [(1 << 20, 1 << 24, 4096), (32768, 100, 65536), (1 << 22, 1, 1), (1 << 23, 1 << 20, 130), (1, 1, 64)])
+def test_a_handle_of_tokens_holds_what_its_header_says(tokens, vocab, width):
+    up = lambda a, b: -(-a // b)
+    p, t = up(tokens + vocab, 1024), max(up(tokens, 96), min(up(tokens, 64), 512))
+    channels = up(width, 128) * 128 if width > 128 else width + 3
+    parts = [16 * tokens, 2048 * (up(tokens, 2048) + 1), max(8 * width * p, 1 << 24), max(8 * p, 16384), 8 * (2 * t + up(t, 16)) * channels, 2 * width + 400]
+    binding.Tokens(1, 1, 1).close()
+    before = torch.cuda.mem_get_info()[0]
+    h = binding.Tokens(tokens, vocab, width)
+    held = before - torch.cuda.mem_get_info()[0]
+    h.close()
+    # an allocation is of whole blocks of 2 MB, or shares one
+    assert abs(held - sum(parts)) <= len(parts) * (2 << 20), (held, parts)
