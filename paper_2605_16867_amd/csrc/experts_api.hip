@@ -10,7 +10,9 @@ namespace {
 template <typename T>
 bool dev_alloc(T** p, size_t n)
 {
-    return hipMalloc(reinterpret_cast<void**>(p), (n ? n : 1) * sizeof(T)) == hipSuccess;
+    if (hipMalloc(reinterpret_cast<void**>(p), (n ? n : 1) * sizeof(T)) == hipSuccess) return true;
+    (void)hipGetLastError();      // (returned as GR_ERR_NOMEM: left behind, it would be the next launch's)
+    return false;
 }
 
 // Rows and choices within what the handle was created for; *rc says what is wrong else.

@@ -54,3 +54,18 @@ def test_a_handle_of_tokens_holds_what_its_header_says(tokens, vocab, width):
     h.close()
     # an allocation is of whole blocks of 2 MB, or shares one
     assert abs(held - sum(parts)) <= len(parts) * (2 << 20), (held, parts)
+
+
+def test_a_handle_that_does_not_fit_leaves_no_error_behind():
+    """Refused for its 12 TB of words between tiles, it changes nothing for the next calls: another handle's, or torch's own."""
+    h, table = binding.Tokens(16, 4, 8), torch.arange(32.0, device="cuda").view(4, 8)
+    token, out = torch.tensor([1, 3], dtype=torch.int32, device="cuda"), torch.empty(2, 8, device="cuda")
+    torch.cuda.synchronize()
+    for after in (lambda: h.gr_token_embed(token, table, out), lambda: torch.index_select(table, 0, token, out=out)):
+        out.fill_(77)
+        with pytest.raises(binding.GoodRouteError) as e:
+            binding.Tokens(1 << 30, 1, 65536)
+        assert e.value.code == -5
+        after()
+        torch.cuda.synchronize()
+        assert torch.equal(out, table[[1, 3]])
