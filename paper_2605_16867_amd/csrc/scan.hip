@@ -4,10 +4,11 @@
 //   D_t = dy_t + c_{t+1}, c_t = f_t D_t;  dx_t = i_t D_t, dgate_t = f_t i_t D_t (h_{t-1} - x_t)
 //
 // Bound by memory: three arrays forward, six backward, read once and written once; near it by vector instructions, 29 for an element forward (half of them
-// the two sigmoids, in all digits of single precision), which keep the units busy for 56 % of the time in 16 bits.  The step from token to token
+// the two sigmoids, to two units of single precision's last digit), which keep the units busy for 57 % of the time in 16 bits.  The step from token to token
 // is linear, so a stretch of tokens is two numbers a channel, and stretches join: work is split over the tokens however long a sequence is.
-// MI355X, us: 262 144 tokens of 1 024 sequences x 1 024 in bfloat16 388 (1.6 GB, 4.2 TB/s), backward 674 (3.2 GB, 4.8 TB/s); 100 000 x 1 024 in single
-// precision 219 (5.6 TB/s); one sequence of 65 536 x 1 024 in float16 118; 3 000 tokens x 256 8.4; a token of 4 096 requests x 1 024 10.
+// MI355X, us: 262 144 tokens of 1 024 sequences x 1 024 in bfloat16 380 (1.6 GB, 4.2 TB/s), backward 659 (3.2 GB, 4.9 TB/s; 582
+// without dy); 100 000 x 1 024 in single precision 211 (5.8 TB/s); one sequence of 65 536 x 1 024 in float16 115; 3 000 tokens x 256 7.7; a token of 4 096
+// requests x 1 024 10, backward 20.5.
 #include <type_traits>
 #include <utility>
 
@@ -70,7 +71,7 @@ constexpr int kThreads = 512, kWaves = kThreads / 64;
 // Of 16 tiles the last publishes a state: one of eight is a longer chain (300 000 x 64 89 us for 71), one of 32 more words to look at (65 536 x 1 024 131
 // for 116).
 constexpr int kGroup = 16, kLeastLanesLog = 2, kNearOffsets = 2048, kMostRuns = kThreads >> kLeastLanesLog;
-// Rows of a run: as many as leave a unit two workgroups (forward 105 registers, backward 115); few where there would not be a tile a unit: 3 000 x 256 in
+// Rows of a run: as many as leave a unit two workgroups (forward 115 registers, backward 124); few where there would not be a tile a unit: 3 000 x 256 in
 // single precision 8.9 us with four (9.8 with two, 9.9 with eight), but 16 000 x 512, 504 tiles of eight, 20 us (24 with four, 33 with two).
 constexpr int kRunForward = 8, kRunBackward = 6, kRunFew = 4;
 constexpr int64_t kFewTiles = 256;
@@ -575,7 +576,7 @@ __global__ __launch_bounds__(kThreads) void k_scan_tiles(TileArgs a)
 
 // ---- a token of every sequence ------------------------------------------------------------------
 
-// Bound by memory, most of it the states in single precision: 4 096 requests x 1 024 in bfloat16 59 MB, 10 us.  Pieces of N channels of a row; a last one
+// Bound by memory, most of it the states in single precision: 4 096 requests x 1 024 in bfloat16 59 MB, 10 us, backward 101 MB, 20.5 us.  Pieces of N channels of a row; a last one
 // that is not whole goes by single channels, as states may be in place.
 template <typename T, int N, bool kBack>
 __global__ __launch_bounds__(kBlock) void k_scan_step(ScanIn in, T* y, T* dgate, T* dx, float* last, int pieces)

@@ -70,7 +70,7 @@ class PromptReader:
         self.h.gr_gated_scan(*self._gates(token, self.rows, self.both), h0=state, out_h=state)
 
     def features_of(self, state: torch.Tensor) -> torch.Tensor:
-        """What a length predictor takes of states."""
+        """What a length predictor takes of states (in single precision the states themselves, which `advance` moves on)."""
         return state.to(self.dtype)
 
     # ---- training -----------------------------------------------------------------------------
